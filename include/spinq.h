@@ -393,6 +393,134 @@ spinq_status spinq_decode_attention_kv4(const void* q, const uint8_t* k_codes, c
                                         int64_t workspace_bytes, void* stream);
 
 /*
+ * The paged 4-bit cache.  K and V of a token lie in one slot of a page; a
+ * page holds page_size tokens of every kv head, and a sequence is the list
+ * of its pages (a row of a page table), in any order:
+ *   k_codes, v_codes [num_pages][kv_heads][page_size][head_dim/2] packed Eq. 1
+ *            codes, 16-byte aligned (K rotated by R3, as spinq_rotate_quant_kv
+ *            stores it);
+ *   scales   [num_pages][kv_heads][page_size][4] fp32, 16-byte aligned:
+ *            (K alpha, K beta, V alpha, V beta) of the token and head.
+ * Slot number s of the cache is slot s % page_size of page s / page_size.
+ * page_size: 16, 32, 64, 128 or 256.  head_dim: 64 or 128.  A slot that no
+ * call has written may hold anything (also values that are not finite): no
+ * call's result depends on slots past a sequence's length.  A page number
+ * outside [0, num_pages) reads no memory out of range; the values of its
+ * tokens are undefined.
+ */
+typedef struct {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* scales;
+  int64_t num_pages;
+  int32_t page_size;
+  int32_t kv_heads;
+  int32_t head_dim;
+} spinq_kv4_pages;
+
+/* Rotary embedding of the first rotary_dim values of a head (Sec. 3.1: RoPE
+ * precedes R3).  rotary_dim: 0 (none), D/4, D/2, 3D/4 or D.  Value pair i <
+ * rotary_dim/2 turns by the angle of table entry [position][i]: values
+ * (i, i + rotary_dim/2) (interleaved = 0) or (2i, 2i + 1) (interleaved = 1).
+ *   positions [T] int32 in [0, max_pos) (others are clamped);
+ *   cos_sin   [max_pos][rotary_dim/2] pairs (cos, sin) fp32, 16-byte aligned:
+ *             scaling for long contexts is in the caller's table. */
+typedef struct {
+  int32_t rotary_dim;
+  int32_t interleaved;
+  const int32_t* positions;
+  const float* cos_sin;
+  int64_t max_pos;
+} spinq_rope_cfg;
+
+/*
+ * spinq_kv4_append -- T new tokens on their way into attention, in one pass:
+ * the norm of each query and key head, the rotary embedding, R3 and the 4-bit
+ * quantizer (Sec. 3.1; Eq. 1), K and V written into their slots of the pages:
+ *   x <- x w / sqrt(mean(x^2) + eps)  (queries with q_weight, keys with k_weight),
+ *   x <- rotary embedding (rope != NULL),  x' = x H_D / sqrt(D)  (queries, keys),
+ *   q_out = fp16(x'),  K codes = Eq. 1 of x',  V codes = Eq. 1 of v.
+ * All of it in fp32 from the fp16 input to the code.
+ *   q [T][Hq][D], k, v [T][kv_heads][D] fp16: a token's heads are contiguous,
+ *          tokens ldq, ldk, ldv elements apart (parts of one projection's
+ *          output, for instance), 16-byte aligned, ld % 8 == 0.
+ *   q_out  [T][Hq][D] fp16 (may equal q when ldq = Hq D).  Hq may be 0.
+ *   q_weight, k_weight  [D] fp16, 16-byte aligned, or NULL (no norm); eps >= 0.
+ *   kvq    bits = 4, symmetric = 0, granularity = SPINQ_PER_GROUP, group_size = D.
+ *   slots  [T] int64 slot numbers, distinct; a token whose number is outside
+ *          the cache (e.g. -1, padding) is not written, its q_out is.
+ */
+spinq_status spinq_kv4_append(const void* q, int64_t ldq, void* q_out, const void* k, int64_t ldk, const void* v,
+                              int64_t ldv, int64_t T, int64_t Hq, const void* q_weight, const void* k_weight,
+                              float eps, const spinq_rope_cfg* rope, const spinq_quant_cfg* kvq,
+                              const spinq_kv4_pages* cache, const int64_t* slots, void* stream);
+
+/*
+ * spinq_kv4_read -- cached tokens expanded to fp16, packed: tokens starts[b],
+ * starts[b] + 1, ... of sequence b at rows cu_tokens[b] .. cu_tokens[b+1] - 1 of
+ *   k, v [total][kv_heads][D] fp16 = fp16(alpha u + beta)  (K still rotated by
+ *        R3, as the rotated queries want it: what spinq_prompt_attention takes
+ *        for the context of a prompt that arrives in chunks).
+ *   page_table [batch][table_width] int32;  starts [batch] int32 or NULL (0);
+ *   cu_tokens [batch + 1] int32 ascending from 0, cu_tokens[batch] = total.
+ *   Tokens past the page table read as zeros.
+ */
+spinq_status spinq_kv4_read(const spinq_kv4_pages* cache, const int32_t* page_table, int64_t batch,
+                            int64_t table_width, const int32_t* starts, const int32_t* cu_tokens, int64_t total,
+                            void* k, void* v, void* stream);
+
+/*
+ * spinq_prompt_attention -- attention over whole prompts, packed, grouped heads:
+ *   o_i = sum_j softmax_j(softmax_scale q_i . k_j) v_j
+ * for query i of a sequence of lq queries and lk >= 0 keys; with causal = 1
+ * over j <= i + lk - lq (the queries are the sequence's last positions), else
+ * over all.  A query that sees no key gives zeros.  Query head h reads kv head
+ * h / (Hq / Hkv).
+ *   q [total_q][Hq][D], k, v [total_k][Hkv][D] fp16, tokens ldq, ldk, ldv
+ *          elements apart as in spinq_kv4_append;  out [total_q][Hq][D] fp16,
+ *          not overlapping the inputs.
+ *   cu_q, cu_k [batch + 1] int32 (device), ascending from 0: sequence b has
+ *          rows cu[b] .. cu[b+1] - 1 (rows of out after the last are not written).
+ *   max_q, max_k  no less than any sequence's lq and lk (host numbers: the
+ *          launch is planned with them).
+ *   workspace  spinq_prompt_attention_workspace_bytes(...) bytes, 16-byte
+ *          aligned (may be NULL when that is 0; no zeroing needed).
+ *   Keys and values of a sequence must be finite; rows of other sequences
+ *   and rows outside every sequence never reach a result.
+ *   Supported: D = 64 or 128, Hq / Hkv whole and at most 128.  Scores and sums
+ *   in fp32, the softmax weights in fp16 for the product with V.
+ */
+int64_t spinq_prompt_attention_workspace_bytes(int64_t batch, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv,
+                                               int64_t D);
+spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                    const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t total_q,
+                                    int64_t total_k, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv, int64_t D,
+                                    int32_t causal, float softmax_scale, void* out, void* workspace,
+                                    int64_t workspace_bytes, void* stream);
+
+/*
+ * spinq_prefix_attention_kv4 -- attention of one decode query per (sequence,
+ * query head) over the paged 4-bit cache, where the sequences share a prefix
+ * (an instruction text, a document) that is read and multiplied once for all:
+ * softmax over the prefix_len tokens of prefix_table, then the sequence's own
+ * lens[b] tokens of page_table[b], K and V as in spinq_decode_attention_kv4.
+ * A sequence without any token gives zeros; prefix_len may be 0.
+ *   q, out [B][Hq][D] fp16, q rotated by R3 (spinq_kv4_append's q_out);
+ *   prefix_table [ceil(prefix_len / page_size)] int32;
+ *   page_table [B][table_width] int32, lens [B] int32 (device), each in
+ *          [0, table_width * page_size] (others are clamped).
+ *   workspace  spinq_prefix_attention_workspace_bytes(...) bytes, 16-byte
+ *          aligned (no zeroing needed).
+ *   Supported: Hq / kv_heads whole and at most 128.
+ */
+int64_t spinq_prefix_attention_workspace_bytes(int64_t B, int64_t prefix_len, int64_t table_width, int32_t page_size,
+                                               int64_t Hq, int64_t Hkv, int64_t D);
+spinq_status spinq_prefix_attention_kv4(const void* q, const spinq_kv4_pages* cache, const int32_t* prefix_table,
+                                        int64_t prefix_len, const int32_t* page_table, int64_t table_width,
+                                        const int32_t* lens, int64_t B, int64_t Hq, float softmax_scale, void* out,
+                                        void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
  * 8-bit variants (main results table, W4A8 rows "4-8-x"; appendix "Latency
  * measurement on GPU": W-fp8-A-fp8 with the dequantization fused into the
  * GEMM epilogue).  They share the rotation convention above and run on the

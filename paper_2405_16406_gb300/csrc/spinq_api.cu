@@ -411,6 +411,209 @@ spinq_status spinq_decode_attention_kv4(const void* q, const uint8_t* k_codes, c
   return from_cuda(launch_decode_attention(a, decode_attention_chunks(B, S, Hkv), static_cast<cudaStream_t>(stream)));
 }
 
+namespace {
+
+// A paged cache's own numbers; the pointers are checked where they are used.
+spinq_status check_pages(const spinq_kv4_pages* c) {
+  if (!c || c->num_pages < 0 || c->kv_heads <= 0 || c->head_dim <= 0 || c->page_size <= 0) return SPINQ_EINVAL;
+  if (c->num_pages > 0 && (!c->k_codes || !c->v_codes || !c->scales)) return SPINQ_EINVAL;
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->scales)) return SPINQ_EINVAL;
+  if (c->head_dim != 64 && c->head_dim != 128) return SPINQ_EUNSUPPORTED;
+  if (c->page_size < 16 || c->page_size > 256 || !is_pow2(c->page_size)) return SPINQ_EUNSUPPORTED;
+  if (c->kv_heads > 65535 || c->num_pages > INT32_MAX) return SPINQ_EUNSUPPORTED;
+  return SPINQ_OK;
+}
+
+// Rows of `width` fp16 values, ld apart, 16-byte aligned.
+bool rows_ok(const void* p, int64_t ld, int64_t width) {
+  return p && aligned16(p) && ld >= width && ld % 8 == 0;
+}
+
+}  // namespace
+
+spinq_status spinq_kv4_append(const void* q, int64_t ldq, void* q_out, const void* k, int64_t ldk, const void* v,
+                              int64_t ldv, int64_t T, int64_t Hq, const void* q_weight, const void* k_weight,
+                              float eps, const spinq_rope_cfg* rope, const spinq_quant_cfg* kvq,
+                              const spinq_kv4_pages* cache, const int64_t* slots, void* stream) {
+  if (!kvq || T < 0 || Hq < 0 || !(eps >= 0.f) || !std::isfinite(eps)) return SPINQ_EINVAL;
+  spinq_status st = check_pages(cache);
+  if (st != SPINQ_OK) return st;
+  const int64_t D = cache->head_dim, Hkv = cache->kv_heads;
+  if (!clip_ok(kvq->clip_ratio)) return SPINQ_EINVAL;
+  if (T > 0) {
+    if (Hq > 0 && (!rows_ok(q, ldq, Hq * D) || !q_out || !aligned16(q_out))) return SPINQ_EINVAL;
+    if (Hq > 0 && q_out == q && ldq != Hq * D) return SPINQ_EINVAL;
+    if (!rows_ok(k, ldk, Hkv * D) || !rows_ok(v, ldv, Hkv * D) || !slots) return SPINQ_EINVAL;
+  }
+  if (!aligned16(q_weight) || !aligned16(k_weight)) return SPINQ_EINVAL;
+  AppendArgs a{};
+  if (rope) {
+    if (rope->rotary_dim < 0 || rope->rotary_dim > D || (rope->interleaved != 0 && rope->interleaved != 1))
+      return SPINQ_EINVAL;
+    if (rope->rotary_dim > 0 && T > 0 && (!rope->positions || !rope->cos_sin || rope->max_pos <= 0))
+      return SPINQ_EINVAL;
+    if (!aligned16(rope->cos_sin)) return SPINQ_EINVAL;
+    if (rope->rotary_dim % (D / 4) != 0) return SPINQ_EUNSUPPORTED;
+    a.rotary = rope->rotary_dim;
+    a.interleaved = rope->interleaved != 0;
+    a.positions = rope->positions;
+    a.cos_sin = rope->cos_sin;
+    a.max_pos = rope->max_pos;
+  }
+  if (kvq->bits != 4 || kvq->symmetric != 0 || kvq->granularity != SPINQ_PER_GROUP || kvq->group_size != D)
+    return SPINQ_EUNSUPPORTED;
+  if (Hq > 65535 || T > INT32_MAX) return SPINQ_EUNSUPPORTED;
+  if (T == 0) return SPINQ_OK;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.q_out = q_out;
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.D = (int)D;
+  a.q_weight = q_weight;
+  a.k_weight = k_weight;
+  a.eps = eps;
+  a.clip = kvq->clip_ratio;
+  a.norm = (float)(1.0 / std::sqrt((double)D));
+  a.k_codes = cache->k_codes;
+  a.v_codes = cache->v_codes;
+  a.scales = cache->scales;
+  a.num_slots = cache->num_pages * cache->page_size;
+  a.page_size = cache->page_size;
+  a.slots = slots;
+  return from_cuda(launch_kv4_append(a, static_cast<cudaStream_t>(stream)));
+}
+
+spinq_status spinq_kv4_read(const spinq_kv4_pages* cache, const int32_t* page_table, int64_t batch,
+                            int64_t table_width, const int32_t* starts, const int32_t* cu_tokens, int64_t total,
+                            void* k, void* v, void* stream) {
+  if (batch < 0 || table_width < 0 || total < 0) return SPINQ_EINVAL;
+  spinq_status st = check_pages(cache);
+  if (st != SPINQ_OK) return st;
+  if (total > 0 && (batch == 0 || !cu_tokens || !k || !v || (table_width > 0 && !page_table))) return SPINQ_EINVAL;
+  if (!aligned16(k) || !aligned16(v)) return SPINQ_EINVAL;
+  if (batch > INT32_MAX || total > INT32_MAX) return SPINQ_EUNSUPPORTED;
+  if (total == 0) return SPINQ_OK;
+  ReadArgs a{cache->k_codes, cache->v_codes, cache->scales, cache->num_pages, cache->kv_heads, cache->page_size,
+             cache->head_dim, page_table, batch, table_width, starts, cu_tokens, total, k, v};
+  return from_cuda(launch_kv4_read(a, static_cast<cudaStream_t>(stream)));
+}
+
+static PromptArgs prompt_shape(int64_t batch, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv, int64_t D) {
+  PromptArgs a{};
+  a.batch = batch;
+  a.max_q = max_q;
+  a.max_k = max_k;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.D = (int)D;
+  return a;
+}
+
+int64_t spinq_prompt_attention_workspace_bytes(int64_t batch, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv,
+                                               int64_t D) {
+  if (batch <= 0 || max_q <= 0 || max_k < 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || (D != 64 && D != 128)) return 0;
+  return prompt_attention_workspace(prompt_shape(batch, max_q, max_k, Hq, Hkv, D));
+}
+
+spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                    const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t total_q,
+                                    int64_t total_k, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv, int64_t D,
+                                    int32_t causal, float softmax_scale, void* out, void* workspace,
+                                    int64_t workspace_bytes, void* stream) {
+  if (batch < 0 || total_q < 0 || total_k < 0 || max_q < 0 || max_k < 0 || Hq <= 0 || Hkv <= 0 || D <= 0)
+    return SPINQ_EINVAL;
+  if (Hq % Hkv != 0 || (causal != 0 && causal != 1) || !std::isfinite(softmax_scale)) return SPINQ_EINVAL;
+  if (total_q > 0) {
+    if (batch == 0 || max_q == 0 || !cu_q || !cu_k || !out || !aligned16(out)) return SPINQ_EINVAL;
+    if (!rows_ok(q, ldq, Hq * D)) return SPINQ_EINVAL;
+    if (total_k > 0 && (!rows_ok(k, ldk, Hkv * D) || !rows_ok(v, ldv, Hkv * D))) return SPINQ_EINVAL;
+  }
+  if ((D != 64 && D != 128) || Hq / Hkv > 128) return SPINQ_EUNSUPPORTED;
+  if (batch > 65535 || Hkv > 65535 || total_q > INT32_MAX || total_k > INT32_MAX || max_q > INT32_MAX ||
+      max_k > INT32_MAX)
+    return SPINQ_EUNSUPPORTED;
+  if (total_q == 0) return SPINQ_OK;
+  PromptArgs a = prompt_shape(batch, max_q, max_k, Hq, Hkv, D);
+  const int64_t need = prompt_attention_workspace(a);
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return SPINQ_EINVAL;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.cu_q = cu_q;
+  a.cu_k = cu_k;
+  a.total_q = total_q;
+  a.total_k = total_k;
+  a.causal = causal != 0;
+  a.scale = softmax_scale;
+  a.out = out;
+  a.workspace = workspace;
+  return from_cuda(launch_prompt_attention(a, static_cast<cudaStream_t>(stream)));
+}
+
+static PrefixArgs prefix_shape(int64_t B, int64_t prefix_len, int64_t table_width, int32_t page_size, int64_t Hq,
+                               int64_t Hkv, int64_t D) {
+  PrefixArgs a{};
+  a.B = B;
+  a.prefix_len = prefix_len;
+  a.table_width = table_width;
+  a.page_size = page_size;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.D = (int)D;
+  return a;
+}
+
+int64_t spinq_prefix_attention_workspace_bytes(int64_t B, int64_t prefix_len, int64_t table_width, int32_t page_size,
+                                               int64_t Hq, int64_t Hkv, int64_t D) {
+  if (B <= 0 || prefix_len < 0 || table_width < 0 || page_size <= 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 ||
+      (D != 64 && D != 128))
+    return 0;
+  return prefix_attention_workspace(prefix_shape(B, prefix_len, table_width, page_size, Hq, Hkv, D));
+}
+
+spinq_status spinq_prefix_attention_kv4(const void* q, const spinq_kv4_pages* cache, const int32_t* prefix_table,
+                                        int64_t prefix_len, const int32_t* page_table, int64_t table_width,
+                                        const int32_t* lens, int64_t B, int64_t Hq, float softmax_scale, void* out,
+                                        void* workspace, int64_t workspace_bytes, void* stream) {
+  if (B < 0 || prefix_len < 0 || table_width < 0 || Hq <= 0 || !std::isfinite(softmax_scale)) return SPINQ_EINVAL;
+  spinq_status st = check_pages(cache);
+  if (st != SPINQ_OK) return st;
+  const int64_t Hkv = cache->kv_heads, D = cache->head_dim;
+  if (Hq % Hkv != 0) return SPINQ_EINVAL;
+  if (B > 0) {
+    if (!q || !out || !lens || !aligned16(q) || !aligned16(out)) return SPINQ_EINVAL;
+    if ((prefix_len > 0 && !prefix_table) || (table_width > 0 && !page_table)) return SPINQ_EINVAL;
+    if ((prefix_len > 0 || table_width > 0) && cache->num_pages == 0) return SPINQ_EINVAL;
+  }
+  if (Hq / Hkv > 128 || B > 65535 || prefix_len > INT32_MAX || table_width > INT32_MAX / cache->page_size)
+    return SPINQ_EUNSUPPORTED;
+  if (B == 0) return SPINQ_OK;
+  PrefixArgs a = prefix_shape(B, prefix_len, table_width, cache->page_size, Hq, Hkv, D);
+  const int64_t need = prefix_attention_workspace(a);
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return SPINQ_EINVAL;
+  a.q = q;
+  a.k_codes = cache->k_codes;
+  a.v_codes = cache->v_codes;
+  a.scales = cache->scales;
+  a.num_pages = cache->num_pages;
+  a.prefix_table = prefix_table;
+  a.table = page_table;
+  a.lens = lens;
+  a.scale = softmax_scale;
+  a.out = out;
+  a.workspace = workspace;
+  return from_cuda(launch_prefix_attention(a, static_cast<cudaStream_t>(stream)));
+}
+
 spinq_status spinq_debug_set_wait_limit_ns(int64_t ns) {
   if (ns <= 0) return SPINQ_EINVAL;
   const uint64_t v = (uint64_t)ns;

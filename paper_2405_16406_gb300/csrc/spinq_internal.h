@@ -99,6 +99,89 @@ struct AttnArgs {
   float* workspace;
 };
 
+// The paged 4-bit cache (kv4_pages.cu): codes [page][kv head][slot][D/2],
+// scales [page][kv head][slot][4].
+struct AppendArgs {
+  const void* q;          // fp16 [T] rows of Hq D values, ldq apart
+  const void* k;          // fp16 [T] rows of Hkv D values
+  const void* v;
+  int64_t ldq, ldk, ldv;  // elements
+  void* q_out;            // fp16 [T][Hq][D]
+  int64_t T, Hq, Hkv;
+  int D;
+  const void* q_weight;   // fp16 [D] or nullptr: no norm
+  const void* k_weight;
+  float eps;
+  int rotary;             // leading values of a head that rotate (0: none)
+  bool interleaved;
+  const int32_t* positions;   // [T]
+  const float* cos_sin;       // [max_pos][rotary/2] (cos, sin) pairs
+  int64_t max_pos;
+  float clip;
+  float norm;             // 1/sqrt(D)
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* scales;
+  int64_t num_slots;      // num_pages * page_size
+  int page_size;
+  const int64_t* slots;   // [T]; outside [0, num_slots): not written
+};
+cudaError_t launch_kv4_append(const AppendArgs& a, cudaStream_t stream);
+
+struct ReadArgs {
+  const uint8_t* k_codes;
+  const uint8_t* v_codes;
+  const float* scales;
+  int64_t num_pages, Hkv;
+  int page_size, D;
+  const int32_t* table;   // [batch][table_width]
+  int64_t batch, table_width;
+  const int32_t* starts;  // [batch] or nullptr (0)
+  const int32_t* cu;      // [batch + 1]
+  int64_t total;
+  void* k;                // fp16 [total][Hkv][D]
+  void* v;
+};
+cudaError_t launch_kv4_read(const ReadArgs& a, cudaStream_t stream);
+
+struct PromptArgs {
+  const void* q;          // fp16 [total_q] rows of Hq D values, ldq apart
+  const void* k;          // fp16 [total_k] rows of Hkv D values
+  const void* v;
+  int64_t ldq, ldk, ldv;
+  const int32_t* cu_q;    // [batch + 1]
+  const int32_t* cu_k;
+  int64_t batch, total_q, total_k, max_q, max_k, Hq, Hkv;
+  int D;
+  bool causal;
+  float scale;
+  void* out;              // fp16 [total_q][Hq][D]
+  void* workspace;
+};
+// Workspace bytes of the call (pointers unused).
+int64_t prompt_attention_workspace(const PromptArgs& a);
+cudaError_t launch_prompt_attention(const PromptArgs& a, cudaStream_t stream);
+
+struct PrefixArgs {
+  const void* q;          // fp16 [B][Hq][D]
+  const uint8_t* k_codes;
+  const uint8_t* v_codes;
+  const float* scales;
+  int64_t num_pages, Hkv;
+  int page_size, D;
+  const int32_t* prefix_table;   // [ceil(prefix_len / page_size)]
+  int64_t prefix_len;
+  const int32_t* table;          // [B][table_width]
+  int64_t table_width;
+  const int32_t* lens;           // [B]
+  int64_t B, Hq;
+  float scale;
+  void* out;              // fp16 [B][Hq][D]
+  void* workspace;
+};
+int64_t prefix_attention_workspace(const PrefixArgs& a);
+cudaError_t launch_prefix_attention(const PrefixArgs& a, cudaStream_t stream);
+
 // Chunks of the cache length that the decode attention splits over (the
 // workspace holds B * Hq * chunks * (D + 2) floats).
 int decode_attention_chunks(int64_t B, int64_t S, int64_t Hkv);

@@ -42,7 +42,8 @@ EXPORTED = (
     "spinq_rope_rotate_quant_kv", "spinq_decode_attention_workspace_bytes", "spinq_decode_attention_kv4",
     "spinq_rotate_quant_act_signed", "spinq_quant_weight_signed", "spinq_rotated_linear_workspace_bytes",
     "spinq_rotated_linear", "spinq_debug_set_wait_limit_ns", "spinq_debug_fail_launches",
-    "spinq_debug_stall_launches",
+    "spinq_debug_stall_launches", "spinq_kv4_append", "spinq_kv4_read", "spinq_prompt_attention_workspace_bytes",
+    "spinq_prompt_attention", "spinq_prefix_attention_workspace_bytes", "spinq_prefix_attention_kv4",
 )
 SPINQ_FMT_INT8_PLANES, SPINQ_FMT_E4M3, SPINQ_FMT_INT4_BYTES = 1, 2, 3
 
@@ -55,6 +56,17 @@ class QuantCfg(ctypes.Structure):
 
 class HadCfg(ctypes.Structure):
     _fields_ = [("n_small", ctypes.c_int32), ("n_pow2", ctypes.c_int32)]
+
+
+class Kv4PagesCfg(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class RopeCfg(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("positions", ctypes.c_void_p),
+                ("cos_sin", ctypes.c_void_p), ("max_pos", ctypes.c_int64)]
 
 
 class SpinqError(RuntimeError):
@@ -135,6 +147,22 @@ _lib.spinq_rotate_quant_kv.restype = ctypes.c_int
 _lib.spinq_rotate_quant_kv.argtypes = [_P, _P, _P, _P, _I64, _I64, _I64, _I64, _I64,
                                        ctypes.POINTER(HadCfg), ctypes.POINTER(QuantCfg),
                                        _P, _P, _P, _P, _P, _P, _P]
+_lib.spinq_kv4_append.restype = ctypes.c_int
+_lib.spinq_kv4_append.argtypes = [_P, _I64, _P, _P, _I64, _P, _I64, _I64, _I64, _P, _P, ctypes.c_float,
+                                  ctypes.POINTER(RopeCfg), ctypes.POINTER(QuantCfg), ctypes.POINTER(Kv4PagesCfg),
+                                  _P, _P]
+_lib.spinq_kv4_read.restype = ctypes.c_int
+_lib.spinq_kv4_read.argtypes = [ctypes.POINTER(Kv4PagesCfg), _P, _I64, _I64, _P, _P, _I64, _P, _P, _P]
+_lib.spinq_prompt_attention_workspace_bytes.restype = ctypes.c_int64
+_lib.spinq_prompt_attention_workspace_bytes.argtypes = [_I64] * 6
+_lib.spinq_prompt_attention.restype = ctypes.c_int
+_lib.spinq_prompt_attention.argtypes = [_P, _I64, _P, _I64, _P, _I64, _P, _P] + [_I64] * 8 + [
+    ctypes.c_int32, ctypes.c_float, _P, _P, _I64, _P]
+_lib.spinq_prefix_attention_workspace_bytes.restype = ctypes.c_int64
+_lib.spinq_prefix_attention_workspace_bytes.argtypes = [_I64, _I64, _I64, ctypes.c_int32, _I64, _I64, _I64]
+_lib.spinq_prefix_attention_kv4.restype = ctypes.c_int
+_lib.spinq_prefix_attention_kv4.argtypes = [_P, ctypes.POINTER(Kv4PagesCfg), _P, _I64, _P, _I64, _P, _I64, _I64,
+                                            ctypes.c_float, _P, _P, _I64, _P]
 
 
 def _check(st: int, where: str) -> None:
@@ -225,6 +253,36 @@ def spinq_rotated_linear_workspace_bytes(M, K) -> int:
 def spinq_rotated_linear(x, M, K, ldx, had, signs, q, w_codes, w_scale, w_rowsum, N, y, ws, ws_bytes, stream) -> int:
     return _lib.spinq_rotated_linear(x, M, K, ldx, had, signs, q, w_codes, w_scale, w_rowsum, N, y, ws, ws_bytes,
                                      stream)
+
+
+def spinq_kv4_append(q, ldq, q_out, k, ldk, v, ldv, T, Hq, q_weight, k_weight, eps, rope, kvq, cache, slots,
+                     stream) -> int:
+    return _lib.spinq_kv4_append(q, ldq, q_out, k, ldk, v, ldv, T, Hq, q_weight, k_weight, eps, rope, kvq, cache,
+                                 slots, stream)
+
+
+def spinq_kv4_read(cache, page_table, batch, table_width, starts, cu_tokens, total, k, v, stream) -> int:
+    return _lib.spinq_kv4_read(cache, page_table, batch, table_width, starts, cu_tokens, total, k, v, stream)
+
+
+def spinq_prompt_attention_workspace_bytes(batch, max_q, max_k, Hq, Hkv, D) -> int:
+    return int(_lib.spinq_prompt_attention_workspace_bytes(batch, max_q, max_k, Hq, Hkv, D))
+
+
+def spinq_prompt_attention(q, ldq, k, ldk, v, ldv, cu_q, cu_k, batch, total_q, total_k, max_q, max_k, Hq, Hkv, D,
+                           causal, scale, out, ws, ws_bytes, stream) -> int:
+    return _lib.spinq_prompt_attention(q, ldq, k, ldk, v, ldv, cu_q, cu_k, batch, total_q, total_k, max_q, max_k, Hq,
+                                       Hkv, D, causal, scale, out, ws, ws_bytes, stream)
+
+
+def spinq_prefix_attention_workspace_bytes(B, prefix_len, table_width, page_size, Hq, Hkv, D) -> int:
+    return int(_lib.spinq_prefix_attention_workspace_bytes(B, prefix_len, table_width, page_size, Hq, Hkv, D))
+
+
+def spinq_prefix_attention_kv4(q, cache, prefix_table, prefix_len, page_table, table_width, lens, B, Hq, scale, out,
+                               ws, ws_bytes, stream) -> int:
+    return _lib.spinq_prefix_attention_kv4(q, cache, prefix_table, prefix_len, page_table, table_width, lens, B, Hq,
+                                           scale, out, ws, ws_bytes, stream)
 
 
 def spinq_debug_set_wait_limit_ns(ns: int) -> int:
@@ -584,3 +642,168 @@ def rotated_linear(x: torch.Tensor, had: Tuple[int, int], w: WeightCodes, signs:
                                      _ptr(w.codes), _ptr(w.scale), _ptr(w.rowsum), N, _ptr(y), _ptr(workspace),
                                      workspace.numel(), _stream(stream)), "spinq_rotated_linear")
     return y
+
+
+@dataclass
+class KV4Pages:
+    """The paged 4-bit cache (spinq_kv4_pages in include/spinq.h)."""
+    k_codes: torch.Tensor   # uint8 [num_pages, Hkv, page_size, D/2]
+    v_codes: torch.Tensor   # uint8 [num_pages, Hkv, page_size, D/2]
+    scales: torch.Tensor    # f32 [num_pages, Hkv, page_size, 4]: K alpha, K beta, V alpha, V beta
+
+
+def kv4_pages(num_pages: int, page_size: int, kv_heads: int, head_dim: int, device=None) -> KV4Pages:
+    """An empty paged cache (its slots are not initialized)."""
+    dev = device or "cuda"
+    shape = (num_pages, kv_heads, page_size)
+    return KV4Pages(torch.empty(shape + (head_dim // 2,), dtype=torch.uint8, device=dev),
+                    torch.empty(shape + (head_dim // 2,), dtype=torch.uint8, device=dev),
+                    torch.empty(shape + (4,), dtype=torch.float32, device=dev))
+
+
+def _pages(cache: KV4Pages) -> Kv4PagesCfg:
+    n, h, p, half = cache.k_codes.shape
+    assert cache.k_codes.dtype == torch.uint8 and cache.k_codes.is_contiguous()
+    assert cache.v_codes.dtype == torch.uint8 and cache.v_codes.is_contiguous()
+    assert cache.v_codes.shape == cache.k_codes.shape
+    assert cache.scales.dtype == torch.float32 and cache.scales.is_contiguous()
+    assert cache.scales.shape == (n, h, p, 4)
+    return Kv4PagesCfg(cache.k_codes.data_ptr(), cache.v_codes.data_ptr(), cache.scales.data_ptr(), n, p, h, 2 * half)
+
+
+def _token_rows(x: torch.Tensor) -> int:
+    """The distance in elements of the tokens of x [T, H, D], whose heads are contiguous."""
+    assert x.dtype == torch.float16 and x.dim() == 3
+    T, H, D = x.shape
+    assert (D == 1 or x.stride(2) == 1) and (H <= 1 or x.stride(1) == D), "a token's heads must be contiguous"
+    return x.stride(0) if T > 1 else max(x.stride(0), (H * D + 7) // 8 * 8)
+
+
+def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """Memory that belongs to the stream the call runs on: the allocator then
+    neither hands out a block that work of another stream still uses nor takes
+    this one back before the call's kernels are done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _ids(x: Optional[torch.Tensor], dtype=torch.int32) -> None:
+    assert x is None or (x.dtype == dtype and x.is_contiguous())
+
+
+def kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: KV4Pages, slots: torch.Tensor,
+               positions: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
+               q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+               interleaved: bool = False, clip: float = 1.0, q_out: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
+    """Norms, RoPE, R3 and the 4-bit quantizer of new tokens q [T, Hq, D], k and
+    v [T, Hkv, D] (strided tokens), K and V written to ``slots`` [T] (int64) of
+    the cache; returns the rotated queries [T, Hq, D].  ``cos_sin``
+    [max_pos, rotary_dim/2, 2] with ``positions`` [T] (int32), or None."""
+    T, Hkv, D = k.shape
+    pages = _pages(cache)
+    assert (Hkv, D) == (pages.kv_heads, pages.head_dim) and v.shape == k.shape
+    _ids(slots, torch.int64)
+    assert slots.numel() == T
+    Hq = 0 if q is None else q.shape[1]
+    if q is not None:
+        assert q.shape == (T, Hq, D)
+        if q_out is None:
+            q_out = _empty((T, Hq, D), torch.float16, q.device, stream)
+        assert q_out.dtype == torch.float16 and q_out.is_contiguous() and q_out.shape == (T, Hq, D)
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == torch.float16 and w.is_contiguous() and w.numel() == D)
+    rope = None
+    if cos_sin is not None:
+        _ids(positions)
+        assert positions is not None and positions.numel() == T
+        assert cos_sin.dtype == torch.float32 and cos_sin.is_contiguous() and cos_sin.shape[2] == 2
+        rope = ctypes.byref(RopeCfg(2 * cos_sin.shape[1], int(bool(interleaved)), positions.data_ptr(),
+                                    cos_sin.data_ptr(), cos_sin.shape[0]))
+    kvq = quant_cfg(4, False, SPINQ_PER_GROUP, D, clip)
+    _check(_lib.spinq_kv4_append(_ptr(q), 0 if q is None else _token_rows(q), _ptr(q_out), _ptr(k), _token_rows(k),
+                                 _ptr(v), _token_rows(v), T, Hq, _ptr(q_weight), _ptr(k_weight), float(eps), rope,
+                                 ctypes.byref(kvq), ctypes.byref(pages), _ptr(slots), _stream(stream)),
+           "spinq_kv4_append")
+    return q_out
+
+
+def kv4_read(cache: KV4Pages, page_table: torch.Tensor, cu_tokens: torch.Tensor, total: int,
+             starts: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None,
+             v: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Cached tokens of the sequences of ``page_table`` [B, W] (int32), from
+    ``starts`` [B] on, as packed fp16 (k, v) [total, Hkv, D]; sequence b fills
+    rows cu_tokens[b] .. cu_tokens[b + 1] - 1."""
+    pages = _pages(cache)
+    batch, width = page_table.shape
+    for x in (page_table, cu_tokens, starts):
+        _ids(x)
+    assert cu_tokens.numel() == batch + 1 and (starts is None or starts.numel() == batch)
+    shape = (total, pages.kv_heads, pages.head_dim)
+    dev = cache.k_codes.device
+    k = _empty(shape, torch.float16, dev, stream) if k is None else k
+    v = _empty(shape, torch.float16, dev, stream) if v is None else v
+    for x in (k, v):
+        assert x.dtype == torch.float16 and x.is_contiguous() and x.shape == shape
+    _check(_lib.spinq_kv4_read(ctypes.byref(pages), _ptr(page_table), batch, width, _ptr(starts), _ptr(cu_tokens),
+                               total, _ptr(k), _ptr(v), _stream(stream)), "spinq_kv4_read")
+    return k, v
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor,
+                     max_q: int, max_k: int, causal: bool = True, scale: Optional[float] = None,
+                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention of packed prompts q [Tq, Hq, D] over k, v [Tk, Hkv, D] (strided
+    tokens); sequence b has rows cu[b] .. cu[b + 1] - 1 (int32 [B + 1])."""
+    Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[0], k.shape[1]
+    assert k.shape == v.shape and k.shape[2] == D
+    for x in (cu_q, cu_k):
+        _ids(x)
+    batch = cu_q.numel() - 1
+    assert cu_k.numel() == batch + 1
+    if out is None:
+        out = _empty((Tq, Hq, D), torch.float16, q.device, stream)
+    assert out.dtype == torch.float16 and out.is_contiguous() and out.shape == q.shape
+    if workspace is None:
+        need = spinq_prompt_attention_workspace_bytes(batch, max_q, max_k, Hq, Hkv, D)
+        workspace = _empty(need, torch.uint8, q.device, stream) if need else None
+    sc = 1.0 / (D ** 0.5) if scale is None else float(scale)
+    _check(_lib.spinq_prompt_attention(_ptr(q), _token_rows(q), _ptr(k), _token_rows(k), _ptr(v), _token_rows(v),
+                                       _ptr(cu_q), _ptr(cu_k), batch, Tq, Tk, max_q, max_k, Hq, Hkv, D,
+                                       int(bool(causal)), sc, _ptr(out), _ptr(workspace),
+                                       0 if workspace is None else workspace.numel(), _stream(stream)),
+           "spinq_prompt_attention")
+    return out
+
+
+def prefix_attention_kv4(q: torch.Tensor, cache: KV4Pages, prefix_table: torch.Tensor, prefix_len: int,
+                         page_table: torch.Tensor, lens: torch.Tensor, scale: Optional[float] = None,
+                         out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Decode attention of q [B, Hq, D] (rotated) over the ``prefix_len`` tokens
+    of ``prefix_table`` that all sequences share, then each sequence's own
+    ``lens`` [B] tokens of ``page_table`` [B, W]."""
+    B, Hq, D = q.shape
+    pages = _pages(cache)
+    assert q.dtype == torch.float16 and q.is_contiguous() and D == pages.head_dim
+    for x in (prefix_table, page_table, lens):
+        _ids(x)
+    width = page_table.shape[1]
+    assert page_table.shape[0] == B and lens.numel() == B
+    assert prefix_table.numel() * pages.page_size >= prefix_len
+    if out is None:
+        out = _empty(q.shape, torch.float16, q.device, stream)
+    assert out.dtype == torch.float16 and out.is_contiguous() and out.shape == q.shape
+    if workspace is None:
+        need = spinq_prefix_attention_workspace_bytes(B, prefix_len, width, pages.page_size, Hq, pages.kv_heads, D)
+        workspace = _empty(need, torch.uint8, q.device, stream) if need else None
+    sc = 1.0 / (D ** 0.5) if scale is None else float(scale)
+    _check(_lib.spinq_prefix_attention_kv4(_ptr(q), ctypes.byref(pages), _ptr(prefix_table), prefix_len,
+                                           _ptr(page_table), width, _ptr(lens), B, Hq, sc, _ptr(out),
+                                           _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                           _stream(stream)), "spinq_prefix_attention_kv4")
+    return out
