@@ -626,14 +626,14 @@ spinq_status spinq_cayley_step(const float* R, const float* grad, int64_t batch,
 /*
  * Testing controls of the failure paths (the paper has no counterpart).
  * spinq_debug_set_wait_limit_ns -- time limit of the ordinary bounded waits
- *   of the Paley rotate+quant, W4A4 and FP8 GEMM kernels on the current
- *   device (2e9 ns by default; the drains of copies and MMAs in flight keep
+ *   of the Paley rotate+quant, W4A4, FP8 GEMM and prompt and prefix attention
+ *   kernels on the current device (2e9 ns by default; the drains of copies and MMAs in flight keep
  *   their full limit).  A test lowers it so that those waits give up, checks
  *   SPINQ_ETIMEOUT through spinq_device_status and sets it back.  Outputs of
  *   a call that gave up are undefined.  SPINQ_EINVAL for ns <= 0.
  * spinq_debug_stall_launches -- the next n launches of the Paley rotate+quant,
- *   the W4A4 prefill (128- and 256-row tiles) and the FP8 GEMM kernels issue
- *   no input copies, so the waits of their consumers run out of time (a
+ *   the W4A4 prefill (128- and 256-row tiles), the FP8 GEMM and the prompt
+ *   attention kernels issue no input copies, so the waits of their consumers run out of time (a
  *   barrier that nothing completes): SPINQ_ETIMEOUT is recorded, every role
  *   leaves its loop, MMAs in flight are drained and tensor memory is freed.
  *   Lower the wait limit first so that this takes a millisecond, not 2 s.

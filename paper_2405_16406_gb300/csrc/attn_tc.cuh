@@ -1,0 +1,148 @@
+// attn_tc.cuh -- what the attention kernels on the 5th-generation tensor core
+// share: bounded waits, tensor-memory stores, MMAs that take their A operand
+// from tensor memory, and the arithmetic of the running softmax.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "spinq_device.cuh"
+
+namespace spinq {
+
+constexpr uint64_t kAttnWaitLimitNs = 2000000000ull;
+constexpr float kAttnLog2e = 1.4426950408889634f;
+// The running maximum moves only when a score exceeds it by more than this
+// (base 2): the weights stay below 2^8 and the accumulator is rescaled rarely.
+constexpr float kAttnSlack = 8.f;
+
+// Non-blocking probe of the phase with `parity`.
+__device__ __forceinline__ bool attn_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
+// Bounded wait that polls; false, with the abort flag up, after `limit_ns`, and false
+// soon after another warp raised it.
+__device__ __forceinline__ bool attn_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
+  if (attn_test(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t k = 1;; ++k) {
+    if (attn_test(bar, parity)) return true;
+    if ((k & 255u) == 0) {
+      if (*abort_flag) return false;
+      if (globaltimer_ns() - t0 > limit_ns) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ float attn_exp2(float x) {   // 2^x: relative error below 2^-22, 0 for -inf
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ float attn_max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
+// 32 lanes x 32 consecutive 32-bit columns to tensor memory.
+__device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t taddr, const uint32_t r[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
+
+// Waits for the tensor-memory loads of r[N] (N a multiple of 16).
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait_all(uint32_t* r) {
+#pragma unroll
+  for (int q = 0; q < N; q += 16) tmem_ld_wait(r + q);
+}
+
+// D[tmem] (+)= A[tmem] * B[smem], fp16 operands: A's rows on the lanes, two
+// values per 32-bit column.
+__device__ __forceinline__ void tc_mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                              uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Instruction descriptor for kind::f16, FP16 x FP16 -> F32, A and B K-major;
+// neg_a multiplies by -A.
+__host__ __device__ constexpr uint32_t umma_idesc_f16_f32(int M, int N, bool neg_a) {
+  return (1u << 4) | ((neg_a ? 1u : 0u) << 13) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// A tile of 128 rows of D fp16 values lies in shared memory as D / 64 atoms
+// of 128 rows x 128 bytes, 128-byte swizzle; kAttnAtom bytes apart.
+constexpr uint32_t kAttnAtom = 128 * 128;
+
+// S[tmem] = Q K^T: both tiles K-major, D / 16 K steps.
+template <int D>
+__device__ __forceinline__ void attn_mma_qk(uint32_t s_tmem, uint32_t q_smem, uint32_t k_smem, uint32_t idesc) {
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) {
+    const uint32_t off = (ks >> 2) * kAttnAtom + (ks & 3) * 32;
+    tc_mma_f16(s_tmem, umma_desc_sw128(q_smem + off), umma_desc_sw128(k_smem + off), idesc, ks > 0 ? 1u : 0u);
+  }
+}
+
+// O[tmem] (+)= P V: P fp16 in tensor memory (128 tokens on 64 columns), V
+// with D contiguous (MN-major), 8 K steps of 16 tokens.
+template <int D>
+__device__ __forceinline__ void attn_mma_pv(uint32_t o_tmem, uint32_t p_tmem, uint32_t v_smem, bool accumulate) {
+  constexpr uint32_t idesc = umma_idesc_f16_f32_bmn(128, D);
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks)
+    tc_mma_f16_ts(o_tmem, p_tmem + ks * 8, umma_desc_sw128_mn(v_smem + ks * 2048, kAttnAtom, 1024), idesc,
+                  accumulate || ks > 0 ? 1u : 0u);
+}
+
+// The largest of 128 scores.
+__device__ __forceinline__ float attn_row_max(const uint32_t* r) {
+  float m[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) m[q] = fmaxf(__uint_as_float(r[2 * q]), __uint_as_float(r[2 * q + 1]));
+#pragma unroll
+  for (int i = 8; i < 128; i += 8)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) m[q] = attn_max3(m[q], __uint_as_float(r[i + 2 * q]), __uint_as_float(r[i + 2 * q + 1]));
+  return fmaxf(attn_max3(m[0], m[1], m[2]), m[3]);
+}
+
+// Rescales this lane's row of an accumulator in tensor memory (D columns).
+template <int D>
+__device__ __forceinline__ void attn_rescale(uint32_t o_tmem, float f) {
+#pragma unroll
+  for (int c = 0; c < D; c += 32) {
+    uint32_t o[32];
+    tmem_ld_32x32b_x32(o_tmem + c, o);
+    tmem_ld_wait_all<32>(o);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+    tmem_st_32x32b_x32(o_tmem + c, o);
+  }
+  tmem_st_wait();
+}
+
+}  // namespace spinq

@@ -310,16 +310,17 @@ struct Fp8GemmArgs {
 // cannot be encoded.
 cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, cudaStream_t stream);
 
-// Launches of the Paley rotate+quant, W4A4 prefill and FP8 GEMM kernels still
+// Launches of the Paley rotate+quant, W4A4 prefill, FP8 GEMM and prompt attention kernels still
 // to issue no input copies (spinq_debug_stall_launches); take_debug_stall()
 // consumes one.
 bool take_debug_stall();
 
-// Limit of the ordinary bounded waits of the Paley rotate+quant, W4A4 and
-// FP8 GEMM kernels (2 s by default; lowered only by tests).
+// Limit of the ordinary bounded waits of the Paley rotate+quant, W4A4, FP8
+// GEMM and attention kernels (2 s by default; lowered only by tests).
 cudaError_t set_wait_limit_paley(uint64_t ns);
 cudaError_t set_wait_limit_gemm(uint64_t ns);
 cudaError_t set_wait_limit_fp8(uint64_t ns);
+cudaError_t set_wait_limit_prompt(uint64_t ns);
 
 // Device status word written by bounded waits that gave up.
 cudaError_t read_and_clear_device_status(int32_t* code, int32_t* detail);
