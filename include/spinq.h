@@ -633,7 +633,7 @@ spinq_status spinq_cayley_step(const float* R, const float* grad, int64_t batch,
  *   a call that gave up are undefined.  SPINQ_EINVAL for ns <= 0.
  * spinq_debug_stall_launches -- the next n launches of the Paley rotate+quant,
  *   the W4A4 prefill (128- and 256-row tiles), the FP8 GEMM and the prompt
- *   attention kernels issue no input copies, so the waits of their consumers run out of time (a
+ *   and prefix attention kernels issue no input copies, so the waits of their consumers run out of time (a
  *   barrier that nothing completes): SPINQ_ETIMEOUT is recorded, every role
  *   leaves its loop, MMAs in flight are drained and tensor memory is freed.
  *   Lower the wait limit first so that this takes a millisecond, not 2 s.

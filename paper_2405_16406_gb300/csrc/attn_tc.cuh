@@ -44,6 +44,12 @@ __device__ __forceinline__ bool attn_wait(uint64_t* bar, uint32_t parity, volati
   }
 }
 
+// The same by a whole warp, with one answer for all its lanes.
+__device__ __forceinline__ bool attn_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                               uint64_t limit_ns) {
+  return __all_sync(0xffffffffu, attn_wait(bar, parity, abort_flag, limit_ns));
+}
+
 __device__ __forceinline__ float attn_exp2(float x) {   // 2^x: relative error below 2^-22, 0 for -inf
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));

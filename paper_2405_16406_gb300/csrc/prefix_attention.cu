@@ -5,104 +5,733 @@
 //   s_t = scale q . k_t,  k_t = alpha_t u_t + beta_t
 //   o   = sum_t softmax_t(s) v_t,  v_t = alpha'_t u'_t + beta'_t
 //
-// over the prefix's tokens, then the sequence's own lens[b].  One warp per
-// (sequence, head): a lane takes a token's score, then D/32 values of the
-// weighted sum; running maximum and sum in fp32.
+// The codes meet the tensor core as the whole numbers u - 8, exact in fp16:
+//   s_t = (scale alpha_t) (q . (u_t - 8)) + scale (beta_t + 8 alpha_t) sum_d q_d
+//   o   = [ sum_t (p_t alpha'_t) (u'_t - 8) + sum_t p_t (beta'_t + 8 alpha'_t) ] / sum_t p_t
+// so the only rounding before the output is that of p alpha' to fp16, on codes
+// about their middle (the offsets, which are larger, stay in fp32).  With
+// M = (running maximum of s, base 2) + log2 r, r about the largest alpha' so far, the
+// weights 2^(s - M) alpha' stay in fp16's range whatever the values' magnitude; M
+// moves only when a score or an alpha' outgrows it by 2^8 or 2^4.
+//
+// Three kernels on the stream:
+//   prefix_tc_kernel   the shared tokens, once for all sequences: an MMA's 128
+//     rows are floor(128 / G) sequences of the G heads of a kv head, two such
+//     tiles per CTA, the prefix split over the grid's z.  S = Q K^T and O += P V on
+//     the 5th-generation tensor core as in the prompt kernel; four warps
+//     expand the pages' codes into the operand tiles.
+//   own_tokens_kernel  each sequence's own tokens: G heads are too few rows for those
+//     tiles, so mma.sync with the tokens on the M side, codes straight
+//     from global memory into fragments.  Bound: the cache's bytes.
+//   combine_kernel     joins the parts (maximum, sum, o) in a fixed order.
 #include <cuda_fp16.h>
+#include <float.h>
 
+#include "../../include/spinq.h"
+#include "attn_tc.cuh"
 #include "launch_util.h"
-#include "spinq_device.cuh"
 #include "spinq_internal.h"
 
 namespace spinq {
 namespace {
 
+__device__ uint64_t g_prefix_wait_ns = kAttnWaitLimitNs;
+constexpr int kPrefixSite = 32;    // wait site recorded on a time-out
+constexpr float kMinValueScale = 8.67361738e-19f;   // 2^-60: values this small are 0 in fp16
+
+// Parts of the result: part p of row (b, head) is max, sum at ml[p][row] and
+// the weighted sum at o[p][row][D] (not written where the sum is 0).
+struct PrefixParams {
+  PrefixArgs a;
+  int G;
+  int tps;         // sequences per tile of 128 rows
+  int nsplit;      // parts of the prefix
+  int nchunk;      // parts of the sequences' own tokens
+  float* o;
+  float2* ml;
+  float scale_log2;
+  int* status;
+  int debug_stall;
+};
+
+__device__ __forceinline__ int64_t page_at(const PrefixArgs& a, const int32_t* table, int64_t t, int shift) {
+  const int64_t page = __ldg(table + (t >> shift));
+  return page < 0 ? 0 : (page >= a.num_pages ? a.num_pages - 1 : page);
+}
+
+// Eight codes of a word as fp16 pairs u - 8: (0, 4), (1, 5), (2, 6), (3, 7).
+__device__ __forceinline__ uint32_t code_pair(uint32_t x) {   // nibbles at bits 0 and 16
+  const uint32_t m = (x & 0x000F000Fu) | 0x64006400u;         // 1024 + u
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x6408)));   // 1032
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint4 code_pairs(uint32_t x) {
+  return make_uint4(code_pair(x), code_pair(x >> 4), code_pair(x >> 8), code_pair(x >> 12));
+}
+
+// --------------------------------------------------------------- the prefix
 template <int D>
-__global__ void __launch_bounds__(128) prefix_rows_kernel(PrefixArgs a) {
-  constexpr int DPL = D / 32;
-  __shared__ float q_s[4][D];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t stride = (int64_t)gridDim.x * 4;
+struct PrefixCfg {
+  static constexpr int TILE = 128 * D * 2;
+  static constexpr int NSTG = 4;                         // operand tiles in flight
+  static constexpr int NCOL = 4;                         // tiles of per-token numbers
+  static constexpr int OFF_KV = 2 * TILE;
+  static constexpr int OFF_COL = OFF_KV + NSTG * TILE;   // [NCOL][2][64] float4
+  static constexpr int OFF_RM = OFF_COL + NCOL * 2048 * 2;   // [NCOL][4] largest alpha' of each warp's tokens
+  static constexpr int OFF_BAR = OFF_RM + NCOL * 16;     // q, full, free [NSTG], col [NCOL], s, p, o [2], drain
+  static constexpr int OFF_MISC = OFF_BAR + (2 * NSTG + NCOL + 8) * 8;
+  static constexpr int BYTES = OFF_MISC + 16 + 1024;
+  static_assert(BYTES <= 232448, "shared memory");
+};
+// four warpgroups: two of softmax with 184 registers a thread, one with the
+// MMAs (56), one that expands the codes (88): 512 = 4 * 128, what the launch holds
+constexpr int kPrefixThreads = 512;
+
+template <int D>
+__global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const PrefixParams p) {
+  using C = PrefixCfg<D>;
+  constexpr int NSTG = C::NSTG, NCOL = C::NCOL;
+  const PrefixArgs& a = p.a;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* qbar = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
+  uint64_t* full = qbar + 1;
+  uint64_t* free_ = full + NSTG;
+  uint64_t* cbar = free_ + NSTG;   // per-token numbers of a tile written
+  uint64_t* sbar = cbar + NCOL;
+  uint64_t* pbar = sbar + 2;
+  uint64_t* obar = pbar + 2;
+  uint64_t* drain = obar + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_MISC + 4);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+  if (tid == 0) {
+    mbar_init(qbar, 8);
+    for (int s = 0; s < NSTG; ++s) {
+      mbar_init(&full[s], 4);
+      mbar_init(&free_[s], 1);
+    }
+    for (int s = 0; s < NCOL; ++s) mbar_init(&cbar[s], 4);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sbar[i], 1);
+      mbar_init(&pbar[i], 4);
+      mbar_init(&obar[i], 1);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 8) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
   pdl_wait();
   pdl_trigger();
-  for (int64_t u = (int64_t)blockIdx.x * 4 + warp; u < a.B * a.Hq; u += stride) {
-    const int64_t b = u / a.Hq, h = u - b * a.Hq, hk = h / (a.Hq / a.Hkv);
-    int64_t own = a.lens[b];
-    own = own < 0 ? 0 : (own > a.table_width * a.page_size ? a.table_width * a.page_size : own);
-    const int64_t n = a.prefix_len + own;
-    __syncwarp();
-    float qsum = 0.f;
-    for (int d = lane; d < D; d += 32) {
-      const float f = __half2float(reinterpret_cast<const __half*>(a.q)[(b * a.Hq + h) * D + d]) * a.scale;
-      q_s[warp][d] = f;
-      qsum += f;
-    }
+
+  const int hk = blockIdx.y, b0 = blockIdx.x * 2 * p.tps;
+  const int ntiles = (int)((a.prefix_len + 127) / 128);
+  const int j0 = (int)((int64_t)ntiles * blockIdx.z / p.nsplit), j1 = (int)((int64_t)ntiles * (blockIdx.z + 1) / p.nsplit);
+  const int nt = j1 - j0;                              // tiles of 128 tokens of this part
+  const int nrow = b0 + p.tps < (int)a.B ? 2 : 1;      // tiles of rows
+  const uint32_t sb = smem_u32(smem);
+
+  if (warp >= 12) {
+    // ---------------- one thread per token of a tile: codes to operand rows
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;\n");
+    const int t = tid & 127, shift = __ffs(a.page_size) - 1;
+    constexpr int NW = D / 32;   // 16-byte pieces of a row of codes
+    auto row_of = [&](int j) {   // index of this thread's token in the page arrays (clamped to the prefix)
+      int64_t tok = (int64_t)j * 128 + t;
+      if (tok >= a.prefix_len) tok = a.prefix_len - 1;
+      return (page_at(a, a.prefix_table, tok, shift) * a.Hkv + hk) * a.page_size + (tok & (a.page_size - 1));
+    };
+    auto expand = [&](const uint4* w, int n) {   // into operand tile n of the ring
+      uint8_t* dst = smem + C::OFF_KV + (n % NSTG) * C::TILE + t * 128;
 #pragma unroll
-    for (int w = 16; w > 0; w >>= 1) qsum += __shfl_xor_sync(0xffffffffu, qsum, w);
-    __syncwarp();
-    float m = -INFINITY, l = 0.f, o[DPL] = {};
-    for (int64_t j0 = 0; j0 < n; j0 += 32) {
-      const int64_t j = j0 + lane;
-      float s = -INFINITY;
-      int64_t at = 0;
-      if (j < n) {
-        const int64_t t = j < a.prefix_len ? j : j - a.prefix_len;
-        const int64_t pi = t / a.page_size;
-        int64_t page = j < a.prefix_len ? a.prefix_table[pi] : a.table[b * a.table_width + pi];
-        page = page < 0 ? 0 : (page >= a.num_pages ? a.num_pages - 1 : page);
-        at = (page * a.Hkv + hk) * a.page_size + (t - pi * a.page_size);
-        const uint32_t* kr = reinterpret_cast<const uint32_t*>(a.k_codes + at * (D / 2));
-        float dot = 0.f;
-        for (int e = 0; e < D / 8; ++e) {
-          const uint32_t w = __ldg(kr + e);
+      for (int k = 0; k < NW; ++k) {
+        const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
 #pragma unroll
-          for (int x = 0; x < 8; ++x) dot = fmaf((float)((w >> (4 * x)) & 15u), q_s[warp][8 * e + x], dot);
-        }
-        s = a.scales[at * 4] * dot + a.scales[at * 4 + 1] * qsum;
-      }
-      float mx = s;
-#pragma unroll
-      for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-      const float mn = fmaxf(m, mx);
-      const float corr = __expf(m - mn), p = __expf(s - mn);
-      l = l * corr + p;
-#pragma unroll
-      for (int e = 0; e < DPL; ++e) o[e] *= corr;
-      const int cnt = n - j0 < 32 ? (int)(n - j0) : 32;
-      for (int x = 0; x < cnt; ++x) {
-        const float px = __shfl_sync(0xffffffffu, p, x);
-        const int64_t ax = __shfl_sync(0xffffffffu, at, x);
-        const float va = a.scales[ax * 4 + 2], vb = a.scales[ax * 4 + 3];
-#pragma unroll
-        for (int e = 0; e < DPL; ++e) {
-          const int d = 32 * e + lane;
-          const uint32_t code = (a.v_codes[ax * (D / 2) + d / 2] >> (4 * (d & 1))) & 15u;
-          o[e] = fmaf(px, fmaf((float)code, va, vb), o[e]);
+        for (int q = 0; q < 4; ++q) {
+          const int ch = 4 * k + q;   // 16-byte chunk (8 values) of the row
+          *reinterpret_cast<uint4*>(dst + (ch >> 3) * kAttnAtom + (((ch & 7) ^ (t & 7)) << 4)) = code_pairs(x[q]);
         }
       }
-      m = mn;
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&full[n % NSTG]);
+    };
+    uint4 kw[NW], vw[NW];
+    float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
+    int64_t at = 0;
+    auto load_k = [&](int j) {
+      at = row_of(j);
+      const uint4* src = reinterpret_cast<const uint4*>(a.k_codes + at * (D / 2));
+#pragma unroll
+      for (int k = 0; k < NW; ++k) kw[k] = __ldg(src + k);
+      sc = __ldg(reinterpret_cast<const float4*>(a.scales) + at);
+    };
+    auto load_v = [&]() {
+      const uint4* src = reinterpret_cast<const uint4*>(a.v_codes + at * (D / 2));
+#pragma unroll
+      for (int k = 0; k < NW; ++k) vw[k] = __ldg(src + k);
+    };
+    const int expand_n = p.debug_stall ? 0 : nt;   // a test of the time-outs expands nothing
+    if (nt > 0) {
+      load_k(j0);
+      load_v();
+    }
+    for (int j = 0; j < expand_n; ++j) {
+      const int n = 2 * j;
+      if (n >= NSTG && !attn_wait_warp(&free_[n % NSTG], (uint32_t)(n / NSTG - 1) & 1u, abort_flag, g_prefix_wait_ns)) break;
+      // the tile's numbers: slot j % NCOL was last read for tile j - NCOL,
+      // whose V tile has been released by now (NSTG operand tiles = 2 tiles of tokens)
+      const bool in = (int64_t)(j0 + j) * 128 + t < a.prefix_len;
+      float* col = reinterpret_cast<float*>(smem + C::OFF_COL + (j % NCOL) * 4096) + (t >> 1) * 4 + (t & 1);
+      col[0] = in ? p.scale_log2 * sc.x : 0.f;
+      col[2] = in ? p.scale_log2 * fmaf(8.f, sc.x, sc.y) : 0.f;
+      const float va = in ? sc.z : 0.f;
+      col[512] = va;
+      col[514] = in ? fmaf(8.f, sc.z, sc.w) : 0.f;
+      float rm = va;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, o));
+      if (lane == 0) reinterpret_cast<float*>(smem + C::OFF_RM + (j % NCOL) * 16)[warp & 3] = rm;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&cbar[j % NCOL]);
+      expand(kw, n);
+      if (j + 1 < nt) load_k(j0 + j + 1);
+      if (n + 1 >= NSTG &&
+          !attn_wait_warp(&free_[(n + 1) % NSTG], (uint32_t)((n + 1) / NSTG - 1) & 1u, abort_flag, g_prefix_wait_ns))
+        break;
+      expand(vw, n + 1);
+      if (j + 1 < nt) load_v();
+    }
+  } else if (warp >= 8) {
+    // ---------------- MMAs
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
+    if (warp == 8) {
+      constexpr uint32_t idesc = umma_idesc_f16_f32(128, 128, false);
+      bool ok = nt == 0 || attn_wait_warp(qbar, 0, abort_flag, g_prefix_wait_ns);
+      auto wait_full = [&](int n) {
+        return attn_wait_warp(&full[n % NSTG], (uint32_t)(n / NSTG) & 1u, abort_flag, g_prefix_wait_ns);
+      };
+      auto qk = [&](int i, int n) {
+        if (lane == 0) {
+          attn_mma_qk<D>(tmem + i * 128, sb + i * C::TILE, sb + C::OFF_KV + (n % NSTG) * C::TILE, idesc);
+          tc_commit(&sbar[i]);
+        }
+      };
+      if (ok && nt > 0 && (ok = wait_full(0))) {
+        tc_fence_after();
+        for (int i = 0; i < nrow; ++i) qk(i, 0);
+        if (lane == 0) tc_commit(&free_[0]);
+      }
+      for (int j = 0; ok && j < nt; ++j) {
+        const int nv = 2 * j + 1, nn = 2 * j + 2;
+        if (!(ok = wait_full(nv))) break;
+        for (int i = 0; i < nrow; ++i) {
+          if (!(ok = attn_wait_warp(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns))) break;
+          tc_fence_after();
+          if (lane == 0)
+            attn_mma_pv<D>(tmem + 256 + i * D, tmem + i * 128, sb + C::OFF_KV + (nv % NSTG) * C::TILE, j > 0);
+          if (j + 1 < nt) {
+            if (i == 0) {
+              if (!(ok = wait_full(nn))) break;
+              tc_fence_after();
+            }
+            qk(i, nn);
+          } else if (lane == 0) {
+            tc_commit(&obar[i]);
+          }
+        }
+        if (!ok) break;
+        if (lane == 0) {
+          tc_commit(&free_[nv % NSTG]);
+          if (j + 1 < nt) tc_commit(&free_[nn % NSTG]);
+        }
+      }
+    }
+  } else {
+    // ---------------- softmax: warps 4i .. 4i + 3 own tile i, thread = row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;\n");
+    const int i = warp >> 2, r = tid & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t st = tmem + i * 128 + lanes, ot = tmem + 256 + i * D + lanes;
+    const int b = b0 + i * p.tps + r / p.G, head = hk * p.G + r % p.G;
+    const bool live = r < p.G * p.tps && b < (int)a.B;
+    const bool work = __any_sync(0xffffffffu, live);   // the warp has a row at all
+    // the row of Q, its pairs in the order of code_pairs, and its sum
+    float qs = 0.f;
+    {
+      const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(a.q) +
+                                                        ((int64_t)b * a.Hq + head) * D);
+#pragma unroll 4
+      for (int ch = 0; ch < D / 8; ++ch) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (live) w = __ldg(src + ch);
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[q]));
+          qs += f.x + f.y;
+        }
+        *reinterpret_cast<uint4*>(smem + i * C::TILE + (ch >> 3) * kAttnAtom + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) =
+            make_uint4(__byte_perm(w.x, w.z, 0x5410), __byte_perm(w.x, w.z, 0x7632), __byte_perm(w.y, w.w, 0x5410),
+                       __byte_perm(w.y, w.w, 0x7632));
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(qbar);
+    }
+    const F2 qs2 = f2_make(qs, qs);
+    float m = -INFINITY, lr = 0.f, rcur = 0.f, l = 0.f, z = 0.f;
+    bool ok = true;
+    for (int j = 0; i < nrow && j < nt; ++j) {
+      if (!(ok = attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns))) break;
+      if (!(ok = attn_wait_warp(&cbar[j % NCOL], (uint32_t)(j / NCOL) & 1u, abort_flag, g_prefix_wait_ns))) break;
+      tc_fence_after();
+      if (work) {
+        uint32_t s[128];
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) tmem_ld_32x32b_x32(st + c, s + c);
+        const uint8_t* colp = smem + C::OFF_COL + (j % NCOL) * 4096;
+        const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(colp);
+        const ulonglong2* az = reinterpret_cast<const ulonglong2*>(colp + 2048);
+        const float4 r4 = *reinterpret_cast<const float4*>(smem + C::OFF_RM + (j % NCOL) * 16);
+        const float rm = fmaxf(attn_max3(r4.x, r4.y, r4.z), r4.w);
+        tmem_ld_wait_all<128>(s);
+#pragma unroll
+        for (int c = 0; c < 128; c += 2) {
+          const ulonglong2 w = ab[c >> 1];
+          const F2 t = f2_fma(f2_from_bits(s[c], s[c + 1]), F2{w.x}, f2_mul(F2{w.y}, qs2));
+          float x, y;
+          f2_split(t, x, y);
+          s[c] = __float_as_uint(x);
+          s[c + 1] = __float_as_uint(y);
+        }
+        const int64_t left = a.prefix_len - (int64_t)(j0 + j) * 128;
+        if (left < 128) {
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c >= (int)left) s[c] = 0xFF800000u;   // -inf
+        }
+        const float mx = attn_row_max(s);
+        const float mn = mx > m + kAttnSlack ? mx : m;
+        if (__any_sync(0xffffffffu, mn != m || rm > 16.f * rcur)) {
+          const float M = m + lr;
+          if (rm > 16.f * rcur) {
+            rcur = fmaxf(rm, kMinValueScale);
+            lr = __log2f(rcur);
+          }
+          if (j > 0) {
+            // the scores' barrier says that every product issued before them is done
+            const float f = m == -INFINITY ? 0.f : attn_exp2(M - (mn + lr));
+            l *= f;
+            z *= f;
+            attn_rescale<D>(ot, f);
+          }
+          m = mn;
+        }
+        const float off = m == -INFINITY ? 0.f : -(m + lr);
+        const F2 of2 = f2_make(off, off);
+        F2 sum = f2_make(l, 0.f), zs = f2_make(z, 0.f);
+#pragma unroll
+        for (int c = 0; c < 128; c += 2) {
+          const ulonglong2 w = az[c >> 1];
+          float x, y;
+          f2_split(f2_add(f2_from_bits(s[c], s[c + 1]), of2), x, y);
+          const F2 e = f2_make(attn_exp2(x), attn_exp2(y));
+          sum = f2_add(sum, e);
+          zs = f2_fma(e, F2{w.y}, zs);
+          f2_split(f2_mul(e, F2{w.x}), x, y);
+          s[c >> 1] = pack_half2_bits(x, y);
+        }
+        float x, y;
+        f2_split(sum, x, y);
+        l = x + y;
+        f2_split(zs, x, y);
+        z = x + y;
+        tmem_st_32x32b_x32(st, s);
+        tmem_st_32x32b_x32(st + 32, s + 32);
+        tmem_st_wait();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&pbar[i]);
+    }
+    if (ok && i < nrow && nt > 0) ok = attn_wait_warp(&obar[i], 0, abort_flag, g_prefix_wait_ns);
+    if (ok && work) {
+      tc_fence_after();
+      const int64_t row = (int64_t)b * a.Hq + head, rows = a.B * a.Hq;
+      const float back = rcur > 0.f ? rcur : 1.f;   // 2^lr: the sums to weights 2^(s - m)
+      if (live) p.ml[(int64_t)blockIdx.z * rows + row] = make_float2(m, l * back);
+      float* out = p.o + ((int64_t)blockIdx.z * rows + row) * D;
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        if (nt > 0) {
+          tmem_ld_32x32b_x32(ot + c, o);
+          tmem_ld_wait_all<32>(o);
+        }
+        if (live && nt > 0) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {   // column 0, 1, .. of eight holds value 0, 4, 1, 5, 2, 6, 3, 7
+            float f[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) f[x] = (__uint_as_float(o[e + x]) + z) * back;
+            *reinterpret_cast<float4*>(out + c + e) = make_float4(f[0], f[2], f[4], f[6]);
+            *reinterpret_cast<float4*>(out + c + e + 4) = make_float4(f[1], f[3], f[5], f[7]);
+          }
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (warp == 8) {   // MMAs in flight finish before tensor memory is given up
+      if (lane == 0) tc_commit(drain);
+      mbar_wait_bounded(drain, 0, kAttnWaitLimitNs);
+    }
+    if (tid == 0 && p.status && atomicCAS(p.status, 0, (int)SPINQ_ETIMEOUT) == 0) atomicExch(p.status + 1, kPrefixSite);
+    __syncthreads();
+  }
+  tc_fence_after();
+  if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+// ------------------------------------------------- the sequences' own tokens
+constexpr int kOwnWarps = 4;
+
+__device__ __forceinline__ uint32_t own_transpose(uint32_t x) {   // 8x8 fp16 transpose over the warp
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// grid (chunk, kv head x group of 8 query heads, sequence).  A warp takes
+// steps of 16 tokens, which lie in one page: the rows of codes it needs are
+// contiguous, and each lane loads its own fragments (lane = 4 g + c): key rows
+// g and g + 8, bytes [c D/8, (c+1) D/8); value rows 2c, 2c+1, 2c+8, 2c+9, bytes
+// [g D/16, (g+1) D/16).  Scores: tokens on M, heads on N; values: head_dim
+// on M, tokens on K, heads on N.
+template <int D>
+__global__ void __launch_bounds__(kOwnWarps * 32) own_tokens_kernel(const PrefixParams p, int hgroups, int chunk_len) {
+  constexpr int KW = D / 32, VW = D / 64, NM = D / 16;
+  const PrefixArgs& a = p.a;
+  __shared__ float o_s[kOwnWarps][8][D];
+  __shared__ float m_s[kOwnWarps][8], l_s[kOwnWarps][8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+  const int hk = blockIdx.y / hgroups, hg = blockIdx.y % hgroups, b = blockIdx.z;
+  const int heads = min(8, p.G - 8 * hg);   // query heads of this CTA
+  pdl_wait();
+  pdl_trigger();
+  const int64_t cap = a.table_width * a.page_size;
+  int64_t len = a.lens[b];
+  len = len < 0 ? 0 : (len > cap ? cap : len);
+  const int t0 = (int)min((int64_t)blockIdx.x * chunk_len, len), t1 = (int)min((int64_t)t0 + chunk_len, len);
+  const int steps = (t1 - t0 + 15) / 16;
+  const int nstep = steps > warp ? (steps - warp + kOwnWarps - 1) / kOwnWarps : 0;
+  const int shift = __ffs(a.page_size) - 1;
+  const int32_t* table = a.table + (int64_t)b * a.table_width;
+  const int64_t row0 = (int64_t)b * a.Hq + hk * p.G + 8 * hg;
+
+  // query fragments of head g (k order as the codes come), their sums
+  uint32_t qb[2 * KW][2];
+  float qs = 0.f;
+  {
+    const __half* qh = reinterpret_cast<const __half*>(a.q) + (row0 + (g < heads ? g : 0)) * D + c * (D / 4);
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      uint4 x = __ldg(reinterpret_cast<const uint4*>(qh + 8 * w));
+      if (g >= heads) x = make_uint4(0, 0, 0, 0);
+      const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&xs[q]));
+        qs += f.x + f.y;
+      }
+      qb[2 * w][0] = __byte_perm(x.x, x.z, 0x5410);
+      qb[2 * w][1] = __byte_perm(x.x, x.z, 0x7632);
+      qb[2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410);
+      qb[2 * w + 1][1] = __byte_perm(x.y, x.w, 0x7632);
+    }
+    qs += __shfl_xor_sync(0xffffffffu, qs, 1);
+    qs += __shfl_xor_sync(0xffffffffu, qs, 2);
+  }
+  const float qsk[2] = {__shfl_sync(0xffffffffu, qs, 8 * c), __shfl_sync(0xffffffffu, qs, 8 * c + 4)};
+
+  struct Step {
+    uint32_t k[2][KW], v[4][VW];
+    float4 sc[2];
+  };
+  auto load = [&](int i, Step& x) {
+    const int t = t0 + 16 * (warp + kOwnWarps * i);   // chunks start at multiples of 16
+    const int64_t at = (page_at(a, table, t, shift) * a.Hkv + hk) * a.page_size + (t & (a.page_size - 1));
+    const uint8_t* kb = a.k_codes + at * (D / 2) + c * (D / 8);
+    const uint8_t* vb = a.v_codes + at * (D / 2) + g * (D / 16);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if constexpr (KW == 4) {
+        const uint4 w = __ldg(reinterpret_cast<const uint4*>(kb + (g + 8 * h) * (D / 2)));
+        x.k[h][0] = w.x, x.k[h][1] = w.y, x.k[h][2] = w.z, x.k[h][3] = w.w;
+      } else {
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(kb + (g + 8 * h) * (D / 2)));
+        x.k[h][0] = w.x, x.k[h][1] = w.y;
+      }
+      x.sc[h] = __ldg(reinterpret_cast<const float4*>(a.scales) + at + g + 8 * h);
     }
 #pragma unroll
-    for (int w = 16; w > 0; w >>= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    for (int q = 0; q < 4; ++q) {
+      const uint8_t* s = vb + (8 * (q >> 1) + 2 * c + (q & 1)) * (D / 2);
+      if constexpr (VW == 2) {
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(s));
+        x.v[q][0] = w.x, x.v[q][1] = w.y;
+      } else {
+        x.v[q][0] = __ldg(reinterpret_cast<const uint32_t*>(s));
+      }
+    }
+  };
+
+  float o[NM][4];
 #pragma unroll
-    for (int e = 0; e < DPL; ++e)
-      reinterpret_cast<__half*>(a.out)[(b * a.Hq + h) * D + 32 * e + lane] = __float2half_rn(o[e] * inv);
+  for (int mu = 0; mu < NM; ++mu) o[mu][0] = o[mu][1] = o[mu][2] = o[mu][3] = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, z[2] = {0.f, 0.f}, lr = 0.f, rcur = 0.f;
+  Step nxt;
+  if (nstep > 0) load(0, nxt);
+  for (int i = 0; i < nstep; ++i) {
+    const Step x = nxt;
+    if (i + 1 < nstep) load(i + 1, nxt);
+    const int left = t1 - (t0 + 16 * (warp + kOwnWarps * i));
+    float sa[4] = {0.f, 0.f, 0.f, 0.f}, sc2[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      const uint4 x0 = code_pairs(x.k[0][w]), x1 = code_pairs(x.k[1][w]);
+      const uint32_t a0[4] = {x0.x, x1.x, x0.y, x1.y}, a1[4] = {x0.z, x1.z, x0.w, x1.w};
+      mma_16816_f16_f32_acc(sa, a0, qb[2 * w][0], qb[2 * w][1]);
+      mma_16816_f16_f32_acc(sc2, a1, qb[2 * w + 1][0], qb[2 * w + 1][1]);
+    }
+    // scores (base 2) of tokens g, g + 8 for heads 2c, 2c + 1; tokens past the
+    // chunk (their slots may hold anything) get -inf and value numbers 0
+    float t[2][2], va[2], vz[2];
+    bool grow = false;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool in = g + 8 * h < left;
+      const float ka = p.scale_log2 * x.sc[h].x, kz = p.scale_log2 * fmaf(8.f, x.sc[h].x, x.sc[h].y);
+      va[h] = in ? x.sc[h].z : 0.f;
+      vz[h] = in ? fmaf(8.f, x.sc[h].z, x.sc[h].w) : 0.f;
+      grow |= va[h] > 16.f * rcur;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        t[h][e] = in ? fmaf(ka, sa[2 * h + e] + sc2[2 * h + e], kz * qsk[e]) : -INFINITY;
+        grow |= t[h][e] > m[e] + kAttnSlack;
+      }
+    }
+    if (__any_sync(0xffffffffu, grow)) {
+      float mx[2] = {fmaxf(t[0][0], t[1][0]), fmaxf(t[0][1], t[1][1])}, rm = fmaxf(va[0], va[1]);
+#pragma unroll
+      for (int w = 4; w < 32; w <<= 1) {
+        mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], w));
+        mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], w));
+        rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, w));
+      }
+      const float lr0 = lr;
+      if (rm > 16.f * rcur) {
+        rcur = fmaxf(rm, kMinValueScale);
+        lr = __log2f(rcur);
+      }
+      float f[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float mn = mx[e] > m[e] + kAttnSlack ? mx[e] : m[e];
+        f[e] = m[e] == -INFINITY ? 0.f : attn_exp2((m[e] + lr0) - (mn + lr));
+        m[e] = mn;
+        l[e] *= f[e];
+        z[e] *= f[e];
+      }
+#pragma unroll
+      for (int mu = 0; mu < NM; ++mu) {
+        o[mu][0] *= f[0], o[mu][2] *= f[0];
+        o[mu][1] *= f[1], o[mu][3] *= f[1];
+      }
+    }
+    float w[2][2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float off = m[e] == -INFINITY ? 0.f : m[e] + lr;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float pe = attn_exp2(t[h][e] - off);
+        l[e] += pe;
+        z[e] = fmaf(pe, vz[h], z[e]);
+        w[h][e] = pe * va[h];
+      }
+    }
+    const uint32_t pb0 = own_transpose(pack_half2_bits(w[0][0], w[0][1]));
+    const uint32_t pb1 = own_transpose(pack_half2_bits(w[1][0], w[1][1]));
+#pragma unroll
+    for (int vw = 0; vw < VW; ++vw)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        // two bytes of two tokens' rows: one dimension of both in a pair
+        const uint32_t xa = __byte_perm(x.v[0][vw], x.v[1][vw], q ? 0x7632 : 0x5410);
+        const uint32_t xb = __byte_perm(x.v[2][vw], x.v[3][vw], q ? 0x7632 : 0x5410);
+        const uint4 ya = code_pairs(xa), yb = code_pairs(xb);
+        const uint32_t a0[4] = {ya.x, ya.y, yb.x, yb.y}, a1[4] = {ya.z, ya.w, yb.z, yb.w};
+        mma_16816_f16_f32_acc(o[4 * vw + 2 * q], a0, pb0, pb1);
+        mma_16816_f16_f32_acc(o[4 * vw + 2 * q + 1], a1, pb0, pb1);
+      }
+  }
+  // join the lanes' shares, then the warps
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int w = 4; w < 32; w <<= 1) {
+      l[e] += __shfl_xor_sync(0xffffffffu, l[e], w);
+      z[e] += __shfl_xor_sync(0xffffffffu, z[e], w);
+    }
+  const float back = rcur > 0.f ? rcur : 1.f;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int h = 2 * c + e;
+#pragma unroll
+    for (int mu = 0; mu < NM; ++mu) {
+      o_s[warp][h][g * (D / 8) + 2 * mu] = (o[mu][e] + z[e]) * back;
+      o_s[warp][h][g * (D / 8) + 2 * mu + 1] = (o[mu][2 + e] + z[e]) * back;
+    }
+    if (g == 0) {
+      m_s[warp][h] = m[e];
+      l_s[warp][h] = l[e] * back;
+    }
+  }
+  __syncthreads();
+  const int64_t rows = a.B * a.Hq, part = (int64_t)p.nsplit + blockIdx.x;
+  for (int e = threadIdx.x; e < heads * D; e += kOwnWarps * 32) {
+    const int h = e / D, d = e % D;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kOwnWarps; ++w) M = fmaxf(M, m_s[w][h]);
+    float val = 0.f, ls = 0.f;
+#pragma unroll
+    for (int w = 0; w < kOwnWarps; ++w) {
+      const float f = l_s[w][h] > 0.f ? attn_exp2(m_s[w][h] - M) : 0.f;
+      val = fmaf(f, o_s[w][h][d], val);
+      ls = fmaf(f, l_s[w][h], ls);
+    }
+    p.o[(part * rows + row0 + h) * D + d] = val;
+    if (d == 0) p.ml[part * rows + row0 + h] = make_float2(M, ls);
   }
 }
 
+// One warp per row joins its parts, in their order.
+template <int D>
+__global__ void __launch_bounds__(128) prefix_combine_kernel(const PrefixParams p) {
+  constexpr int DPL = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int64_t rows = p.a.B * p.a.Hq, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  pdl_wait();
+  pdl_trigger();
+  if (row >= rows) return;
+  const int parts = p.nsplit + p.nchunk;
+  float M = -INFINITY;
+  for (int i = lane; i < parts; i += 32) {
+    const float2 x = p.ml[i * rows + row];
+    if (x.y > 0.f) M = fmaxf(M, x.x);
+  }
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, w));
+  float o[DPL] = {}, l = 0.f;
+  for (int i = 0; i < parts; ++i) {
+    const float2 x = p.ml[i * rows + row];
+    if (!(x.y > 0.f)) continue;
+    const float f = attn_exp2(x.x - M);
+    l = fmaf(f, x.y, l);
+    const float* s = p.o + (i * rows + row) * D + lane * DPL;
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) o[e] = fmaf(f, s[e], o[e]);
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  __half* out = reinterpret_cast<__half*>(p.a.out) + row * D + lane * DPL;
+#pragma unroll
+  for (int e = 0; e < DPL; e += 2) *reinterpret_cast<__half2*>(out + e) = __floats2half2_rn(o[e] * inv, o[e + 1] * inv);
+}
+
+// ------------------------------------------------------------------- plan
+int row_blocks(const PrefixArgs& a) {
+  const int64_t tps = 128 / (a.Hq / a.Hkv);
+  return (int)((a.B + 2 * tps - 1) / (2 * tps));
+}
+
+int prefix_splits(const PrefixArgs& a) {
+  if (a.prefix_len == 0) return 0;
+  const int64_t tiles = (a.prefix_len + 127) / 128;
+  int64_t n = device_sm_count() / (row_blocks(a) * a.Hkv);   // one CTA per SM
+  n = n < 1 ? 1 : n;
+  return (int)(n > tiles ? tiles : n);
+}
+
+int own_chunks(const PrefixArgs& a) {
+  const int64_t cap = a.table_width * a.page_size;
+  if (cap == 0) return 0;
+  const int64_t ctas = a.B * a.Hkv * ((a.Hq / a.Hkv + 7) / 8);
+  int64_t n = 8 * (int64_t)device_sm_count() / ctas;
+  const int64_t by_len = (cap + 255) / 256;
+  n = n > by_len ? by_len : n;
+  return (int)(n < 1 ? 1 : n);
+}
+
+int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
+
 template <int D>
 cudaError_t launch_t(const PrefixArgs& a, cudaStream_t stream) {
-  int64_t blocks = (a.B * a.Hq + 3) / 4;
-  const int64_t cap = (int64_t)device_sm_count() * 16;
-  if (blocks > cap) blocks = cap;
-  const cudaError_t e = launch_pdl(prefix_rows_kernel<D>, dim3((unsigned)blocks), dim3(128), 0, stream, 1, a);
+  PrefixParams p{};
+  p.a = a;
+  p.G = (int)(a.Hq / a.Hkv);
+  p.tps = 128 / p.G;
+  p.nsplit = prefix_splits(a);
+  p.nchunk = own_chunks(a);
+  const int64_t rows = a.B * a.Hq;
+  p.ml = static_cast<float2*>(a.workspace);
+  p.o = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256((p.nsplit + p.nchunk) * rows * 8));
+  p.scale_log2 = a.scale * kAttnLog2e;
+  p.status = device_status_word();
+  cudaError_t e = cudaSuccess;
+  if (p.nsplit > 0) {
+    p.debug_stall = take_debug_stall() ? 1 : 0;
+    int per_sm = 0;
+    e = prepare_launch_tmem(prefix_tc_kernel<D>, kPrefixThreads, PrefixCfg<D>::BYTES, 512, &per_sm);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(prefix_tc_kernel<D>, dim3((unsigned)row_blocks(a), (unsigned)a.Hkv, (unsigned)p.nsplit),
+                   dim3(kPrefixThreads), PrefixCfg<D>::BYTES, stream, 1, p);
+    if (e != cudaSuccess) return e;
+  }
+  if (p.nchunk > 0) {
+    const int64_t cap = a.table_width * a.page_size;
+    const int chunk = (int)(((cap + p.nchunk - 1) / p.nchunk + 15) / 16 * 16);
+    const int hgroups = (p.G + 7) / 8;
+    e = launch_pdl(own_tokens_kernel<D>, dim3((unsigned)p.nchunk, (unsigned)(a.Hkv * hgroups), (unsigned)a.B),
+                   dim3(kOwnWarps * 32), 0, stream, 1, p, hgroups, chunk);
+    if (e != cudaSuccess) return e;
+  }
+  e = launch_pdl(prefix_combine_kernel<D>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, stream, 1, p);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
-int64_t prefix_attention_workspace(const PrefixArgs&) { return 0; }
+cudaError_t set_wait_limit_prefix(uint64_t ns) { return cudaMemcpyToSymbol(g_prefix_wait_ns, &ns, sizeof(ns)); }
+
+int64_t prefix_attention_workspace(const PrefixArgs& a) {
+  const int64_t parts = prefix_splits(a) + own_chunks(a), rows = a.B * a.Hq;
+  return align256(parts * rows * 8) + parts * rows * a.D * 4;
+}
 
 cudaError_t launch_prefix_attention(const PrefixArgs& a, cudaStream_t stream) {
   if (a.D == 128) return launch_t<128>(a, stream);

@@ -165,9 +165,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
       }
     } else if (warp == 9) {
       // ---------------- MMAs (the whole warp walks the loop, one lane issues)
-      bool ok = ntile == 0 || attn_wait(qbar, 0, abort_flag, g_prompt_wait_ns);
+      bool ok = ntile == 0 || attn_wait_warp(qbar, 0, abort_flag, g_prompt_wait_ns);
       auto wait_full = [&](int n) {
-        return attn_wait(&full[n % NSTG], (uint32_t)(n / NSTG) & 1u, abort_flag, g_prompt_wait_ns);
+        return attn_wait_warp(&full[n % NSTG], (uint32_t)(n / NSTG) & 1u, abort_flag, g_prompt_wait_ns);
       };
       auto qk = [&](int i, int n) {   // scores of tile i with the K tile in ring position n
         if (lane == 0) {
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           if (j >= nt[i]) continue;
-          if (!(ok = attn_wait(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prompt_wait_ns))) break;
+          if (!(ok = attn_wait_warp(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prompt_wait_ns))) break;
           tc_fence_after();
           if (lane == 0) attn_mma_pv<D>(tmem + 256 + i * D, tmem + i * 128, vb, j > 0);
           if (j + 1 < nt[i]) {
@@ -234,8 +234,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     for (int j = 0; j < nti; ++j) {
-      if (!(ok = attn_wait(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prompt_wait_ns))) break;
-      __syncwarp();
+      if (!(ok = attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prompt_wait_ns))) break;
       tc_fence_after();
       uint32_t s[128];
 #pragma unroll
@@ -279,8 +278,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&pbar[i]);
     }
-    if (ok && nti > 0) ok = attn_wait(&obar[i], 0, abort_flag, g_prompt_wait_ns);
-    __syncwarp();
+    if (ok && nti > 0) ok = attn_wait_warp(&obar[i], 0, abort_flag, g_prompt_wait_ns);
     if (ok) {
       tc_fence_after();
       const float inv = l > 0.f ? 1.f / l : 0.f;

@@ -534,7 +534,7 @@ spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, i
     if (!rows_ok(q, ldq, Hq * D)) return SPINQ_EINVAL;
     if (total_k > 0 && (!rows_ok(k, ldk, Hkv * D) || !rows_ok(v, ldv, Hkv * D))) return SPINQ_EINVAL;
   }
-  if ((D != 64 && D != 128) || Hq / Hkv > 128) return SPINQ_EUNSUPPORTED;
+  if ((D != 64 && D != 128) || Hq / Hkv > 128 || Hq > 65535) return SPINQ_EUNSUPPORTED;
   if (batch > 65535 || Hkv > 65535 || total_q > INT32_MAX || total_k > INT32_MAX || max_q > INT32_MAX ||
       max_k > INT32_MAX)
     return SPINQ_EUNSUPPORTED;
@@ -594,7 +594,7 @@ spinq_status spinq_prefix_attention_kv4(const void* q, const spinq_kv4_pages* ca
     if ((prefix_len > 0 && !prefix_table) || (table_width > 0 && !page_table)) return SPINQ_EINVAL;
     if ((prefix_len > 0 || table_width > 0) && cache->num_pages == 0) return SPINQ_EINVAL;
   }
-  if (Hq / Hkv > 128 || B > 65535 || prefix_len > INT32_MAX || table_width > INT32_MAX / cache->page_size)
+  if (Hq / Hkv > 128 || Hq > 65535 || B > 65535 || prefix_len > INT32_MAX || table_width > INT32_MAX / cache->page_size)
     return SPINQ_EUNSUPPORTED;
   if (B == 0) return SPINQ_OK;
   PrefixArgs a = prefix_shape(B, prefix_len, table_width, cache->page_size, Hq, Hkv, D);
@@ -618,7 +618,8 @@ spinq_status spinq_debug_set_wait_limit_ns(int64_t ns) {
   if (ns <= 0) return SPINQ_EINVAL;
   const uint64_t v = (uint64_t)ns;
   if (set_wait_limit_paley(v) != cudaSuccess || set_wait_limit_gemm(v) != cudaSuccess ||
-      set_wait_limit_fp8(v) != cudaSuccess || set_wait_limit_prompt(v) != cudaSuccess)
+      set_wait_limit_fp8(v) != cudaSuccess || set_wait_limit_prompt(v) != cudaSuccess ||
+      set_wait_limit_prefix(v) != cudaSuccess)
     return SPINQ_ECUDA;
   return SPINQ_OK;
 }

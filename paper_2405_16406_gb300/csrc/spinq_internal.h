@@ -321,6 +321,7 @@ cudaError_t set_wait_limit_paley(uint64_t ns);
 cudaError_t set_wait_limit_gemm(uint64_t ns);
 cudaError_t set_wait_limit_fp8(uint64_t ns);
 cudaError_t set_wait_limit_prompt(uint64_t ns);
+cudaError_t set_wait_limit_prefix(uint64_t ns);
 
 // Device status word written by bounded waits that gave up.
 cudaError_t read_and_clear_device_status(int32_t* code, int32_t* detail);

@@ -32,3 +32,34 @@ def test_prompt_attention_gives_up_and_recovers(n, D):
     torch.cuda.synchronize()
     assert spinq.spinq_device_status()[0] == spinq.SPINQ_OK
     assert torch.equal(good, again)
+
+
+def test_prefix_attention_gives_up_and_recovers():
+    import numpy as np
+
+    import kv4_util as ku
+    from paper_2405_16406_gb300 import spinq
+    rng = np.random.default_rng(0)
+    cache = ku.random_cache(spinq, rng, 20, 64, 2, 128)
+    q = torch.from_numpy(rng.standard_normal((3, 8, 128)).astype(np.float16)).cuda()
+    args = (q, cache, torch.arange(16, dtype=torch.int32, device="cuda"), 1000,
+            torch.tensor([[16], [17], [18]], dtype=torch.int32, device="cuda"),
+            torch.tensor([5, 0, 64], dtype=torch.int32, device="cuda"))
+    good = spinq.prefix_attention_kv4(*args)
+    torch.cuda.synchronize()
+    assert spinq.spinq_device_status()[0] == spinq.SPINQ_OK
+    try:
+        assert spinq.spinq_debug_set_wait_limit_ns(1_000_000) == spinq.SPINQ_OK
+        assert spinq.spinq_debug_stall_launches(1) == 0
+        spinq.prefix_attention_kv4(*args)
+        torch.cuda.synchronize()
+        st, site = spinq.spinq_device_status()
+        assert spinq.spinq_debug_stall_launches(0) == 0
+    finally:
+        spinq.spinq_debug_stall_launches(0)
+        assert spinq.spinq_debug_set_wait_limit_ns(DEFAULT_NS) == spinq.SPINQ_OK
+    assert st == spinq.SPINQ_ETIMEOUT and site > 0
+    again = spinq.prefix_attention_kv4(*args)
+    torch.cuda.synchronize()
+    assert spinq.spinq_device_status()[0] == spinq.SPINQ_OK
+    assert torch.equal(good, again)
