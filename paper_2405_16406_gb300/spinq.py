@@ -661,22 +661,24 @@ def kv4_pages(num_pages: int, page_size: int, kv_heads: int, head_dim: int, devi
                     torch.empty(shape + (4,), dtype=torch.float32, device=dev))
 
 
+_F16, _F32, _U8, _I32, _I64T = torch.float16, torch.float32, torch.uint8, torch.int32, torch.int64
+
+
 def _pages(cache: KV4Pages) -> Kv4PagesCfg:
-    n, h, p, half = cache.k_codes.shape
-    assert cache.k_codes.dtype == torch.uint8 and cache.k_codes.is_contiguous()
-    assert cache.v_codes.dtype == torch.uint8 and cache.v_codes.is_contiguous()
-    assert cache.v_codes.shape == cache.k_codes.shape
-    assert cache.scales.dtype == torch.float32 and cache.scales.is_contiguous()
-    assert cache.scales.shape == (n, h, p, 4)
-    return Kv4PagesCfg(cache.k_codes.data_ptr(), cache.v_codes.data_ptr(), cache.scales.data_ptr(), n, p, h, 2 * half)
+    kc, vc, sc = cache.k_codes, cache.v_codes, cache.scales
+    shape = kc.shape
+    n, h, p, half = shape
+    assert kc.dtype == _U8 and kc.is_contiguous() and vc.dtype == _U8 and vc.is_contiguous() and vc.shape == shape
+    assert sc.dtype == _F32 and sc.is_contiguous() and sc.shape == (n, h, p, 4)
+    return Kv4PagesCfg(kc.data_ptr(), vc.data_ptr(), sc.data_ptr(), n, p, h, 2 * half)
 
 
 def _token_rows(x: torch.Tensor) -> int:
     """The distance in elements of the tokens of x [T, H, D], whose heads are contiguous."""
-    assert x.dtype == torch.float16 and x.dim() == 3
     T, H, D = x.shape
-    assert (D == 1 or x.stride(2) == 1) and (H <= 1 or x.stride(1) == D), "a token's heads must be contiguous"
-    return x.stride(0) if T > 1 else max(x.stride(0), (H * D + 7) // 8 * 8)
+    st = x.stride()
+    assert x.dtype == _F16 and (D == 1 or st[2] == 1) and (H <= 1 or st[1] == D), "a token's heads must be contiguous"
+    return st[0] if T > 1 else max(st[0], (H * D + 7) // 8 * 8)
 
 
 def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
@@ -689,8 +691,15 @@ def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.T
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _ids(x: Optional[torch.Tensor], dtype=torch.int32) -> None:
-    assert x is None or (x.dtype == dtype and x.is_contiguous())
+def _full(x: torch.Tensor, dtype, shape) -> int:
+    """The address of a contiguous tensor of this type and shape."""
+    assert x.dtype == dtype and x.is_contiguous() and x.shape == shape, "wrong type, layout or shape"
+    return x.data_ptr()
+
+
+def _queue(stream: Optional[torch.cuda.Stream], x: torch.Tensor) -> int:
+    """The raw handle of the stream a call runs on (by default the current one of x's device)."""
+    return torch._C._cuda_getCurrentRawStream(x.get_device()) if stream is None else stream.cuda_stream
 
 
 def kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: KV4Pages, slots: torch.Tensor,
@@ -704,29 +713,27 @@ def kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cach
     [max_pos, rotary_dim/2, 2] with ``positions`` [T] (int32), or None."""
     T, Hkv, D = k.shape
     pages = _pages(cache)
-    assert (Hkv, D) == (pages.kv_heads, pages.head_dim) and v.shape == k.shape
-    _ids(slots, torch.int64)
-    assert slots.numel() == T
-    Hq = 0 if q is None else q.shape[1]
+    assert Hkv == pages.kv_heads and D == pages.head_dim and v.shape == k.shape
+    Hq = ldq = 0
+    q_ptr = out_ptr = None
     if q is not None:
+        Hq = q.shape[1]
         assert q.shape == (T, Hq, D)
+        ldq, q_ptr = _token_rows(q), q.data_ptr()
         if q_out is None:
-            q_out = _empty((T, Hq, D), torch.float16, q.device, stream)
-        assert q_out.dtype == torch.float16 and q_out.is_contiguous() and q_out.shape == (T, Hq, D)
-    for w in (q_weight, k_weight):
-        assert w is None or (w.dtype == torch.float16 and w.is_contiguous() and w.numel() == D)
+            q_out = _empty((T, Hq, D), _F16, q.device, stream)
+        out_ptr = _full(q_out, _F16, (T, Hq, D))
     rope = None
     if cos_sin is not None:
-        _ids(positions)
-        assert positions is not None and positions.numel() == T
-        assert cos_sin.dtype == torch.float32 and cos_sin.is_contiguous() and cos_sin.shape[2] == 2
-        rope = ctypes.byref(RopeCfg(2 * cos_sin.shape[1], int(bool(interleaved)), positions.data_ptr(),
-                                    cos_sin.data_ptr(), cos_sin.shape[0]))
-    kvq = quant_cfg(4, False, SPINQ_PER_GROUP, D, clip)
-    _check(_lib.spinq_kv4_append(_ptr(q), 0 if q is None else _token_rows(q), _ptr(q_out), _ptr(k), _token_rows(k),
-                                 _ptr(v), _token_rows(v), T, Hq, _ptr(q_weight), _ptr(k_weight), float(eps), rope,
-                                 ctypes.byref(kvq), ctypes.byref(pages), _ptr(slots), _stream(stream)),
-           "spinq_kv4_append")
+        assert positions is not None and cos_sin.dim() == 3
+        n, half, _ = cos_sin.shape
+        rope = ctypes.byref(RopeCfg(2 * half, int(bool(interleaved)), _full(positions, _I32, (T,)),
+                                    _full(cos_sin, _F32, (n, half, 2)), n))
+    _check(_lib.spinq_kv4_append(q_ptr, ldq, out_ptr, k.data_ptr(), _token_rows(k), v.data_ptr(), _token_rows(v), T, Hq,
+                                 None if q_weight is None else _full(q_weight, _F16, (D,)),
+                                 None if k_weight is None else _full(k_weight, _F16, (D,)), eps, rope,
+                                 QuantCfg(4, 0, SPINQ_PER_GROUP, D, clip), pages, _full(slots, _I64T, (T,)),
+                                 _queue(stream, k)), "spinq_kv4_append")
     return q_out
 
 
@@ -738,17 +745,15 @@ def kv4_read(cache: KV4Pages, page_table: torch.Tensor, cu_tokens: torch.Tensor,
     rows cu_tokens[b] .. cu_tokens[b + 1] - 1."""
     pages = _pages(cache)
     batch, width = page_table.shape
-    for x in (page_table, cu_tokens, starts):
-        _ids(x)
-    assert cu_tokens.numel() == batch + 1 and (starts is None or starts.numel() == batch)
     shape = (total, pages.kv_heads, pages.head_dim)
-    dev = cache.k_codes.device
-    k = _empty(shape, torch.float16, dev, stream) if k is None else k
-    v = _empty(shape, torch.float16, dev, stream) if v is None else v
-    for x in (k, v):
-        assert x.dtype == torch.float16 and x.is_contiguous() and x.shape == shape
-    _check(_lib.spinq_kv4_read(ctypes.byref(pages), _ptr(page_table), batch, width, _ptr(starts), _ptr(cu_tokens),
-                               total, _ptr(k), _ptr(v), _stream(stream)), "spinq_kv4_read")
+    if k is None:
+        k = _empty(shape, _F16, cache.k_codes.device, stream)
+    if v is None:
+        v = _empty(shape, _F16, cache.k_codes.device, stream)
+    _check(_lib.spinq_kv4_read(pages, _full(page_table, _I32, (batch, width)), batch, width,
+                               None if starts is None else _full(starts, _I32, (batch,)),
+                               _full(cu_tokens, _I32, (batch + 1,)), total, _full(k, _F16, shape),
+                               _full(v, _F16, shape), _queue(stream, k)), "spinq_kv4_read")
     return k, v
 
 
@@ -759,23 +764,24 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     """Attention of packed prompts q [Tq, Hq, D] over k, v [Tk, Hkv, D] (strided
     tokens); sequence b has rows cu[b] .. cu[b + 1] - 1 (int32 [B + 1])."""
     Tq, Hq, D = q.shape
-    Tk, Hkv = k.shape[0], k.shape[1]
+    Tk, Hkv, _ = k.shape
     assert k.shape == v.shape and k.shape[2] == D
-    for x in (cu_q, cu_k):
-        _ids(x)
-    batch = cu_q.numel() - 1
-    assert cu_k.numel() == batch + 1
+    batch = cu_q.shape[0] - 1
     if out is None:
-        out = _empty((Tq, Hq, D), torch.float16, q.device, stream)
-    assert out.dtype == torch.float16 and out.is_contiguous() and out.shape == q.shape
-    if workspace is None:
-        need = spinq_prompt_attention_workspace_bytes(batch, max_q, max_k, Hq, Hkv, D)
-        workspace = _empty(need, torch.uint8, q.device, stream) if need else None
-    sc = 1.0 / (D ** 0.5) if scale is None else float(scale)
-    _check(_lib.spinq_prompt_attention(_ptr(q), _token_rows(q), _ptr(k), _token_rows(k), _ptr(v), _token_rows(v),
-                                       _ptr(cu_q), _ptr(cu_k), batch, Tq, Tk, max_q, max_k, Hq, Hkv, D,
-                                       int(bool(causal)), sc, _ptr(out), _ptr(workspace),
-                                       0 if workspace is None else workspace.numel(), _stream(stream)),
+        out = _empty((Tq, Hq, D), _F16, q.device, stream)
+    ws, need = None, 0
+    if workspace is not None:
+        ws, need = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    else:
+        need = _lib.spinq_prompt_attention_workspace_bytes(batch, max_q, max_k, Hq, Hkv, D)
+        if need:
+            workspace = _empty(need, _U8, q.device, stream)
+            ws = workspace.data_ptr()
+    _check(_lib.spinq_prompt_attention(q.data_ptr(), _token_rows(q), k.data_ptr(), _token_rows(k), v.data_ptr(),
+                                       _token_rows(v), _full(cu_q, _I32, (batch + 1,)),
+                                       _full(cu_k, _I32, (batch + 1,)), batch, Tq, Tk, max_q, max_k, Hq, Hkv, D,
+                                       int(bool(causal)), D ** -0.5 if scale is None else scale,
+                                       _full(out, _F16, (Tq, Hq, D)), ws, need, _queue(stream, q)),
            "spinq_prompt_attention")
     return out
 
@@ -789,21 +795,22 @@ def prefix_attention_kv4(q: torch.Tensor, cache: KV4Pages, prefix_table: torch.T
     ``lens`` [B] tokens of ``page_table`` [B, W]."""
     B, Hq, D = q.shape
     pages = _pages(cache)
-    assert q.dtype == torch.float16 and q.is_contiguous() and D == pages.head_dim
-    for x in (prefix_table, page_table, lens):
-        _ids(x)
+    assert D == pages.head_dim
     width = page_table.shape[1]
-    assert page_table.shape[0] == B and lens.numel() == B
     assert prefix_table.numel() * pages.page_size >= prefix_len
     if out is None:
-        out = _empty(q.shape, torch.float16, q.device, stream)
-    assert out.dtype == torch.float16 and out.is_contiguous() and out.shape == q.shape
-    if workspace is None:
-        need = spinq_prefix_attention_workspace_bytes(B, prefix_len, width, pages.page_size, Hq, pages.kv_heads, D)
-        workspace = _empty(need, torch.uint8, q.device, stream) if need else None
-    sc = 1.0 / (D ** 0.5) if scale is None else float(scale)
-    _check(_lib.spinq_prefix_attention_kv4(_ptr(q), ctypes.byref(pages), _ptr(prefix_table), prefix_len,
-                                           _ptr(page_table), width, _ptr(lens), B, Hq, sc, _ptr(out),
-                                           _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                                           _stream(stream)), "spinq_prefix_attention_kv4")
+        out = _empty((B, Hq, D), _F16, q.device, stream)
+    ws, need = None, 0
+    if workspace is not None:
+        ws, need = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    else:
+        need = _lib.spinq_prefix_attention_workspace_bytes(B, prefix_len, width, pages.page_size, Hq, pages.kv_heads, D)
+        if need:
+            workspace = _empty(need, _U8, q.device, stream)
+            ws = workspace.data_ptr()
+    _check(_lib.spinq_prefix_attention_kv4(_full(q, _F16, (B, Hq, D)), pages,
+                                           _full(prefix_table, _I32, prefix_table.shape), prefix_len,
+                                           _full(page_table, _I32, (B, width)), width, _full(lens, _I32, (B,)), B, Hq,
+                                           D ** -0.5 if scale is None else scale, _full(out, _F16, (B, Hq, D)), ws,
+                                           need, _queue(stream, q)), "spinq_prefix_attention_kv4")
     return out
