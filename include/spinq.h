@@ -449,6 +449,7 @@ typedef struct {
  *   kvq    bits = 4, symmetric = 0, granularity = SPINQ_PER_GROUP, group_size = D.
  *   slots  [T] int64 slot numbers, distinct; a token whose number is outside
  *          the cache (e.g. -1, padding) is not written, its q_out is.
+ *   Supported: T times the larger head count below 2^31.
  */
 spinq_status spinq_kv4_append(const void* q, int64_t ldq, void* q_out, const void* k, int64_t ldk, const void* v,
                               int64_t ldv, int64_t T, int64_t Hq, const void* q_weight, const void* k_weight,
@@ -463,7 +464,7 @@ spinq_status spinq_kv4_append(const void* q, int64_t ldq, void* q_out, const voi
  *        for the context of a prompt that arrives in chunks).
  *   page_table [batch][table_width] int32;  starts [batch] int32 or NULL (0);
  *   cu_tokens [batch + 1] int32 ascending from 0, cu_tokens[batch] = total.
- *   Tokens past the page table read as zeros.
+ *   Tokens past the page table read as zeros.  total * kv_heads < 2^31.
  */
 spinq_status spinq_kv4_read(const spinq_kv4_pages* cache, const int32_t* page_table, int64_t batch,
                             int64_t table_width, const int32_t* starts, const int32_t* cu_tokens, int64_t total,

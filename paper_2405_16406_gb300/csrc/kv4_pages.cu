@@ -17,11 +17,17 @@
 // bit 1, ... (the norm's sum of squares and the butterflies alike), so the
 // result does not depend on how the rows are spread over the lanes.
 //
-// Layout.  A quad of lanes owns a row, a warp 8 rows of one token.  Lane c
-// holds the values [Cc, Cc + C) and [D/2 + Cc, D/2 + Cc + C), C = D/8: the
-// pairs (i, i + D/2) of the rotate-half form over the whole head sit in one
-// lane, as do neighbouring pairs, and only the two middle bits of the transform go
-// through shuffles.
+// Append layout.  A quad of lanes owns a row, a warp 8 rows of one kind (all
+// query heads of all tokens, then key heads, then value heads).  Lane c holds
+// the runs [Cc, Cc + C) and [D/2 + Cc, D/2 + Cc + C), C = D/8, as pairs (i, i + D/2)
+// in packed fp32: a rotate-half pair over the whole head is one register
+// pair, every butterfly but the last works on packed pairs, and only the two
+// middle bits of the transform go through shuffles.  Bound: instruction
+// issue (about 400 per warp and 8 rows) close to the memory's time.
+//
+// Read layout.  A warp expands 16 tokens of one kv head, whose codes are one
+// run of a page wherever the tokens are; the warps of a block take the heads of the same
+// tokens, whose output rows lie next to one another.
 #include <cuda_fp16.h>
 #include <float.h>
 
@@ -35,255 +41,242 @@ namespace {
 constexpr int kAppendWarps = 4;
 constexpr int kReadWarps = 8;
 
+// The product of two packed pairs, rounded before whatever is added to it:
+// a product written as such is fused with a following packed sum
+// (one rounding instead of two), which the fixed order of this file's sums excludes.
+__device__ __forceinline__ F2 f2_product(F2 a, F2 b) { return f2_fma(a, b, f2_make(0.f, 0.f)); }
+
 enum RopeForm { kRopeNone = 0, kRopePairs = 1, kRopeHalves = 2, kRopePartHalves = 3 };
 
 // D = head_dim, ROPE one of RopeForm:
 //   kRopePairs       neighbouring pairs (2i, 2i+1) of the first R values;
-//   kRopeHalves      pairs (i, i + D/2), R = D: both in the lane;
+//   kRopeHalves      pairs (i, i + D/2), R = D: one register pair;
 //   kRopePartHalves  pairs (i, i + R/2), R < D a multiple of D/4: the partner
 //                    is a whole C-value run of another lane of the quad.
 template <int D, bool CLAMP, int ROPE>
-__global__ void __launch_bounds__(kAppendWarps * 32) kv4_append_kernel(AppendArgs a, int64_t units, int groups) {
+__global__ void __launch_bounds__(kAppendWarps * 32) kv4_append_kernel(AppendArgs a, uint32_t uq, uint32_t uk) {
   constexpr int C = D / 8;    // values per run; a lane holds two runs
   constexpr int CV = C / 8;   // 16-byte loads per run
   const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const int64_t stride = (int64_t)gridDim.x * kAppendWarps;
+  const uint32_t units = uq + 2 * uk, stride = gridDim.x * kAppendWarps;
   pdl_wait();
   pdl_trigger();
-  for (int64_t u = (int64_t)blockIdx.x * kAppendWarps + (threadIdx.x >> 5); u < units; u += stride) {
-    const int64_t t = u / groups;
-    const int row = (int)(u - t * groups) * 8 + g;   // query heads, then key heads, then value heads
-    const int rows = (int)(a.Hq + 2 * a.Hkv);
-    const bool valid = row < rows;
-    const int kind = row < a.Hq ? 0 : (row < a.Hq + a.Hkv ? 1 : 2);
-    const int h = kind == 0 ? row : (kind == 1 ? row - (int)a.Hq : row - (int)(a.Hq + a.Hkv));
+  for (uint32_t u = blockIdx.x * kAppendWarps + (threadIdx.x >> 5); u < units; u += stride) {
+    const int kind = u < uq ? 0 : (u < uq + uk ? 1 : 2);   // the warp's rows: queries, keys or values
+    const uint32_t H = (uint32_t)(kind == 0 ? a.Hq : a.Hkv);
+    const uint32_t row = (kind == 0 ? u : (kind == 1 ? u - uq : u - uq - uk)) * 8 + g;
+    const uint32_t t = row / H, h = row - t * H;
+    const bool valid = t < (uint32_t)a.T;
     const __half* src = reinterpret_cast<const __half*>(kind == 0 ? a.q : (kind == 1 ? a.k : a.v)) +
-                        t * (kind == 0 ? a.ldq : (kind == 1 ? a.ldk : a.ldv)) + (int64_t)h * D;
-    float y[2][C];
+                        (int64_t)t * (kind == 0 ? a.ldq : (kind == 1 ? a.ldk : a.ldv)) + h * D + c * C;
+    uint4 in[2][CV];
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
+      for (int i = 0; i < CV; ++i)
+        in[s][i] = valid ? __ldg(reinterpret_cast<const uint4*>(src + s * (D / 2)) + i) : make_uint4(0, 0, 0, 0);
+    F2 y[C];   // (value Cc + i, value D/2 + Cc + i)
+    auto pairs = [&](const uint4 (&w)[2][CV], F2* out) {
+#pragma unroll
       for (int i = 0; i < CV; ++i) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (valid) w = __ldg(reinterpret_cast<const uint4*>(src + s * (D / 2) + c * C) + i);
-        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+        const uint32_t lo[4] = {w[0][i].x, w[0][i].y, w[0][i].z, w[0][i].w};
+        const uint32_t hi[4] = {w[1][i].x, w[1][i].y, w[1][i].z, w[1][i].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&ws[j]));
-          y[s][8 * i + 2 * j] = f.x;
-          y[s][8 * i + 2 * j + 1] = f.y;
+          const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&lo[j]));
+          const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&hi[j]));
+          out[8 * i + 2 * j] = f2_make(p.x, q.x);
+          out[8 * i + 2 * j + 1] = f2_make(p.y, q.y);
         }
       }
+    };
+    pairs(in, y);
 
-    // ---- norm of the head (queries and keys)
-    const __half* wt = reinterpret_cast<const __half*>(kind == 0 ? a.q_weight : a.k_weight);
-    const bool norm = valid && kind != 2 && wt != nullptr;
-    if (__any_sync(0xffffffffu, norm)) {
-      float part[2];
+    if (kind != 2) {
+      // ---- norm of the head
+      const __half* wt = reinterpret_cast<const __half*>(kind == 0 ? a.q_weight : a.k_weight);
+      if (wt != nullptr) {
+        F2 sq[C];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        float sq[C];
-#pragma unroll
-        for (int i = 0; i < C; ++i) sq[i] = __fmul_rn(y[s][i], y[s][i]);
+        for (int i = 0; i < C; ++i) sq[i] = f2_product(y[i], y[i]);
 #pragma unroll
         for (int w = C / 2; w >= 1; w >>= 1)   // neighbours first
 #pragma unroll
-          for (int i = 0; i < w; ++i) sq[i] = __fadd_rn(sq[2 * i], sq[2 * i + 1]);
-        part[s] = sq[0];
-        part[s] = __fadd_rn(part[s], __shfl_xor_sync(0xffffffffu, part[s], 1));
-        part[s] = __fadd_rn(part[s], __shfl_xor_sync(0xffffffffu, part[s], 2));
-      }
-      if (norm) {
-        const float ms = __fadd_rn(part[0], part[1]) * (1.f / D);   // D is a power of two: exact
-        const float r = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(ms, a.eps)));
+          for (int i = 0; i < w; ++i) sq[i] = f2_add(sq[2 * i], sq[2 * i + 1]);
+        float p0, p1;
+        f2_split(sq[0], p0, p1);
+#pragma unroll
+        for (int b = 1; b < 4; b <<= 1) {
+          p0 = __fadd_rn(p0, __shfl_xor_sync(0xffffffffu, p0, b));
+          p1 = __fadd_rn(p1, __shfl_xor_sync(0xffffffffu, p1, b));
+        }
+        const float ms = __fadd_rn(p0, p1) * (1.f / D);   // D is a power of two: exact
+        const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(ms, a.eps)));
+        uint4 ww[2][CV];
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int i = 0; i < CV; ++i) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4*>(wt + s * (D / 2) + c * C) + i);
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+          for (int i = 0; i < CV; ++i) ww[s][i] = __ldg(reinterpret_cast<const uint4*>(wt + s * (D / 2) + c * C) + i);
+        F2 wf[C];
+        pairs(ww, wf);
+        const F2 rr = f2_make(r, r);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&ws[j]));
-              y[s][8 * i + 2 * j] = __fmul_rn(__fmul_rn(y[s][8 * i + 2 * j], r), f.x);
-              y[s][8 * i + 2 * j + 1] = __fmul_rn(__fmul_rn(y[s][8 * i + 2 * j + 1], r), f.y);
-            }
-          }
+        for (int i = 0; i < C; ++i) y[i] = f2_product(f2_product(y[i], rr), wf[i]);
       }
-    }
 
-    // ---- rotary embedding of the first R values (queries and keys)
-    if (ROPE != kRopeNone) {
-      const int half = a.rotary / 2;
-      int64_t pos = valid ? (int64_t)a.positions[t] : 0;
-      pos = pos < 0 ? 0 : (pos >= a.max_pos ? a.max_pos - 1 : pos);
-      const float2* cs = reinterpret_cast<const float2*>(a.cos_sin) + pos * half;
-      if (ROPE == kRopePairs) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
+      // ---- rotary embedding of the first R values
+      if (ROPE != kRopeNone) {
+        const int half = a.rotary / 2;
+        int64_t pos = valid ? (int64_t)__ldg(a.positions + t) : 0;
+        pos = pos < 0 ? 0 : (pos >= a.max_pos ? a.max_pos - 1 : pos);
+        const float2* cs = reinterpret_cast<const float2*>(a.cos_sin) + pos * half;
+        if (ROPE == kRopePairs) {
+          // the runs' neighbouring pairs, angles (Cc + i)/2 and D/4 + (Cc + i)/2; past R: cos 1, sin 0
 #pragma unroll
           for (int i = 0; i < C; i += 2) {
-            const int e = s * (D / 2) + c * C + i;
-            if (kind != 2 && e < a.rotary) {
-              const float2 f = __ldg(cs + e / 2);
-              const float p = y[s][i], q = y[s][i + 1];
-              y[s][i] = __fsub_rn(__fmul_rn(p, f.x), __fmul_rn(q, f.y));
-              y[s][i + 1] = __fadd_rn(__fmul_rn(p, f.y), __fmul_rn(q, f.x));
-            }
+            const int e = (c * C + i) / 2;
+            const float2 f0 = e < half ? __ldg(cs + e) : make_float2(1.f, 0.f);
+            const float2 f1 = e + D / 4 < half ? __ldg(cs + e + D / 4) : make_float2(1.f, 0.f);
+            const F2 co = f2_make(f0.x, f1.x), si = f2_make(f0.y, f1.y);
+            const F2 p = y[i], q = y[i + 1];
+            y[i] = f2_sub(f2_product(p, co), f2_product(q, si));
+            y[i + 1] = f2_add(f2_product(p, si), f2_product(q, co));
           }
-      } else if (ROPE == kRopeHalves) {
-        if (kind != 2) {
+        } else if (ROPE == kRopeHalves) {
 #pragma unroll
           for (int i = 0; i < C; i += 2) {
             const float4 f = __ldg(reinterpret_cast<const float4*>(cs + c * C + i));
-            const float p0 = y[0][i], q0 = y[1][i], p1 = y[0][i + 1], q1 = y[1][i + 1];
-            y[0][i] = __fsub_rn(__fmul_rn(p0, f.x), __fmul_rn(q0, f.y));
-            y[1][i] = __fadd_rn(__fmul_rn(p0, f.y), __fmul_rn(q0, f.x));
-            y[0][i + 1] = __fsub_rn(__fmul_rn(p1, f.z), __fmul_rn(q1, f.w));
-            y[1][i + 1] = __fadd_rn(__fmul_rn(p1, f.w), __fmul_rn(q1, f.z));
+            float p, q;
+            f2_split(y[i], p, q);
+            y[i] = f2_add(f2_product(y[i], f2_make(f.x, f.x)), f2_product(f2_make(q, p), f2_make(-f.y, f.y)));
+            f2_split(y[i + 1], p, q);
+            y[i + 1] = f2_add(f2_product(y[i + 1], f2_make(f.z, f.z)), f2_product(f2_make(q, p), f2_make(-f.w, f.w)));
           }
-        }
-      } else {
-        // run number c + 4 s; the partner run is R/2 values away
-        const int hop = half / C;
-        float o[2][C];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int run = c + 4 * s, other = run < hop ? run + hop : run - hop;
-          const int from = (lane & ~3) | (other & 3);
+        } else {
+          // run number c (first of the pair) or c + 4 (second); the partner run is R/2 values away
+          const int hop = half / C;
+          const int o0 = c < hop ? c + hop : c - hop, o1 = c + 4 < hop ? c + 4 + hop : c + 4 - hop;
+          const bool turn0 = c < 2 * hop, turn1 = c + 4 < 2 * hop, first0 = c < hop, first1 = c + 4 < hop;
+          const float2* f0 = cs + (first0 ? c : c - hop) * C;
+          const float2* f1 = cs + (first1 ? c + 4 : c + 4 - hop) * C;
 #pragma unroll
           for (int i = 0; i < C; ++i) {
-            const float lo = __shfl_sync(0xffffffffu, y[0][i], from), hi = __shfl_sync(0xffffffffu, y[1][i], from);
-            o[s][i] = other & 4 ? hi : lo;
-          }
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int run = c + 4 * s;
-          if (kind != 2 && run < 2 * hop) {
-            const bool first = run < hop;
-            const float2* f0 = cs + (first ? run : run - hop) * C;
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
+            float v0, v1;
+            f2_split(y[i], v0, v1);
+            const int from0 = (lane & ~3) | (o0 & 3), from1 = (lane & ~3) | (o1 & 3);
+            const float a0 = __shfl_sync(0xffffffffu, v0, from0), b0 = __shfl_sync(0xffffffffu, v1, from0);
+            const float a1 = __shfl_sync(0xffffffffu, v0, from1), b1 = __shfl_sync(0xffffffffu, v1, from1);
+            if (turn0) {
               const float2 f = __ldg(f0 + i);
-              const float p = __fmul_rn(y[s][i], f.x), q = __fmul_rn(o[s][i], f.y);
-              y[s][i] = first ? __fsub_rn(p, q) : __fadd_rn(p, q);
+              const float p = __fmul_rn(v0, f.x), q = __fmul_rn(o0 & 4 ? b0 : a0, f.y);
+              v0 = first0 ? __fsub_rn(p, q) : __fadd_rn(p, q);
             }
+            if (turn1) {
+              const float2 f = __ldg(f1 + i);
+              const float p = __fmul_rn(v1, f.x), q = __fmul_rn(o1 & 4 ? b1 : a1, f.y);
+              v1 = first1 ? __fsub_rn(p, q) : __fadd_rn(p, q);
+            }
+            y[i] = f2_make(v0, v1);
           }
         }
       }
-    }
 
-    // ---- R3: bits 0 .. log2 C - 1 in the lane, the two lane bits, the top bit in the lane
-    if (__any_sync(0xffffffffu, valid && kind != 2)) {
-      float z[2][C];
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < C; ++i) z[s][i] = y[s][i];
+      // ---- R3: bits 0 .. log2 C - 1 in the lane, the two lane bits, the pair's bit
 #pragma unroll
       for (int bit = 1; bit < C; bit <<= 1)
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int i = 0; i < C; ++i)
-            if (!(i & bit)) {
-              const float p = z[s][i], q = z[s][i | bit];
-              z[s][i] = __fadd_rn(p, q);
-              z[s][i | bit] = __fsub_rn(p, q);
-            }
+        for (int i = 0; i < C; ++i)
+          if (!(i & bit)) f2_bfly(y[i], y[i | bit]);
 #pragma unroll
       for (int bit = 1; bit < 4; bit <<= 1) {
-        const float sg = c & bit ? -1.f : 1.f;
+        const float sg = c & bit ? -1.f : 1.f;   // the upper lane's value enters with a minus sign (exact product)
+        const F2 sg2 = f2_make(sg, sg);
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int i = 0; i < C; ++i)   // the upper lane's value enters with a minus sign (exact product)
-            z[s][i] = fmaf(z[s][i], sg, __shfl_xor_sync(0xffffffffu, z[s][i], bit));
+        for (int i = 0; i < C; ++i) {
+          float p, q;
+          f2_split(y[i], p, q);
+          y[i] = f2_fma(y[i], sg2, f2_make(__shfl_xor_sync(0xffffffffu, p, bit), __shfl_xor_sync(0xffffffffu, q, bit)));
+        }
       }
 #pragma unroll
-      for (int i = 0; i < C; ++i) {
-        const float p = z[0][i], q = z[1][i];
-        z[0][i] = __fadd_rn(p, q);
-        z[1][i] = __fsub_rn(p, q);
-      }
-      if (kind != 2) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int i = 0; i < C; ++i) y[s][i] = z[s][i];
-      }
+      for (int i = 0; i < C; ++i) f2_bfly_inner(y[i]);
     }
 
-    if (valid && kind == 0) {
-      __half* dst = reinterpret_cast<__half*>(a.q_out) + (t * a.Hq + h) * D + c * C;
+    if (kind == 0) {
+      if (valid) {
+        __half* dst = reinterpret_cast<__half*>(a.q_out) + (int64_t)row * D + c * C;
+        const F2 nn = f2_make(a.norm, a.norm);
+        uint32_t w[2][C / 2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < CV; ++i) {
-          uint4 w;
-          w.x = pack_half2_bits(y[s][8 * i] * a.norm, y[s][8 * i + 1] * a.norm);
-          w.y = pack_half2_bits(y[s][8 * i + 2] * a.norm, y[s][8 * i + 3] * a.norm);
-          w.z = pack_half2_bits(y[s][8 * i + 4] * a.norm, y[s][8 * i + 5] * a.norm);
-          w.w = pack_half2_bits(y[s][8 * i + 6] * a.norm, y[s][8 * i + 7] * a.norm);
-          reinterpret_cast<uint4*>(dst + s * (D / 2))[i] = w;
+        for (int i = 0; i < C; i += 2) {
+          float p0, q0, p1, q1;
+          f2_split(f2_product(y[i], nn), p0, q0);
+          f2_split(f2_product(y[i + 1], nn), p1, q1);
+          w[0][i / 2] = pack_half2_bits(p0, p1);
+          w[1][i / 2] = pack_half2_bits(q0, q1);
         }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int i = 0; i < CV; ++i)
+            reinterpret_cast<uint4*>(dst + s * (D / 2))[i] =
+                make_uint4(w[s][4 * i], w[s][4 * i + 1], w[s][4 * i + 2], w[s][4 * i + 3]);
+      }
+      continue;
     }
 
     // ---- Eq. 1 over the row, into its slot
-    if (__any_sync(0xffffffffu, valid && kind != 0)) {
-      float hi = -FLT_MAX, lo = FLT_MAX;
+    float hi = -FLT_MAX, lo = FLT_MAX;
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+    for (int i = 0; i < C; ++i) {
+      float p, q;
+      f2_split(y[i], p, q);
+      asm("max.f32 %0, %0, %1, %2;\n" : "+f"(hi) : "f"(p), "f"(q));
+      asm("min.f32 %0, %0, %1, %2;\n" : "+f"(lo) : "f"(p), "f"(q));
+    }
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-          hi = fmaxf(hi, y[s][i]);
-          lo = fminf(lo, y[s][i]);
-        }
+    for (int b = 1; b < 4; b <<= 1) {
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, b));
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, b));
+    }
+    if (CLAMP) {
+      hi *= a.clip;
+      lo *= a.clip;
+    }
+    const float span = __fsub_rn(hi, lo);
+    // one reciprocal per row, a product per value: a code differs from Eq. 1's
+    // quotient only for a value within 2^-20 of the middle of two codes
+    const float inv = span > 0.f ? __fmul_rn(__frcp_rn(span), 15.f) : 0.f;
+    const F2 lo2 = f2_make(lo, lo), inv2 = f2_make(inv, inv), mg2 = f2_make(kRoundMagic, kRoundMagic);
+    uint32_t r[2][C];
 #pragma unroll
-      for (int b = 1; b < 4; b <<= 1) {
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, b));
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, b));
-      }
+    for (int i = 0; i < C; ++i) {
+      F2 v = f2_product(f2_sub(y[i], lo2), inv2);
+      float p, q;
       if (CLAMP) {
-        hi *= a.clip;
-        lo *= a.clip;
+        f2_split(v, p, q);
+        v = f2_make(fminf(fmaxf(p, 0.f), 15.f), fminf(fmaxf(q, 0.f), 15.f));
       }
-      const float span = __fsub_rn(hi, lo);
-      // one reciprocal per row, a product per value: a code differs from Eq. 1's
-      // quotient only for a value within 2^-20 of the middle of two codes
-      const float inv = span > 0.f ? __fmul_rn(__frcp_rn(span), 15.f) : 0.f;
-      uint32_t words[2][CV];
+      f2_split(f2_add(v, mg2), p, q);
+      r[0][i] = __float_as_uint(p);
+      r[1][i] = __float_as_uint(q);
+    }
+    const int64_t slot = valid ? __ldg(a.slots + t) : -1;
+    if (slot >= 0 && slot < a.num_slots) {
+      const int64_t page = slot >> a.page_shift, in_page = slot & (a.page_size - 1);
+      const int64_t at = (page * a.Hkv + h) * a.page_size + in_page;
+      uint8_t* codes = (kind == 1 ? a.k_codes : a.v_codes) + at * (D / 2) + c * (C / 2);
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < CV; ++i) {
-          uint32_t r[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float v = __fmul_rn(__fsub_rn(y[s][8 * i + j], lo), inv);
-            if (CLAMP) v = fminf(fmaxf(v, 0.f), 15.f);
-            r[j] = round_bits(v);
-          }
-          words[s][i] = pack8_nibbles(r);
-        }
-      const int64_t slot = valid && kind != 0 ? a.slots[t] : -1;
-      if (slot >= 0 && slot < a.num_slots) {
-        const int64_t page = slot / a.page_size, in_page = slot - page * a.page_size;
-        const int64_t at = (page * a.Hkv + h) * a.page_size + in_page;
-        uint8_t* codes = (kind == 1 ? a.k_codes : a.v_codes) + at * (D / 2) + c * (C / 2);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          if (CV == 2)
-            *reinterpret_cast<uint2*>(codes + s * (D / 4)) = make_uint2(words[s][0], words[s][1 % CV]);
-          else
-            *reinterpret_cast<uint32_t*>(codes + s * (D / 4)) = words[s][0];
-        }
-        if (c == 0) {
-          const float nrm = kind == 1 ? a.norm : 1.f;
-          reinterpret_cast<float2*>(a.scales + at * 4)[kind - 1] =
-              make_float2(__fmul_rn(__fdiv_rn(span, 15.f), nrm), __fmul_rn(lo, nrm));
-        }
+      for (int s = 0; s < 2; ++s) {
+        if constexpr (CV == 2)
+          *reinterpret_cast<uint2*>(codes + s * (D / 4)) = make_uint2(pack8_nibbles(r[s]), pack8_nibbles(r[s] + 8));
+        else
+          *reinterpret_cast<uint32_t*>(codes + s * (D / 4)) = pack8_nibbles(r[s]);
+      }
+      if (c == 0) {
+        const float nrm = kind == 1 ? a.norm : 1.f;
+        reinterpret_cast<float2*>(a.scales + at * 4)[kind - 1] =
+            make_float2(__fmul_rn(__fdiv_rn(span, 15.f), nrm), __fmul_rn(lo, nrm));
       }
     }
   }
@@ -291,8 +284,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv4_append_kernel(AppendArg
 
 template <int D, bool CLAMP, int ROPE>
 cudaError_t append_t(const AppendArgs& a, cudaStream_t stream) {
-  const int groups = (int)((a.Hq + 2 * a.Hkv + 7) / 8);
-  const int64_t units = a.T * groups;
+  const uint32_t uq = (uint32_t)((a.T * a.Hq + 7) / 8), uk = (uint32_t)((a.T * a.Hkv + 7) / 8);
+  const int64_t units = (int64_t)uq + 2 * (int64_t)uk;
   int per_sm = 1;
   cudaError_t e = prepare_launch(kv4_append_kernel<D, CLAMP, ROPE>, kAppendWarps * 32, 0, &per_sm);
   if (e != cudaSuccess) return e;
@@ -300,7 +293,7 @@ cudaError_t append_t(const AppendArgs& a, cudaStream_t stream) {
   const int64_t cap = (int64_t)device_sm_count() * per_sm;
   if (blocks > cap) blocks = cap;
   e = launch_pdl(kv4_append_kernel<D, CLAMP, ROPE>, dim3((unsigned)blocks), dim3(kAppendWarps * 32), 0, stream, 1, a,
-                 units, groups);
+                 uq, uk);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -311,49 +304,61 @@ cudaError_t append_c(const AppendArgs& a, cudaStream_t stream) {
   return a.rotary == D ? append_t<D, CLAMP, kRopeHalves>(a, stream) : append_t<D, CLAMP, kRopePartHalves>(a, stream);
 }
 
-// One warp per output token: it looks the token's page up once and walks the
-// kv heads.  D / 8 lanes share a row of codes (4 bytes, 8 values and one
-// 16-byte store per lane); a warp covers 32 / (D / 8) rows, K and V side by
-// side.
+// A warp takes 16 output tokens of one kv head: lane n looks token n % 16 up
+// and loads its scales, then D / 8 lanes share a row of codes (4 bytes, 8 values
+// and one 16-byte store per lane), K and V side by side.
 template <int D>
-__global__ void __launch_bounds__(kReadWarps * 32) kv4_read_kernel(ReadArgs a) {
+__global__ void __launch_bounds__(kReadWarps * 32) kv4_read_kernel(ReadArgs a, uint32_t units) {
   constexpr int LPR = D / 8;          // lanes per row
-  constexpr int HPS = 32 / LPR / 2;   // kv heads per step (K and V of each)
+  constexpr int TPS = 32 / LPR / 2;   // tokens per step (K and V of each)
   const int lane = threadIdx.x & 31;
-  const int part = lane % LPR, which = (lane / LPR) & 1, hs = lane / (2 * LPR);
-  const int64_t stride = (int64_t)gridDim.x * kReadWarps;
+  const int part = lane % LPR, which = (lane / LPR) & 1, ts = lane / (2 * LPR);
+  const uint32_t stride = gridDim.x * kReadWarps, heads = (uint32_t)a.Hkv;
   pdl_wait();
   pdl_trigger();
-  for (int64_t i = (int64_t)blockIdx.x * kReadWarps + (threadIdx.x >> 5); i < a.total; i += stride) {
-    // the last sequence whose offset is <= i
-    int lo = 0, hi = (int)a.batch - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if ((int64_t)__ldg(a.cu + mid) <= i) lo = mid; else hi = mid - 1;
-    }
-    const int64_t t = i - __ldg(a.cu + lo) + (a.starts ? __ldg(a.starts + lo) : 0);
-    const int64_t pi = t >= 0 ? t / a.page_size : -1;
-    int64_t page = -1;
-    if (pi >= 0 && pi < a.table_width) page = __ldg(a.table + (int64_t)lo * a.table_width + pi);
-    const bool in = page >= 0 && page < a.num_pages && i < __ldg(a.cu + a.batch);
-    const int64_t at0 = in ? (page * a.Hkv) * a.page_size + (t - pi * a.page_size) : 0;
-    const uint8_t* codes = which ? a.v_codes : a.k_codes;
-    __half* out = reinterpret_cast<__half*>(which ? a.v : a.k) + i * a.Hkv * D + part * 8;
-#pragma unroll 4
-    for (int h = hs; h < a.Hkv; h += HPS) {
-      uint4 w = make_uint4(0, 0, 0, 0);   // tokens without a page read as zeros
-      if (in) {
-        const int64_t at = at0 + (int64_t)h * a.page_size;
-        const uint32_t c = __ldg(reinterpret_cast<const uint32_t*>(codes + at * (D / 2)) + part);
-        const float2 f = __ldg(reinterpret_cast<const float2*>(a.scales + at * 4) + which);
-        uint32_t o[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          o[j] = pack_half2_bits(fmaf((float)((c >> (8 * j)) & 15u), f.x, f.y),
-                                 fmaf((float)((c >> (8 * j + 4)) & 15u), f.x, f.y));
-        w = make_uint4(o[0], o[1], o[2], o[3]);
+  const int end = __ldg(a.cu + a.batch);
+  for (uint32_t u = blockIdx.x * kReadWarps + (threadIdx.x >> 5); u < units; u += stride) {
+    const uint32_t grp = u / heads, h = u - grp * heads;
+    const int64_t i0 = (int64_t)grp * 16, i = i0 + (lane & 15);
+    int64_t at = -1;   // the token's place in the page arrays
+    float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < a.total && i < end) {
+      int lo = 0, hi = (int)a.batch - 1;   // the last sequence whose offset is <= i
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__ldg(a.cu + mid) <= (int)i) lo = mid; else hi = mid - 1;
       }
-      *reinterpret_cast<uint4*>(out + (int64_t)h * D) = w;
+      const int64_t t = i - __ldg(a.cu + lo) + (a.starts ? __ldg(a.starts + lo) : 0);
+      const int64_t pi = t >> a.page_shift;
+      if (t >= 0 && pi < a.table_width) {
+        const int64_t page = __ldg(a.table + (int64_t)lo * a.table_width + pi);
+        if (page >= 0 && page < a.num_pages) {
+          at = (page * heads + h) * a.page_size + (t & (a.page_size - 1));
+          sc = __ldg(reinterpret_cast<const float4*>(a.scales) + at);
+        }
+      }
+    }
+    const uint32_t* codes = reinterpret_cast<const uint32_t*>(which ? a.v_codes : a.k_codes) + part;
+    uint32_t w[16 / TPS];
+#pragma unroll
+    for (int s = 0; s < 16 / TPS; ++s) {
+      const int64_t ax = __shfl_sync(0xffffffffu, at, s * TPS + ts);
+      w[s] = ax >= 0 ? __ldg(codes + ax * (D / 8)) : 0u;
+    }
+    __half* out = reinterpret_cast<__half*>(which ? a.v : a.k) + (i0 * heads + h) * D + part * 8;
+#pragma unroll
+    for (int s = 0; s < 16 / TPS; ++s) {
+      const int n = s * TPS + ts;   // tokens without a page have scales 0 and read as zeros
+      const float ka = __shfl_sync(0xffffffffu, sc.x, n), kb = __shfl_sync(0xffffffffu, sc.y, n);
+      const float va = __shfl_sync(0xffffffffu, sc.z, n), vb = __shfl_sync(0xffffffffu, sc.w, n);
+      const float al = which ? va : ka, be = which ? vb : kb;
+      uint32_t o[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        o[j] = pack_half2_bits(fmaf((float)((w[s] >> (8 * j)) & 15u), al, be),
+                               fmaf((float)((w[s] >> (8 * j + 4)) & 15u), al, be));
+      if (i0 + n < a.total)
+        *reinterpret_cast<uint4*>(out + (int64_t)n * heads * D) = make_uint4(o[0], o[1], o[2], o[3]);
     }
   }
 }
@@ -363,10 +368,12 @@ cudaError_t read_t(const ReadArgs& a, cudaStream_t stream) {
   int per_sm = 1;
   cudaError_t e = prepare_launch(kv4_read_kernel<D>, kReadWarps * 32, 0, &per_sm);
   if (e != cudaSuccess) return e;
-  int64_t blocks = (a.total + kReadWarps - 1) / kReadWarps;
+  const int64_t units = (a.total + 15) / 16 * a.Hkv;
+  int64_t blocks = (units + kReadWarps - 1) / kReadWarps;
   const int64_t cap = (int64_t)device_sm_count() * per_sm;
   if (blocks > cap) blocks = cap;
-  e = launch_pdl(kv4_read_kernel<D>, dim3((unsigned)blocks), dim3(kReadWarps * 32), 0, stream, 1, a);
+  e = launch_pdl(kv4_read_kernel<D>, dim3((unsigned)blocks), dim3(kReadWarps * 32), 0, stream, 1, a,
+                 (uint32_t)units);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -424,6 +424,12 @@ spinq_status check_pages(const spinq_kv4_pages* c) {
   return SPINQ_OK;
 }
 
+int log2_of(int64_t pow2) {
+  int n = 0;
+  while ((1ll << n) < pow2) ++n;
+  return n;
+}
+
 // Rows of `width` fp16 values, ld apart, 16-byte aligned.
 bool rows_ok(const void* p, int64_t ld, int64_t width) {
   return p && aligned16(p) && ld >= width && ld % 8 == 0;
@@ -462,7 +468,7 @@ spinq_status spinq_kv4_append(const void* q, int64_t ldq, void* q_out, const voi
   }
   if (kvq->bits != 4 || kvq->symmetric != 0 || kvq->granularity != SPINQ_PER_GROUP || kvq->group_size != D)
     return SPINQ_EUNSUPPORTED;
-  if (Hq > 65535 || T > INT32_MAX) return SPINQ_EUNSUPPORTED;
+  if (Hq > 65535 || T > INT32_MAX || T * (Hq > Hkv ? Hq : Hkv) > INT32_MAX) return SPINQ_EUNSUPPORTED;
   if (T == 0) return SPINQ_OK;
   a.q = q;
   a.k = k;
@@ -485,6 +491,7 @@ spinq_status spinq_kv4_append(const void* q, int64_t ldq, void* q_out, const voi
   a.scales = cache->scales;
   a.num_slots = cache->num_pages * cache->page_size;
   a.page_size = cache->page_size;
+  a.page_shift = log2_of(cache->page_size);
   a.slots = slots;
   return from_cuda(launch_kv4_append(a, static_cast<cudaStream_t>(stream)));
 }
@@ -497,10 +504,10 @@ spinq_status spinq_kv4_read(const spinq_kv4_pages* cache, const int32_t* page_ta
   if (st != SPINQ_OK) return st;
   if (total > 0 && (batch == 0 || !cu_tokens || !k || !v || (table_width > 0 && !page_table))) return SPINQ_EINVAL;
   if (!aligned16(k) || !aligned16(v)) return SPINQ_EINVAL;
-  if (batch > INT32_MAX || total > INT32_MAX) return SPINQ_EUNSUPPORTED;
+  if (batch > INT32_MAX || total > INT32_MAX || total * cache->kv_heads > INT32_MAX) return SPINQ_EUNSUPPORTED;
   if (total == 0) return SPINQ_OK;
   ReadArgs a{cache->k_codes, cache->v_codes, cache->scales, cache->num_pages, cache->kv_heads, cache->page_size,
-             cache->head_dim, page_table, batch, table_width, starts, cu_tokens, total, k, v};
+             log2_of(cache->page_size), cache->head_dim, page_table, batch, table_width, starts, cu_tokens, total, k, v};
   return from_cuda(launch_kv4_read(a, static_cast<cudaStream_t>(stream)));
 }
 

@@ -123,7 +123,7 @@ struct AppendArgs {
   uint8_t* v_codes;
   float* scales;
   int64_t num_slots;      // num_pages * page_size
-  int page_size;
+  int page_size, page_shift;   // page_size = 1 << page_shift
   const int64_t* slots;   // [T]; outside [0, num_slots): not written
 };
 cudaError_t launch_kv4_append(const AppendArgs& a, cudaStream_t stream);
@@ -133,7 +133,7 @@ struct ReadArgs {
   const uint8_t* v_codes;
   const float* scales;
   int64_t num_pages, Hkv;
-  int page_size, D;
+  int page_size, page_shift, D;
   const int32_t* table;   // [batch][table_width]
   int64_t batch, table_width;
   const int32_t* starts;  // [batch] or nullptr (0)
