@@ -18,12 +18,13 @@
 // result does not depend on how the rows are spread over the lanes.
 //
 // Append layout.  A quad of lanes owns a row, a warp 8 rows of one kind (all
-// query heads of all tokens, then key heads, then value heads).  Lane c holds
-// the runs [Cc, Cc + C) and [D/2 + Cc, D/2 + Cc + C), C = D/8, as pairs (i, i + D/2)
-// in packed fp32: a rotate-half pair over the whole head is one register
-// pair, every butterfly but the last works on packed pairs, and only the two
-// middle bits of the transform go through shuffles.  Bound: instruction
-// issue (about 400 per warp and 8 rows) close to the memory's time.
+// query heads of all tokens, then key heads, then value heads).  The row's
+// 8-value pieces go to the lanes in turn (a quad's loads and stores are runs of
+// 64 bytes): lane c holds values D/2 s + 32 v + 8 c + e, as pairs (s = 0, s = 1) in
+// packed fp32.  A rotate-half pair over the whole head is one register pair, every
+// butterfly but the last works on packed pairs, and only bits 3 and 4 of
+// the transform go through shuffles.  The next row's data are loaded before this
+// one's are worked on.
 //
 // Read layout.  A warp expands 16 tokens of one kv head, whose codes are one
 // run of a page wherever the tokens are; the warps of a block take the heads of the same
@@ -51,176 +52,211 @@ enum RopeForm { kRopeNone = 0, kRopePairs = 1, kRopeHalves = 2, kRopePartHalves 
 // D = head_dim, ROPE one of RopeForm:
 //   kRopePairs       neighbouring pairs (2i, 2i+1) of the first R values;
 //   kRopeHalves      pairs (i, i + D/2), R = D: one register pair;
-//   kRopePartHalves  pairs (i, i + R/2), R < D a multiple of D/4: the partner
-//                    is a whole C-value run of another lane of the quad.
+//   kRopePartHalves  pairs (i, i + R/2), R < D: the partner's 8-value piece is
+//                    loaded a second time (it is another lane's).
 template <int D, bool CLAMP, int ROPE>
 __global__ void __launch_bounds__(kAppendWarps * 32) kv4_append_kernel(AppendArgs a, uint32_t uq, uint32_t uk) {
-  constexpr int C = D / 8;    // values per run; a lane holds two runs
-  constexpr int CV = C / 8;   // 16-byte loads per run
+  constexpr int V = D / 64;   // pieces of 8 values per lane and half of the row
   const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const uint32_t units = uq + 2 * uk, stride = gridDim.x * kAppendWarps;
-  pdl_wait();
-  pdl_trigger();
-  for (uint32_t u = blockIdx.x * kAppendWarps + (threadIdx.x >> 5); u < units; u += stride) {
-    const int kind = u < uq ? 0 : (u < uq + uk ? 1 : 2);   // the warp's rows: queries, keys or values
-    const uint32_t H = (uint32_t)(kind == 0 ? a.Hq : a.Hkv);
-    const uint32_t row = (kind == 0 ? u : (kind == 1 ? u - uq : u - uq - uk)) * 8 + g;
-    const uint32_t t = row / H, h = row - t * H;
-    const bool valid = t < (uint32_t)a.T;
-    const __half* src = reinterpret_cast<const __half*>(kind == 0 ? a.q : (kind == 1 ? a.k : a.v)) +
-                        (int64_t)t * (kind == 0 ? a.ldq : (kind == 1 ? a.ldk : a.ldv)) + h * D + c * C;
-    uint4 in[2][CV];
+  struct Row {
+    int kind;        // the warp's rows: 0 queries, 1 keys, 2 values
+    uint32_t row, t, h;
+    bool valid;
+    const __half* src;
+    uint4 in[2][V];
+    int pos;
+  };
+  auto fetch = [&](uint32_t u, Row& x) {
+    x.kind = u < uq ? 0 : (u < uq + uk ? 1 : 2);
+    const uint32_t H = (uint32_t)(x.kind == 0 ? a.Hq : a.Hkv);
+    x.row = (x.kind == 0 ? u : (x.kind == 1 ? u - uq : u - uq - uk)) * 8 + g;
+    x.t = x.row / H;
+    x.h = x.row - x.t * H;
+    x.valid = x.t < (uint32_t)a.T;
+    x.src = reinterpret_cast<const __half*>(x.kind == 0 ? a.q : (x.kind == 1 ? a.k : a.v)) +
+            (int64_t)x.t * (x.kind == 0 ? a.ldq : (x.kind == 1 ? a.ldk : a.ldv)) + x.h * D;
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int i = 0; i < CV; ++i)
-        in[s][i] = valid ? __ldg(reinterpret_cast<const uint4*>(src + s * (D / 2)) + i) : make_uint4(0, 0, 0, 0);
-    F2 y[C];   // (value Cc + i, value D/2 + Cc + i)
-    auto pairs = [&](const uint4 (&w)[2][CV], F2* out) {
+      for (int v = 0; v < V; ++v)
+        x.in[s][v] = x.valid ? __ldg(reinterpret_cast<const uint4*>(x.src + s * (D / 2)) + 4 * v + c)
+                             : make_uint4(0, 0, 0, 0);
+    x.pos = ROPE != kRopeNone && x.valid && x.kind != 2 ? __ldg(a.positions + x.t) : 0;
+  };
+  // packed pairs (piece of the first half, piece of the second) as fp32
+  auto widen = [](const uint4& p, const uint4& q, F2* out) {
+    const uint32_t lo[4] = {p.x, p.y, p.z, p.w}, hi[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-      for (int i = 0; i < CV; ++i) {
-        const uint32_t lo[4] = {w[0][i].x, w[0][i].y, w[0][i].z, w[0][i].w};
-        const uint32_t hi[4] = {w[1][i].x, w[1][i].y, w[1][i].z, w[1][i].w};
+    for (int j = 0; j < 4; ++j) {
+      const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo[j]));
+      const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&hi[j]));
+      out[2 * j] = f2_make(x.x, y.x);
+      out[2 * j + 1] = f2_make(x.y, y.y);
+    }
+  };
+  pdl_wait();
+  pdl_trigger();
+  Row next;
+  uint32_t u = blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
+  if (u < units) fetch(u, next);
+  for (; u < units; u += stride) {
+    const Row x = next;
+    if (u + stride < units) fetch(u + stride, next);
+    F2 y[V][8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&lo[j]));
-          const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&hi[j]));
-          out[8 * i + 2 * j] = f2_make(p.x, q.x);
-          out[8 * i + 2 * j + 1] = f2_make(p.y, q.y);
-        }
-      }
-    };
-    pairs(in, y);
+    for (int v = 0; v < V; ++v) widen(x.in[0][v], x.in[1][v], y[v]);
 
-    if (kind != 2) {
+    if (x.kind != 2) {
       // ---- norm of the head
-      const __half* wt = reinterpret_cast<const __half*>(kind == 0 ? a.q_weight : a.k_weight);
+      const __half* wt = reinterpret_cast<const __half*>(x.kind == 0 ? a.q_weight : a.k_weight);
+      const uint4* w4 = reinterpret_cast<const uint4*>(wt);
+      float r = 1.f;
       if (wt != nullptr) {
-        F2 sq[C];
+        float part[2];
+        F2 sum[V];
 #pragma unroll
-        for (int i = 0; i < C; ++i) sq[i] = f2_product(y[i], y[i]);
+        for (int v = 0; v < V; ++v) {
+          F2 sq[8];
 #pragma unroll
-        for (int w = C / 2; w >= 1; w >>= 1)   // neighbours first
+          for (int i = 0; i < 8; ++i) sq[i] = f2_product(y[v][i], y[v][i]);
 #pragma unroll
-          for (int i = 0; i < w; ++i) sq[i] = f2_add(sq[2 * i], sq[2 * i + 1]);
-        float p0, p1;
-        f2_split(sq[0], p0, p1);
+          for (int w = 4; w >= 1; w >>= 1)   // neighbours first
 #pragma unroll
-        for (int b = 1; b < 4; b <<= 1) {
-          p0 = __fadd_rn(p0, __shfl_xor_sync(0xffffffffu, p0, b));
-          p1 = __fadd_rn(p1, __shfl_xor_sync(0xffffffffu, p1, b));
+            for (int i = 0; i < w; ++i) sq[i] = f2_add(sq[2 * i], sq[2 * i + 1]);
+#pragma unroll
+          for (int b = 1; b < 4; b <<= 1) {
+            float p, q;
+            f2_split(sq[0], p, q);
+            sq[0] = f2_add(sq[0], f2_make(__shfl_xor_sync(0xffffffffu, p, b), __shfl_xor_sync(0xffffffffu, q, b)));
+          }
+          sum[v] = sq[0];
         }
-        const float ms = __fadd_rn(p0, p1) * (1.f / D);   // D is a power of two: exact
-        const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(ms, a.eps)));
-        uint4 ww[2][CV];
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int i = 0; i < CV; ++i) ww[s][i] = __ldg(reinterpret_cast<const uint4*>(wt + s * (D / 2) + c * C) + i);
-        F2 wf[C];
-        pairs(ww, wf);
+        if (V == 2) sum[0] = f2_add(sum[0], sum[V - 1]);
+        f2_split(sum[0], part[0], part[1]);
+        const float ms = __fadd_rn(part[0], part[1]) * (1.f / D);   // D is a power of two: exact
+        r = __frcp_rn(__fsqrt_rn(__fadd_rn(ms, a.eps)));
         const F2 rr = f2_make(r, r);
 #pragma unroll
-        for (int i = 0; i < C; ++i) y[i] = f2_product(f2_product(y[i], rr), wf[i]);
+        for (int v = 0; v < V; ++v) {
+          F2 wf[8];
+          widen(__ldg(w4 + 4 * v + c), __ldg(w4 + D / 16 + 4 * v + c), wf);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[v][i] = f2_product(f2_product(y[v][i], rr), wf[i]);
+        }
       }
 
       // ---- rotary embedding of the first R values
       if (ROPE != kRopeNone) {
         const int half = a.rotary / 2;
-        int64_t pos = valid ? (int64_t)__ldg(a.positions + t) : 0;
-        pos = pos < 0 ? 0 : (pos >= a.max_pos ? a.max_pos - 1 : pos);
+        const int64_t pos = x.pos < 0 ? 0 : ((int64_t)x.pos >= a.max_pos ? a.max_pos - 1 : x.pos);
         const float2* cs = reinterpret_cast<const float2*>(a.cos_sin) + pos * half;
-        if (ROPE == kRopePairs) {
-          // the runs' neighbouring pairs, angles (Cc + i)/2 and D/4 + (Cc + i)/2; past R: cos 1, sin 0
 #pragma unroll
-          for (int i = 0; i < C; i += 2) {
-            const int e = (c * C + i) / 2;
-            const float2 f0 = e < half ? __ldg(cs + e) : make_float2(1.f, 0.f);
-            const float2 f1 = e + D / 4 < half ? __ldg(cs + e + D / 4) : make_float2(1.f, 0.f);
-            const F2 co = f2_make(f0.x, f1.x), si = f2_make(f0.y, f1.y);
-            const F2 p = y[i], q = y[i + 1];
-            y[i] = f2_sub(f2_product(p, co), f2_product(q, si));
-            y[i + 1] = f2_add(f2_product(p, si), f2_product(q, co));
-          }
-        } else if (ROPE == kRopeHalves) {
+        for (int v = 0; v < V; ++v) {
+          const int e0 = 32 * v + 8 * c;   // first value of the piece (and e0 + D/2)
+          if (ROPE == kRopePairs) {
+            // angles e/2 and D/4 + e/2; past R: cos 1, sin 0
 #pragma unroll
-          for (int i = 0; i < C; i += 2) {
-            const float4 f = __ldg(reinterpret_cast<const float4*>(cs + c * C + i));
-            float p, q;
-            f2_split(y[i], p, q);
-            y[i] = f2_add(f2_product(y[i], f2_make(f.x, f.x)), f2_product(f2_make(q, p), f2_make(-f.y, f.y)));
-            f2_split(y[i + 1], p, q);
-            y[i + 1] = f2_add(f2_product(y[i + 1], f2_make(f.z, f.z)), f2_product(f2_make(q, p), f2_make(-f.w, f.w)));
-          }
-        } else {
-          // run number c (first of the pair) or c + 4 (second); the partner run is R/2 values away
-          const int hop = half / C;
-          const int o0 = c < hop ? c + hop : c - hop, o1 = c + 4 < hop ? c + 4 + hop : c + 4 - hop;
-          const bool turn0 = c < 2 * hop, turn1 = c + 4 < 2 * hop, first0 = c < hop, first1 = c + 4 < hop;
-          const float2* f0 = cs + (first0 ? c : c - hop) * C;
-          const float2* f1 = cs + (first1 ? c + 4 : c + 4 - hop) * C;
-#pragma unroll
-          for (int i = 0; i < C; ++i) {
-            float v0, v1;
-            f2_split(y[i], v0, v1);
-            const int from0 = (lane & ~3) | (o0 & 3), from1 = (lane & ~3) | (o1 & 3);
-            const float a0 = __shfl_sync(0xffffffffu, v0, from0), b0 = __shfl_sync(0xffffffffu, v1, from0);
-            const float a1 = __shfl_sync(0xffffffffu, v0, from1), b1 = __shfl_sync(0xffffffffu, v1, from1);
-            if (turn0) {
-              const float2 f = __ldg(f0 + i);
-              const float p = __fmul_rn(v0, f.x), q = __fmul_rn(o0 & 4 ? b0 : a0, f.y);
-              v0 = first0 ? __fsub_rn(p, q) : __fadd_rn(p, q);
+            for (int i = 0; i < 8; i += 2) {
+              const int e = (e0 + i) / 2;
+              const float2 f0 = e < half ? __ldg(cs + e) : make_float2(1.f, 0.f);
+              const float2 f1 = e + D / 4 < half ? __ldg(cs + e + D / 4) : make_float2(1.f, 0.f);
+              const F2 co = f2_make(f0.x, f1.x), si = f2_make(f0.y, f1.y);
+              const F2 p = y[v][i], q = y[v][i + 1];
+              y[v][i] = f2_sub(f2_product(p, co), f2_product(q, si));
+              y[v][i + 1] = f2_add(f2_product(p, si), f2_product(q, co));
             }
-            if (turn1) {
-              const float2 f = __ldg(f1 + i);
-              const float p = __fmul_rn(v1, f.x), q = __fmul_rn(o1 & 4 ? b1 : a1, f.y);
-              v1 = first1 ? __fsub_rn(p, q) : __fadd_rn(p, q);
+          } else if (ROPE == kRopeHalves) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+              const float4 f = __ldg(reinterpret_cast<const float4*>(cs + e0 + i));
+              float p, q;
+              f2_split(y[v][i], p, q);
+              y[v][i] = f2_add(f2_product(y[v][i], f2_make(f.x, f.x)), f2_product(f2_make(q, p), f2_make(-f.y, f.y)));
+              f2_split(y[v][i + 1], p, q);
+              y[v][i + 1] =
+                  f2_add(f2_product(y[v][i + 1], f2_make(f.z, f.z)), f2_product(f2_make(q, p), f2_make(-f.w, f.w)));
             }
-            y[i] = f2_make(v0, v1);
+          } else {
+            float z[2][8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f2_split(y[v][i], z[0][i], z[1][i]);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              const int e = e0 + s * (D / 2);
+              if (e < a.rotary) {
+                const bool first = e < half;
+                const int o = first ? e + half : e - half, f0 = first ? e : e - half;
+                const uint4 xo = x.valid ? __ldg(reinterpret_cast<const uint4*>(x.src + o)) : make_uint4(0, 0, 0, 0);
+                const uint4 wo = wt != nullptr ? __ldg(reinterpret_cast<const uint4*>(wt + o)) : make_uint4(0, 0, 0, 0);
+                F2 xw[8];   // (partner value, its weight)
+                widen(xo, wo, xw);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  float q, w;
+                  f2_split(xw[i], q, w);
+                  if (wt != nullptr) q = __fmul_rn(__fmul_rn(q, r), w);
+                  const float2 f = __ldg(cs + f0 + i);
+                  const float p = __fmul_rn(z[s][i], f.x), n = __fmul_rn(q, f.y);
+                  z[s][i] = first ? __fsub_rn(p, n) : __fadd_rn(p, n);
+                }
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[v][i] = f2_make(z[0][i], z[1][i]);
           }
         }
       }
 
-      // ---- R3: bits 0 .. log2 C - 1 in the lane, the two lane bits, the pair's bit
+      // ---- R3: bits 0-2 in the lane, the two lane bits, bit 5 (D = 128) and the pair's bit
 #pragma unroll
-      for (int bit = 1; bit < C; bit <<= 1)
+      for (int v = 0; v < V; ++v) {
 #pragma unroll
-        for (int i = 0; i < C; ++i)
-          if (!(i & bit)) f2_bfly(y[i], y[i | bit]);
+        for (int bit = 1; bit < 8; bit <<= 1)
 #pragma unroll
-      for (int bit = 1; bit < 4; bit <<= 1) {
-        const float sg = c & bit ? -1.f : 1.f;   // the upper lane's value enters with a minus sign (exact product)
-        const F2 sg2 = f2_make(sg, sg);
+          for (int i = 0; i < 8; ++i)
+            if (!(i & bit)) f2_bfly(y[v][i], y[v][i | bit]);
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-          float p, q;
-          f2_split(y[i], p, q);
-          y[i] = f2_fma(y[i], sg2, f2_make(__shfl_xor_sync(0xffffffffu, p, bit), __shfl_xor_sync(0xffffffffu, q, bit)));
+        for (int bit = 1; bit < 4; bit <<= 1) {
+          const float sg = c & bit ? -1.f : 1.f;   // the upper lane's value enters with a minus sign (exact product)
+          const F2 sg2 = f2_make(sg, sg);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float p, q;
+            f2_split(y[v][i], p, q);
+            y[v][i] =
+                f2_fma(y[v][i], sg2, f2_make(__shfl_xor_sync(0xffffffffu, p, bit), __shfl_xor_sync(0xffffffffu, q, bit)));
+          }
         }
       }
+      if (V == 2) {
 #pragma unroll
-      for (int i = 0; i < C; ++i) f2_bfly_inner(y[i]);
+        for (int i = 0; i < 8; ++i) f2_bfly(y[0][i], y[V - 1][i]);
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f2_bfly_inner(y[v][i]);
     }
 
-    if (kind == 0) {
-      if (valid) {
-        __half* dst = reinterpret_cast<__half*>(a.q_out) + (int64_t)row * D + c * C;
+    if (x.kind == 0) {
+      if (x.valid) {
+        uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__half*>(a.q_out) + (int64_t)x.row * D) + c;
         const F2 nn = f2_make(a.norm, a.norm);
-        uint32_t w[2][C / 2];
 #pragma unroll
-        for (int i = 0; i < C; i += 2) {
-          float p0, q0, p1, q1;
-          f2_split(f2_product(y[i], nn), p0, q0);
-          f2_split(f2_product(y[i + 1], nn), p1, q1);
-          w[0][i / 2] = pack_half2_bits(p0, p1);
-          w[1][i / 2] = pack_half2_bits(q0, q1);
+        for (int v = 0; v < V; ++v) {
+          uint32_t w[2][4];
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            float p0, q0, p1, q1;
+            f2_split(f2_product(y[v][i], nn), p0, q0);
+            f2_split(f2_product(y[v][i + 1], nn), p1, q1);
+            w[0][i / 2] = pack_half2_bits(p0, p1);
+            w[1][i / 2] = pack_half2_bits(q0, q1);
+          }
+#pragma unroll
+          for (int s = 0; s < 2; ++s) dst[s * (D / 16) + 4 * v] = make_uint4(w[s][0], w[s][1], w[s][2], w[s][3]);
         }
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int i = 0; i < CV; ++i)
-            reinterpret_cast<uint4*>(dst + s * (D / 2))[i] =
-                make_uint4(w[s][4 * i], w[s][4 * i + 1], w[s][4 * i + 2], w[s][4 * i + 3]);
       }
       continue;
     }
@@ -228,12 +264,14 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv4_append_kernel(AppendArg
     // ---- Eq. 1 over the row, into its slot
     float hi = -FLT_MAX, lo = FLT_MAX;
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      float p, q;
-      f2_split(y[i], p, q);
-      asm("max.f32 %0, %0, %1, %2;\n" : "+f"(hi) : "f"(p), "f"(q));
-      asm("min.f32 %0, %0, %1, %2;\n" : "+f"(lo) : "f"(p), "f"(q));
-    }
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float p, q;
+        f2_split(y[v][i], p, q);
+        asm("max.f32 %0, %0, %1, %2;\n" : "+f"(hi) : "f"(p), "f"(q));
+        asm("min.f32 %0, %0, %1, %2;\n" : "+f"(lo) : "f"(p), "f"(q));
+      }
 #pragma unroll
     for (int b = 1; b < 4; b <<= 1) {
       hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, b));
@@ -248,34 +286,53 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv4_append_kernel(AppendArg
     // quotient only for a value within 2^-20 of the middle of two codes
     const float inv = span > 0.f ? __fmul_rn(__frcp_rn(span), 15.f) : 0.f;
     const F2 lo2 = f2_make(lo, lo), inv2 = f2_make(inv, inv), mg2 = f2_make(kRoundMagic, kRoundMagic);
-    uint32_t r[2][C];
+    uint32_t word[4];   // codes of the pieces (s, v): word 2 s + v (D = 128) or s
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      F2 v = f2_product(f2_sub(y[i], lo2), inv2);
-      float p, q;
-      if (CLAMP) {
-        f2_split(v, p, q);
-        v = f2_make(fminf(fmaxf(p, 0.f), 15.f), fminf(fmaxf(q, 0.f), 15.f));
+    for (int v = 0; v < V; ++v) {
+      uint32_t r[2][8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        F2 t = f2_product(f2_sub(y[v][i], lo2), inv2);
+        float p, q;
+        if (CLAMP) {
+          f2_split(t, p, q);
+          t = f2_make(fminf(fmaxf(p, 0.f), 15.f), fminf(fmaxf(q, 0.f), 15.f));
+        }
+        f2_split(f2_add(t, mg2), p, q);
+        r[0][i] = __float_as_uint(p);
+        r[1][i] = __float_as_uint(q);
       }
-      f2_split(f2_add(v, mg2), p, q);
-      r[0][i] = __float_as_uint(p);
-      r[1][i] = __float_as_uint(q);
+      word[v] = pack8_nibbles(r[0]);
+      word[V + v] = pack8_nibbles(r[1]);
     }
-    const int64_t slot = valid ? __ldg(a.slots + t) : -1;
+    if (V == 2) {
+      // 4 x 4 transpose over the quad: lane c ends with the words of piece
+      // group c of all four lanes, 16 contiguous bytes of the row
+#pragma unroll
+      for (int bit = 1; bit < 4; bit <<= 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(i & bit)) {
+            const bool up = (c & bit) != 0;
+            const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? word[i] : word[i | bit], bit);
+            if (up) word[i] = got; else word[i | bit] = got;
+          }
+      }
+    }
+    const int64_t slot = x.valid ? __ldg(a.slots + x.t) : -1;
     if (slot >= 0 && slot < a.num_slots) {
       const int64_t page = slot >> a.page_shift, in_page = slot & (a.page_size - 1);
-      const int64_t at = (page * a.Hkv + h) * a.page_size + in_page;
-      uint8_t* codes = (kind == 1 ? a.k_codes : a.v_codes) + at * (D / 2) + c * (C / 2);
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if constexpr (CV == 2)
-          *reinterpret_cast<uint2*>(codes + s * (D / 4)) = make_uint2(pack8_nibbles(r[s]), pack8_nibbles(r[s] + 8));
-        else
-          *reinterpret_cast<uint32_t*>(codes + s * (D / 4)) = pack8_nibbles(r[s]);
+      const int64_t at = (page * a.Hkv + x.h) * a.page_size + in_page;
+      uint8_t* codes = (x.kind == 1 ? a.k_codes : a.v_codes) + at * (D / 2);
+      if (V == 2) {
+        *reinterpret_cast<uint4*>(codes + 16 * c) = make_uint4(word[0], word[1], word[2], word[3]);
+      } else {
+        *reinterpret_cast<uint32_t*>(codes + 4 * c) = word[0];
+        *reinterpret_cast<uint32_t*>(codes + 16 + 4 * c) = word[1];
       }
       if (c == 0) {
-        const float nrm = kind == 1 ? a.norm : 1.f;
-        reinterpret_cast<float2*>(a.scales + at * 4)[kind - 1] =
+        const float nrm = x.kind == 1 ? a.norm : 1.f;
+        reinterpret_cast<float2*>(a.scales + at * 4)[x.kind - 1] =
             make_float2(__fmul_rn(__fdiv_rn(span, 15.f), nrm), __fmul_rn(lo, nrm));
       }
     }
