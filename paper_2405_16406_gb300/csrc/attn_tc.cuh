@@ -28,18 +28,21 @@ __device__ __forceinline__ bool attn_test(uint64_t* bar, uint32_t parity) {
 }
 
 // Bounded wait that polls; false, with the abort flag up, after `limit_ns`, and false
-// soon after another warp raised it.
+// soon after another warp raised it.  The clock and the flag are looked at only
+// every 512 polls: reading the timer costs hundreds of cycles, which a wait on
+// the path from the scores to the weights would pay on every tile.
 __device__ __forceinline__ bool attn_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
-  if (attn_test(bar, parity)) return true;
-  const uint64_t t0 = globaltimer_ns();
-  for (uint32_t k = 1;; ++k) {
-    if (attn_test(bar, parity)) return true;
-    if ((k & 255u) == 0) {
-      if (*abort_flag) return false;
-      if (globaltimer_ns() - t0 > limit_ns) {
-        *abort_flag = 1;
-        return false;
-      }
+  uint64_t t0 = 0;
+  while (true) {
+#pragma unroll 1
+    for (int k = 0; k < 512; ++k)
+      if (attn_test(bar, parity)) return true;
+    if (*abort_flag) return false;
+    const uint64_t t = globaltimer_ns();
+    if (t0 == 0) t0 = t;
+    if (t - t0 > limit_ns) {
+      *abort_flag = 1;
+      return false;
     }
   }
 }
@@ -82,14 +85,38 @@ __device__ __forceinline__ void tmem_ld_wait_all(uint32_t* r) {
   for (int q = 0; q < N; q += 16) tmem_ld_wait(r + q);
 }
 
-// D[tmem] (+)= A[tmem] * B[smem], fp16 operands: A's rows on the lanes, two
-// values per 32-bit column.
-__device__ __forceinline__ void tc_mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                              uint32_t accumulate) {
+// The issuing thread of a warp (one, always the same).
+__device__ __forceinline__ bool attn_elect() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(p));
+  return p != 0;
+}
+
+// Shared-memory descriptors (spinq_device.cuh: umma_desc_sw128, ..._mn) by
+// halves.  The high one is the same for every operand here (8-row groups 1024
+// bytes apart, 128-byte swizzle); the low one holds the address, so a step within or
+// between tiles is one addition of bytes / 16.
+constexpr uint32_t kAttnDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t attn_desc_k(uint32_t addr) { return (addr >> 4) | (1u << 16); }              // K-major
+__device__ __forceinline__ uint32_t attn_desc_mn(uint32_t addr) { return (addr >> 4) | ((16384u >> 4) << 16); }  // MN-major
+
+// D[tmem] (+)= A[smem] * B[smem], fp16 operands.
+template <bool ACC>
+__device__ __forceinline__ void attn_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n mov.b64 a, {%1, %4};\n mov.b64 b, {%2, %4};\n setp.ne.b32 p, %5, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(kAttnDescHi), "n"(ACC ? 1 : 0)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem]: A's rows on the lanes, two values per
+// 32-bit column.
+template <bool ACC>
+__device__ __forceinline__ void attn_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 b;\n mov.b64 b, {%2, %4};\n setp.ne.b32 p, %5, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_lo), "r"(idesc), "n"(kAttnDescHi), "n"(ACC ? 1 : 0)
       : "memory");
 }
 
@@ -103,25 +130,28 @@ __host__ __device__ constexpr uint32_t umma_idesc_f16_f32(int M, int N, bool neg
 // of 128 rows x 128 bytes, 128-byte swizzle; kAttnAtom bytes apart.
 constexpr uint32_t kAttnAtom = 128 * 128;
 
-// S[tmem] = Q K^T: both tiles K-major, D / 16 K steps.
+// S[tmem] = Q K^T: both tiles K-major (descriptors of their starts), D / 16 K steps.
 template <int D>
-__device__ __forceinline__ void attn_mma_qk(uint32_t s_tmem, uint32_t q_smem, uint32_t k_smem, uint32_t idesc) {
+__device__ __forceinline__ void attn_mma_qk(uint32_t s_tmem, uint32_t q_lo, uint32_t k_lo, uint32_t idesc) {
+  attn_mma_ss<false>(s_tmem, q_lo, k_lo, idesc);
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) {
-    const uint32_t off = (ks >> 2) * kAttnAtom + (ks & 3) * 32;
-    tc_mma_f16(s_tmem, umma_desc_sw128(q_smem + off), umma_desc_sw128(k_smem + off), idesc, ks > 0 ? 1u : 0u);
+  for (int ks = 1; ks < D / 16; ++ks) {
+    const uint32_t off = ((ks >> 2) * kAttnAtom + (ks & 3) * 32) >> 4;
+    attn_mma_ss<true>(s_tmem, q_lo + off, k_lo + off, idesc);
   }
 }
 
 // O[tmem] (+)= P V: P fp16 in tensor memory (128 tokens on 64 columns), V
 // with D contiguous (MN-major), 8 K steps of 16 tokens.
 template <int D>
-__device__ __forceinline__ void attn_mma_pv(uint32_t o_tmem, uint32_t p_tmem, uint32_t v_smem, bool accumulate) {
+__device__ __forceinline__ void attn_mma_pv(uint32_t o_tmem, uint32_t p_tmem, uint32_t v_lo, bool accumulate) {
   constexpr uint32_t idesc = umma_idesc_f16_f32_bmn(128, D);
+  if (accumulate)
+    attn_mma_ts<true>(o_tmem, p_tmem, v_lo, idesc);
+  else
+    attn_mma_ts<false>(o_tmem, p_tmem, v_lo, idesc);
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks)
-    tc_mma_f16_ts(o_tmem, p_tmem + ks * 8, umma_desc_sw128_mn(v_smem + ks * 2048, kAttnAtom, 1024), idesc,
-                  accumulate || ks > 0 ? 1u : 0u);
+  for (int ks = 1; ks < 8; ++ks) attn_mma_ts<true>(o_tmem, p_tmem + ks * 8, v_lo + ks * (2048 >> 4), idesc);
 }
 
 // The largest of 128 scores.

@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = 0;   // all 512 columns are this CTA's: they start at column 0
   pdl_wait();
   pdl_trigger();
 
@@ -214,47 +214,55 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
   } else if (warp >= 8) {
     // ---------------- MMAs
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
-    if (warp == 8) {
+    if (warp == 8 && nt > 0 && attn_elect()) {
       constexpr uint32_t idesc = umma_idesc_f16_f32(128, 128, false);
-      bool ok = nt == 0 || attn_wait_warp(qbar, 0, abort_flag, g_prefix_wait_ns);
-      auto wait_full = [&](int n) {
-        return attn_wait_warp(&full[n % NSTG], (uint32_t)(n / NSTG) & 1u, abort_flag, g_prefix_wait_ns);
-      };
-      auto qk = [&](int i, int n) {
-        if (lane == 0) {
-          attn_mma_qk<D>(tmem + i * 128, sb + i * C::TILE, sb + C::OFF_KV + (n % NSTG) * C::TILE, idesc);
-          tc_commit(&sbar[i]);
-        }
-      };
-      if (ok && nt > 0 && (ok = wait_full(0))) {
+      bool ok = attn_wait(qbar, 0, abort_flag, g_prefix_wait_ns);
+      const uint32_t q_lo = attn_desc_k(sb), k_lo = attn_desc_k(sb + C::OFF_KV), v_lo = attn_desc_mn(sb + C::OFF_KV);
+      int sk = 0, pk = 0;   // ring stage of the next tile to wait for, its phase
+      auto wait_tile = [&]() {
+        ok = attn_wait(&full[sk], pk, abort_flag, g_prefix_wait_ns);
         tc_fence_after();
-        for (int i = 0; i < nrow; ++i) qk(i, 0);
-        if (lane == 0) tc_commit(&free_[0]);
+        const int s = sk;
+        if (++sk == NSTG) sk = 0, pk ^= 1;
+        return s;
+      };
+      int s = ok ? wait_tile() : 0;
+      if (ok) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (i < nrow) {
+            attn_mma_qk<D>(i * 128, q_lo + i * (C::TILE >> 4), k_lo + s * (C::TILE >> 4), idesc);
+            tc_commit(&sbar[i]);
+          }
+        tc_commit(&free_[s]);
       }
+#pragma unroll 1
       for (int j = 0; ok && j < nt; ++j) {
-        const int nv = 2 * j + 1, nn = 2 * j + 2;
-        if (!(ok = wait_full(nv))) break;
-        for (int i = 0; i < nrow; ++i) {
-          if (!(ok = attn_wait_warp(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns))) break;
+        const int sv = wait_tile();
+        int sn = -1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (!ok || i >= nrow) continue;
+          if (!(ok = attn_wait(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns))) continue;
           tc_fence_after();
-          if (lane == 0)
-            attn_mma_pv<D>(tmem + 256 + i * D, tmem + i * 128, sb + C::OFF_KV + (nv % NSTG) * C::TILE, j > 0);
+          attn_mma_pv<D>(256 + i * D, i * 128, v_lo + sv * (C::TILE >> 4), j > 0);
           if (j + 1 < nt) {
             if (i == 0) {
-              if (!(ok = wait_full(nn))) break;
-              tc_fence_after();
+              sn = wait_tile();
+              if (!ok) continue;
             }
-            qk(i, nn);
-          } else if (lane == 0) {
+            attn_mma_qk<D>(i * 128, q_lo + i * (C::TILE >> 4), k_lo + sn * (C::TILE >> 4), idesc);
+            tc_commit(&sbar[i]);
+          } else {
             tc_commit(&obar[i]);
           }
         }
         if (!ok) break;
-        if (lane == 0) {
-          tc_commit(&free_[nv % NSTG]);
-          if (j + 1 < nt) tc_commit(&free_[nn % NSTG]);
-        }
+        tc_commit(&free_[sv]);
+        if (sn >= 0) tc_commit(&free_[sn]);
       }
+      tc_commit(drain);   // what is in flight finishes before tensor memory is given up
+      mbar_wait_bounded(drain, 0, kAttnWaitLimitNs);
     }
   } else {
     // ---------------- softmax: warps 4i .. 4i + 3 own tile i, thread = row
@@ -395,15 +403,10 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
   tc_fence_before();
   __syncthreads();
   if (*abort_flag) {
-    if (warp == 8) {   // MMAs in flight finish before tensor memory is given up
-      if (lane == 0) tc_commit(drain);
-      mbar_wait_bounded(drain, 0, kAttnWaitLimitNs);
-    }
     if (tid == 0 && p.status && atomicCAS(p.status, 0, (int)SPINQ_ETIMEOUT) == 0) atomicExch(p.status + 1, kPrefixSite);
-    __syncthreads();
   }
   tc_fence_after();
-  if (warp == 8) tmem_dealloc(tmem, 512);
+  if (warp == 8) tmem_dealloc(*tmem_slot, 512);
 }
 
 // ------------------------------------------------- the sequences' own tokens

@@ -20,14 +20,15 @@
 //    rescaled) and sum in fp32 registers;
 //  * warp 8: one thread copies Q, then the K and V tiles of 128 tokens into
 //    a ring of stages by TMA (128-byte swizzle);
-//  * warp 9: issues the MMAs: PV and the next QK of tile 0, then of tile 1,
+//  * warp 10: zeroes the last V tile's rows past the sequence;
+//  * warp 9: one thread issues the MMAs: PV and the next QK of tile 0, then of tile 1,
 //    so that each tile's softmax runs under the other tile's products.
 // Bound: the tensor core (4 D flops per visible pair of a query head and a
 // key).
 //
 // A sequence's last V tile may hold rows of the next sequence or of no
-// sequence: they meet weights 0, which is not enough if they are not finite, so warp 9
-// zeroes them; K's such rows only reach scores that the mask replaces.
+// sequence: they meet weights 0, which is not enough if they are not finite, so they are
+// zeroed; K's such rows only reach scores that the mask replaces.
 //
 // Every wait is bounded; one that gives up raises the CTA's abort flag, the
 // MMAs and copies in flight are drained and the status word is set.
@@ -64,8 +65,8 @@ struct PromptCfg {
   static constexpr int TILE = 128 * D * 2;               // bytes of a Q, K or V tile
   static constexpr int NSTG = D == 128 ? 5 : 8;
   static constexpr int OFF_KV = 2 * TILE;
-  static constexpr int OFF_BAR = OFF_KV + NSTG * TILE;   // q, full[NSTG], free[NSTG], s[2], p[2], o[2]
-  static constexpr int OFF_MISC = OFF_BAR + (2 * NSTG + 7) * 8;
+  static constexpr int OFF_BAR = OFF_KV + NSTG * TILE;   // q, full[NSTG], free[NSTG], s[2], p[2], o[2], z[2], drain
+  static constexpr int OFF_MISC = OFF_BAR + (2 * NSTG + 10) * 8;
   static constexpr int BYTES = OFF_MISC + 16 + 1024;
   static_assert(BYTES <= 232448, "shared memory");
 };
@@ -87,6 +88,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
   uint64_t* sbar = free_ + NSTG;   // scores of tile i written
   uint64_t* pbar = sbar + 2;       // weights of tile i written (4 warps)
   uint64_t* obar = pbar + 2;       // last product of tile i done
+  uint64_t* zreq = obar + 2;       // the sequence's last V tile is in,
+  uint64_t* zbar = zreq + 1;       // its rows past the sequence are zeroed
+  uint64_t* drain = zbar + 1;      // every MMA done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_MISC + 4);
   int* issued = reinterpret_cast<int*>(smem + C::OFF_MISC + 8);   // K and V tiles copied (0: Q neither)
@@ -103,6 +107,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
       mbar_init(&pbar[i], 4);
       mbar_init(&obar[i], 1);
     }
+    mbar_init(zreq, 1);
+    mbar_init(zbar, 1);
+    mbar_init(drain, 1);
     *abort_flag = 0;
     *issued = -1;
     fence_mbar_init();
@@ -117,7 +124,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = 0;   // all 512 columns are this CTA's: they start at column 0
   pdl_wait();
   pdl_trigger();
 
@@ -164,62 +171,74 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         }
       }
     } else if (warp == 9) {
-      // ---------------- MMAs (the whole warp walks the loop, one lane issues)
-      bool ok = ntile == 0 || attn_wait_warp(qbar, 0, abort_flag, g_prompt_wait_ns);
-      auto wait_full = [&](int n) {
-        return attn_wait_warp(&full[n % NSTG], (uint32_t)(n / NSTG) & 1u, abort_flag, g_prompt_wait_ns);
-      };
-      auto qk = [&](int i, int n) {   // scores of tile i with the K tile in ring position n
-        if (lane == 0) {
-          attn_mma_qk<D>(tmem + i * 128, sb + i * C::TILE, sb + C::OFF_KV + (n % NSTG) * C::TILE, a.idesc_qk);
-          tc_commit(&sbar[i]);
-        }
-      };
-      auto release = [&](int n) {
-        if (lane == 0) tc_commit(&free_[n % NSTG]);
-      };
-      if (ok && ntile > 0) {
-        ok = wait_full(0);
-        if (ok) {
+      // ---------------- MMAs, by one thread
+      if (ntile > 0 && attn_elect()) {
+        bool ok = attn_wait(qbar, 0, abort_flag, g_prompt_wait_ns);
+        const uint32_t q_lo = attn_desc_k(sb), k_lo = attn_desc_k(sb + C::OFF_KV), v_lo = attn_desc_mn(sb + C::OFF_KV);
+        int sk = 0, pk = 0;   // ring stage of the next tile to wait for, its phase
+        auto wait_tile = [&]() {
+          ok = attn_wait(&full[sk], pk, abort_flag, g_prompt_wait_ns);
           tc_fence_after();
-          if (nt[0] > 0) qk(0, 0);
-          if (nt[1] > 0) qk(1, 0);
-          release(0);
+          const int s = sk;
+          if (++sk == NSTG) sk = 0, pk ^= 1;
+          return s;
+        };
+        int s = ok ? wait_tile() : 0;
+        if (ok) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (nt[i] > 0) {
+              attn_mma_qk<D>(i * 128, q_lo + i * (C::TILE >> 4), k_lo + s * (C::TILE >> 4), a.idesc_qk);
+              tc_commit(&sbar[i]);
+            }
+          tc_commit(&free_[s]);
         }
+#pragma unroll 1
+        for (int j = 0; ok && j < ntile; ++j) {
+          const int sv = wait_tile();
+          if (!ok) break;
+          if (j * 128 + 128 > lk) {   // the sequence's last V tile ends past it
+            mbar_arrive(zreq);
+            if (!(ok = attn_wait(zbar, 0, abort_flag, g_prompt_wait_ns))) break;
+          }
+          int sn = -1;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (!ok || j >= nt[i]) continue;
+            if (!(ok = attn_wait(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prompt_wait_ns))) continue;
+            tc_fence_after();
+            attn_mma_pv<D>(256 + i * D, i * 128, v_lo + sv * (C::TILE >> 4), j > 0);
+            if (j + 1 < nt[i]) {
+              if (sn < 0) {
+                sn = wait_tile();
+                if (!ok) continue;
+              }
+              attn_mma_qk<D>(i * 128, q_lo + i * (C::TILE >> 4), k_lo + sn * (C::TILE >> 4), a.idesc_qk);
+              tc_commit(&sbar[i]);
+            } else {
+              tc_commit(&obar[i]);
+            }
+          }
+          if (!ok) break;
+          tc_commit(&free_[sv]);
+          if (sn >= 0) tc_commit(&free_[sn]);
+        }
+        tc_commit(drain);   // what is in flight finishes before tensor memory is given up
+        mbar_wait_bounded(drain, 0, kAttnWaitLimitNs);
       }
-      for (int j = 0; ok && j < ntile; ++j) {
-        const int nv = 2 * j + 1, nn = 2 * j + 2;
-        if (!(ok = wait_full(nv))) break;
-        const uint32_t vb = sb + C::OFF_KV + (nv % NSTG) * C::TILE;
-        if (j * 128 + 128 > lk) {   // rows past the sequence
-          const int from = (lk - j * 128) * 128;   // byte offset in each atom
+    } else if (warp == 10) {
+      // ---------------- rows of the last V tile past the sequence: zeroed
+      if (ntile * 128 > lk) {
+        const int n = 2 * ntile - 1;
+        if (attn_wait_warp(zreq, 0, abort_flag, g_prompt_wait_ns)) {   // the tile is in
+          const uint32_t vb = sb + C::OFF_KV + (n % NSTG) * C::TILE, from = (lk - (ntile - 1) * 128) * 128;
           for (int at = 0; at < D / 64; ++at)
             for (uint32_t o = from + lane * 16; o < kAttnAtom; o += 512)
               sts128(vb + at * kAttnAtom + o, make_uint4(0, 0, 0, 0));
           fence_proxy_async_smem();
           __syncwarp();
+          if (lane == 0) mbar_arrive(zbar);
         }
-        bool have_k = false;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (j >= nt[i]) continue;
-          if (!(ok = attn_wait_warp(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prompt_wait_ns))) break;
-          tc_fence_after();
-          if (lane == 0) attn_mma_pv<D>(tmem + 256 + i * D, tmem + i * 128, vb, j > 0);
-          if (j + 1 < nt[i]) {
-            if (!have_k) {
-              if (!(ok = wait_full(nn))) break;
-              tc_fence_after();
-              have_k = true;
-            }
-            qk(i, nn);
-          } else if (lane == 0) {
-            tc_commit(&obar[i]);
-          }
-        }
-        if (!ok) break;
-        release(nv);
-        if (have_k) release(nn);
       }
     }
   } else {
@@ -308,13 +327,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
   tc_fence_before();
   __syncthreads();
   if (*abort_flag) {
-    // let the MMAs and copies in flight finish before the memory is given up
-    if (warp == 9) {
-      const bool q_in = *issued >= 0;
-      if (q_in) mbar_wait_bounded(qbar, 0, kAttnWaitLimitNs);
-      if (lane == 0) tc_commit(qbar);
-      mbar_wait_bounded(qbar, q_in ? 1u : 0u, kAttnWaitLimitNs);
-    }
+    // the copies in flight land before the memory is given up
+    if (tid == 0 && *issued >= 0) mbar_wait_bounded(qbar, 0, kAttnWaitLimitNs);
     if (tid == 0)
       for (int n = max(0, *issued - NSTG); n < *issued; ++n)
         mbar_wait_bounded(&full[n % NSTG], (uint32_t)(n / NSTG) & 1u, kAttnWaitLimitNs);
@@ -322,7 +336,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
     __syncthreads();
   }
   tc_fence_after();
-  if (warp == 9) tmem_dealloc(tmem, 512);
+  if (warp == 9) tmem_dealloc(*tmem_slot, 512);
 }
 
 // fp16 [tokens] rows of H heads of D values, ld elements apart, in boxes of 64
