@@ -78,8 +78,8 @@ struct PrefixCfg {
   static constexpr int OFF_KV = 2 * TILE;
   static constexpr int OFF_COL = OFF_KV + NSTG * TILE;   // [NCOL][2][64] float4
   static constexpr int OFF_RM = OFF_COL + NCOL * 2048 * 2;   // [NCOL][4] largest alpha' of each warp's tokens
-  static constexpr int OFF_BAR = OFF_RM + NCOL * 16;     // q, full, free [NSTG], col [NCOL], s, p, o [2], drain
-  static constexpr int OFF_MISC = OFF_BAR + (2 * NSTG + NCOL + 8) * 8;
+  static constexpr int OFF_BAR = OFF_RM + NCOL * 16;     // q, full, free [NSTG], col [NCOL], s, p, o, drain [2]
+  static constexpr int OFF_MISC = OFF_BAR + (2 * NSTG + NCOL + 9) * 8;
   static constexpr int BYTES = OFF_MISC + 16 + 1024;
   static_assert(BYTES <= 232448, "shared memory");
 };
@@ -106,19 +106,21 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_MISC + 4);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
+  const int b0 = blockIdx.x * 2 * p.tps;
+  const int nrow = b0 + p.tps < (int)a.B ? 2 : 1;   // tiles of rows
   if (tid == 0) {
     mbar_init(qbar, 8);
     for (int s = 0; s < NSTG; ++s) {
       mbar_init(&full[s], 4);
-      mbar_init(&free_[s], 1);
+      mbar_init(&free_[s], nrow);
     }
     for (int s = 0; s < NCOL; ++s) mbar_init(&cbar[s], 4);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sbar[i], 1);
       mbar_init(&pbar[i], 4);
       mbar_init(&obar[i], 1);
+      mbar_init(&drain[i], 1);
     }
-    mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -133,11 +135,10 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
   pdl_wait();
   pdl_trigger();
 
-  const int hk = blockIdx.y, b0 = blockIdx.x * 2 * p.tps;
+  const int hk = blockIdx.y;
   const int ntiles = (int)((a.prefix_len + 127) / 128);
   const int j0 = (int)((int64_t)ntiles * blockIdx.z / p.nsplit), j1 = (int)((int64_t)ntiles * (blockIdx.z + 1) / p.nsplit);
   const int nt = j1 - j0;                              // tiles of 128 tokens of this part
-  const int nrow = b0 + p.tps < (int)a.B ? 2 : 1;      // tiles of rows
   const uint32_t sb = smem_u32(smem);
 
   if (warp >= 12) {
@@ -214,55 +215,45 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
   } else if (warp >= 8) {
     // ---------------- MMAs
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
-    if (warp == 8 && nt > 0 && attn_elect()) {
+    const int i = warp - 8;   // tile of rows whose MMAs this warp's thread issues
+    if (i < nrow && nt > 0 && attn_elect()) {
       constexpr uint32_t idesc = umma_idesc_f16_f32(128, 128, false);
       bool ok = attn_wait(qbar, 0, abort_flag, g_prefix_wait_ns);
-      const uint32_t q_lo = attn_desc_k(sb), k_lo = attn_desc_k(sb + C::OFF_KV), v_lo = attn_desc_mn(sb + C::OFF_KV);
+      const uint32_t q_lo = attn_desc_k(sb + i * C::TILE), k_lo = attn_desc_k(sb + C::OFF_KV),
+                     v_lo = attn_desc_mn(sb + C::OFF_KV);
       int sk = 0, pk = 0;   // ring stage of the next tile to wait for, its phase
       auto wait_tile = [&]() {
         ok = attn_wait(&full[sk], pk, abort_flag, g_prefix_wait_ns);
-        tc_fence_after();
         const int s = sk;
         if (++sk == NSTG) sk = 0, pk ^= 1;
         return s;
       };
-      int s = ok ? wait_tile() : 0;
+      const int s0 = ok ? wait_tile() : 0;
       if (ok) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (i < nrow) {
-            attn_mma_qk<D>(i * 128, q_lo + i * (C::TILE >> 4), k_lo + s * (C::TILE >> 4), idesc);
-            tc_commit(&sbar[i]);
-          }
-        tc_commit(&free_[s]);
+        tc_fence_after();
+        attn_mma_qk<D>(i * 128, q_lo, k_lo + s0 * (C::TILE >> 4), idesc);
+        tc_commit(&sbar[i]);
+        tc_commit(&free_[s0]);
       }
 #pragma unroll 1
       for (int j = 0; ok && j < nt; ++j) {
         const int sv = wait_tile();
-        int sn = -1;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (!ok || i >= nrow) continue;
-          if (!(ok = attn_wait(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns))) continue;
-          tc_fence_after();
-          attn_mma_pv<D>(256 + i * D, i * 128, v_lo + sv * (C::TILE >> 4), j > 0);
-          if (j + 1 < nt) {
-            if (i == 0) {
-              sn = wait_tile();
-              if (!ok) continue;
-            }
-            attn_mma_qk<D>(i * 128, q_lo + i * (C::TILE >> 4), k_lo + sn * (C::TILE >> 4), idesc);
-            tc_commit(&sbar[i]);
-          } else {
-            tc_commit(&obar[i]);
-          }
-        }
         if (!ok) break;
-        tc_commit(&free_[sv]);
-        if (sn >= 0) tc_commit(&free_[sn]);
+        const int sn = j + 1 < nt ? wait_tile() : -1;   // ahead of the weights, as in the prompt kernel
+        if (!ok || !(ok = attn_wait(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns))) break;
+        tc_fence_after();
+        attn_mma_pv<D>(256 + i * D, i * 128, v_lo + sv * (C::TILE >> 4), j > 0);
+        if (sn >= 0) {
+          attn_mma_qk<D>(i * 128, q_lo, k_lo + sn * (C::TILE >> 4), idesc);
+          tc_commit(&sbar[i]);
+          tc_commit(&free_[sv]);
+          tc_commit(&free_[sn]);
+        } else {
+          tc_commit(&obar[i]);
+        }
       }
-      tc_commit(drain);   // what is in flight finishes before tensor memory is given up
-      mbar_wait_bounded(drain, 0, kAttnWaitLimitNs);
+      tc_commit(&drain[i]);   // what is in flight finishes before tensor memory is given up
+      mbar_wait_bounded(&drain[i], 0, kAttnWaitLimitNs);
     }
   } else {
     // ---------------- softmax: warps 4i .. 4i + 3 own tile i, thread = row

@@ -20,9 +20,12 @@
 //    rescaled) and sum in fp32 registers;
 //  * warp 8: one thread copies Q, then the K and V tiles of 128 tokens into
 //    a ring of stages by TMA (128-byte swizzle);
-//  * warp 10: zeroes the last V tile's rows past the sequence;
-//  * warp 9: one thread issues the MMAs: PV and the next QK of tile 0, then of tile 1,
-//    so that each tile's softmax runs under the other tile's products.
+//  * warps 9 and 10: one thread each issues the MMAs of tile 0 and 1, PV then the
+//    next QK.  An issue blocks while the tensor core is busy, and a wait on a
+//    barrier costs 150 to 230 cycles beside MMAs that read shared memory at its full
+//    rate: with one issuing thread for both tiles the tensor core idled
+//    through those waits (4 x 4096: 484 us so, XXX with two);
+//  * warp 11: zeroes the last V tile's rows past the sequence.
 // Bound: the tensor core (4 D flops per visible pair of a query head and a
 // key).
 //
@@ -65,8 +68,8 @@ struct PromptCfg {
   static constexpr int TILE = 128 * D * 2;               // bytes of a Q, K or V tile
   static constexpr int NSTG = D == 128 ? 5 : 8;
   static constexpr int OFF_KV = 2 * TILE;
-  static constexpr int OFF_BAR = OFF_KV + NSTG * TILE;   // q, full[NSTG], free[NSTG], s[2], p[2], o[2], z[2], drain
-  static constexpr int OFF_MISC = OFF_BAR + (2 * NSTG + 10) * 8;
+  static constexpr int OFF_BAR = OFF_KV + NSTG * TILE;   // q, full[NSTG], free[NSTG], s[2], p[2], o[2], z[2], drain[2]
+  static constexpr int OFF_MISC = OFF_BAR + (2 * NSTG + 11) * 8;
   static constexpr int BYTES = OFF_MISC + 16 + 1024;
   static_assert(BYTES <= 232448, "shared memory");
 };
@@ -90,7 +93,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
   uint64_t* obar = pbar + 2;       // last product of tile i done
   uint64_t* zreq = obar + 2;       // the sequence's last V tile is in,
   uint64_t* zbar = zreq + 1;       // its rows past the sequence are zeroed
-  uint64_t* drain = zbar + 1;      // every MMA done
+  uint64_t* drain = zbar + 1;      // every MMA of tile i done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_MISC + 4);
   int* issued = reinterpret_cast<int*>(smem + C::OFF_MISC + 8);   // K and V tiles copied (0: Q neither)
@@ -100,16 +103,16 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
     mbar_init(qbar, 1);
     for (int s = 0; s < NSTG; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&free_[s], 1);
+      mbar_init(&free_[s], 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sbar[i], 1);
       mbar_init(&pbar[i], 4);
       mbar_init(&obar[i], 1);
+      mbar_init(&drain[i], 1);
     }
     mbar_init(zreq, 1);
     mbar_init(zbar, 1);
-    mbar_init(drain, 1);
     *abort_flag = 0;
     *issued = -1;
     fence_mbar_init();
@@ -170,63 +173,59 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
           *issued = n + 1;
         }
       }
-    } else if (warp == 9) {
-      // ---------------- MMAs, by one thread
+    } else if (warp < 11) {
+      // ---------------- MMAs of tile i, by one thread
+      const int i = warp - 9, nti = i ? nt[1] : nt[0];
       if (ntile > 0 && attn_elect()) {
         bool ok = attn_wait(qbar, 0, abort_flag, g_prompt_wait_ns);
-        const uint32_t q_lo = attn_desc_k(sb), k_lo = attn_desc_k(sb + C::OFF_KV), v_lo = attn_desc_mn(sb + C::OFF_KV);
-        int sk = 0, pk = 0;   // ring stage of the next tile to wait for, its phase
+        const uint32_t q_lo = attn_desc_k(sb + i * C::TILE), k_lo = attn_desc_k(sb + C::OFF_KV),
+                       v_lo = attn_desc_mn(sb + C::OFF_KV);
+        int sk = 0, pk = 0;   // ring stage of the next K or V tile, its phase
         auto wait_tile = [&]() {
           ok = attn_wait(&full[sk], pk, abort_flag, g_prompt_wait_ns);
-          tc_fence_after();
           const int s = sk;
           if (++sk == NSTG) sk = 0, pk ^= 1;
           return s;
         };
-        int s = ok ? wait_tile() : 0;
+        const int s0 = ok ? wait_tile() : 0;
         if (ok) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            if (nt[i] > 0) {
-              attn_mma_qk<D>(i * 128, q_lo + i * (C::TILE >> 4), k_lo + s * (C::TILE >> 4), a.idesc_qk);
-              tc_commit(&sbar[i]);
-            }
-          tc_commit(&free_[s]);
+          tc_fence_after();
+          if (nti > 0) {
+            attn_mma_qk<D>(i * 128, q_lo, k_lo + s0 * (C::TILE >> 4), a.idesc_qk);
+            tc_commit(&sbar[i]);
+          }
+          tc_commit(&free_[s0]);
         }
 #pragma unroll 1
         for (int j = 0; ok && j < ntile; ++j) {
           const int sv = wait_tile();
           if (!ok) break;
-          if (j * 128 + 128 > lk) {   // the sequence's last V tile ends past it
-            mbar_arrive(zreq);
-            if (!(ok = attn_wait(zbar, 0, abort_flag, g_prompt_wait_ns))) break;
-          }
-          int sn = -1;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (!ok || j >= nt[i]) continue;
-            if (!(ok = attn_wait(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prompt_wait_ns))) continue;
+          // everything else is waited for ahead of the weights: what follows
+          // those is on the path from this tile's softmax to its next scores
+          const int sn = j + 1 < ntile ? wait_tile() : -1;
+          if (!ok) break;
+          if (j < nti) {
+            if (j * 128 + 128 > lk) {   // the sequence's last V tile ends past it
+              if (i == 0 || nt[0] < ntile) mbar_arrive(zreq);
+              if (!(ok = attn_wait(zbar, 0, abort_flag, g_prompt_wait_ns))) break;
+            }
+            if (!(ok = attn_wait(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prompt_wait_ns))) break;
             tc_fence_after();
             attn_mma_pv<D>(256 + i * D, i * 128, v_lo + sv * (C::TILE >> 4), j > 0);
-            if (j + 1 < nt[i]) {
-              if (sn < 0) {
-                sn = wait_tile();
-                if (!ok) continue;
-              }
-              attn_mma_qk<D>(i * 128, q_lo + i * (C::TILE >> 4), k_lo + sn * (C::TILE >> 4), a.idesc_qk);
+            if (j + 1 < nti) {
+              attn_mma_qk<D>(i * 128, q_lo, k_lo + sn * (C::TILE >> 4), a.idesc_qk);
               tc_commit(&sbar[i]);
             } else {
               tc_commit(&obar[i]);
             }
           }
-          if (!ok) break;
           tc_commit(&free_[sv]);
           if (sn >= 0) tc_commit(&free_[sn]);
         }
-        tc_commit(drain);   // what is in flight finishes before tensor memory is given up
-        mbar_wait_bounded(drain, 0, kAttnWaitLimitNs);
+        tc_commit(&drain[i]);   // what is in flight finishes before tensor memory is given up
+        mbar_wait_bounded(&drain[i], 0, kAttnWaitLimitNs);
       }
-    } else if (warp == 10) {
+    } else {
       // ---------------- rows of the last V tile past the sequence: zeroed
       if (ntile * 128 > lk) {
         const int n = 2 * ntile - 1;
