@@ -76,6 +76,14 @@ __device__ __forceinline__ void tmem_st_32x32b_x32(uint32_t taddr, const uint32_
       "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_t r[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 
 // Waits for the tensor-memory loads of r[N] (N a multiple of 16).
@@ -166,17 +174,18 @@ __device__ __forceinline__ float attn_row_max(const uint32_t* r) {
   return fmaxf(attn_max3(m[0], m[1], m[2]), m[3]);
 }
 
-// Rescales this lane's row of an accumulator in tensor memory (D columns).
-template <int D>
+// Rescales this lane's row of an accumulator in tensor memory (N columns), 16
+// at a time: it runs while the row's scores are held in registers.
+template <int N>
 __device__ __forceinline__ void attn_rescale(uint32_t o_tmem, float f) {
 #pragma unroll
-  for (int c = 0; c < D; c += 32) {
-    uint32_t o[32];
-    tmem_ld_32x32b_x32(o_tmem + c, o);
-    tmem_ld_wait_all<32>(o);
+  for (int c = 0; c < N; c += 16) {
+    uint32_t o[16];
+    tmem_ld_32x32b_x16(o_tmem + c, o);
+    tmem_ld_wait(o);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-    tmem_st_32x32b_x32(o_tmem + c, o);
+    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+    tmem_st_32x32b_x16(o_tmem + c, o);
   }
   tmem_st_wait();
 }
