@@ -409,17 +409,42 @@ __device__ __forceinline__ uint32_t own_transpose(uint32_t x) {   // 8x8 fp16 tr
   return y;
 }
 
-// grid (chunk, kv head x group of 8 query heads, sequence).  A warp takes
-// steps of 16 tokens, which lie in one page: the rows of codes it needs are
-// contiguous, and each lane loads its own fragments (lane = 4 g + c): key rows
-// g and g + 8, bytes [c D/8, (c+1) D/8); value rows 2c, 2c+1, 2c+8, 2c+9, bytes
-// [g D/16, (g+1) D/16).  Scores: tokens on M, heads on N; values: head_dim
-// on M, tokens on K, heads on N.
+constexpr int kOwnStages = 4;
+
+__device__ __forceinline__ void own_copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+
+// A warp's ring of stages: 16 tokens' key rows, value rows (D/2 bytes each) and
+// scales.  Key rows lie as in the page (a fragment load covers eight whole rows);
+// a fragment load of the values takes 8 or 4 bytes of rows 0, 2, 4, 6 (or 1, 3,
+// ..), so their 16-byte pieces are moved about to fall in different banks.
 template <int D>
-__global__ void __launch_bounds__(kOwnWarps * 32) own_tokens_kernel(const PrefixParams p, int hgroups, int chunk_len) {
+struct OwnRing {
+  static constexpr int KB = 16 * (D / 2), STAGE = 2 * KB + 256, WARP = kOwnStages * STAGE;
+  static constexpr int CPR = D / 32;   // 16-byte pieces of a row
+  static __device__ __forceinline__ int value_at(int row, int piece) {   // byte offset of a value row's piece
+    if (D == 128) {
+      const int pair = row >> 1;
+      return pair * 128 + (((row ^ pair) & 1) << 6) + ((piece ^ (pair & 2)) << 4);
+    }
+    return row * 32 + ((piece ^ ((row >> 2) & 1)) << 4);
+  }
+};
+
+// grid (chunk, kv head x group of 8 query heads, sequence).  A warp takes
+// steps of 16 tokens, which lie in one page, so its rows of codes are one run of
+// memory, copied three steps ahead into the warp's ring.  Fragments of lane
+// 4 g + c: key rows g and g + 8, bytes [c D/8, (c+1) D/8); value rows 2c, 2c+1, 2c+8,
+// 2c+9, bytes [g D/16, (g+1) D/16).  Scores: tokens on M, heads on N; values:
+// head_dim on M, tokens on K, heads on N.
+template <int D>
+__global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const PrefixParams p, int hgroups, int chunk_len) {
   constexpr int KW = D / 32, VW = D / 64, NM = D / 16;
   const PrefixArgs& a = p.a;
-  __shared__ float o_s[kOwnWarps][8][D];
+  using Ring = OwnRing<D>;
+  __shared__ __align__(16) uint8_t ring_s[kOwnWarps][Ring::WARP];   // after the loop: float o [8][D]
+  static_assert(8 * D * 4 <= Ring::WARP, "the output fits in the ring");
   __shared__ float m_s[kOwnWarps][8], l_s[kOwnWarps][8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   const int hk = blockIdx.y / hgroups, hg = blockIdx.y % hgroups, b = blockIdx.z;
@@ -436,11 +461,19 @@ __global__ void __launch_bounds__(kOwnWarps * 32) own_tokens_kernel(const Prefix
   const int32_t* table = a.table + (int64_t)b * a.table_width;
   const int64_t row0 = (int64_t)b * a.Hq + hk * p.G + 8 * hg;
 
-  // query fragments of head g (k order as the codes come), their sums
+  // query fragments of head g (k order as the codes come), their sums.  A key
+  // code is masked out of its word in place: as fp16 bits the nibbles at bits 0 and 16
+  // are u 2^-24, those at bits 4 and 20 are 16 u 2^-24, both exact operands; the
+  // latter meet query values divided by 16.
   uint32_t qb[2 * KW][2];
   float qs = 0.f;
   {
     const __half* qh = reinterpret_cast<const __half*>(a.q) + (row0 + (g < heads ? g : 0)) * D + c * (D / 4);
+    const __half2 sixteenth = __float2half2_rn(0.0625f);
+    auto over16 = [&](uint32_t x) {
+      const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&x), sixteenth);
+      return *reinterpret_cast<const uint32_t*>(&h);
+    };
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
       uint4 x = __ldg(reinterpret_cast<const uint4*>(qh + 8 * w));
@@ -452,91 +485,118 @@ __global__ void __launch_bounds__(kOwnWarps * 32) own_tokens_kernel(const Prefix
         qs += f.x + f.y;
       }
       qb[2 * w][0] = __byte_perm(x.x, x.z, 0x5410);
-      qb[2 * w][1] = __byte_perm(x.x, x.z, 0x7632);
+      qb[2 * w][1] = over16(__byte_perm(x.x, x.z, 0x7632));
       qb[2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410);
-      qb[2 * w + 1][1] = __byte_perm(x.y, x.w, 0x7632);
+      qb[2 * w + 1][1] = over16(__byte_perm(x.y, x.w, 0x7632));
     }
     qs += __shfl_xor_sync(0xffffffffu, qs, 1);
     qs += __shfl_xor_sync(0xffffffffu, qs, 2);
   }
-  const float qsk[2] = {__shfl_sync(0xffffffffu, qs, 8 * c), __shfl_sync(0xffffffffu, qs, 8 * c + 4)};
+  const float qsk[2] = {p.scale_log2 * __shfl_sync(0xffffffffu, qs, 8 * c),
+                        p.scale_log2 * __shfl_sync(0xffffffffu, qs, 8 * c + 4)};
+  const float ks24 = p.scale_log2 * 16777216.f;
 
-  struct Step {
-    uint32_t k[2][KW], v[4][VW];
-    float4 sc[2];
-  };
-  auto load = [&](int i, Step& x) {
-    const int t = t0 + 16 * (warp + kOwnWarps * i);   // chunks start at multiples of 16
-    const int64_t at = (page_at(a, table, t, shift) * a.Hkv + hk) * a.page_size + (t & (a.page_size - 1));
-    const uint8_t* kb = a.k_codes + at * (D / 2) + c * (D / 8);
-    const uint8_t* vb = a.v_codes + at * (D / 2) + g * (D / 16);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if constexpr (KW == 4) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>(kb + (g + 8 * h) * (D / 2)));
-        x.k[h][0] = w.x, x.k[h][1] = w.y, x.k[h][2] = w.z, x.k[h][3] = w.w;
-      } else {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(kb + (g + 8 * h) * (D / 2)));
-        x.k[h][0] = w.x, x.k[h][1] = w.y;
+  // Lane n holds the place in the page arrays of the warp's step 32 b + n (of
+  // head hk, in tokens): one look-up for 32 steps.
+  int64_t place = 0;
+  const uint32_t ring = smem_u32(ring_s[warp]);
+  auto issue = [&](int i) {   // copies of step i (an empty group past the end keeps the count)
+    if (i < nstep) {
+      if ((i & 31) == 0) {
+        if (i + lane < nstep) {
+          const int t = t0 + 16 * (warp + kOwnWarps * (i + lane));   // chunks start at multiples of 16
+          place = (page_at(a, table, t, shift) * a.Hkv + hk) * a.page_size + (t & (a.page_size - 1));
+        }
       }
-      x.sc[h] = __ldg(reinterpret_cast<const float4*>(a.scales) + at + g + 8 * h);
-    }
+      const int64_t at = __shfl_sync(0xffffffffu, place, i & 31);
+      const uint32_t st = ring + (uint32_t)(i % kOwnStages) * Ring::STAGE;
+      const uint8_t* kr = a.k_codes + at * (D / 2);
+      const uint8_t* vr = a.v_codes + at * (D / 2);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint8_t* s = vb + (8 * (q >> 1) + 2 * c + (q & 1)) * (D / 2);
-      if constexpr (VW == 2) {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(s));
-        x.v[q][0] = w.x, x.v[q][1] = w.y;
-      } else {
-        x.v[q][0] = __ldg(reinterpret_cast<const uint32_t*>(s));
+      for (int n = 0; n < D / 64; ++n) {
+        const int piece = lane + 32 * n;
+        own_copy16(st + piece * 16, kr + piece * 16);
+        own_copy16(st + Ring::KB + Ring::value_at(piece / Ring::CPR, piece % Ring::CPR), vr + piece * 16);
       }
+      if (lane < 16) own_copy16(st + 2 * Ring::KB + lane * 16, a.scales + (at + lane) * 4);
     }
+    asm volatile("cp.async.commit_group;\n" ::: "memory");
   };
 
   float o[NM][4];
 #pragma unroll
   for (int mu = 0; mu < NM; ++mu) o[mu][0] = o[mu][1] = o[mu][2] = o[mu][3] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, z[2] = {0.f, 0.f}, lr = 0.f, rcur = 0.f;
-  Step nxt;
-  if (nstep > 0) load(0, nxt);
+  // M = m + lr: the weights are 2^(s - M) alpha'
+  float m[2] = {-INFINITY, -INFINITY}, off[2] = {0.f, 0.f}, l[2] = {0.f, 0.f}, z[2] = {0.f, 0.f}, lr = 0.f, rcur = 0.f;
+#pragma unroll
+  for (int i = 0; i < kOwnStages - 1; ++i) issue(i);
   for (int i = 0; i < nstep; ++i) {
-    const Step x = nxt;
-    if (i + 1 < nstep) load(i + 1, nxt);
-    const int left = t1 - (t0 + 16 * (warp + kOwnWarps * i));
+    asm volatile("cp.async.wait_group %0;\n" ::"n"(kOwnStages - 2) : "memory");
+    __syncwarp();   // step i has landed for every lane, and step i - 1's stage has been read
+    issue(i + kOwnStages - 1);
+    const uint8_t* st = ring_s[warp] + (i % kOwnStages) * Ring::STAGE;
+    struct {
+      uint32_t k[2][KW], v[4][VW];
+      float4 sc[2];
+    } x;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* kr = st + (g + 8 * h) * (D / 2) + c * (D / 8);
+      if constexpr (KW == 4) {
+        const uint4 w = *reinterpret_cast<const uint4*>(kr);
+        x.k[h][0] = w.x, x.k[h][1] = w.y, x.k[h][2] = w.z, x.k[h][3] = w.w;
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(kr);
+        x.k[h][0] = w.x, x.k[h][1] = w.y;
+      }
+      x.sc[h] = *reinterpret_cast<const float4*>(st + 2 * Ring::KB + (g + 8 * h) * 16);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int row = 8 * (q >> 1) + 2 * c + (q & 1);
+      const uint8_t* vr = st + Ring::KB + Ring::value_at(row, g * (D / 16) / 16) + g * (D / 16) % 16;
+      if constexpr (VW == 2) {
+        const uint2 w = *reinterpret_cast<const uint2*>(vr);
+        x.v[q][0] = w.x, x.v[q][1] = w.y;
+      } else {
+        x.v[q][0] = *reinterpret_cast<const uint32_t*>(vr);
+      }
+    }
     float sa[4] = {0.f, 0.f, 0.f, 0.f}, sc2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
-      const uint4 x0 = code_pairs(x.k[0][w]), x1 = code_pairs(x.k[1][w]);
-      const uint32_t a0[4] = {x0.x, x1.x, x0.y, x1.y}, a1[4] = {x0.z, x1.z, x0.w, x1.w};
+      const uint32_t x0 = x.k[0][w], x1 = x.k[1][w], y0 = x0 >> 8, y1 = x1 >> 8;
+      const uint32_t a0[4] = {x0 & 0x000F000Fu, x1 & 0x000F000Fu, x0 & 0x00F000F0u, x1 & 0x00F000F0u};
+      const uint32_t a1[4] = {y0 & 0x000F000Fu, y1 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x00F000F0u};
       mma_16816_f16_f32_acc(sa, a0, qb[2 * w][0], qb[2 * w][1]);
       mma_16816_f16_f32_acc(sc2, a1, qb[2 * w + 1][0], qb[2 * w + 1][1]);
     }
     // scores (base 2) of tokens g, g + 8 for heads 2c, 2c + 1; tokens past the
     // chunk (their slots may hold anything) get -inf and value numbers 0
     float t[2][2], va[2], vz[2];
-    bool grow = false;
+    const int left = t1 - (t0 + 16 * (warp + kOwnWarps * i));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const bool in = g + 8 * h < left;
-      const float ka = p.scale_log2 * x.sc[h].x, kz = p.scale_log2 * fmaf(8.f, x.sc[h].x, x.sc[h].y);
-      va[h] = in ? x.sc[h].z : 0.f;
-      vz[h] = in ? fmaf(8.f, x.sc[h].z, x.sc[h].w) : 0.f;
-      grow |= va[h] > 16.f * rcur;
+      const float ka = ks24 * x.sc[h].x;
+      va[h] = x.sc[h].z;
+      vz[h] = fmaf(8.f, x.sc[h].z, x.sc[h].w);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        t[h][e] = in ? fmaf(ka, sa[2 * h + e] + sc2[2 * h + e], kz * qsk[e]) : -INFINITY;
-        grow |= t[h][e] > m[e] + kAttnSlack;
-      }
+      for (int e = 0; e < 2; ++e) t[h][e] = fmaf(ka, sa[2 * h + e] + sc2[2 * h + e], x.sc[h].y * qsk[e]);
     }
-    if (__any_sync(0xffffffffu, grow)) {
-      float mx[2] = {fmaxf(t[0][0], t[1][0]), fmaxf(t[0][1], t[1][1])}, rm = fmaxf(va[0], va[1]);
+    if (left < 16) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (g + 8 * h >= left) t[h][0] = t[h][1] = -INFINITY, va[h] = vz[h] = 0.f;
+    }
+    const float rm0 = fmaxf(va[0], va[1]), mx0 = fmaxf(t[0][0], t[1][0]), mx1 = fmaxf(t[0][1], t[1][1]);
+    if (__any_sync(0xffffffffu, rm0 > 16.f * rcur || mx0 > m[0] + kAttnSlack || mx1 > m[1] + kAttnSlack)) {
+      float mx[2] = {mx0, mx1}, rm = rm0;
 #pragma unroll
       for (int w = 4; w < 32; w <<= 1) {
         mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], w));
         mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], w));
         rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, w));
       }
-      const float lr0 = lr;
       if (rm > 16.f * rcur) {
         rcur = fmaxf(rm, kMinValueScale);
         lr = __log2f(rcur);
@@ -545,8 +605,10 @@ __global__ void __launch_bounds__(kOwnWarps * 32) own_tokens_kernel(const Prefix
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float mn = mx[e] > m[e] + kAttnSlack ? mx[e] : m[e];
-        f[e] = m[e] == -INFINITY ? 0.f : attn_exp2((m[e] + lr0) - (mn + lr));
+        const float to = mn == -INFINITY ? 0.f : mn + lr;
+        f[e] = m[e] == -INFINITY ? 0.f : attn_exp2(off[e] - to);
         m[e] = mn;
+        off[e] = to;
         l[e] *= f[e];
         z[e] *= f[e];
       }
@@ -558,16 +620,14 @@ __global__ void __launch_bounds__(kOwnWarps * 32) own_tokens_kernel(const Prefix
     }
     float w[2][2];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float off = m[e] == -INFINITY ? 0.f : m[e] + lr;
+    for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float pe = attn_exp2(t[h][e] - off);
+        const float pe = attn_exp2(t[h][e] - off[e]);
         l[e] += pe;
         z[e] = fmaf(pe, vz[h], z[e]);
         w[h][e] = pe * va[h];
       }
-    }
     const uint32_t pb0 = own_transpose(pack_half2_bits(w[0][0], w[0][1]));
     const uint32_t pb1 = own_transpose(pack_half2_bits(w[1][0], w[1][1]));
 #pragma unroll
@@ -592,13 +652,16 @@ __global__ void __launch_bounds__(kOwnWarps * 32) own_tokens_kernel(const Prefix
       z[e] += __shfl_xor_sync(0xffffffffu, z[e], w);
     }
   const float back = rcur > 0.f ? rcur : 1.f;
+  asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+  __syncwarp();   // the ring is free
+  float* o_w = reinterpret_cast<float*>(ring_s[warp]);
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int h = 2 * c + e;
 #pragma unroll
     for (int mu = 0; mu < NM; ++mu) {
-      o_s[warp][h][g * (D / 8) + 2 * mu] = (o[mu][e] + z[e]) * back;
-      o_s[warp][h][g * (D / 8) + 2 * mu + 1] = (o[mu][2 + e] + z[e]) * back;
+      o_w[h * D + g * (D / 8) + 2 * mu] = (o[mu][e] + z[e]) * back;
+      o_w[h * D + g * (D / 8) + 2 * mu + 1] = (o[mu][2 + e] + z[e]) * back;
     }
     if (g == 0) {
       m_s[warp][h] = m[e];
@@ -616,7 +679,7 @@ __global__ void __launch_bounds__(kOwnWarps * 32) own_tokens_kernel(const Prefix
 #pragma unroll
     for (int w = 0; w < kOwnWarps; ++w) {
       const float f = l_s[w][h] > 0.f ? attn_exp2(m_s[w][h] - M) : 0.f;
-      val = fmaf(f, o_s[w][h][d], val);
+      val = fmaf(f, reinterpret_cast<const float*>(ring_s[w])[h * D + d], val);
       ls = fmaf(f, l_s[w][h], ls);
     }
     p.o[(part * rows + row0 + h) * D + d] = val;
