@@ -264,24 +264,37 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
     const int b = b0 + i * p.tps + r / p.G, head = hk * p.G + r % p.G;
     const bool live = r < p.G * p.tps && b < (int)a.B;
     const bool work = __any_sync(0xffffffffu, live);   // the warp has a row at all
-    // the row of Q, its pairs in the order of code_pairs, and its sum
+    // The warp's rows of Q, their pairs in the order of code_pairs, and the sum of
+    // this thread's: D / 8 lanes share a row, every load is under way at once.
     float qs = 0.f;
     {
-      const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(a.q) +
-                                                        ((int64_t)b * a.Hq + head) * D);
-#pragma unroll 4
-      for (int ch = 0; ch < D / 8; ++ch) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (live) w = __ldg(src + ch);
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+      constexpr int LPR = D / 8, RPL = 32 / LPR;   // lanes per row, rows per load
+      const int64_t at = live ? ((int64_t)b * a.Hq + head) * D : -1;   // this thread's row
+      const int ch = lane % LPR;
+      uint4 w[32 / RPL];
+#pragma unroll
+      for (int k = 0; k < 32 / RPL; ++k) {
+        const int64_t src = __shfl_sync(0xffffffffu, at, k * RPL + lane / LPR);
+        w[k] = src >= 0 ? __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(a.q) + src) + ch)
+                        : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int k = 0; k < 32 / RPL; ++k) {
+        const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+        float sum = 0.f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[q]));
-          qs += f.x + f.y;
+          sum += f.x + f.y;
         }
-        *reinterpret_cast<uint4*>(smem + i * C::TILE + (ch >> 3) * kAttnAtom + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) =
-            make_uint4(__byte_perm(w.x, w.z, 0x5410), __byte_perm(w.x, w.z, 0x7632), __byte_perm(w.y, w.w, 0x5410),
-                       __byte_perm(w.y, w.w, 0x7632));
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const float mine = __shfl_sync(0xffffffffu, sum, (lane % RPL) * LPR);
+        if (lane / RPL == k) qs = mine;
+        const int row = (warp & 3) * 32 + k * RPL + lane / LPR;
+        *reinterpret_cast<uint4*>(smem + i * C::TILE + (ch >> 3) * kAttnAtom + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) =
+            make_uint4(__byte_perm(x[0], x[2], 0x5410), __byte_perm(x[0], x[2], 0x7632), __byte_perm(x[1], x[3], 0x5410),
+                       __byte_perm(x[1], x[3], 0x7632));
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -369,22 +382,38 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
       const int64_t row = (int64_t)b * a.Hq + head, rows = a.B * a.Hq;
       const float back = rcur > 0.f ? rcur : 1.f;   // 2^lr: the sums to weights 2^(s - m)
       if (live) p.ml[(int64_t)blockIdx.z * rows + row] = make_float2(m, l * back);
-      float* out = p.o + ((int64_t)blockIdx.z * rows + row) * D;
+      // 64 values of each row at a time through the tile's Q rows, which no product
+      // reads any more, so that a row's values leave in one run
+      const int64_t at = live ? ((int64_t)blockIdx.z * rows + row) * D : -1;
+      uint8_t* buf = smem + i * C::TILE + (warp & 3) * (C::TILE / 4);
+      if (nt > 0) {
 #pragma unroll
-      for (int c = 0; c < D; c += 32) {
-        uint32_t o[32];
-        if (nt > 0) {
+        for (int c = 0; c < D; c += 64) {
+          uint32_t o[64];
           tmem_ld_32x32b_x32(ot + c, o);
-          tmem_ld_wait_all<32>(o);
-        }
-        if (live && nt > 0) {
+          tmem_ld_32x32b_x32(ot + c + 32, o + 32);
+          tmem_ld_wait_all<64>(o);
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {   // column 0, 1, .. of eight holds value 0, 4, 1, 5, 2, 6, 3, 7
-            float f[8];
+          for (int part = 0; part < 64; part += D / 2) {   // what a quarter of the tile holds: D / 2 values of 32 rows
+            __syncwarp();
 #pragma unroll
-            for (int x = 0; x < 8; ++x) f[x] = (__uint_as_float(o[e + x]) + z) * back;
-            *reinterpret_cast<float4*>(out + c + e) = make_float4(f[0], f[2], f[4], f[6]);
-            *reinterpret_cast<float4*>(out + c + e + 4) = make_float4(f[1], f[3], f[5], f[7]);
+            for (int e = 0; e < D / 2; e += 8) {   // column 0, 1, .. of eight holds value 0, 4, 1, 5, 2, 6, 3, 7
+              float f[8];
+#pragma unroll
+              for (int x = 0; x < 8; ++x) f[x] = (__uint_as_float(o[part + e + x]) + z) * back;
+              uint8_t* dst = buf + lane * (2 * D);
+              *reinterpret_cast<float4*>(dst + (((e >> 2) ^ (lane & 7)) << 4)) = make_float4(f[0], f[2], f[4], f[6]);
+              *reinterpret_cast<float4*>(dst + (((e >> 2) + 1 ^ (lane & 7)) << 4)) = make_float4(f[1], f[3], f[5], f[7]);
+            }
+            __syncwarp();
+            constexpr int LPR = D / 8, RPL = 32 / LPR;   // lanes per row, rows per store
+#pragma unroll
+            for (int k = 0; k < 32 / RPL; ++k) {
+              const int rr = k * RPL + lane / LPR, ch = lane % LPR;
+              const int64_t to = __shfl_sync(0xffffffffu, at, rr);
+              const float4 v = *reinterpret_cast<const float4*>(buf + rr * (2 * D) + ((ch ^ (rr & 7)) << 4));
+              if (to >= 0) *reinterpret_cast<float4*>(p.o + to + c + part + ch * 4) = v;
+            }
           }
         }
       }
