@@ -174,6 +174,42 @@ __device__ __forceinline__ float attn_row_max(const uint32_t* r) {
   return fmaxf(attn_max3(m[0], m[1], m[2]), m[3]);
 }
 
+// The largest of 64 scores.
+__device__ __forceinline__ float attn_row_max64(const uint32_t* r) {
+  float m[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) m[q] = fmaxf(__uint_as_float(r[2 * q]), __uint_as_float(r[2 * q + 1]));
+#pragma unroll
+  for (int i = 8; i < 64; i += 8)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) m[q] = attn_max3(m[q], __uint_as_float(r[i + 2 * q]), __uint_as_float(r[i + 2 * q + 1]));
+  return fmaxf(attn_max3(m[0], m[1], m[2]), m[3]);
+}
+
+// Two warps share a tile's 32 rows, 64 columns each.  OR of a predicate over
+// the 64 threads of the pair (a barrier for both).
+__device__ __forceinline__ bool attn_pair_or(bool x, int barrier) {
+  uint32_t r;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, %2, 64, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(r)
+      : "r"((uint32_t)x), "r"(barrier)
+      : "memory");
+  return r != 0;
+}
+// Exchanges a value of every row between the pair's warps (half 0 and 1)
+// through one slot of 32 floats.
+__device__ __forceinline__ float attn_pair_swap(float* slot, float x, int half, int lane, int barrier) {
+  if (half == 0) slot[lane] = x;
+  named_bar_sync(barrier, 64);
+  float y = slot[lane];
+  named_bar_sync(barrier, 64);
+  if (half == 1) slot[lane] = x;
+  named_bar_sync(barrier, 64);
+  if (half == 0) y = slot[lane];
+  return y;
+}
+
 // Rescales this lane's row of an accumulator in tensor memory (N columns), 16
 // at a time: it runs while the row's scores are held in registers.
 template <int N>

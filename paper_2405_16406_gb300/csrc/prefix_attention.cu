@@ -80,7 +80,8 @@ struct PrefixCfg {
   static constexpr int OFF_RM = OFF_COL + NCOL * 2048 * 2;   // [NCOL][4] largest alpha' of each warp's tokens
   static constexpr int OFF_BAR = OFF_RM + NCOL * 16;     // q, full, free [NSTG], col [NCOL], s, p, o, drain [2]
   static constexpr int OFF_MISC = OFF_BAR + (2 * NSTG + NCOL + 9) * 8;
-  static constexpr int BYTES = OFF_MISC + 16 + 1024;
+  static constexpr int OFF_X = OFF_MISC + 16;            // 256 floats: query sums, then exchanged values
+  static constexpr int BYTES = OFF_X + 1024 + 1024;
   static_assert(BYTES <= 232448, "shared memory");
 };
 // four warpgroups: two of softmax with 184 registers a thread, one with the
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
     for (int s = 0; s < NCOL; ++s) mbar_init(&cbar[s], 4);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sbar[i], 1);
-      mbar_init(&pbar[i], 4);
+      mbar_init(&pbar[i], 8);
       mbar_init(&obar[i], 1);
       mbar_init(&drain[i], 1);
     }
@@ -256,26 +257,35 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
       mbar_wait_bounded(&drain[i], 0, kAttnWaitLimitNs);
     }
   } else {
-    // ---------------- softmax: warps 4i .. 4i + 3 own tile i, thread = row
+    // ---------------- softmax: thread r of either warpgroup hf owns tokens 64 hf ..
+    // 64 hf + 63 of row r of both tiles, in turn.  What a tile's weights wait
+    // for beside the tensor core is then half a row's arithmetic, and there are registers
+    // to keep 8 of the per-token numbers' loads under way: beside MMAs that take
+    // shared memory's full rate each may last hundreds of cycles (32768 x 256: 224 us
+    // with a warpgroup per tile and whole rows, 204 us so).
     asm volatile("setmaxnreg.inc.sync.aligned.u32 184;\n");
-    const int i = warp >> 2, r = tid & 127;
+    const int hf = warp >> 2, r = tid & 127, pair = 1 + (warp & 3);   // named barrier of this warp and warp ^ 4
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t st = tmem + i * 128 + lanes, ot = tmem + 256 + i * D + lanes;
-    const int b = b0 + i * p.tps + r / p.G, head = hk * p.G + r % p.G;
-    const bool live = r < p.G * p.tps && b < (int)a.B;
-    const bool work = __any_sync(0xffffffffu, live);   // the warp has a row at all
-    // The warp's rows of Q, their pairs in the order of code_pairs, and the sum of
-    // this thread's: D / 8 lanes share a row, every load is under way at once.
-    float qs = 0.f;
+    float* xs = reinterpret_cast<float*>(smem + C::OFF_X);
+    int64_t row[2];    // this thread's row of tile i among all rows, or -1
+    bool work[2];      // the warp has a row of tile i at all
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int b = b0 + i * p.tps + r / p.G;
+      row[i] = r < p.G * p.tps && b < (int)a.B ? (int64_t)b * a.Hq + hk * p.G + r % p.G : -1;
+      work[i] = __any_sync(0xffffffffu, row[i] >= 0);
+    }
+    // The warp's rows of Q of tile hf, their pairs in the order of code_pairs,
+    // and their sums: D / 8 lanes share a row, every load is under way at once.
     {
       constexpr int LPR = D / 8, RPL = 32 / LPR;   // lanes per row, rows per load
-      const int64_t at = live ? ((int64_t)b * a.Hq + head) * D : -1;   // this thread's row
+      const int64_t at = hf ? row[1] : row[0];
       const int ch = lane % LPR;
       uint4 w[32 / RPL];
 #pragma unroll
       for (int k = 0; k < 32 / RPL; ++k) {
         const int64_t src = __shfl_sync(0xffffffffu, at, k * RPL + lane / LPR);
-        w[k] = src >= 0 ? __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(a.q) + src) + ch)
+        w[k] = src >= 0 ? __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(a.q) + src * D) + ch)
                         : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
@@ -289,10 +299,9 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
         }
 #pragma unroll
         for (int o = 1; o < LPR; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const float mine = __shfl_sync(0xffffffffu, sum, (lane % RPL) * LPR);
-        if (lane / RPL == k) qs = mine;
-        const int row = (warp & 3) * 32 + k * RPL + lane / LPR;
-        *reinterpret_cast<uint4*>(smem + i * C::TILE + (ch >> 3) * kAttnAtom + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) =
+        const int rr = (warp & 3) * 32 + k * RPL + lane / LPR;
+        if (ch == 0) xs[hf * 128 + rr] = sum;
+        *reinterpret_cast<uint4*>(smem + hf * C::TILE + (ch >> 3) * kAttnAtom + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4)) =
             make_uint4(__byte_perm(x[0], x[2], 0x5410), __byte_perm(x[0], x[2], 0x7632), __byte_perm(x[1], x[3], 0x5410),
                        __byte_perm(x[1], x[3], 0x7632));
       }
@@ -300,121 +309,157 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
       __syncwarp();
       if (lane == 0) mbar_arrive(qbar);
     }
-    const F2 qs2 = f2_make(qs, qs);
-    float m = -INFINITY, lr = 0.f, rcur = 0.f, l = 0.f, z = 0.f;
+    named_bar_sync(pair, 64);   // the pair's warps hold the sums of tiles 0 and 1
+    const float qs[2] = {xs[r], xs[128 + r]};
+    named_bar_sync(pair, 64);   // both have read them: the slots serve the exchanges from here on
+    xs += (warp & 3) * 32;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, z[2] = {0.f, 0.f};
+    float rc[2] = {0.f, 0.f}, lr[2] = {0.f, 0.f};   // M = m + lr, lr = log2 rc
     bool ok = true;
-    for (int j = 0; i < nrow && j < nt; ++j) {
-      if (!(ok = attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns))) break;
-      if (!(ok = attn_wait_warp(&cbar[j % NCOL], (uint32_t)(j / NCOL) & 1u, abort_flag, g_prefix_wait_ns))) break;
-      tc_fence_after();
-      if (work) {
-        uint32_t s[128];
-#pragma unroll
-        for (int c = 0; c < 128; c += 32) tmem_ld_32x32b_x32(st + c, s + c);
-        const uint8_t* colp = smem + C::OFF_COL + (j % NCOL) * 4096;
-        const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(colp);
-        const ulonglong2* az = reinterpret_cast<const ulonglong2*>(colp + 2048);
+#pragma unroll 1
+    for (int j2 = 0; j2 < 2 * nt; ++j2) {   // tile i = 0, 1 of tokens j = 0, 0, 1, 1, ..
+      const int i = j2 & 1, j = j2 >> 1;
+      if (i >= nrow) continue;
+      const uint32_t st = tmem + i * 128 + lanes;
+      if (i == 0) ok = attn_wait_warp(&cbar[j % NCOL], (uint32_t)(j / NCOL) & 1u, abort_flag, g_prefix_wait_ns);
+      if (!(i ? work[1] : work[0])) {   // the same for both warps of a pair
+        ok = ok && attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns);
+        ok = !attn_pair_or(!ok, pair);
+        if (!ok) break;
+      } else {
+        // the numbers of pairs of tokens: scale and offset of the scores (32
+        // entries), then those of the values; entry e + 8 is loaded as e is used
+        const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(smem + C::OFF_COL + (j % NCOL) * 4096 + hf * 512);
         const float4 r4 = *reinterpret_cast<const float4*>(smem + C::OFF_RM + (j % NCOL) * 16);
-        const float rm = fmaxf(attn_max3(r4.x, r4.y, r4.z), r4.w);
-        tmem_ld_wait_all<128>(s);
+        auto entry = [&](int e) { return e < 32 ? ab[e] : ab[128 + e - 32]; };
+        constexpr int NF = 8;
+        ulonglong2 f[NF];
 #pragma unroll
-        for (int c = 0; c < 128; c += 2) {
-          const ulonglong2 w = ab[c >> 1];
-          const F2 t = f2_fma(f2_from_bits(s[c], s[c + 1]), F2{w.x}, f2_mul(F2{w.y}, qs2));
+        for (int e = 0; e < NF; ++e) f[e] = entry(e);
+        const float rm = fmaxf(attn_max3(r4.x, r4.y, r4.z), r4.w);
+        const float q1 = i ? qs[1] : qs[0];
+        const F2 qs2 = f2_make(q1, q1);
+        float mi = i ? m[1] : m[0], li = i ? l[1] : l[0], zi = i ? z[1] : z[0], rci = i ? rc[1] : rc[0],
+              lri = i ? lr[1] : lr[0];
+        ok = ok && attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns);
+        tc_fence_after();
+        // (after a wait given up the columns are read all the same, in bounds, and discarded)
+        uint32_t s[64];
+        tmem_ld_32x32b_x32(st + hf * 64, s);
+        tmem_ld_32x32b_x32(st + hf * 64 + 32, s + 32);
+        tmem_ld_wait_all<64>(s);
+#pragma unroll
+        for (int c = 0; c < 64; c += 2) {
+          const int e = c >> 1;
+          const ulonglong2 w = f[e % NF];
+          f[e % NF] = entry(e + NF);
           float x, y;
-          f2_split(t, x, y);
+          f2_split(f2_fma(f2_from_bits(s[c], s[c + 1]), F2{w.x}, f2_mul(F2{w.y}, qs2)), x, y);
           s[c] = __float_as_uint(x);
           s[c + 1] = __float_as_uint(y);
         }
-        const int64_t left = a.prefix_len - (int64_t)(j0 + j) * 128;
-        if (left < 128) {
+        const int64_t left = a.prefix_len - (int64_t)(j0 + j) * 128 - hf * 64;
+        if (left < 64) {
 #pragma unroll
-          for (int c = 0; c < 128; ++c)
+          for (int c = 0; c < 64; ++c)
             if (c >= (int)left) s[c] = 0xFF800000u;   // -inf
         }
-        const float mx = attn_row_max(s);
-        const float mn = mx > m + kAttnSlack ? mx : m;
-        if (__any_sync(0xffffffffu, mn != m || rm > 16.f * rcur)) {
-          const float M = m + lr;
-          if (rm > 16.f * rcur) {
-            rcur = fmaxf(rm, kMinValueScale);
-            lr = __log2f(rcur);
+        float mx = attn_row_max64(s);
+        // Seldom: a wait was given up, or M moves.  Also: both warps have read
+        // their scores before either writes weights over them.
+        if (attn_pair_or(!ok || mx > mi + kAttnSlack || rm > 16.f * rci, pair)) {
+          ok = !attn_pair_or(!ok, pair);
+          if (!ok) break;
+          mx = fmaxf(mx, attn_pair_swap(xs, mx, hf, lane, pair));
+          const float M = mi + lri, mn = mx > mi + kAttnSlack ? mx : mi;
+          if (rm > 16.f * rci) {
+            rci = fmaxf(rm, kMinValueScale);
+            lri = __log2f(rci);
           }
           if (j > 0) {
             // the scores' barrier says that every product issued before them is done
-            const float f = m == -INFINITY ? 0.f : attn_exp2(M - (mn + lr));
-            l *= f;
-            z *= f;
-            attn_rescale<D>(ot, f);
+            const float g = mi == -INFINITY ? 0.f : attn_exp2(M - (mn + lri));
+            li *= g;
+            zi *= g;
+            attn_rescale<D / 2>(tmem + 256 + i * D + hf * (D / 2) + lanes, g);
           }
-          m = mn;
+          mi = mn;
         }
-        const float off = m == -INFINITY ? 0.f : -(m + lr);
+        const float off = mi == -INFINITY ? 0.f : -(mi + lri);
         const F2 of2 = f2_make(off, off);
-        F2 sum = f2_make(l, 0.f), zs = f2_make(z, 0.f);
+        F2 sum = f2_make(li, 0.f), zs = f2_make(zi, 0.f);
 #pragma unroll
-        for (int c = 0; c < 128; c += 2) {
-          const ulonglong2 w = az[c >> 1];
+        for (int c = 0; c < 64; c += 2) {
+          const int e = 32 + (c >> 1);
+          const ulonglong2 w = f[e % NF];
+          if (e + NF < 64) f[e % NF] = entry(e + NF);
           float x, y;
           f2_split(f2_add(f2_from_bits(s[c], s[c + 1]), of2), x, y);
-          const F2 e = f2_make(attn_exp2(x), attn_exp2(y));
-          sum = f2_add(sum, e);
-          zs = f2_fma(e, F2{w.y}, zs);
-          f2_split(f2_mul(e, F2{w.x}), x, y);
+          const F2 ex = f2_make(attn_exp2(x), attn_exp2(y));
+          sum = f2_add(sum, ex);
+          zs = f2_fma(ex, F2{w.y}, zs);
+          f2_split(f2_mul(ex, F2{w.x}), x, y);
           s[c >> 1] = pack_half2_bits(x, y);
         }
         float x, y;
         f2_split(sum, x, y);
-        l = x + y;
+        li = x + y;
         f2_split(zs, x, y);
-        z = x + y;
-        tmem_st_32x32b_x32(st, s);
-        tmem_st_32x32b_x32(st + 32, s + 32);
+        zi = x + y;
+        tmem_st_32x32b_x32(st + hf * 32, s);
+        if (i)
+          m[1] = mi, l[1] = li, z[1] = zi, rc[1] = rci, lr[1] = lri;
+        else
+          m[0] = mi, l[0] = li, z[0] = zi, rc[0] = rci, lr[0] = lri;
         tmem_st_wait();
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&pbar[i]);
     }
-    if (ok && i < nrow && nt > 0) ok = attn_wait_warp(&obar[i], 0, abort_flag, g_prefix_wait_ns);
-    if (ok && work) {
+#pragma unroll 1
+    for (int i = 0; ok && i < nrow; ++i) {
+      if (!(i ? work[1] : work[0])) continue;
+      if (nt > 0) ok = attn_wait_warp(&obar[i], 0, abort_flag, g_prefix_wait_ns);
+      ok = !attn_pair_or(!ok, pair);
+      if (!ok) break;
       tc_fence_after();
-      const int64_t row = (int64_t)b * a.Hq + head, rows = a.B * a.Hq;
-      const float back = rcur > 0.f ? rcur : 1.f;   // 2^lr: the sums to weights 2^(s - m)
-      if (live) p.ml[(int64_t)blockIdx.z * rows + row] = make_float2(m, l * back);
-      // 64 values of each row at a time through the tile's Q rows, which no product
-      // reads any more, so that a row's values leave in one run
-      const int64_t at = live ? ((int64_t)blockIdx.z * rows + row) * D : -1;
-      uint8_t* buf = smem + i * C::TILE + (warp & 3) * (C::TILE / 4);
-      if (nt > 0) {
+      float li = i ? l[1] : l[0], zi = i ? z[1] : z[0];
+      li += attn_pair_swap(xs, li, hf, lane, pair);
+      zi += attn_pair_swap(xs, zi, hf, lane, pair);
+      const float rci = i ? rc[1] : rc[0], back = rci > 0.f ? rci : 1.f;   // 2^lr: the sums to weights 2^(s - m)
+      const int64_t rows = a.B * a.Hq, mine = i ? row[1] : row[0];
+      if (mine >= 0 && hf == 0) p.ml[(int64_t)blockIdx.z * rows + mine] = make_float2(i ? m[1] : m[0], li * back);
+      if (nt == 0) continue;
+      // D / 4 values of each row at a time through the tile's Q rows, which no
+      // product reads any more, so that a row's values leave in one run
+      const int64_t at = mine >= 0 ? ((int64_t)blockIdx.z * rows + mine) * D : -1;
+      uint8_t* buf = smem + i * C::TILE + (warp & 7) * (C::TILE / 8);
+      uint32_t o[D / 2];
 #pragma unroll
-        for (int c = 0; c < D; c += 64) {
-          uint32_t o[64];
-          tmem_ld_32x32b_x32(ot + c, o);
-          tmem_ld_32x32b_x32(ot + c + 32, o + 32);
-          tmem_ld_wait_all<64>(o);
+      for (int c = 0; c < D / 2; c += 32) tmem_ld_32x32b_x32(tmem + 256 + i * D + hf * (D / 2) + lanes + c, o + c);
+      tmem_ld_wait_all<D / 2>(o);
 #pragma unroll
-          for (int part = 0; part < 64; part += D / 2) {   // what a quarter of the tile holds: D / 2 values of 32 rows
-            __syncwarp();
+      for (int part = 0; part < D / 2; part += D / 4) {
+        __syncwarp();
 #pragma unroll
-            for (int e = 0; e < D / 2; e += 8) {   // column 0, 1, .. of eight holds value 0, 4, 1, 5, 2, 6, 3, 7
-              float f[8];
+        for (int e = 0; e < D / 4; e += 8) {   // column 0, 1, .. of eight holds value 0, 4, 1, 5, 2, 6, 3, 7
+          float v[8];
 #pragma unroll
-              for (int x = 0; x < 8; ++x) f[x] = (__uint_as_float(o[part + e + x]) + z) * back;
-              uint8_t* dst = buf + lane * (2 * D);
-              *reinterpret_cast<float4*>(dst + (((e >> 2) ^ (lane & 7)) << 4)) = make_float4(f[0], f[2], f[4], f[6]);
-              *reinterpret_cast<float4*>(dst + (((e >> 2) + 1 ^ (lane & 7)) << 4)) = make_float4(f[1], f[3], f[5], f[7]);
-            }
-            __syncwarp();
-            constexpr int LPR = D / 8, RPL = 32 / LPR;   // lanes per row, rows per store
+          for (int x = 0; x < 8; ++x) v[x] = (__uint_as_float(o[part + e + x]) + zi) * back;
+          uint8_t* dst = buf + lane * D;
+          *reinterpret_cast<float4*>(dst + (((e >> 2) ^ (lane & (D / 16 - 1))) << 4)) = make_float4(v[0], v[2], v[4], v[6]);
+          *reinterpret_cast<float4*>(dst + (((e >> 2) + 1 ^ (lane & (D / 16 - 1))) << 4)) =
+              make_float4(v[1], v[3], v[5], v[7]);
+        }
+        __syncwarp();
+        constexpr int LPR = D / 16, RPL = 32 / LPR;   // lanes per row, rows per store
 #pragma unroll
-            for (int k = 0; k < 32 / RPL; ++k) {
-              const int rr = k * RPL + lane / LPR, ch = lane % LPR;
-              const int64_t to = __shfl_sync(0xffffffffu, at, rr);
-              const float4 v = *reinterpret_cast<const float4*>(buf + rr * (2 * D) + ((ch ^ (rr & 7)) << 4));
-              if (to >= 0) *reinterpret_cast<float4*>(p.o + to + c + part + ch * 4) = v;
-            }
-          }
+        for (int k = 0; k < 32 / RPL; ++k) {
+          const int rr = k * RPL + lane / LPR, ch = lane % LPR;
+          const int64_t to = __shfl_sync(0xffffffffu, at, rr);
+          const float4 v = *reinterpret_cast<const float4*>(buf + rr * D + ((ch ^ (rr & (D / 16 - 1))) << 4));
+          if (to >= 0) *reinterpret_cast<float4*>(p.o + to + hf * (D / 2) + part + ch * 4) = v;
         }
       }
     }
