@@ -14,16 +14,16 @@
 // weights 2^(s - M) alpha' stay in fp16's range whatever the values' magnitude; M
 // moves only when a score or an alpha' outgrows it by 2^8 or 2^4.
 //
-// Three kernels on the stream:
+// Two or three kernels on the stream:
 //   prefix_tc_kernel   the shared tokens, once for all sequences: an MMA's 128
 //     rows are floor(128 / G) sequences of the G heads of a kv head, two such
 //     tiles per CTA, the prefix split over the grid's z.  S = Q K^T and O += P V on
 //     the 5th-generation tensor core as in the prompt kernel; four warps
 //     expand the pages' codes into the operand tiles.
 //   own_tokens_kernel  each sequence's own tokens: G heads are too few rows for those
-//     tiles, so mma.sync with the tokens on the M side, codes straight
-//     from global memory into fragments.  Bound: the cache's bytes.
-//   combine_kernel     joins the parts (maximum, sum, o) in a fixed order.
+//     tiles, so mma.sync with the tokens on the M side, codes copied as they are.  Bound: the cache's bytes.  Where one CTA
+//     has all of a sequence's own tokens it also joins them with the prefix's parts.
+//   prefix_combine_kernel  else joins the parts (maximum, sum, o) in a fixed order.
 #include <cuda_fp16.h>
 #include <float.h>
 
@@ -68,6 +68,8 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t x) {   // nibbles at bits
 __device__ __forceinline__ uint4 code_pairs(uint32_t x) {
   return make_uint4(code_pair(x), code_pair(x >> 4), code_pair(x >> 8), code_pair(x >> 12));
 }
+
+constexpr int kMaxSplits = 160;   // parts of the prefix at most
 
 // --------------------------------------------------------------- the prefix
 template <int D>
@@ -744,20 +746,67 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
   }
   __syncthreads();
   const int64_t rows = a.B * a.Hq, part = (int64_t)p.nsplit + blockIdx.x;
-  for (int e = threadIdx.x; e < heads * D; e += kOwnWarps * 32) {
-    const int h = e / D, d = e % D;
-    float M = -INFINITY;
+  if (p.nchunk > 1) {
+    for (int e = threadIdx.x; e < heads * D; e += kOwnWarps * 32) {
+      const int h = e / D, d = e % D;
+      float M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kOwnWarps; ++w) M = fmaxf(M, m_s[w][h]);
-    float val = 0.f, ls = 0.f;
+      for (int w = 0; w < kOwnWarps; ++w) M = fmaxf(M, m_s[w][h]);
+      float val = 0.f, ls = 0.f;
 #pragma unroll
-    for (int w = 0; w < kOwnWarps; ++w) {
-      const float f = l_s[w][h] > 0.f ? attn_exp2(m_s[w][h] - M) : 0.f;
-      val = fmaf(f, reinterpret_cast<const float*>(ring_s[w])[h * D + d], val);
-      ls = fmaf(f, l_s[w][h], ls);
+      for (int w = 0; w < kOwnWarps; ++w) {
+        const float f = l_s[w][h] > 0.f ? attn_exp2(m_s[w][h] - M) : 0.f;
+        val = fmaf(f, reinterpret_cast<const float*>(ring_s[w])[h * D + d], val);
+        ls = fmaf(f, l_s[w][h], ls);
+      }
+      p.o[(part * rows + row0 + h) * D + d] = val;
+      if (d == 0) p.ml[part * rows + row0 + h] = make_float2(M, ls);
     }
-    p.o[(part * rows + row0 + h) * D + d] = val;
-    if (d == 0) p.ml[part * rows + row0 + h] = make_float2(M, ls);
+    return;
+  }
+  // The only part of these rows' own tokens: joined with the prefix's here.
+  // f_s[h][0 .. 3] the warps' factors, then the prefix parts', all over the sum.
+  __shared__ float f_s[8][kOwnWarps + kMaxSplits];
+  for (int h = warp; h < heads; h += kOwnWarps) {
+    const float2* ml = p.ml + row0 + h;
+    float M = -INFINITY, sum = 0.f;
+    for (int q = lane; q < kOwnWarps + p.nsplit; q += 32) {
+      const float2 x = q < kOwnWarps ? make_float2(m_s[q][h], l_s[q][h]) : ml[(q - kOwnWarps) * rows];
+      if (x.y > 0.f) M = fmaxf(M, x.x);
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, w));
+    for (int q = lane; q < kOwnWarps + p.nsplit; q += 32) {
+      const float2 x = q < kOwnWarps ? make_float2(m_s[q][h], l_s[q][h]) : ml[(q - kOwnWarps) * rows];
+      const float f = x.y > 0.f ? attn_exp2(x.x - M) : 0.f;
+      f_s[h][q] = f;
+      sum = fmaf(f, x.y, sum);
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    __syncwarp();
+    for (int q = lane; q < kOwnWarps + p.nsplit; q += 32) f_s[h][q] *= inv;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < heads * (D / 4); e += kOwnWarps * 32) {   // four values of a row
+    const int h = e / (D / 4), d = e % (D / 4) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float f, const float4& x) {
+      v.x = fmaf(f, x.x, v.x), v.y = fmaf(f, x.y, v.y), v.z = fmaf(f, x.z, v.z), v.w = fmaf(f, x.w, v.w);
+    };
+    const float* parts = p.o + (row0 + h) * D + d;
+#pragma unroll 8
+    for (int q = 0; q < p.nsplit; ++q) {   // a part without a sum was not written
+      const float f = f_s[h][kOwnWarps + q];
+      const float4 x = *reinterpret_cast<const float4*>(parts + q * rows * D);
+      if (f != 0.f) add(f, x);
+    }
+#pragma unroll
+    for (int w = 0; w < kOwnWarps; ++w)
+      add(f_s[h][w], *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring_s[w]) + h * D + d));
+    *reinterpret_cast<uint2*>(reinterpret_cast<__half*>(a.out) + (row0 + h) * D + d) =
+        make_uint2(pack_half2_bits(v.x, v.y), pack_half2_bits(v.z, v.w));
   }
 }
 
@@ -804,18 +853,19 @@ int prefix_splits(const PrefixArgs& a) {
   if (a.prefix_len == 0) return 0;
   const int64_t tiles = (a.prefix_len + 127) / 128;
   int64_t n = device_sm_count() / (row_blocks(a) * a.Hkv);   // one CTA per SM
-  n = n < 1 ? 1 : n;
+  n = n < 1 ? 1 : (n > kMaxSplits ? kMaxSplits : n);
   return (int)(n > tiles ? tiles : n);
 }
 
+// Parts of the sequences' own tokens.  One, where that gives every SM a CTA: the
+// kernel then joins its rows with the prefix's parts itself.  Else so many that
+// there are eight CTAs per SM, of 256 tokens at least.
 int own_chunks(const PrefixArgs& a) {
-  const int64_t cap = a.table_width * a.page_size;
-  if (cap == 0) return 0;
+  const int64_t cap = a.table_width * a.page_size, sms = device_sm_count();
   const int64_t ctas = a.B * a.Hkv * ((a.Hq / a.Hkv + 7) / 8);
-  int64_t n = 8 * (int64_t)device_sm_count() / ctas;
-  const int64_t by_len = (cap + 255) / 256;
-  n = n > by_len ? by_len : n;
-  return (int)(n < 1 ? 1 : n);
+  if (cap <= 256 || ctas >= sms) return 1;
+  const int64_t n = 8 * sms / ctas, by_len = (cap + 255) / 256;
+  return (int)(n > by_len ? by_len : n);
 }
 
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
@@ -830,7 +880,7 @@ cudaError_t launch_t(const PrefixArgs& a, cudaStream_t stream) {
   p.nchunk = own_chunks(a);
   const int64_t rows = a.B * a.Hq;
   p.ml = static_cast<float2*>(a.workspace);
-  p.o = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256((p.nsplit + p.nchunk) * rows * 8));
+  p.o = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256((p.nsplit + (p.nchunk > 1 ? p.nchunk : 0)) * rows * 8));
   p.scale_log2 = a.scale * kAttnLog2e;
   p.status = device_status_word();
   cudaError_t e = cudaSuccess;
@@ -843,13 +893,13 @@ cudaError_t launch_t(const PrefixArgs& a, cudaStream_t stream) {
                    dim3(kPrefixThreads), PrefixCfg<D>::BYTES, stream, 1, p);
     if (e != cudaSuccess) return e;
   }
-  if (p.nchunk > 0) {
+  {
     const int64_t cap = a.table_width * a.page_size;
     const int chunk = (int)(((cap + p.nchunk - 1) / p.nchunk + 15) / 16 * 16);
     const int hgroups = (p.G + 7) / 8;
     e = launch_pdl(own_tokens_kernel<D>, dim3((unsigned)p.nchunk, (unsigned)(a.Hkv * hgroups), (unsigned)a.B),
                    dim3(kOwnWarps * 32), 0, stream, 1, p, hgroups, chunk);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || p.nchunk == 1) return e != cudaSuccess ? e : cudaGetLastError();
   }
   e = launch_pdl(prefix_combine_kernel<D>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, stream, 1, p);
   return e != cudaSuccess ? e : cudaGetLastError();
@@ -860,7 +910,8 @@ cudaError_t launch_t(const PrefixArgs& a, cudaStream_t stream) {
 cudaError_t set_wait_limit_prefix(uint64_t ns) { return cudaMemcpyToSymbol(g_prefix_wait_ns, &ns, sizeof(ns)); }
 
 int64_t prefix_attention_workspace(const PrefixArgs& a) {
-  const int64_t parts = prefix_splits(a) + own_chunks(a), rows = a.B * a.Hq;
+  const int chunks = own_chunks(a);
+  const int64_t parts = prefix_splits(a) + (chunks > 1 ? chunks : 0), rows = a.B * a.Hq;
   return align256(parts * rows * 8) + parts * rows * a.D * 4;
 }
 
