@@ -1063,7 +1063,8 @@ def relaunch(args_n):
 
 
 PROFILE_CASES = ("attention", "rope_kv", "fp8_gemm", "w4a8_gemm", "rq8_paley", "cayley", "paley", "gemm",
-                 "gemm_gate_up", "decode_gemm", "decode_gemm16", "rq_h8192", "kv2048", "act_quant")
+                 "gemm_gate_up", "decode_gemm", "decode_gemm16", "rq_h8192", "kv2048", "act_quant",
+                 "kv4_append", "kv4_read", "prompt_attention", "prefix_attention")
 
 
 def profile_case(name, reps):
@@ -1082,7 +1083,10 @@ def profile_case(name, reps):
     rq_h8192: the 4-bit R4 kernel with H8192 on 8192 x 8192 (asymmetric);
     kv2048: R3 + KV4 on the step's 2048 tokens (32 / 8 heads, D 128);
     act_quant: the step's gate_up activation quantizer (2048 x 4096, no
-    rotation, asymmetric)."""
+    rotation, asymmetric).  On the paged cache, 32 / 8 heads, D 128, pages of 64:
+    kv4_append: 2 x 4096 new tokens with norms and RoPE; kv4_read: those tokens
+    back; prompt_attention: one causal prompt of 4096; prefix_attention: 64
+    requests behind 8192 shared tokens, 256 own tokens each."""
     import numpy as np
     import torch
 
@@ -1151,6 +1155,35 @@ def profile_case(name, reps):
         c = synth.llama3_8b_gate_up()
         x = torch.from_numpy(c.x).to(dev)
         fn = lambda: spinq.rotate_quant_act(x, None, False)
+    elif name in ("kv4_append", "kv4_read", "prompt_attention", "prefix_attention"):
+        hq, hk, d, page = 32, 8, 128, 64
+        n = 8192
+        half = lambda *shape: torch.randn(shape, device=dev).half()
+        ints = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
+        if name == "prompt_attention":
+            q, k, v, cu = half(4096, hq, d), half(4096, hk, d), half(4096, hk, d), ints([0, 4096])
+            fn = lambda: spinq.prompt_attention(q, k, v, cu, cu, 4096, 4096)
+        else:
+            cache = spinq.kv4_pages((n + 64 * 256) // page, page, hk, d)
+            th = 500000.0 ** (-torch.arange(d // 2, device=dev, dtype=torch.float64) / (d // 2))
+            ang = torch.arange(n, device=dev, dtype=torch.float64)[:, None] * th
+            cs = torch.stack((ang.cos(), ang.sin()), -1).float()
+            q, k, v, w = half(n, hq, d), half(n, hk, d), half(n, hk, d), half(d)
+            slots, pos = torch.arange(n, device=dev), torch.arange(n, dtype=torch.int32, device=dev) % 4096
+            append = lambda s: spinq.kv4_append(q, k, v, cache, s, pos, cs, w, w)
+            if name == "kv4_append":
+                fn = lambda: append(slots)
+            else:
+                for at in range(0, n + 64 * 256, n):
+                    append(slots + at)
+                pages = torch.arange((n + 64 * 256) // page, dtype=torch.int32, device=dev)
+                if name == "kv4_read":
+                    table, cu = pages[:n // page].view(2, -1), ints([0, 4096, 8192])
+                    fn = lambda: spinq.kv4_read(cache, table, cu, n)
+                else:
+                    qd, lens = half(64, hq, d), ints([256] * 64)
+                    shared, own = pages[:n // page], pages[n // page:].view(64, -1)
+                    fn = lambda: spinq.prefix_attention_kv4(qd, cache, shared, n, own, lens)
     elif name == "cayley":
         rng = np.random.default_rng(0)
         R = np.stack([np.linalg.qr(rng.standard_normal((128, 128)))[0] for _ in range(152)]).astype(np.float32)
