@@ -146,3 +146,17 @@ def test_no_queries_is_no_launch(S):
     z = torch.zeros((0, 8, 64), dtype=torch.float16, device="cuda")
     cu = torch.zeros(1, dtype=torch.int32, device="cuda")
     assert S.prompt_attention(z, z[:, :2], z[:, :2], cu, cu, 0, 0).shape == (0, 8, 64)
+
+
+def test_a_query_that_is_not_a_number_gives_its_own_row_only(S):
+    rng = np.random.default_rng(5)
+    cu = torch.tensor([0, 200, 260], dtype=torch.int32, device="cuda")
+    q, k, v = (torch.from_numpy(rng.standard_normal((260, h, 128)).astype(np.float16)).cuda() for h in (8, 2, 2))
+    clean = S.prompt_attention(q, k, v, cu, cu, 200, 200)
+    q[77, 3, 5] = float("nan")
+    q[201, 6, 0] = float("inf")
+    out = S.prompt_attention(q, k, v, cu, cu, 200, 200)
+    torch.cuda.synchronize()
+    bad = torch.zeros(260, 8, dtype=torch.bool, device="cuda")
+    bad[77, 3] = bad[201, 6] = True
+    assert out[77, 3].isnan().all() and torch.equal(out[~bad], clean[~bad])
