@@ -755,7 +755,7 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
       float val = 0.f, ls = 0.f;
 #pragma unroll
       for (int w = 0; w < kOwnWarps; ++w) {
-        const float f = l_s[w][h] > 0.f ? attn_exp2(m_s[w][h] - M) : 0.f;
+        const float f = l_s[w][h] != 0.f ? attn_exp2(m_s[w][h] - M) : 0.f;
         val = fmaf(f, reinterpret_cast<const float*>(ring_s[w])[h * D + d], val);
         ls = fmaf(f, l_s[w][h], ls);
       }
@@ -772,19 +772,19 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
     float M = -INFINITY, sum = 0.f;
     for (int q = lane; q < kOwnWarps + p.nsplit; q += 32) {
       const float2 x = q < kOwnWarps ? make_float2(m_s[q][h], l_s[q][h]) : ml[(q - kOwnWarps) * rows];
-      if (x.y > 0.f) M = fmaxf(M, x.x);
+      if (x.y != 0.f) M = fmaxf(M, x.x);
     }
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, w));
     for (int q = lane; q < kOwnWarps + p.nsplit; q += 32) {
       const float2 x = q < kOwnWarps ? make_float2(m_s[q][h], l_s[q][h]) : ml[(q - kOwnWarps) * rows];
-      const float f = x.y > 0.f ? attn_exp2(x.x - M) : 0.f;
+      const float f = x.y != 0.f ? attn_exp2(x.x - M) : 0.f;   // (a sum that is not a number stays one)
       f_s[h][q] = f;
       sum = fmaf(f, x.y, sum);
     }
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
     __syncwarp();
     for (int q = lane; q < kOwnWarps + p.nsplit; q += 32) f_s[h][q] *= inv;
   }
@@ -823,21 +823,21 @@ __global__ void __launch_bounds__(128) prefix_combine_kernel(const PrefixParams 
   float M = -INFINITY;
   for (int i = lane; i < parts; i += 32) {
     const float2 x = p.ml[i * rows + row];
-    if (x.y > 0.f) M = fmaxf(M, x.x);
+    if (x.y != 0.f) M = fmaxf(M, x.x);
   }
 #pragma unroll
   for (int w = 16; w > 0; w >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, w));
   float o[DPL] = {}, l = 0.f;
   for (int i = 0; i < parts; ++i) {
     const float2 x = p.ml[i * rows + row];
-    if (!(x.y > 0.f)) continue;
+    if (x.y == 0.f) continue;
     const float f = attn_exp2(x.x - M);
     l = fmaf(f, x.y, l);
     const float* s = p.o + (i * rows + row) * D + lane * DPL;
 #pragma unroll
     for (int e = 0; e < DPL; ++e) o[e] = fmaf(f, s[e], o[e]);
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = l != 0.f ? 1.f / l : 0.f;
   __half* out = reinterpret_cast<__half*>(p.a.out) + row * D + lane * DPL;
 #pragma unroll
   for (int e = 0; e < DPL; e += 2) *reinterpret_cast<__half2*>(out + e) = __floats2half2_rn(o[e] * inv, o[e + 1] * inv);

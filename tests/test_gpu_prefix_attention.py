@@ -175,3 +175,16 @@ def test_lengths_are_clamped_to_the_table(S):
     d = S.prefix_attention_kv4(q, cache, ptab, prefix, table, full * 0)
     torch.cuda.synchronize()
     assert torch.equal(a, b) and torch.equal(c, d)
+
+
+@pytest.mark.parametrize("prefix,lens", [(300, [0, 20, 5]), (0, [9, 20, 5]), (300, [3000, 20, 9000])])
+def test_a_query_that_is_not_a_number_gives_its_own_row_only(S, prefix, lens):
+    args, _ = _run(S, prefix, lens, 8, 2, 128, 16, seed=6)
+    q = args[0].clone()
+    clean = S.prefix_attention_kv4(*args)
+    q[0, 3, 5] = float("nan")
+    out = S.prefix_attention_kv4(q, *args[1:])
+    torch.cuda.synchronize()
+    bad = torch.zeros(3, 8, dtype=torch.bool, device="cuda")
+    bad[0, 3] = True
+    assert out[0, 3].isnan().all() and torch.equal(out[~bad], clean[~bad])
