@@ -86,6 +86,39 @@ __device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 
+// 16 lanes x 8 groups of 8 columns from tensor memory: lane 4 g + c gets columns
+// 8 k + 2 c and + 1 of row g in r[4 k], r[4 k + 1], of row g + 8 in r[4 k + 2], r[4 k + 3].
+__device__ __forceinline__ void tmem_ld_16x256b_x8(uint32_t taddr, uint32_t r[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+// The same of 2 groups, with the wait.
+__device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, uint32_t r[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n tcgen05.wait::ld.sync.aligned;\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_16x256b_x2(uint32_t taddr, const uint32_t r[8]) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+// 16 lanes x 8 groups of 4 columns to tensor memory: lane 4 g + c gives column
+// 4 k + c of row g in r[2 k], of row g + 8 in r[2 k + 1].
+__device__ __forceinline__ void tmem_st_16x128b_x8(uint32_t taddr, const uint32_t r[16]) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n" ::"r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+               "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+               : "memory");
+}
+
 // Waits for the tensor-memory loads of r[N] (N a multiple of 16).
 template <int N>
 __device__ __forceinline__ void tmem_ld_wait_all(uint32_t* r) {
@@ -174,18 +207,6 @@ __device__ __forceinline__ float attn_row_max(const uint32_t* r) {
   return fmaxf(attn_max3(m[0], m[1], m[2]), m[3]);
 }
 
-// The largest of 64 scores.
-__device__ __forceinline__ float attn_row_max64(const uint32_t* r) {
-  float m[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) m[q] = fmaxf(__uint_as_float(r[2 * q]), __uint_as_float(r[2 * q + 1]));
-#pragma unroll
-  for (int i = 8; i < 64; i += 8)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) m[q] = attn_max3(m[q], __uint_as_float(r[i + 2 * q]), __uint_as_float(r[i + 2 * q + 1]));
-  return fmaxf(attn_max3(m[0], m[1], m[2]), m[3]);
-}
-
 // Two warps share a tile's 32 rows, 64 columns each.  OR of a predicate over
 // the 64 threads of the pair (a barrier for both).
 __device__ __forceinline__ bool attn_pair_or(bool x, int barrier) {
@@ -223,6 +244,24 @@ __device__ __forceinline__ void attn_rescale(uint32_t o_tmem, float f) {
     for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
     tmem_st_32x32b_x16(o_tmem + c, o);
   }
+  tmem_st_wait();
+}
+
+// The same for the 32 rows of a warp in the spread layout: lane 4 g + c has the
+// factors of rows g, g + 8, g + 16, g + 24.
+template <int N>
+__device__ __forceinline__ void attn_rescale_rows(uint32_t o_tmem, const float f[4]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int c = 0; c < N; c += 16) {
+      uint32_t o[8];
+      const uint32_t at = o_tmem + ((uint32_t)(16 * h) << 16) + c;
+      tmem_ld_16x256b_x2(at, o);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f[2 * h + ((x >> 1) & 1)]);
+      tmem_st_16x256b_x2(at, o);
+    }
   tmem_st_wait();
 }
 

@@ -312,126 +312,173 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
       if (lane == 0) mbar_arrive(qbar);
     }
     named_bar_sync(pair, 64);   // the pair's warps hold the sums of tiles 0 and 1
-    const float qs[2] = {xs[r], xs[128 + r]};
+    const int g = lane >> 2, c = lane & 3;
+    float qs[2][4];   // of rows 8 e + g of the warp
+#pragma unroll
+    for (int e = 0; e < 4; ++e) qs[0][e] = xs[(warp & 3) * 32 + 8 * e + g], qs[1][e] = xs[128 + (warp & 3) * 32 + 8 * e + g];
     named_bar_sync(pair, 64);   // both have read them: the slots serve the exchanges from here on
     xs += (warp & 3) * 32;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, z[2] = {0.f, 0.f};
+    // a value of each of the lane's four rows (the same in a quad) as one per lane, of row 8 c + g
+    auto gather = [&](const float (&v)[4]) { return c < 2 ? (c == 0 ? v[0] : v[1]) : (c == 2 ? v[2] : v[3]); };
+    float m[2][4], l[2][4], z[2][4];   // l, z: of this lane's tokens
     float rc[2] = {0.f, 0.f}, lr[2] = {0.f, 0.f};   // M = m + lr, lr = log2 rc
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m[0][e] = m[1][e] = -INFINITY, l[0][e] = l[1][e] = z[0][e] = z[1][e] = 0.f;
     bool ok = true;
 #pragma unroll 1
-    for (int j2 = 0; j2 < 2 * nt; ++j2) {   // tile i = 0, 1 of tokens j = 0, 0, 1, 1, ..
-      const int i = j2 & 1, j = j2 >> 1;
-      if (i >= nrow) continue;
-      const uint32_t st = tmem + i * 128 + lanes;
-      if (i == 0) ok = attn_wait_warp(&cbar[j % NCOL], (uint32_t)(j / NCOL) & 1u, abort_flag, g_prefix_wait_ns);
-      if (!(i ? work[1] : work[0])) {   // the same for both warps of a pair
-        ok = ok && attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns);
-        ok = !attn_pair_or(!ok, pair);
-        if (!ok) break;
-      } else {
-        // the numbers of pairs of tokens: scale and offset of the scores (32
-        // entries), then those of the values; entry e + 8 is loaded as e is used
-        const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(smem + C::OFF_COL + (j % NCOL) * 4096 + hf * 512);
-        const float4 r4 = *reinterpret_cast<const float4*>(smem + C::OFF_RM + (j % NCOL) * 16);
-        auto entry = [&](int e) { return e < 32 ? ab[e] : ab[128 + e - 32]; };
-        constexpr int NF = 8;
-        ulonglong2 f[NF];
+    for (int j = 0; ok && j < nt; ++j)
 #pragma unroll
-        for (int e = 0; e < NF; ++e) f[e] = entry(e);
-        const float rm = fmaxf(attn_max3(r4.x, r4.y, r4.z), r4.w);
-        const float q1 = i ? qs[1] : qs[0];
-        const F2 qs2 = f2_make(q1, q1);
-        float mi = i ? m[1] : m[0], li = i ? l[1] : l[0], zi = i ? z[1] : z[0], rci = i ? rc[1] : rc[0],
-              lri = i ? lr[1] : lr[0];
-        ok = ok && attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns);
-        tc_fence_after();
-        // (after a wait given up the columns are read all the same, in bounds, and discarded)
-        uint32_t s[64];
-        tmem_ld_32x32b_x32(st + hf * 64, s);
-        tmem_ld_32x32b_x32(st + hf * 64 + 32, s + 32);
-        tmem_ld_wait_all<64>(s);
-#pragma unroll
-        for (int c = 0; c < 64; c += 2) {
-          const int e = c >> 1;
-          const ulonglong2 w = f[e % NF];
-          f[e % NF] = entry(e + NF);
-          float x, y;
-          f2_split(f2_fma(f2_from_bits(s[c], s[c + 1]), F2{w.x}, f2_mul(F2{w.y}, qs2)), x, y);
-          s[c] = __float_as_uint(x);
-          s[c + 1] = __float_as_uint(y);
-        }
-        const int64_t left = a.prefix_len - (int64_t)(j0 + j) * 128 - hf * 64;
-        if (left < 64) {
-#pragma unroll
-          for (int c = 0; c < 64; ++c)
-            if (c >= (int)left) s[c] = 0xFF800000u;   // -inf
-        }
-        float mx = attn_row_max64(s);
-        // Seldom: a wait was given up, or M moves.  Also: both warps have read
-        // their scores before either writes weights over them.
-        if (attn_pair_or(!ok || mx > mi + kAttnSlack || rm > 16.f * rci, pair)) {
+      for (int i = 0; i < 2; ++i) {
+        if (i >= nrow || !ok) continue;
+        const uint32_t st = tmem + i * 128 + lanes;
+        if (i == 0) ok = attn_wait_warp(&cbar[j % NCOL], (uint32_t)(j / NCOL) & 1u, abort_flag, g_prefix_wait_ns);
+        if (!work[i]) {   // the same for both warps of a pair
+          ok = ok && attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns);
           ok = !attn_pair_or(!ok, pair);
-          if (!ok) break;
-          mx = fmaxf(mx, attn_pair_swap(xs, mx, hf, lane, pair));
-          const float M = mi + lri, mn = mx > mi + kAttnSlack ? mx : mi;
-          if (rm > 16.f * rci) {
-            rci = fmaxf(rm, kMinValueScale);
-            lri = __log2f(rci);
-          }
-          if (j > 0) {
-            // the scores' barrier says that every product issued before them is done
-            const float g = mi == -INFINITY ? 0.f : attn_exp2(M - (mn + lri));
-            li *= g;
-            zi *= g;
-            attn_rescale<D / 2>(tmem + 256 + i * D + hf * (D / 2) + lanes, g);
-          }
-          mi = mn;
-        }
-        const float off = mi == -INFINITY ? 0.f : -(mi + lri);
-        const F2 of2 = f2_make(off, off);
-        F2 sum = f2_make(li, 0.f), zs = f2_make(zi, 0.f);
+          if (!ok) continue;
+        } else {
+          // the numbers of tokens 8 k + 2 c, 8 k + 2 c + 1: scale and offset of the scores,
+          // k = 0 .. 7, then those of the values; the latter are loaded as the former are used
+          const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(smem + C::OFF_COL + (j % NCOL) * 4096 + hf * 512) + c;
+          const float4 r4 = *reinterpret_cast<const float4*>(smem + C::OFF_RM + (j % NCOL) * 16);
+          ulonglong2 f[8];
 #pragma unroll
-        for (int c = 0; c < 64; c += 2) {
-          const int e = 32 + (c >> 1);
-          const ulonglong2 w = f[e % NF];
-          if (e + NF < 64) f[e % NF] = entry(e + NF);
-          float x, y;
-          f2_split(f2_add(f2_from_bits(s[c], s[c + 1]), of2), x, y);
-          const F2 ex = f2_make(attn_exp2(x), attn_exp2(y));
-          sum = f2_add(sum, ex);
-          zs = f2_fma(ex, F2{w.y}, zs);
-          f2_split(f2_mul(ex, F2{w.x}), x, y);
-          s[c >> 1] = pack_half2_bits(x, y);
+          for (int k = 0; k < 8; ++k) f[k] = ab[4 * k];
+          const float rm = fmaxf(attn_max3(r4.x, r4.y, r4.z), r4.w);
+          ok = ok && attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns);
+          tc_fence_after();
+          // (after a wait given up the columns are read all the same, in bounds, and discarded)
+          uint32_t s[2][32];   // s[h][4 k + 2 e + x]: row 16 h + 8 e + g, token 8 k + 2 c + x
+          tmem_ld_16x256b_x8(st + hf * 64, s[0]);
+          tmem_ld_16x256b_x8(st + (16u << 16) + hf * 64, s[1]);
+          tmem_ld_wait_all<32>(s[0]);
+          tmem_ld_wait_all<32>(s[1]);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const ulonglong2 w = f[k];
+            f[k] = ab[128 + 4 * k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t* v = &s[e >> 1][4 * k + 2 * (e & 1)];
+              float x, y;
+              f2_split(f2_fma(f2_from_bits(v[0], v[1]), F2{w.x}, f2_mul(F2{w.y}, f2_make(qs[i][e], qs[i][e]))), x, y);
+              v[0] = __float_as_uint(x);
+              v[1] = __float_as_uint(y);
+            }
+          }
+          const int64_t left = a.prefix_len - (int64_t)(j0 + j) * 128 - hf * 64;
+          if (left < 64) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+                if (8 * k + 2 * c + x >= (int)left)
+                  s[0][4 * k + x] = s[0][4 * k + 2 + x] = s[1][4 * k + x] = s[1][4 * k + 2 + x] = 0xFF800000u;   // -inf
+          }
+          float mx[4];
+          bool grow = !ok || rm > 16.f * rc[i];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t* v = &s[e >> 1][2 * (e & 1)];
+            float p0 = fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1])), p1 = fmaxf(__uint_as_float(v[4]), __uint_as_float(v[5]));
+#pragma unroll
+            for (int k = 2; k < 8; k += 2) {
+              p0 = attn_max3(p0, __uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]));
+              p1 = attn_max3(p1, __uint_as_float(v[4 * k + 4]), __uint_as_float(v[4 * k + 5]));
+            }
+            mx[e] = fmaxf(p0, p1);
+            grow |= mx[e] > m[i][e] + kAttnSlack;
+          }
+          // Seldom: a wait was given up, or M moves.  Also: both warps have read
+          // their scores before either writes weights over them.
+          if (attn_pair_or(grow, pair)) {
+            ok = !attn_pair_or(!ok, pair);
+            if (!ok) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
+              mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
+            }
+            const float other = attn_pair_swap(xs, gather(mx), hf, lane, pair), was = lr[i];
+            if (rm > 16.f * rc[i]) {
+              rc[i] = fmaxf(rm, kMinValueScale);
+              lr[i] = __log2f(rc[i]);
+            }
+            float fr[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float t = fmaxf(mx[e], __shfl_sync(0xffffffffu, other, (lane & 28) + e));
+              const float mn = t > m[i][e] + kAttnSlack ? t : m[i][e];
+              fr[e] = m[i][e] == -INFINITY ? 0.f : attn_exp2((m[i][e] + was) - (mn + lr[i]));
+              m[i][e] = mn;
+              l[i][e] *= fr[e];
+              z[i][e] *= fr[e];
+            }
+            // the scores' barrier says that every product issued before them is done
+            if (j > 0) attn_rescale_rows<D / 2>(tmem + 256 + i * D + hf * (D / 2) + lanes, fr);
+          }
+          F2 of2[4], sum[4], zs[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float off = m[i][e] == -INFINITY ? 0.f : -(m[i][e] + lr[i]);
+            of2[e] = f2_make(off, off);
+            sum[e] = f2_make(l[i][e], 0.f);
+            zs[e] = f2_make(z[i][e], 0.f);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t* v = &s[e >> 1][4 * k + 2 * (e & 1)];
+              float x, y;
+              f2_split(f2_add(f2_from_bits(v[0], v[1]), of2[e]), x, y);
+              const F2 ex = f2_make(attn_exp2(x), attn_exp2(y));
+              sum[e] = f2_add(sum[e], ex);
+              zs[e] = f2_fma(ex, F2{f[k].y}, zs[e]);
+              f2_split(f2_mul(ex, F2{f[k].x}), x, y);
+              s[e >> 1][2 * k + (e & 1)] = pack_half2_bits(x, y);   // 32-bit column 4 k + c of this half's P
+            }
+          tmem_st_16x128b_x8(st + hf * 32, s[0]);
+          tmem_st_16x128b_x8(st + (16u << 16) + hf * 32, s[1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x, y;
+            f2_split(sum[e], x, y);
+            l[i][e] = x + y;
+            f2_split(zs[e], x, y);
+            z[i][e] = x + y;
+          }
+          tmem_st_wait();
         }
-        float x, y;
-        f2_split(sum, x, y);
-        li = x + y;
-        f2_split(zs, x, y);
-        zi = x + y;
-        tmem_st_32x32b_x32(st + hf * 32, s);
-        if (i)
-          m[1] = mi, l[1] = li, z[1] = zi, rc[1] = rci, lr[1] = lri;
-        else
-          m[0] = mi, l[0] = li, z[0] = zi, rc[0] = rci, lr[0] = lri;
-        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&pbar[i]);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&pbar[i]);
-    }
-#pragma unroll 1
-    for (int i = 0; ok && i < nrow; ++i) {
-      if (!(i ? work[1] : work[0])) continue;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (!ok || i >= nrow || !work[i]) continue;
       if (nt > 0) ok = attn_wait_warp(&obar[i], 0, abort_flag, g_prefix_wait_ns);
       ok = !attn_pair_or(!ok, pair);
-      if (!ok) break;
+      if (!ok) continue;
       tc_fence_after();
-      float li = i ? l[1] : l[0], zi = i ? z[1] : z[0];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int w = 1; w < 4; w <<= 1) {
+          l[i][e] += __shfl_xor_sync(0xffffffffu, l[i][e], w);
+          z[i][e] += __shfl_xor_sync(0xffffffffu, z[i][e], w);
+        }
+      // of row 8 c + g, and from there to the row's lane
+      float mi = gather(m[i]), li = gather(l[i]), zi = gather(z[i]);
       li += attn_pair_swap(xs, li, hf, lane, pair);
       zi += attn_pair_swap(xs, zi, hf, lane, pair);
-      const float rci = i ? rc[1] : rc[0], back = rci > 0.f ? rci : 1.f;   // 2^lr: the sums to weights 2^(s - m)
-      const int64_t rows = a.B * a.Hq, mine = i ? row[1] : row[0];
-      if (mine >= 0 && hf == 0) p.ml[(int64_t)blockIdx.z * rows + mine] = make_float2(i ? m[1] : m[0], li * back);
+      const int from = 4 * (lane & 7) + (lane >> 3);
+      mi = __shfl_sync(0xffffffffu, mi, from);
+      li = __shfl_sync(0xffffffffu, li, from);
+      zi = __shfl_sync(0xffffffffu, zi, from);
+      const float back = rc[i] > 0.f ? rc[i] : 1.f;   // 2^lr: the sums to weights 2^(s - m)
+      const int64_t rows = a.B * a.Hq, mine = row[i];
+      if (mine >= 0 && hf == 0) p.ml[(int64_t)blockIdx.z * rows + mine] = make_float2(mi, li * back);
       if (nt == 0) continue;
       // D / 4 values of each row at a time through the tile's Q rows, which no
       // product reads any more, so that a row's values leave in one run
