@@ -20,9 +20,15 @@
 //     tiles per CTA, the prefix split over the grid's z.  S = Q K^T and O += P V on
 //     the 5th-generation tensor core as in the prompt kernel; four warps
 //     expand the pages' codes into the operand tiles.
-//   own_tokens_kernel  each sequence's own tokens: G heads are too few rows for those
-//     tiles, so mma.sync with the tokens on the M side, codes copied as they are.  Bound: the cache's bytes.  Where one CTA
-//     has all of a sequence's own tokens it also joins them with the prefix's parts.
+//     Bound: the softmax.  128 tokens for both tiles are 2052 cycles of MMAs and
+//     about 5900 in all: two warps per scheduler, whose packed fp32 work is about 3300, and
+//     waits between.  32768 tokens, 256 sequences, 32 / 8 heads, D 128, on 128 SMs: 204
+//     us with an empty join, 0.67 PFLOP/s.
+//   own_tokens_kernel  each sequence's own tokens, beside the prefix kernel where it
+//     leaves SMs: G heads are too few rows for those tiles, so mma.sync with the
+//     tokens on the M side, codes copied as they are.  Bound: the cache's bytes (256
+//     sequences of 523 tokens on average, 154 MB: 46 us alone, 3.4 TB/s).  Where one CTA has all of a
+//     sequence's own tokens it may also join them with the prefix's parts.
 //   prefix_combine_kernel  else joins the parts (maximum, sum, o) in a fixed order.
 #include <cuda_fp16.h>
 #include <float.h>
@@ -47,6 +53,7 @@ struct PrefixParams {
   int tps;         // sequences per tile of 128 rows
   int nsplit;      // parts of the prefix
   int nchunk;      // parts of the sequences' own tokens
+  bool join;       // the own-tokens kernel joins the parts itself
   float* o;
   float2* ml;
   float scale_log2;
@@ -259,12 +266,14 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
       mbar_wait_bounded(&drain[i], 0, kAttnWaitLimitNs);
     }
   } else {
-    // ---------------- softmax: thread r of either warpgroup hf owns tokens 64 hf ..
-    // 64 hf + 63 of row r of both tiles, in turn.  What a tile's weights wait
-    // for beside the tensor core is then half a row's arithmetic, and there are registers
-    // to keep 8 of the per-token numbers' loads under way: beside MMAs that take
-    // shared memory's full rate each may last hundreds of cycles (32768 x 256: 224 us
-    // with a warpgroup per tile and whole rows, 204 us so).
+    // ---------------- softmax: either warpgroup hf owns tokens 64 hf ..
+    // 64 hf + 63 of both tiles, in turn.  What a tile's weights wait for beside the
+    // tensor core is then half a row's arithmetic (32768 x 256, this kernel: 224 us with a
+    // warpgroup per tile and whole rows, 204 us so).  Lane 4 g + c holds rows g, g + 8,
+    // g + 16, g + 24 of its warp and tokens 8 k + 2 c, 8 k + 2 c + 1: the per-token numbers
+    // are loaded for a quarter of the tokens and serve four rows.  With a row
+    // per lane those loads, beside MMAs that take shared memory's full rate, were 2048 of
+    // 4750 of its passes per 128 tokens (204 us; 200 us so).
     asm volatile("setmaxnreg.inc.sync.aligned.u32 184;\n");
     const int hf = warp >> 2, r = tid & 127, pair = 1 + (warp & 3);   // named barrier of this warp and warp ^ 4
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -572,7 +581,9 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   const int hk = blockIdx.y / hgroups, hg = blockIdx.y % hgroups, b = blockIdx.z;
   const int heads = min(8, p.G - 8 * hg);   // query heads of this CTA
-  pdl_wait();
+  // Behind a prefix this kernel starts beside it, on the SMs that it leaves: the
+  // prefix kernel lets it start once all its CTAs have seen the end of the work before.
+  if (p.nsplit == 0) pdl_wait();
   pdl_trigger();
   const int64_t cap = a.table_width * a.page_size;
   int64_t len = a.lens[b];
@@ -793,7 +804,7 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
   }
   __syncthreads();
   const int64_t rows = a.B * a.Hq, part = (int64_t)p.nsplit + blockIdx.x;
-  if (p.nchunk > 1) {
+  if (!p.join) {
     for (int e = threadIdx.x; e < heads * D; e += kOwnWarps * 32) {
       const int h = e / D, d = e % D;
       float M = -INFINITY;
@@ -809,8 +820,12 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
       p.o[(part * rows + row0 + h) * D + d] = val;
       if (d == 0) p.ml[part * rows + row0 + h] = make_float2(M, ls);
     }
+    // one CTA stays until the prefix's parts are written, and with it the grid that the
+    // combine kernel waits for
+    if (p.nsplit > 0 && blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1 && blockIdx.z == gridDim.z - 1) pdl_wait();
     return;
   }
+  if (p.nsplit > 0) pdl_wait();   // the prefix's parts
   // The only part of these rows' own tokens: joined with the prefix's here.
   // f_s[h][0 .. 3] the warps' factors, then the prefix parts', all over the sum.
   __shared__ float f_s[8][kOwnWarps + kMaxSplits];
@@ -915,6 +930,17 @@ int own_chunks(const PrefixArgs& a) {
   return (int)(n > by_len ? by_len : n);
 }
 
+// Whether the own-tokens kernel joins the parts.  Not where the prefix kernel
+// leaves an eighth of the SMs or more and there are several waves of own-tokens CTAs:
+// those that join wait for the prefix in their slots, the others pass through the idle
+// SMs beside it (32768 x 256, 128 of 152 SMs: 247 us with the own tokens after the
+// prefix and joined there, 221 us so; few CTAs save the third kernel's 3 us).
+bool own_joins(const PrefixArgs& a) {
+  if (own_chunks(a) > 1) return false;
+  const int64_t sms = device_sm_count(), ctas = a.B * a.Hkv * ((a.Hq / a.Hkv + 7) / 8);
+  return prefix_splits(a) == 0 || 8 * row_blocks(a) * a.Hkv * prefix_splits(a) > 7 * sms || ctas <= 8 * sms;
+}
+
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
 template <int D>
@@ -925,9 +951,10 @@ cudaError_t launch_t(const PrefixArgs& a, cudaStream_t stream) {
   p.tps = 128 / p.G;
   p.nsplit = prefix_splits(a);
   p.nchunk = own_chunks(a);
+  p.join = own_joins(a);
   const int64_t rows = a.B * a.Hq;
   p.ml = static_cast<float2*>(a.workspace);
-  p.o = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256((p.nsplit + (p.nchunk > 1 ? p.nchunk : 0)) * rows * 8));
+  p.o = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256((p.nsplit + (p.join ? 0 : p.nchunk)) * rows * 8));
   p.scale_log2 = a.scale * kAttnLog2e;
   p.status = device_status_word();
   cudaError_t e = cudaSuccess;
@@ -946,7 +973,7 @@ cudaError_t launch_t(const PrefixArgs& a, cudaStream_t stream) {
     const int hgroups = (p.G + 7) / 8;
     e = launch_pdl(own_tokens_kernel<D>, dim3((unsigned)p.nchunk, (unsigned)(a.Hkv * hgroups), (unsigned)a.B),
                    dim3(kOwnWarps * 32), 0, stream, 1, p, hgroups, chunk);
-    if (e != cudaSuccess || p.nchunk == 1) return e != cudaSuccess ? e : cudaGetLastError();
+    if (e != cudaSuccess || p.join) return e != cudaSuccess ? e : cudaGetLastError();
   }
   e = launch_pdl(prefix_combine_kernel<D>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, stream, 1, p);
   return e != cudaSuccess ? e : cudaGetLastError();
@@ -957,8 +984,7 @@ cudaError_t launch_t(const PrefixArgs& a, cudaStream_t stream) {
 cudaError_t set_wait_limit_prefix(uint64_t ns) { return cudaMemcpyToSymbol(g_prefix_wait_ns, &ns, sizeof(ns)); }
 
 int64_t prefix_attention_workspace(const PrefixArgs& a) {
-  const int chunks = own_chunks(a);
-  const int64_t parts = prefix_splits(a) + (chunks > 1 ? chunks : 0), rows = a.B * a.Hq;
+  const int64_t parts = prefix_splits(a) + (own_joins(a) ? 0 : own_chunks(a)), rows = a.B * a.Hq;
   return align256(parts * rows * 8) + parts * rows * a.D * 4;
 }
 
