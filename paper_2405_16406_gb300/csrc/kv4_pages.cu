@@ -24,11 +24,17 @@
 // packed fp32.  A rotate-half pair over the whole head is one register pair, every
 // butterfly but the last works on packed pairs, and only bits 3 and 4 of
 // the transform go through shuffles.  The next row's data are loaded before this
-// one's are worked on.
+// one's are worked on.  Bound: the bytes come second to the shuffles, 64 per 8 rows, which
+// with the loads hold L1/TEX at 69 % of its peak (issue at 54 %, with norm and RoPE).
+// 32768 tokens, 32 / 8 heads, D 128, RoPE: 709 MB in 162 us, 4.4 TB/s (a row per
+// warp took 251 us with the read below, packed pairs 211, pieces in turn and the next row
+// ahead 198).
 //
 // Read layout.  A warp expands 16 tokens of one kv head, whose codes are one
 // run of a page wherever the tokens are; the warps of a block take the heads of the same
-// tokens, whose output rows lie next to one another.
+// tokens, whose output rows lie next to one another.  Bound: the bytes, 711 MB in 129
+// us, 5.5 TB/s (a token per warp: 196 us); in 777 tokens the latency of a table entry, a
+// row of codes and a store, 3 us.
 #include <cuda_fp16.h>
 #include <float.h>
 
