@@ -916,7 +916,10 @@ int prefix_splits(const PrefixArgs& a) {
   const int64_t tiles = (a.prefix_len + 127) / 128;
   int64_t n = device_sm_count() / (row_blocks(a) * a.Hkv);   // one CTA per SM
   n = n < 1 ? 1 : (n > kMaxSplits ? kMaxSplits : n);
-  return (int)(n > tiles ? tiles : n);
+  // no more than the longest part's length asks for: fewer parts to write and join, and
+  // SMs for the own tokens (8191 x 64, 64 tiles: 34.4 us in 19 parts, 33.4 us in 16)
+  const int64_t longest = (tiles + n - 1) / n;
+  return (int)((tiles + longest - 1) / longest);
 }
 
 // Parts of the sequences' own tokens.  One, where that gives every SM a CTA: the
