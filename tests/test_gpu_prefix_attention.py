@@ -188,3 +188,42 @@ def test_a_query_that_is_not_a_number_gives_its_own_row_only(S, prefix, lens):
     bad = torch.zeros(3, 8, dtype=torch.bool, device="cuda")
     bad[0, 3] = True
     assert out[0, 3].isnan().all() and torch.equal(out[~bad], clean[~bad])
+
+
+def test_many_sequences_beside_a_short_prefix(S):
+    """Few SMs have a part of the prefix, the own tokens many CTAs."""
+    rng = np.random.default_rng(9)
+    lens = rng.integers(0, 60, 160).tolist()
+    _run(S, 300, lens, 8, 8, 64, 16, check=[0, 1, 80, 159])
+    _run(S, 300, lens, 8, 8, 128, 16, check=[0, 1, 80, 159])
+
+
+@pytest.mark.parametrize("B,prefix", [(160, 700), (3, 700), (5, 0)])
+def test_tokens_appended_just_before_are_seen(S, B, prefix):
+    """Append and attention back to back, and with everything finished between them."""
+    rng = np.random.default_rng(10)
+    Hkv, D, P, own = 8, 128, 16, 64
+    pages = -(-prefix // P) + B * own // P
+    cache = ku.random_cache(S, rng, pages, P, Hkv, D, poison=False)
+    order = torch.from_numpy(rng.permutation(pages).astype(np.int32)).cuda()
+    table, shared = order[:B * own // P].view(B, -1).contiguous(), order[B * own // P:].contiguous()
+    if prefix == 0:
+        shared = torch.zeros(1, dtype=torch.int32, device="cuda")
+    T = B * 16   # 16 new tokens per sequence, at positions 48 .. 63
+    slots = (table[:, 3].long()[:, None] * P + torch.arange(P, device="cuda")).flatten()
+    lens = torch.full((B,), own, dtype=torch.int32, device="cuda")
+    q = torch.from_numpy(rng.standard_normal((B, 16, D)).astype(np.float16)).cuda()
+    new = [[torch.from_numpy(rng.standard_normal((T, Hkv, D)).astype(np.float16)).cuda() for _ in range(2)] for _ in range(4)]
+    want = []
+    for k, v in new:
+        S.kv4_append(None, k, v, cache, slots)
+        torch.cuda.synchronize()
+        want.append(S.prefix_attention_kv4(q, cache, shared, prefix, table, lens))
+        torch.cuda.synchronize()
+    got = []
+    for k, v in new:
+        S.kv4_append(None, k, v, cache, slots)
+        got.append(S.prefix_attention_kv4(q, cache, shared, prefix, table, lens))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert not torch.equal(want[0], want[1])
