@@ -38,8 +38,7 @@
 //    through those waits (4 x 4096: 484 us against 431 us);
 //  * warp 11: one thread fetches the items and leaves out those past a
 //    sequence's end.
-// Bound: the tensor core (4 D flops per visible pair of a query head and a
-// key).
+// Floor: the tensor core (4 D flops per visible pair of a query head and a key).
 //
 // A sequence's last V tile may hold rows of the next sequence or of no
 // sequence: they meet weights 0, which is not enough if they are not finite, so the
