@@ -762,8 +762,13 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
         z[e] = fmaf(pe, vz[h], z[e]);
         w[h][e] = pe * va[h];
       }
-    const uint32_t pb0 = own_transpose(pack_half2_bits(w[0][0], w[0][1]));
-    const uint32_t pb1 = own_transpose(pack_half2_bits(w[1][0], w[1][1]));
+    // the weights as two fp16 parts, the second what the first leaves: with one part the
+    // few weights that carry a short sequence's row would all but double its error
+    const uint32_t h0 = pack_half2_bits(w[0][0], w[0][1]), h1 = pack_half2_bits(w[1][0], w[1][1]);
+    const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+    const uint32_t pb0 = own_transpose(h0), pb1 = own_transpose(h1);
+    const uint32_t pc0 = own_transpose(pack_half2_bits(w[0][0] - f0.x, w[0][1] - f0.y));
+    const uint32_t pc1 = own_transpose(pack_half2_bits(w[1][0] - f1.x, w[1][1] - f1.y));
 #pragma unroll
     for (int vw = 0; vw < VW; ++vw)
 #pragma unroll
@@ -775,6 +780,8 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
         const uint32_t a0[4] = {ya.x, ya.y, yb.x, yb.y}, a1[4] = {ya.z, ya.w, yb.z, yb.w};
         mma_16816_f16_f32_acc(o[4 * vw + 2 * q], a0, pb0, pb1);
         mma_16816_f16_f32_acc(o[4 * vw + 2 * q + 1], a1, pb0, pb1);
+        mma_16816_f16_f32_acc(o[4 * vw + 2 * q], a0, pc0, pc1);
+        mma_16816_f16_f32_acc(o[4 * vw + 2 * q + 1], a1, pc0, pc1);
       }
   }
   // join the lanes' shares, then the warps
