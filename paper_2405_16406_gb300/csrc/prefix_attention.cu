@@ -9,7 +9,8 @@
 //   s_t = (scale alpha_t) (q . (u_t - 8)) + scale (beta_t + 8 alpha_t) sum_d q_d
 //   o   = [ sum_t (p_t alpha'_t) (u'_t - 8) + sum_t p_t (beta'_t + 8 alpha'_t) ] / sum_t p_t
 // so the only rounding before the output is that of p alpha' to fp16, on codes
-// about their middle (the offsets, which are larger, stay in fp32).  With
+// about their middle (the offsets, which are larger, stay in fp32); the own tokens and
+// a prefix with few sequences carry p alpha' as two fp16 parts.  With
 // M = (running maximum of s, base 2) + log2 r, r about the largest alpha' so far, the
 // weights 2^(s - M) alpha' stay in fp16's range whatever the values' magnitude; M
 // moves only when a score or an alpha' outgrows it by 2^8 or 2^4.
@@ -97,7 +98,9 @@ struct PrefixCfg {
 // MMAs (56), one that expands the codes (88): 512 = 4 * 128, what the launch holds
 constexpr int kPrefixThreads = 512;
 
-template <int D>
+// TWO: the weights as two fp16 parts, the second (what the first leaves) in the
+// columns of S behind the first's, with a product of its own; one tile of rows.
+template <int D, bool TWO>
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const PrefixParams p) {
   using C = PrefixCfg<D>;
   constexpr int NSTG = C::NSTG, NCOL = C::NCOL;
@@ -117,7 +120,8 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   const int b0 = blockIdx.x * 2 * p.tps;
-  const int nrow = b0 + p.tps < (int)a.B ? 2 : 1;   // tiles of rows
+  constexpr int NROW = TWO ? 1 : 2;
+  const int nrow = !TWO && b0 + p.tps < (int)a.B ? 2 : 1;   // tiles of rows
   if (tid == 0) {
     mbar_init(qbar, 8);
     for (int s = 0; s < NSTG; ++s) {
@@ -253,6 +257,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
         if (!ok || !(ok = attn_wait(&pbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns))) break;
         tc_fence_after();
         attn_mma_pv<D>(256 + i * D, i * 128, v_lo + sv * (C::TILE >> 4), j > 0);
+        if (TWO) attn_mma_pv<D>(256 + i * D, i * 128 + 64, v_lo + sv * (C::TILE >> 4), true);
         if (sn >= 0) {
           attn_mma_qk<D>(i * 128, q_lo, k_lo + sn * (C::TILE >> 4), idesc);
           tc_commit(&sbar[i]);
@@ -337,7 +342,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
 #pragma unroll 1
     for (int j = 0; ok && j < nt; ++j)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < NROW; ++i) {
         if (i >= nrow || !ok) continue;
         const uint32_t st = tmem + i * 128 + lanes;
         if (i == 0) ok = attn_wait_warp(&cbar[j % NCOL], (uint32_t)(j / NCOL) & 1u, abort_flag, g_prefix_wait_ns);
@@ -434,6 +439,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
             sum[e] = f2_make(l[i][e], 0.f);
             zs[e] = f2_make(z[i][e], 0.f);
           }
+          uint32_t rest[2][16];   // second parts
 #pragma unroll
           for (int k = 0; k < 8; ++k)
 #pragma unroll
@@ -445,8 +451,17 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
               sum[e] = f2_add(sum[e], ex);
               zs[e] = f2_fma(ex, F2{f[k].y}, zs[e]);
               f2_split(f2_mul(ex, F2{f[k].x}), x, y);
-              s[e >> 1][2 * k + (e & 1)] = pack_half2_bits(x, y);   // 32-bit column 4 k + c of this half's P
+              const uint32_t h = pack_half2_bits(x, y);
+              s[e >> 1][2 * k + (e & 1)] = h;   // 32-bit column 4 k + c of this half's P
+              if (TWO) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                rest[e >> 1][2 * k + (e & 1)] = pack_half2_bits(x - f.x, y - f.y);
+              }
             }
+          if (TWO) {
+            tmem_st_16x128b_x8(st + 64 + hf * 32, rest[0]);
+            tmem_st_16x128b_x8(st + (16u << 16) + 64 + hf * 32, rest[1]);
+          }
           tmem_st_16x128b_x8(st + hf * 32, s[0]);
           tmem_st_16x128b_x8(st + (16u << 16) + hf * 32, s[1]);
 #pragma unroll
@@ -464,7 +479,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
         if (lane == 0) mbar_arrive(&pbar[i]);
       }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NROW; ++i) {
       if (!ok || i >= nrow || !work[i]) continue;
       if (nt > 0) ok = attn_wait_warp(&obar[i], 0, abort_flag, g_prefix_wait_ns);
       ok = !attn_pair_or(!ok, pair);
@@ -971,9 +986,16 @@ cudaError_t launch_t(const PrefixArgs& a, cudaStream_t stream) {
   if (p.nsplit > 0) {
     p.debug_stall = take_debug_stall() ? 1 : 0;
     int per_sm = 0;
-    e = prepare_launch_tmem(prefix_tc_kernel<D>, kPrefixThreads, PrefixCfg<D>::BYTES, 512, &per_sm);
+    // A few rows may be carried by few weights, whose rounding then nearly doubles the
+    // error of the whole output; many rows average it (0.00028 against 0.00021 of the
+    // output's own rounding).  So one tile of rows takes second parts (a row carried by few
+    // weights: 0.00031 with one part, 0.00021 with two; 1000 x 4: 9.8 and 10.3 us, 24000 x
+    // 32: 38.9 and 44.8); the softmax of two tiles bounds its kernel and has no
+    // registers for them (52 bytes of spills).
+    auto kernel = a.B <= p.tps ? prefix_tc_kernel<D, true> : prefix_tc_kernel<D, false>;
+    e = prepare_launch_tmem(kernel, kPrefixThreads, PrefixCfg<D>::BYTES, 512, &per_sm);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(prefix_tc_kernel<D>, dim3((unsigned)row_blocks(a), (unsigned)a.Hkv, (unsigned)p.nsplit),
+    e = launch_pdl(kernel, dim3((unsigned)row_blocks(a), (unsigned)a.Hkv, (unsigned)p.nsplit),
                    dim3(kPrefixThreads), PrefixCfg<D>::BYTES, stream, 1, p);
     if (e != cudaSuccess) return e;
   }
