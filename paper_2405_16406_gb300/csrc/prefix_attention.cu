@@ -28,7 +28,7 @@
 //   own_tokens_kernel  each sequence's own tokens, beside the prefix kernel where it
 //     leaves SMs: G heads are too few rows for those tiles, so mma.sync with the
 //     tokens on the M side, codes copied as they are.  Bound: the cache's bytes (256
-//     sequences of 523 tokens on average, 154 MB: 46 us alone, 3.4 TB/s).  Where one CTA has all of a
+//     sequences of 523 tokens on average, 154 MB: 48 us alone, 3.2 TB/s).  Where one CTA has all of a
 //     sequence's own tokens it may also join them with the prefix's parts.
 //   prefix_combine_kernel  else joins the parts (maximum, sum, o) in a fixed order.
 #include <cuda_fp16.h>
@@ -959,7 +959,7 @@ int own_chunks(const PrefixArgs& a) {
 // leaves an eighth of the SMs or more and there are several waves of own-tokens CTAs:
 // those that join wait for the prefix in their slots, the others pass through the idle
 // SMs beside it (32768 x 256, 128 of 152 SMs: 247 us with the own tokens after the
-// prefix and joined there, 221 us so; few CTAs save the third kernel's 3 us).
+// prefix and joined there, 222 us so; few CTAs save the third kernel's 3 us).
 bool own_joins(const PrefixArgs& a) {
   if (own_chunks(a) > 1) return false;
   const int64_t sms = device_sm_count(), ctas = a.B * a.Hkv * ((a.Hq / a.Hkv + 7) / 8);
