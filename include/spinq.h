@@ -400,7 +400,8 @@ spinq_status spinq_decode_attention_kv4(const void* q, const uint8_t* k_codes, c
  *            codes, 16-byte aligned (K rotated by R3, as spinq_rotate_quant_kv
  *            stores it);
  *   scales   [num_pages][kv_heads][page_size][4] fp32, 16-byte aligned:
- *            (K alpha, K beta, V alpha, V beta) of the token and head.
+ *            (K alpha, K beta, V alpha, V beta) of the token and head, alpha >= 0
+            (Eq. 1's step; a V alpha below 2^-40 counts as 2^-40 in attention).
  * Slot number s of the cache is slot s % page_size of page s / page_size.
  * page_size: 16, 32, 64, 128 or 256.  head_dim: 64 or 128.  A slot that no
  * call has written may hold anything (also values that are not finite): no

@@ -5,15 +5,17 @@
 //   s_t = scale q . k_t,  k_t = alpha_t u_t + beta_t
 //   o   = sum_t softmax_t(s) v_t,  v_t = alpha'_t u'_t + beta'_t
 //
-// The codes meet the tensor core as the whole numbers u - 8, exact in fp16:
+// The codes meet the tensor core as the whole numbers u - 8, exact in fp16, and the
+// weights are those that the codes have in the output, w = 2^(s + log2 alpha' - M)
+// with M the running maximum of s + log2 alpha' (base 2):
 //   s_t = (scale alpha_t) (q . (u_t - 8)) + scale (beta_t + 8 alpha_t) sum_d q_d
-//   o   = [ sum_t (p_t alpha'_t) (u'_t - 8) + sum_t p_t (beta'_t + 8 alpha'_t) ] / sum_t p_t
-// so the only rounding before the output is that of p alpha' to fp16, on codes
-// about their middle (the offsets, which are larger, stay in fp32); the own tokens and
-// a prefix with few sequences carry p alpha' as two fp16 parts.  With
-// M = (running maximum of s, base 2) + log2 r, r about the largest alpha' so far, the
-// weights 2^(s - M) alpha' stay in fp16's range whatever the values' magnitude; M
-// moves only when a score or an alpha' outgrows it by 2^8 or 2^4.
+//   o   = [ sum_t w_t (u'_t - 8) + sum_t w_t (beta'_t + 8 alpha'_t) / alpha'_t ] / sum_t w_t / alpha'_t
+// so the only rounding before the output is that of w to fp16, on codes about
+// their middle (the two other sums stay in fp32); the own tokens and a prefix with few
+// sequences carry w as two fp16 parts.  The token that weighs most has w near 1 (M moves
+// only when a token outgrows it by 2^8): a large alpha' of a token without weight in the softmax
+// does not push the others' w below fp16's range, as one scale for scores and one for
+// alpha' apart would.
 //
 // Two or three kernels on the stream:
 //   prefix_tc_kernel   the shared tokens, once for all sequences: an MMA's 128
@@ -44,10 +46,14 @@ namespace {
 
 __device__ uint64_t g_prefix_wait_ns = kAttnWaitLimitNs;
 constexpr int kPrefixSite = 32;    // wait site recorded on a time-out
-constexpr float kMinValueScale = 8.67361738e-19f;   // 2^-60: values this small are 0 in fp16
+// A row of values with a smaller scale (equal values have 0) counts as one of this scale, 2^-40:
+// 15 steps of it, 2^-36, are nothing beside fp16's smallest step, 2^-24, and w stays
+// above 2^-126 beside any alpha' up to 2^80.  (A scale that is not a number stays one.)
+constexpr float kMinValueScale = 9.094947017729282e-13f;
+__device__ __forceinline__ float value_scale(float x) { return x < kMinValueScale ? kMinValueScale : x; }
 
-// Parts of the result: part p of row (b, head) is max, sum at ml[p][row] and
-// the weighted sum at o[p][row][D] (not written where the sum is 0).
+// Parts of the result: part p of row (b, head) is M and sum of w / alpha' at ml[p][row] and
+// the weighted sum of the values at o[p][row][D] (not written where the sum is 0).
 struct PrefixParams {
   PrefixArgs a;
   int G;
@@ -86,9 +92,11 @@ struct PrefixCfg {
   static constexpr int NSTG = 4;                         // operand tiles in flight
   static constexpr int NCOL = 4;                         // tiles of per-token numbers
   static constexpr int OFF_KV = 2 * TILE;
-  static constexpr int OFF_COL = OFF_KV + NSTG * TILE;   // [NCOL][2][64] float4
-  static constexpr int OFF_RM = OFF_COL + NCOL * 2048 * 2;   // [NCOL][4] largest alpha' of each warp's tokens
-  static constexpr int OFF_BAR = OFF_RM + NCOL * 16;     // q, full, free [NSTG], col [NCOL], s, p, o, drain [2]
+  // a tile's numbers: 64 pairs of tokens' score scales and offsets, 64 pairs of the factors
+  // of the two sums, 64 pairs of log2 alpha'
+  static constexpr int COL_V = 1024, COL_LOG = 2048, COL = 2560;
+  static constexpr int OFF_COL = OFF_KV + NSTG * TILE;
+  static constexpr int OFF_BAR = OFF_COL + NCOL * COL;   // q, full, free [NSTG], col [NCOL], s, p, o, drain [2]
   static constexpr int OFF_MISC = OFF_BAR + (2 * NSTG + NCOL + 9) * 8;
   static constexpr int OFF_X = OFF_MISC + 16;            // 256 floats: query sums, then exchanged values
   static constexpr int BYTES = OFF_X + 1024 + 1024;
@@ -206,16 +214,14 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
       // the tile's numbers: slot j % NCOL was last read for tile j - NCOL,
       // whose V tile has been released by now (NSTG operand tiles = 2 tiles of tokens)
       const bool in = (int64_t)(j0 + j) * 128 + t < a.prefix_len;
-      float* col = reinterpret_cast<float*>(smem + C::OFF_COL + (j % NCOL) * 4096) + (t >> 1) * 4 + (t & 1);
+      uint8_t* cols = smem + C::OFF_COL + (j % NCOL) * C::COL;
+      float* col = reinterpret_cast<float*>(cols) + (t >> 1) * 4 + (t & 1);
       col[0] = in ? p.scale_log2 * sc.x : 0.f;
       col[2] = in ? p.scale_log2 * fmaf(8.f, sc.x, sc.y) : 0.f;
-      const float va = in ? sc.z : 0.f;
-      col[512] = va;
-      col[514] = in ? fmaf(8.f, sc.z, sc.w) : 0.f;
-      float rm = va;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, o));
-      if (lane == 0) reinterpret_cast<float*>(smem + C::OFF_RM + (j % NCOL) * 16)[warp & 3] = rm;
+      const float va = in ? value_scale(sc.z) : 1.f, rv = __frcp_rn(va);
+      col[C::COL_V / 4] = rv;
+      col[C::COL_V / 4 + 2] = in ? rv * fmaf(8.f, va, sc.w) : 0.f;
+      reinterpret_cast<float*>(cols + C::COL_LOG)[t] = __log2f(va);
       __syncwarp();
       if (lane == 0) mbar_arrive(&cbar[j % NCOL]);
       expand(kw, n);
@@ -334,8 +340,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
     xs += (warp & 3) * 32;
     // a value of each of the lane's four rows (the same in a quad) as one per lane, of row 8 c + g
     auto gather = [&](const float (&v)[4]) { return c < 2 ? (c == 0 ? v[0] : v[1]) : (c == 2 ? v[2] : v[3]); };
-    float m[2][4], l[2][4], z[2][4];   // l, z: of this lane's tokens
-    float rc[2] = {0.f, 0.f}, lr[2] = {0.f, 0.f};   // M = m + lr, lr = log2 rc
+    float m[2][4], l[2][4], z[2][4];   // M; l, z: of this lane's tokens
 #pragma unroll
     for (int e = 0; e < 4; ++e) m[0][e] = m[1][e] = -INFINITY, l[0][e] = l[1][e] = z[0][e] = z[1][e] = 0.f;
     bool ok = true;
@@ -352,13 +357,14 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
           if (!ok) continue;
         } else {
           // the numbers of tokens 8 k + 2 c, 8 k + 2 c + 1: scale and offset of the scores,
-          // k = 0 .. 7, then those of the values; the latter are loaded as the former are used
-          const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(smem + C::OFF_COL + (j % NCOL) * 4096 + hf * 512) + c;
-          const float4 r4 = *reinterpret_cast<const float4*>(smem + C::OFF_RM + (j % NCOL) * 16);
+          // k = 0 .. 7, then the factors of the sums; the latter are loaded as the former are used
+          const uint8_t* cols = smem + C::OFF_COL + (j % NCOL) * C::COL;
+          const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(cols + hf * 512) + c;
+          const ulonglong2* fv = reinterpret_cast<const ulonglong2*>(cols + C::COL_V + hf * 512) + c;
+          const unsigned long long* la = reinterpret_cast<const unsigned long long*>(cols + C::COL_LOG + hf * 256) + c;
           ulonglong2 f[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) f[k] = ab[4 * k];
-          const float rm = fmaxf(attn_max3(r4.x, r4.y, r4.z), r4.w);
           ok = ok && attn_wait_warp(&sbar[i], (uint32_t)j & 1u, abort_flag, g_prefix_wait_ns);
           tc_fence_after();
           // (after a wait given up the columns are read all the same, in bounds, and discarded)
@@ -370,12 +376,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             const ulonglong2 w = f[k];
-            f[k] = ab[128 + 4 * k];
+            const F2 lg = F2{la[4 * k]};
+            f[k] = fv[4 * k];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               uint32_t* v = &s[e >> 1][4 * k + 2 * (e & 1)];
               float x, y;
-              f2_split(f2_fma(f2_from_bits(v[0], v[1]), F2{w.x}, f2_mul(F2{w.y}, f2_make(qs[i][e], qs[i][e]))), x, y);
+              f2_split(f2_fma(f2_from_bits(v[0], v[1]), F2{w.x}, f2_fma(F2{w.y}, f2_make(qs[i][e], qs[i][e]), lg)), x, y);
               v[0] = __float_as_uint(x);
               v[1] = __float_as_uint(y);
             }
@@ -390,7 +397,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
                   s[0][4 * k + x] = s[0][4 * k + 2 + x] = s[1][4 * k + x] = s[1][4 * k + 2 + x] = 0xFF800000u;   // -inf
           }
           float mx[4];
-          bool grow = !ok || rm > 16.f * rc[i];
+          bool grow = !ok;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint32_t* v = &s[e >> 1][2 * (e & 1)];
@@ -413,17 +420,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
               mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
               mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
             }
-            const float other = attn_pair_swap(xs, gather(mx), hf, lane, pair), was = lr[i];
-            if (rm > 16.f * rc[i]) {
-              rc[i] = fmaxf(rm, kMinValueScale);
-              lr[i] = __log2f(rc[i]);
-            }
+            const float other = attn_pair_swap(xs, gather(mx), hf, lane, pair);
             float fr[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float t = fmaxf(mx[e], __shfl_sync(0xffffffffu, other, (lane & 28) + e));
               const float mn = t > m[i][e] + kAttnSlack ? t : m[i][e];
-              fr[e] = m[i][e] == -INFINITY ? 0.f : attn_exp2((m[i][e] + was) - (mn + lr[i]));
+              fr[e] = m[i][e] == -INFINITY ? 0.f : attn_exp2(m[i][e] - mn);
               m[i][e] = mn;
               l[i][e] *= fr[e];
               z[i][e] *= fr[e];
@@ -434,7 +437,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
           F2 of2[4], sum[4], zs[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float off = m[i][e] == -INFINITY ? 0.f : -(m[i][e] + lr[i]);
+            const float off = m[i][e] == -INFINITY ? 0.f : -m[i][e];
             of2[e] = f2_make(off, off);
             sum[e] = f2_make(l[i][e], 0.f);
             zs[e] = f2_make(z[i][e], 0.f);
@@ -448,9 +451,9 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
               float x, y;
               f2_split(f2_add(f2_from_bits(v[0], v[1]), of2[e]), x, y);
               const F2 ex = f2_make(attn_exp2(x), attn_exp2(y));
-              sum[e] = f2_add(sum[e], ex);
+              sum[e] = f2_fma(ex, F2{f[k].x}, sum[e]);
               zs[e] = f2_fma(ex, F2{f[k].y}, zs[e]);
-              f2_split(f2_mul(ex, F2{f[k].x}), x, y);
+              f2_split(ex, x, y);
               const uint32_t h = pack_half2_bits(x, y);
               s[e >> 1][2 * k + (e & 1)] = h;   // 32-bit column 4 k + c of this half's P
               if (TWO) {
@@ -500,9 +503,8 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
       mi = __shfl_sync(0xffffffffu, mi, from);
       li = __shfl_sync(0xffffffffu, li, from);
       zi = __shfl_sync(0xffffffffu, zi, from);
-      const float back = rc[i] > 0.f ? rc[i] : 1.f;   // 2^lr: the sums to weights 2^(s - m)
       const int64_t rows = a.B * a.Hq, mine = row[i];
-      if (mine >= 0 && hf == 0) p.ml[(int64_t)blockIdx.z * rows + mine] = make_float2(mi, li * back);
+      if (mine >= 0 && hf == 0) p.ml[(int64_t)blockIdx.z * rows + mine] = make_float2(mi, li);
       if (nt == 0) continue;
       // D / 4 values of each row at a time through the tile's Q rows, which no
       // product reads any more, so that a row's values leave in one run
@@ -519,7 +521,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
         for (int e = 0; e < D / 4; e += 8) {   // column 0, 1, .. of eight holds value 0, 4, 1, 5, 2, 6, 3, 7
           float v[8];
 #pragma unroll
-          for (int x = 0; x < 8; ++x) v[x] = (__uint_as_float(o[part + e + x]) + zi) * back;
+          for (int x = 0; x < 8; ++x) v[x] = __uint_as_float(o[part + e + x]) + zi;
           uint8_t* dst = buf + lane * D;
           *reinterpret_cast<float4*>(dst + (((e >> 2) ^ (lane & (D / 16 - 1))) << 4)) = make_float4(v[0], v[2], v[4], v[6]);
           *reinterpret_cast<float4*>(dst + (((e >> 2) + 1 ^ (lane & (D / 16 - 1))) << 4)) =
@@ -675,8 +677,7 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
   float o[NM][4];
 #pragma unroll
   for (int mu = 0; mu < NM; ++mu) o[mu][0] = o[mu][1] = o[mu][2] = o[mu][3] = 0.f;
-  // M = m + lr: the weights are 2^(s - M) alpha'
-  float m[2] = {-INFINITY, -INFINITY}, off[2] = {0.f, 0.f}, l[2] = {0.f, 0.f}, z[2] = {0.f, 0.f}, lr = 0.f, rcur = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, off[2] = {0.f, 0.f}, l[2] = {0.f, 0.f}, z[2] = {0.f, 0.f};   // m: M
 #pragma unroll
   for (int i = 0; i < kOwnStages - 1; ++i) issue(i);
   for (int i = 0; i < nstep; ++i) {
@@ -720,41 +721,37 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
       mma_16816_f16_f32_acc(sa, a0, qb[2 * w][0], qb[2 * w][1]);
       mma_16816_f16_f32_acc(sc2, a1, qb[2 * w + 1][0], qb[2 * w + 1][1]);
     }
-    // scores (base 2) of tokens g, g + 8 for heads 2c, 2c + 1; tokens past the
-    // chunk (their slots may hold anything) get -inf and value numbers 0
-    float t[2][2], va[2], vz[2];
+    // s + log2 alpha' (base 2) of tokens g, g + 8 for heads 2c, 2c + 1; tokens past the
+    // chunk (their slots may hold anything) get -inf and factors 0
+    float t[2][2], rv[2], vz[2];
     const int left = t1 - (t0 + 16 * (warp + kOwnWarps * i));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float ka = ks24 * x.sc[h].x;
-      va[h] = x.sc[h].z;
-      vz[h] = fmaf(8.f, x.sc[h].z, x.sc[h].w);
+      const float va = value_scale(x.sc[h].z), la = __log2f(va);
+      rv[h] = __frcp_rn(va);
+      vz[h] = rv[h] * fmaf(8.f, va, x.sc[h].w);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) t[h][e] = fmaf(ka, sa[2 * h + e] + sc2[2 * h + e], x.sc[h].y * qsk[e]);
+      for (int e = 0; e < 2; ++e) t[h][e] = fmaf(ka, sa[2 * h + e] + sc2[2 * h + e], fmaf(x.sc[h].y, qsk[e], la));
     }
     if (left < 16) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        if (g + 8 * h >= left) t[h][0] = t[h][1] = -INFINITY, va[h] = vz[h] = 0.f;
+        if (g + 8 * h >= left) t[h][0] = t[h][1] = -INFINITY, rv[h] = vz[h] = 0.f;
     }
-    const float rm0 = fmaxf(va[0], va[1]), mx0 = fmaxf(t[0][0], t[1][0]), mx1 = fmaxf(t[0][1], t[1][1]);
-    if (__any_sync(0xffffffffu, rm0 > 16.f * rcur || mx0 > m[0] + kAttnSlack || mx1 > m[1] + kAttnSlack)) {
-      float mx[2] = {mx0, mx1}, rm = rm0;
+    const float mx0 = fmaxf(t[0][0], t[1][0]), mx1 = fmaxf(t[0][1], t[1][1]);
+    if (__any_sync(0xffffffffu, mx0 > m[0] + kAttnSlack || mx1 > m[1] + kAttnSlack)) {
+      float mx[2] = {mx0, mx1};
 #pragma unroll
       for (int w = 4; w < 32; w <<= 1) {
         mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], w));
         mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], w));
-        rm = fmaxf(rm, __shfl_xor_sync(0xffffffffu, rm, w));
-      }
-      if (rm > 16.f * rcur) {
-        rcur = fmaxf(rm, kMinValueScale);
-        lr = __log2f(rcur);
       }
       float f[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float mn = mx[e] > m[e] + kAttnSlack ? mx[e] : m[e];
-        const float to = mn == -INFINITY ? 0.f : mn + lr;
+        const float to = mn == -INFINITY ? 0.f : mn;
         f[e] = m[e] == -INFINITY ? 0.f : attn_exp2(off[e] - to);
         m[e] = mn;
         off[e] = to;
@@ -772,10 +769,9 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float pe = attn_exp2(t[h][e] - off[e]);
-        l[e] += pe;
-        z[e] = fmaf(pe, vz[h], z[e]);
-        w[h][e] = pe * va[h];
+        w[h][e] = attn_exp2(t[h][e] - off[e]);
+        l[e] = fmaf(w[h][e], rv[h], l[e]);
+        z[e] = fmaf(w[h][e], vz[h], z[e]);
       }
     // the weights as two fp16 parts, the second what the first leaves: with one part the
     // few weights that carry a short sequence's row would all but double its error
@@ -807,7 +803,6 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
       l[e] += __shfl_xor_sync(0xffffffffu, l[e], w);
       z[e] += __shfl_xor_sync(0xffffffffu, z[e], w);
     }
-  const float back = rcur > 0.f ? rcur : 1.f;
   asm volatile("cp.async.wait_group 0;\n" ::: "memory");
   __syncwarp();   // the ring is free
   float* o_w = reinterpret_cast<float*>(ring_s[warp]);
@@ -816,12 +811,12 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
     const int h = 2 * c + e;
 #pragma unroll
     for (int mu = 0; mu < NM; ++mu) {
-      o_w[h * D + g * (D / 8) + 2 * mu] = (o[mu][e] + z[e]) * back;
-      o_w[h * D + g * (D / 8) + 2 * mu + 1] = (o[mu][2 + e] + z[e]) * back;
+      o_w[h * D + g * (D / 8) + 2 * mu] = o[mu][e] + z[e];
+      o_w[h * D + g * (D / 8) + 2 * mu + 1] = o[mu][2 + e] + z[e];
     }
     if (g == 0) {
       m_s[warp][h] = m[e];
-      l_s[warp][h] = l[e] * back;
+      l_s[warp][h] = l[e];
     }
   }
   __syncthreads();
