@@ -512,8 +512,8 @@ spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, i
  *   page_table [B][table_width] int32, lens [B] int32 (device), each in
  *          [0, table_width * page_size] (others are clamped).
  *   workspace  spinq_prefix_attention_workspace_bytes(...) bytes, 16-byte
- *          aligned (no zeroing needed).
- *   Supported: Hq / kv_heads whole and at most 128.
+ *          aligned (no zeroing needed); 0 where the call refuses the sizes.
+ *   Supported: Hq / kv_heads whole and at most 128, Hq and B at most 65535.
  */
 int64_t spinq_prefix_attention_workspace_bytes(int64_t B, int64_t prefix_len, int64_t table_width, int32_t page_size,
                                                int64_t Hq, int64_t Hkv, int64_t D);

@@ -413,13 +413,15 @@ spinq_status spinq_decode_attention_kv4(const void* q, const uint8_t* k_codes, c
 
 namespace {
 
+bool page_size_ok(int64_t n) { return n >= 16 && n <= 256 && is_pow2(n); }
+
 // A paged cache's own numbers; the pointers are checked where they are used.
 spinq_status check_pages(const spinq_kv4_pages* c) {
   if (!c || c->num_pages < 0 || c->kv_heads <= 0 || c->head_dim <= 0 || c->page_size <= 0) return SPINQ_EINVAL;
   if (c->num_pages > 0 && (!c->k_codes || !c->v_codes || !c->scales)) return SPINQ_EINVAL;
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->scales)) return SPINQ_EINVAL;
   if (c->head_dim != 64 && c->head_dim != 128) return SPINQ_EUNSUPPORTED;
-  if (c->page_size < 16 || c->page_size > 256 || !is_pow2(c->page_size)) return SPINQ_EUNSUPPORTED;
+  if (!page_size_ok(c->page_size)) return SPINQ_EUNSUPPORTED;
   if (c->kv_heads > 65535 || c->num_pages > INT32_MAX) return SPINQ_EUNSUPPORTED;
   return SPINQ_OK;
 }
@@ -579,10 +581,16 @@ static PrefixArgs prefix_shape(int64_t B, int64_t prefix_len, int64_t table_widt
   return a;
 }
 
+// What the launch and its plan hold for; the workspace query plans too.
+static bool prefix_limits_ok(int64_t B, int64_t prefix_len, int64_t table_width, int64_t page_size, int64_t Hq,
+                             int64_t Hkv) {
+  return Hq / Hkv <= 128 && Hq <= 65535 && B <= 65535 && prefix_len <= INT32_MAX && table_width <= INT32_MAX / page_size;
+}
+
 int64_t spinq_prefix_attention_workspace_bytes(int64_t B, int64_t prefix_len, int64_t table_width, int32_t page_size,
                                                int64_t Hq, int64_t Hkv, int64_t D) {
-  if (B <= 0 || prefix_len < 0 || table_width < 0 || page_size <= 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 ||
-      (D != 64 && D != 128))
+  if (B <= 0 || prefix_len < 0 || table_width < 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || (D != 64 && D != 128) ||
+      !page_size_ok(page_size) || !prefix_limits_ok(B, prefix_len, table_width, page_size, Hq, Hkv))
     return 0;
   return prefix_attention_workspace(prefix_shape(B, prefix_len, table_width, page_size, Hq, Hkv, D));
 }
@@ -601,8 +609,7 @@ spinq_status spinq_prefix_attention_kv4(const void* q, const spinq_kv4_pages* ca
     if ((prefix_len > 0 && !prefix_table) || (table_width > 0 && !page_table)) return SPINQ_EINVAL;
     if ((prefix_len > 0 || table_width > 0) && cache->num_pages == 0) return SPINQ_EINVAL;
   }
-  if (Hq / Hkv > 128 || Hq > 65535 || B > 65535 || prefix_len > INT32_MAX || table_width > INT32_MAX / cache->page_size)
-    return SPINQ_EUNSUPPORTED;
+  if (!prefix_limits_ok(B, prefix_len, table_width, cache->page_size, Hq, Hkv)) return SPINQ_EUNSUPPORTED;
   if (B == 0) return SPINQ_OK;
   PrefixArgs a = prefix_shape(B, prefix_len, table_width, cache->page_size, Hq, Hkv, D);
   const int64_t need = prefix_attention_workspace(a);
