@@ -661,23 +661,43 @@ def kv4_pages(num_pages: int, page_size: int, kv_heads: int, head_dim: int, devi
                     torch.empty(shape + (4,), dtype=torch.float32, device=dev))
 
 
+_KV4_CFG = {D: QuantCfg(4, 0, SPINQ_PER_GROUP, D, 1.0) for D in (64, 128)}   # Eq. 1 over a head, not clipped
 _F16, _F32, _U8, _I32, _I64T = torch.float16, torch.float32, torch.uint8, torch.int32, torch.int64
 
 
-def _pages(cache: KV4Pages) -> Kv4PagesCfg:
+def _refuse(what: str) -> None:
+    raise ValueError(what)
+
+
+_current_device, _current_queue = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _queue(x: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> Tuple[int, int]:
+    """The GPU a call runs on, which is that of x and of the stream and the current one (the library
+    launches there), and the raw handle of the stream (by default the current one)."""
+    dev = x.get_device()
+    if dev < 0 or dev != _current_device() or (stream is not None and stream.device_index != dev):
+        _refuse("the tensors and the stream must be on the current GPU")
+    return dev, _current_queue(dev) if stream is None else stream.cuda_stream
+
+
+def _pages(cache: KV4Pages, dev: int) -> Kv4PagesCfg:
     kc, vc, sc = cache.k_codes, cache.v_codes, cache.scales
     shape = kc.shape
     n, h, p, half = shape
-    assert kc.dtype == _U8 and kc.is_contiguous() and vc.dtype == _U8 and vc.is_contiguous() and vc.shape == shape
-    assert sc.dtype == _F32 and sc.is_contiguous() and sc.shape == (n, h, p, 4)
+    if (kc.dtype is not _U8 or vc.dtype is not _U8 or sc.dtype is not _F32 or kc.get_device() != dev
+            or vc.get_device() != dev or sc.get_device() != dev or not kc.is_contiguous() or not vc.is_contiguous()
+            or not sc.is_contiguous() or vc.shape != shape or sc.shape != (n, h, p, 4)):
+        _refuse("wrong type, device, layout or shape of the pages")
     return Kv4PagesCfg(kc.data_ptr(), vc.data_ptr(), sc.data_ptr(), n, p, h, 2 * half)
 
 
-def _token_rows(x: torch.Tensor) -> int:
+def _token_rows(x: torch.Tensor, dev: int) -> int:
     """The distance in elements of the tokens of x [T, H, D], whose heads are contiguous."""
     T, H, D = x.shape
     st = x.stride()
-    assert x.dtype == _F16 and (D == 1 or st[2] == 1) and (H <= 1 or st[1] == D), "a token's heads must be contiguous"
+    if x.dtype is not _F16 or x.get_device() != dev or (D != 1 and st[2] != 1) or (H > 1 and st[1] != D):
+        _refuse("wrong type or device, or a token's heads are not contiguous")
     return st[0] if T > 1 else max(st[0], (H * D + 7) // 8 * 8)
 
 
@@ -691,15 +711,18 @@ def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.T
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _full(x: torch.Tensor, dtype, shape) -> int:
-    """The address of a contiguous tensor of this type and shape."""
-    assert x.dtype == dtype and x.is_contiguous() and x.shape == shape, "wrong type, layout or shape"
+def _full(x: torch.Tensor, dtype, shape, dev: int) -> int:
+    """The address of a contiguous tensor of this type and shape on GPU ``dev``."""
+    if x.dtype is not dtype or x.get_device() != dev or not x.is_contiguous() or x.shape != shape:
+        _refuse("wrong type, device, layout or shape")
     return x.data_ptr()
 
 
-def _queue(stream: Optional[torch.cuda.Stream], x: torch.Tensor) -> int:
-    """The raw handle of the stream a call runs on (by default the current one of x's device)."""
-    return torch._C._cuda_getCurrentRawStream(x.get_device()) if stream is None else stream.cuda_stream
+def _space(workspace: torch.Tensor, dev: int):
+    """Address and bytes of a caller's workspace."""
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse("wrong device or layout of the workspace")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: KV4Pages, slots: torch.Tensor,
@@ -712,28 +735,35 @@ def kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cach
     the cache; returns the rotated queries [T, Hq, D].  ``cos_sin``
     [max_pos, rotary_dim/2, 2] with ``positions`` [T] (int32), or None."""
     T, Hkv, D = k.shape
-    pages = _pages(cache)
-    assert Hkv == pages.kv_heads and D == pages.head_dim and v.shape == k.shape
+    dev, queue = _queue(k, stream)
+    pages = _pages(cache, dev)
+    if Hkv != pages.kv_heads or D != pages.head_dim or v.shape != k.shape:
+        _refuse("keys, values and pages differ in shape")
     Hq = ldq = 0
     q_ptr = out_ptr = None
     if q is not None:
         Hq = q.shape[1]
-        assert q.shape == (T, Hq, D)
-        ldq, q_ptr = _token_rows(q), q.data_ptr()
+        if q.shape != (T, Hq, D):
+            _refuse("queries and keys differ in shape")
+        ldq, q_ptr = _token_rows(q, dev), q.data_ptr()
         if q_out is None:
             q_out = _empty((T, Hq, D), _F16, q.device, stream)
-        out_ptr = _full(q_out, _F16, (T, Hq, D))
+            out_ptr = q_out.data_ptr()
+        else:
+            out_ptr = _full(q_out, _F16, (T, Hq, D), dev)
     rope = None
     if cos_sin is not None:
-        assert positions is not None and cos_sin.dim() == 3
+        if positions is None or cos_sin.dim() != 3:
+            _refuse("cos_sin is [max_pos, rotary_dim / 2, 2] and wants positions")
         n, half, _ = cos_sin.shape
-        rope = ctypes.byref(RopeCfg(2 * half, int(bool(interleaved)), _full(positions, _I32, (T,)),
-                                    _full(cos_sin, _F32, (n, half, 2)), n))
-    _check(_lib.spinq_kv4_append(q_ptr, ldq, out_ptr, k.data_ptr(), _token_rows(k), v.data_ptr(), _token_rows(v), T, Hq,
-                                 None if q_weight is None else _full(q_weight, _F16, (D,)),
-                                 None if k_weight is None else _full(k_weight, _F16, (D,)), eps, rope,
-                                 QuantCfg(4, 0, SPINQ_PER_GROUP, D, clip), pages, _full(slots, _I64T, (T,)),
-                                 _queue(stream, k)), "spinq_kv4_append")
+        rope = ctypes.byref(RopeCfg(2 * half, int(bool(interleaved)), _full(positions, _I32, (T,), dev),
+                                    _full(cos_sin, _F32, (n, half, 2), dev), n))
+    _check(_lib.spinq_kv4_append(q_ptr, ldq, out_ptr, k.data_ptr(), _token_rows(k, dev), v.data_ptr(),
+                                 _token_rows(v, dev), T, Hq,
+                                 None if q_weight is None else _full(q_weight, _F16, (D,), dev),
+                                 None if k_weight is None else _full(k_weight, _F16, (D,), dev), eps, rope,
+                                 _KV4_CFG[D] if clip == 1.0 and D in _KV4_CFG else QuantCfg(4, 0, SPINQ_PER_GROUP, D, clip), pages, _full(slots, _I64T, (T,), dev),
+                                 queue), "spinq_kv4_append")
     return q_out
 
 
@@ -743,17 +773,22 @@ def kv4_read(cache: KV4Pages, page_table: torch.Tensor, cu_tokens: torch.Tensor,
     """Cached tokens of the sequences of ``page_table`` [B, W] (int32), from
     ``starts`` [B] on, as packed fp16 (k, v) [total, Hkv, D]; sequence b fills
     rows cu_tokens[b] .. cu_tokens[b + 1] - 1."""
-    pages = _pages(cache)
+    dev, queue = _queue(cache.k_codes, stream)
+    pages = _pages(cache, dev)
     batch, width = page_table.shape
     shape = (total, pages.kv_heads, pages.head_dim)
+    k_ptr = None if k is None else _full(k, _F16, shape, dev)
+    v_ptr = None if v is None else _full(v, _F16, shape, dev)
     if k is None:
         k = _empty(shape, _F16, cache.k_codes.device, stream)
+        k_ptr = k.data_ptr()
     if v is None:
         v = _empty(shape, _F16, cache.k_codes.device, stream)
-    _check(_lib.spinq_kv4_read(pages, _full(page_table, _I32, (batch, width)), batch, width,
-                               None if starts is None else _full(starts, _I32, (batch,)),
-                               _full(cu_tokens, _I32, (batch + 1,)), total, _full(k, _F16, shape),
-                               _full(v, _F16, shape), _queue(stream, k)), "spinq_kv4_read")
+        v_ptr = v.data_ptr()
+    _check(_lib.spinq_kv4_read(pages, _full(page_table, _I32, (batch, width), dev), batch, width,
+                               None if starts is None else _full(starts, _I32, (batch,), dev),
+                               _full(cu_tokens, _I32, (batch + 1,), dev), total, k_ptr, v_ptr, queue),
+           "spinq_kv4_read")
     return k, v
 
 
@@ -765,24 +800,28 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
     tokens); sequence b has rows cu[b] .. cu[b + 1] - 1 (int32 [B + 1])."""
     Tq, Hq, D = q.shape
     Tk, Hkv, _ = k.shape
-    assert k.shape == v.shape and k.shape[2] == D
+    dev, queue = _queue(q, stream)
+    if k.shape != v.shape or k.shape[2] != D:
+        _refuse("queries, keys and values differ in shape")
     batch = cu_q.shape[0] - 1
     if out is None:
         out = _empty((Tq, Hq, D), _F16, q.device, stream)
+        out_ptr = out.data_ptr()
+    else:
+        out_ptr = _full(out, _F16, (Tq, Hq, D), dev)
     ws, need = None, 0
     if workspace is not None:
-        ws, need = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        ws, need = _space(workspace, dev)
     else:
         need = _lib.spinq_prompt_attention_workspace_bytes(batch, max_q, max_k, Hq, Hkv, D)
         if need:
             workspace = _empty(need, _U8, q.device, stream)
             ws = workspace.data_ptr()
-    _check(_lib.spinq_prompt_attention(q.data_ptr(), _token_rows(q), k.data_ptr(), _token_rows(k), v.data_ptr(),
-                                       _token_rows(v), _full(cu_q, _I32, (batch + 1,)),
-                                       _full(cu_k, _I32, (batch + 1,)), batch, Tq, Tk, max_q, max_k, Hq, Hkv, D,
+    _check(_lib.spinq_prompt_attention(q.data_ptr(), _token_rows(q, dev), k.data_ptr(), _token_rows(k, dev),
+                                       v.data_ptr(), _token_rows(v, dev), _full(cu_q, _I32, (batch + 1,), dev),
+                                       _full(cu_k, _I32, (batch + 1,), dev), batch, Tq, Tk, max_q, max_k, Hq, Hkv, D,
                                        int(bool(causal)), D ** -0.5 if scale is None else scale,
-                                       _full(out, _F16, (Tq, Hq, D)), ws, need, _queue(stream, q)),
-           "spinq_prompt_attention")
+                                       out_ptr, ws, need, queue), "spinq_prompt_attention")
     return out
 
 
@@ -794,23 +833,27 @@ def prefix_attention_kv4(q: torch.Tensor, cache: KV4Pages, prefix_table: torch.T
     of ``prefix_table`` that all sequences share, then each sequence's own
     ``lens`` [B] tokens of ``page_table`` [B, W]."""
     B, Hq, D = q.shape
-    pages = _pages(cache)
-    assert D == pages.head_dim
+    dev, queue = _queue(q, stream)
+    pages = _pages(cache, dev)
     width = page_table.shape[1]
-    assert prefix_table.numel() * pages.page_size >= prefix_len
+    if D != pages.head_dim or prefix_table.numel() * pages.page_size < prefix_len:
+        _refuse("queries and pages differ in head_dim, or the prefix's table is too short")
     if out is None:
         out = _empty((B, Hq, D), _F16, q.device, stream)
+        out_ptr = out.data_ptr()
+    else:
+        out_ptr = _full(out, _F16, (B, Hq, D), dev)
     ws, need = None, 0
     if workspace is not None:
-        ws, need = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        ws, need = _space(workspace, dev)
     else:
         need = _lib.spinq_prefix_attention_workspace_bytes(B, prefix_len, width, pages.page_size, Hq, pages.kv_heads, D)
         if need:
             workspace = _empty(need, _U8, q.device, stream)
             ws = workspace.data_ptr()
-    _check(_lib.spinq_prefix_attention_kv4(_full(q, _F16, (B, Hq, D)), pages,
-                                           _full(prefix_table, _I32, prefix_table.shape), prefix_len,
-                                           _full(page_table, _I32, (B, width)), width, _full(lens, _I32, (B,)), B, Hq,
-                                           D ** -0.5 if scale is None else scale, _full(out, _F16, (B, Hq, D)), ws,
-                                           need, _queue(stream, q)), "spinq_prefix_attention_kv4")
+    _check(_lib.spinq_prefix_attention_kv4(_full(q, _F16, (B, Hq, D), dev), pages,
+                                           _full(prefix_table, _I32, prefix_table.shape, dev), prefix_len,
+                                           _full(page_table, _I32, (B, width), dev), width,
+                                           _full(lens, _I32, (B,), dev), B, Hq, D ** -0.5 if scale is None else scale,
+                                           out_ptr, ws, need, queue), "spinq_prefix_attention_kv4")
     return out
