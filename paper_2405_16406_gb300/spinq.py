@@ -762,8 +762,8 @@ def kv4_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cach
                                  _token_rows(v, dev), T, Hq,
                                  None if q_weight is None else _full(q_weight, _F16, (D,), dev),
                                  None if k_weight is None else _full(k_weight, _F16, (D,), dev), eps, rope,
-                                 _KV4_CFG[D] if clip == 1.0 and D in _KV4_CFG else QuantCfg(4, 0, SPINQ_PER_GROUP, D, clip), pages, _full(slots, _I64T, (T,), dev),
-                                 queue), "spinq_kv4_append")
+                                 _KV4_CFG[D] if clip == 1.0 and D in _KV4_CFG else QuantCfg(4, 0, SPINQ_PER_GROUP, D, clip),
+                                 pages, _full(slots, _I64T, (T,), dev), queue), "spinq_kv4_append")
     return q_out
 
 
