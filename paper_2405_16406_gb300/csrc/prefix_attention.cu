@@ -614,17 +614,12 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
 
   // query fragments of head g (k order as the codes come), their sums.  A key
   // code is masked out of its word in place: as fp16 bits the nibbles at bits 0 and 16
-  // are u 2^-24, those at bits 4 and 20 are 16 u 2^-24, both exact operands; the
-  // latter meet query values divided by 16.
-  uint32_t qb[2 * KW][2];
+  // are u 2^-24, those at bits 4 and 20 are 16 u 2^-24, both exact operands; each
+  // kind has a product of its own, the latter's is divided by 16 in fp32.
+  uint32_t qb[KW][4];
   float qs = 0.f;
   {
     const __half* qh = reinterpret_cast<const __half*>(a.q) + (row0 + (g < heads ? g : 0)) * D + c * (D / 4);
-    const __half2 sixteenth = __float2half2_rn(0.0625f);
-    auto over16 = [&](uint32_t x) {
-      const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&x), sixteenth);
-      return *reinterpret_cast<const uint32_t*>(&h);
-    };
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
       uint4 x = __ldg(reinterpret_cast<const uint4*>(qh + 8 * w));
@@ -635,10 +630,10 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&xs[q]));
         qs += f.x + f.y;
       }
-      qb[2 * w][0] = __byte_perm(x.x, x.z, 0x5410);
-      qb[2 * w][1] = over16(__byte_perm(x.x, x.z, 0x7632));
-      qb[2 * w + 1][0] = __byte_perm(x.y, x.w, 0x5410);
-      qb[2 * w + 1][1] = over16(__byte_perm(x.y, x.w, 0x7632));
+      qb[w][0] = __byte_perm(x.x, x.z, 0x5410);
+      qb[w][1] = __byte_perm(x.y, x.w, 0x5410);
+      qb[w][2] = __byte_perm(x.x, x.z, 0x7632);
+      qb[w][3] = __byte_perm(x.y, x.w, 0x7632);
     }
     qs += __shfl_xor_sync(0xffffffffu, qs, 1);
     qs += __shfl_xor_sync(0xffffffffu, qs, 2);
@@ -712,14 +707,14 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
         x.v[q][0] = *reinterpret_cast<const uint32_t*>(vr);
       }
     }
-    float sa[4] = {0.f, 0.f, 0.f, 0.f}, sc2[4] = {0.f, 0.f, 0.f, 0.f};
+    float sa[4] = {0.f, 0.f, 0.f, 0.f}, s16[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
       const uint32_t x0 = x.k[0][w], x1 = x.k[1][w], y0 = x0 >> 8, y1 = x1 >> 8;
-      const uint32_t a0[4] = {x0 & 0x000F000Fu, x1 & 0x000F000Fu, x0 & 0x00F000F0u, x1 & 0x00F000F0u};
-      const uint32_t a1[4] = {y0 & 0x000F000Fu, y1 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x00F000F0u};
-      mma_16816_f16_f32_acc(sa, a0, qb[2 * w][0], qb[2 * w][1]);
-      mma_16816_f16_f32_acc(sc2, a1, qb[2 * w + 1][0], qb[2 * w + 1][1]);
+      const uint32_t a0[4] = {x0 & 0x000F000Fu, x1 & 0x000F000Fu, y0 & 0x000F000Fu, y1 & 0x000F000Fu};
+      const uint32_t a1[4] = {x0 & 0x00F000F0u, x1 & 0x00F000F0u, y0 & 0x00F000F0u, y1 & 0x00F000F0u};
+      mma_16816_f16_f32_acc(sa, a0, qb[w][0], qb[w][1]);
+      mma_16816_f16_f32_acc(s16, a1, qb[w][2], qb[w][3]);
     }
     // s + log2 alpha' (base 2) of tokens g, g + 8 for heads 2c, 2c + 1; tokens past the
     // chunk (their slots may hold anything) get -inf and factors 0
@@ -732,7 +727,7 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
       rv[h] = __frcp_rn(va);
       vz[h] = rv[h] * fmaf(8.f, va, x.sc[h].w);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) t[h][e] = fmaf(ka, sa[2 * h + e] + sc2[2 * h + e], fmaf(x.sc[h].y, qsk[e], la));
+      for (int e = 0; e < 2; ++e) t[h][e] = fmaf(ka, fmaf(0.0625f, s16[2 * h + e], sa[2 * h + e]), fmaf(x.sc[h].y, qsk[e], la));
     }
     if (left < 16) {
 #pragma unroll
