@@ -267,7 +267,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv4_append_kernel(AppendArg
       continue;
     }
 
-    // ---- Eq. 1 over the row, into its slot
+    // ---- Eq. 1 over the row, into its slot.  A value that is not a number makes the extremes
+    // and with them the row's scales NaN: the cache does not turn it into a number.
     float hi = -FLT_MAX, lo = FLT_MAX;
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -275,13 +276,14 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv4_append_kernel(AppendArg
       for (int i = 0; i < 8; ++i) {
         float p, q;
         f2_split(y[v][i], p, q);
-        asm("max.f32 %0, %0, %1, %2;\n" : "+f"(hi) : "f"(p), "f"(q));
-        asm("min.f32 %0, %0, %1, %2;\n" : "+f"(lo) : "f"(p), "f"(q));
+        asm("max.NaN.f32 %0, %0, %1, %2;\n" : "+f"(hi) : "f"(p), "f"(q));
+        asm("min.NaN.f32 %0, %0, %1, %2;\n" : "+f"(lo) : "f"(p), "f"(q));
       }
 #pragma unroll
     for (int b = 1; b < 4; b <<= 1) {
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, b));
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, b));
+      const float oh = __shfl_xor_sync(0xffffffffu, hi, b), ol = __shfl_xor_sync(0xffffffffu, lo, b);
+      asm("max.NaN.f32 %0, %0, %1;\n" : "+f"(hi) : "f"(oh));
+      asm("min.NaN.f32 %0, %0, %1;\n" : "+f"(lo) : "f"(ol));
     }
     if (CLAMP) {
       hi *= a.clip;
