@@ -482,7 +482,8 @@ spinq_status spinq_kv4_read(const spinq_kv4_pages* cache, const int32_t* page_ta
  *          elements apart as in spinq_kv4_append;  out [total_q][Hq][D] fp16,
  *          not overlapping the inputs.
  *   cu_q, cu_k [batch + 1] int32 (device), ascending from 0: sequence b has
- *          rows cu[b] .. cu[b+1] - 1 (rows of out after the last are not written).
+ *          rows cu[b] .. cu[b+1] - 1 (rows of out after the last are not written;
+ *          offsets outside [0, total] are clamped).
  *   max_q, max_k  no less than any sequence's lq and lk (host numbers: the
  *          launch is planned with them).
  *   workspace  spinq_prompt_attention_workspace_bytes(...) bytes, 16-byte

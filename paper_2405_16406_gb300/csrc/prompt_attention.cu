@@ -286,8 +286,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         // the last queries first, over all heads and sequences
         const uint32_t heads = (uint32_t)(a.Hkv * a.batch), tile = id / heads, hb = id - tile * heads;
         const int b = (int)(hb / (uint32_t)a.Hkv), t0 = (a.tiles - 1 - (int)tile) * 2 * a.tpt;
-        const int64_t q0 = __ldg(a.cu_q + b), q1 = min((int64_t)__ldg(a.cu_q + b + 1), a.total_q);
-        const int64_t k0 = __ldg(a.cu_k + b), k1 = min((int64_t)__ldg(a.cu_k + b + 1), a.total_k);
+        // (offsets outside the rows are clamped: nothing is written or read out of range)
+        const int64_t q0 = max(0, __ldg(a.cu_q + b)), q1 = min((int64_t)__ldg(a.cu_q + b + 1), a.total_q);
+        const int64_t k0 = max(0, __ldg(a.cu_k + b)), k1 = min((int64_t)__ldg(a.cu_k + b + 1), a.total_k);
         if (!more || q0 + t0 < q1) {
           if (it >= 2 && !attn_wait(&taken[it & 1], (uint32_t)((it >> 1) - 1) & 1u, abort_flag, g_prompt_wait_ns)) break;
           volatile PromptItem& x = const_cast<volatile PromptItem&>(items[it & 1]);
