@@ -484,10 +484,10 @@ spinq_status spinq_kv4_read(const spinq_kv4_pages* cache, const int32_t* page_ta
  *   cu_q, cu_k [batch + 1] int32 (device), ascending from 0: sequence b has
  *          rows cu[b] .. cu[b+1] - 1 (rows of out after the last are not written;
  *          offsets outside [0, total] are clamped).
- *   max_q, max_k  no less than any sequence's lq and lk (host numbers: the
- *          launch is planned with them).
- *   workspace  spinq_prompt_attention_workspace_bytes(...) bytes, 16-byte
- *          aligned (may be NULL when that is 0; no zeroing needed).
+ *   max_q, max_k  no less than any sequence's lq and lk (host numbers; the
+ *          launch is planned with max_q, max_k is only checked).
+ *   workspace  spinq_prompt_attention_workspace_bytes(...) bytes: 0 for every
+ *          argument, so that it may be NULL; what is given is not used.
  *   Keys and values of a sequence must be finite; rows of other sequences
  *   and rows outside every sequence never reach a result.
  *   Supported: D = 64 or 128, Hq / Hkv whole and at most 128.  Scores and sums

@@ -536,8 +536,6 @@ cudaError_t launch_t(const PromptArgs& a, cudaStream_t stream) {
 
 cudaError_t set_wait_limit_prompt(uint64_t ns) { return cudaMemcpyToSymbol(g_prompt_wait_ns, &ns, sizeof(ns)); }
 
-int64_t prompt_attention_workspace(const PromptArgs&) { return 0; }
-
 cudaError_t launch_prompt_attention(const PromptArgs& a, cudaStream_t stream) {
   if (a.D == 128) return launch_t<128>(a, stream);
   if (a.D == 64) return launch_t<64>(a, stream);

@@ -513,28 +513,13 @@ spinq_status spinq_kv4_read(const spinq_kv4_pages* cache, const int32_t* page_ta
   return from_cuda(launch_kv4_read(a, static_cast<cudaStream_t>(stream)));
 }
 
-static PromptArgs prompt_shape(int64_t batch, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv, int64_t D) {
-  PromptArgs a{};
-  a.batch = batch;
-  a.max_q = max_q;
-  a.max_k = max_k;
-  a.Hq = Hq;
-  a.Hkv = Hkv;
-  a.D = (int)D;
-  return a;
-}
-
-int64_t spinq_prompt_attention_workspace_bytes(int64_t batch, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv,
-                                               int64_t D) {
-  if (batch <= 0 || max_q <= 0 || max_k < 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || (D != 64 && D != 128)) return 0;
-  return prompt_attention_workspace(prompt_shape(batch, max_q, max_k, Hq, Hkv, D));
-}
+// The kernel keeps everything on the chip.
+int64_t spinq_prompt_attention_workspace_bytes(int64_t, int64_t, int64_t, int64_t, int64_t, int64_t) { return 0; }
 
 spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                                     const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t total_q,
                                     int64_t total_k, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv, int64_t D,
-                                    int32_t causal, float softmax_scale, void* out, void* workspace,
-                                    int64_t workspace_bytes, void* stream) {
+                                    int32_t causal, float softmax_scale, void* out, void*, int64_t, void* stream) {
   if (batch < 0 || total_q < 0 || total_k < 0 || max_q < 0 || max_k < 0 || Hq <= 0 || Hkv <= 0 || D <= 0)
     return SPINQ_EINVAL;
   if (Hq % Hkv != 0 || (causal != 0 && causal != 1) || !std::isfinite(softmax_scale)) return SPINQ_EINVAL;
@@ -548,9 +533,12 @@ spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, i
       max_k > INT32_MAX)
     return SPINQ_EUNSUPPORTED;
   if (total_q == 0) return SPINQ_OK;
-  PromptArgs a = prompt_shape(batch, max_q, max_k, Hq, Hkv, D);
-  const int64_t need = prompt_attention_workspace(a);
-  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return SPINQ_EINVAL;
+  PromptArgs a{};
+  a.batch = batch;
+  a.max_q = max_q;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.D = (int)D;
   a.q = q;
   a.k = k;
   a.v = v;
@@ -564,7 +552,6 @@ spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, i
   a.causal = causal != 0;
   a.scale = softmax_scale;
   a.out = out;
-  a.workspace = workspace;
   return from_cuda(launch_prompt_attention(a, static_cast<cudaStream_t>(stream)));
 }
 

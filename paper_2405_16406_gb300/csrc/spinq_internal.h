@@ -151,15 +151,12 @@ struct PromptArgs {
   int64_t ldq, ldk, ldv;
   const int32_t* cu_q;    // [batch + 1]
   const int32_t* cu_k;
-  int64_t batch, total_q, total_k, max_q, max_k, Hq, Hkv;
+  int64_t batch, total_q, total_k, max_q, Hq, Hkv;
   int D;
   bool causal;
   float scale;
   void* out;              // fp16 [total_q][Hq][D]
-  void* workspace;
 };
-// Workspace bytes of the call (pointers unused).
-int64_t prompt_attention_workspace(const PromptArgs& a);
 cudaError_t launch_prompt_attention(const PromptArgs& a, cudaStream_t stream);
 
 struct PrefixArgs {

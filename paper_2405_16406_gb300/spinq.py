@@ -809,19 +809,12 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: to
         out_ptr = out.data_ptr()
     else:
         out_ptr = _full(out, _F16, (Tq, Hq, D), dev)
-    ws, need = None, 0
-    if workspace is not None:
-        ws, need = _space(workspace, dev)
-    else:
-        need = _lib.spinq_prompt_attention_workspace_bytes(batch, max_q, max_k, Hq, Hkv, D)
-        if need:
-            workspace = _empty(need, _U8, q.device, stream)
-            ws = workspace.data_ptr()
+    ws, size = (None, 0) if workspace is None else _space(workspace, dev)
     _check(_lib.spinq_prompt_attention(q.data_ptr(), _token_rows(q, dev), k.data_ptr(), _token_rows(k, dev),
                                        v.data_ptr(), _token_rows(v, dev), _full(cu_q, _I32, (batch + 1,), dev),
                                        _full(cu_k, _I32, (batch + 1,), dev), batch, Tq, Tk, max_q, max_k, Hq, Hkv, D,
                                        int(bool(causal)), D ** -0.5 if scale is None else scale,
-                                       out_ptr, ws, need, queue), "spinq_prompt_attention")
+                                       out_ptr, ws, size, queue), "spinq_prompt_attention")
     return out
 
 

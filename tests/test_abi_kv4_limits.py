@@ -35,3 +35,8 @@ def test_too_many_query_heads_for_a_kv_head_are_refused(S):
     with pytest.raises(S.SpinqError) as e:
         S.prefix_attention_kv4(torch.zeros((1, 256, 128), dtype=torch.float16, device="cuda"), cache, one[0], 16, one, one[0])
     assert e.value.status == S.SPINQ_EUNSUPPORTED
+
+
+def test_prompt_attention_wants_no_workspace(S):
+    for shape in ((1, 1, 1, 8, 8, 64), (16, 4096, 100000, 32, 8, 128), (1, 0, 0, 0, 0, 0)):
+        assert S.spinq_prompt_attention_workspace_bytes(*shape) == 0
