@@ -9,7 +9,7 @@
 // weights are those that the codes have in the output, w = 2^(s + log2 alpha' - M)
 // with M the running maximum of s + log2 alpha' (base 2):
 //   s_t = (scale alpha_t) (q . (u_t - 8)) + scale (beta_t + 8 alpha_t) sum_d q_d
-//   o   = [ sum_t w_t (u'_t - 8) + sum_t w_t (beta'_t + 8 alpha'_t) / alpha'_t ] / sum_t w_t / alpha'_t
+//   o   = [ sum_t w_t (u'_t - 8) + sum_t w_t (8 + beta'_t / alpha'_t) ] / sum_t w_t / alpha'_t
 // so the only rounding before the output is that of w to fp16, on codes about
 // their middle (the two other sums stay in fp32); the own tokens and a prefix with few
 // sequences carry w as two fp16 parts.  The token that weighs most has w near 1 (M moves
@@ -51,6 +51,16 @@ constexpr int kPrefixSite = 32;    // wait site recorded on a time-out
 // above 2^-126 beside any alpha' up to 2^80.  (A scale that is not a number stays one.)
 constexpr float kMinValueScale = 9.094947017729282e-13f;
 __device__ __forceinline__ float value_scale(float x) { return x < kMinValueScale ? kMinValueScale : x; }
+__device__ __forceinline__ float log2_of_scale(float x) {   // within 2^-22; no subnormal numbers come here
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float one_over_scale(float x) {   // within 2^-23
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // Parts of the result: part p of row (b, head) is M and sum of w / alpha' at ml[p][row] and
 // the weighted sum of the values at o[p][row][D] (not written where the sum is 0).
@@ -218,10 +228,10 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
       float* col = reinterpret_cast<float*>(cols) + (t >> 1) * 4 + (t & 1);
       col[0] = in ? p.scale_log2 * sc.x : 0.f;
       col[2] = in ? p.scale_log2 * fmaf(8.f, sc.x, sc.y) : 0.f;
-      const float va = in ? value_scale(sc.z) : 1.f, rv = __frcp_rn(va);
+      const float va = in ? value_scale(sc.z) : 1.f, rv = one_over_scale(va);
       col[C::COL_V / 4] = rv;
-      col[C::COL_V / 4 + 2] = in ? rv * fmaf(8.f, va, sc.w) : 0.f;
-      reinterpret_cast<float*>(cols + C::COL_LOG)[t] = __log2f(va);
+      col[C::COL_V / 4 + 2] = in ? fmaf(rv, sc.w, 8.f) : 0.f;
+      reinterpret_cast<float*>(cols + C::COL_LOG)[t] = log2_of_scale(va);
       __syncwarp();
       if (lane == 0) mbar_arrive(&cbar[j % NCOL]);
       expand(kw, n);
@@ -723,9 +733,9 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_tokens_kernel(const Pre
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float ka = ks24 * x.sc[h].x;
-      const float va = value_scale(x.sc[h].z), la = __log2f(va);
-      rv[h] = __frcp_rn(va);
-      vz[h] = rv[h] * fmaf(8.f, va, x.sc[h].w);
+      const float va = value_scale(x.sc[h].z), la = log2_of_scale(va);
+      rv[h] = one_over_scale(va);
+      vz[h] = fmaf(rv[h], x.sc[h].w, 8.f);
 #pragma unroll
       for (int e = 0; e < 2; ++e) t[h][e] = fmaf(ka, fmaf(0.0625f, s16[2 * h + e], sa[2 * h + e]), fmaf(x.sc[h].y, qsk[e], la));
     }
