@@ -231,7 +231,9 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
       const float va = in ? value_scale(sc.z) : 1.f, rv = one_over_scale(va);
       col[C::COL_V / 4] = rv;
       col[C::COL_V / 4 + 2] = in ? fmaf(rv, sc.w, 8.f) : 0.f;
-      reinterpret_cast<float*>(cols + C::COL_LOG)[t] = log2_of_scale(va);
+      // (in the order of the lanes: pairs c of groups 2 k and 2 k + 1 of eight tokens in one load)
+      const int to = (t & 64) + (t >> 4 & 3) * 16 + (t >> 1 & 3) * 4 + (t >> 3 & 1) * 2 + (t & 1);
+      reinterpret_cast<float*>(cols + C::COL_LOG)[to] = log2_of_scale(va);
       __syncwarp();
       if (lane == 0) mbar_arrive(&cbar[j % NCOL]);
       expand(kw, n);
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
           const uint8_t* cols = smem + C::OFF_COL + (j % NCOL) * C::COL;
           const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(cols + hf * 512) + c;
           const ulonglong2* fv = reinterpret_cast<const ulonglong2*>(cols + C::COL_V + hf * 512) + c;
-          const unsigned long long* la = reinterpret_cast<const unsigned long long*>(cols + C::COL_LOG + hf * 256) + c;
+          const ulonglong2* la = reinterpret_cast<const ulonglong2*>(cols + C::COL_LOG + hf * 256) + c;
           ulonglong2 f[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) f[k] = ab[4 * k];
@@ -385,8 +387,8 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
           tmem_ld_wait_all<32>(s[1]);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const ulonglong2 w = f[k];
-            const F2 lg = F2{la[4 * k]};
+            const ulonglong2 w = f[k], l2 = la[4 * (k >> 1)];
+            const F2 lg = F2{k & 1 ? l2.y : l2.x};
             f[k] = fv[4 * k];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
