@@ -401,7 +401,7 @@ spinq_status spinq_decode_attention_kv4(const void* q, const uint8_t* k_codes, c
  *            stores it);
  *   scales   [num_pages][kv_heads][page_size][4] fp32, 16-byte aligned:
  *            (K alpha, K beta, V alpha, V beta) of the token and head, alpha >= 0
-            (Eq. 1's step; a V alpha below 2^-40 counts as 2^-40 in attention).
+ *            (Eq. 1's step; a V alpha below 2^-40 counts as 2^-40 in attention).
  * Slot number s of the cache is slot s % page_size of page s / page_size.
  * page_size: 16, 32, 64, 128 or 256.  head_dim: 64 or 128.  A slot that no
  * call has written may hold anything (also values that are not finite): no
@@ -450,6 +450,9 @@ typedef struct {
  *   kvq    bits = 4, symmetric = 0, granularity = SPINQ_PER_GROUP, group_size = D.
  *   slots  [T] int64 slot numbers, distinct; a token whose number is outside
  *          the cache (e.g. -1, padding) is not written, its q_out is.
+ *   A row with a value that is not a number is cached with NaN scales.  Codes are
+ *   Eq. 1 in fp32; at the middle of two they may differ by one from those
+ *   that spinq_rotate_quant_kv writes.
  *   Supported: T times the larger head count below 2^31.
  */
 spinq_status spinq_kv4_append(const void* q, int64_t ldq, void* q_out, const void* k, int64_t ldk, const void* v,
@@ -515,6 +518,11 @@ spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, i
  *   workspace  spinq_prefix_attention_workspace_bytes(...) bytes, 16-byte
  *          aligned (no zeroing needed); 0 where the call refuses the sizes.
  *   Supported: Hq / kv_heads whole and at most 128, Hq and B at most 65535.
+ *   Scores and sums in fp32.  For the product with V's codes the weights p
+ *   alpha are fp16: one number for the prefix of more than floor(128 / (Hq /
+ *   kv_heads)) sequences, two parts (2^-22) else and for the own tokens.  That
+ *   limit and the parts that the prefix is split into depend on B, so a sequence's
+ *   output may change in its last bits when the batch does.
  */
 int64_t spinq_prefix_attention_workspace_bytes(int64_t B, int64_t prefix_len, int64_t table_width, int32_t page_size,
                                                int64_t Hq, int64_t Hkv, int64_t D);

@@ -24,13 +24,15 @@
 //     the 5th-generation tensor core as in the prompt kernel; four warps
 //     expand the pages' codes into the operand tiles.
 //     Bound: the softmax.  128 tokens for both tiles are 2052 cycles of MMAs and
-//     about 5900 in all: two warps per scheduler, whose packed fp32 work is about 3300, and
-//     waits between.  32768 tokens, 256 sequences, 32 / 8 heads, D 128, on 128 SMs: 204
-//     us with an empty join, 0.67 PFLOP/s.
+//     about 6000 in all: two warps per scheduler, whose packed fp32 work is about 2800, and
+//     waits between.  32768 tokens, 256 sequences, 32 / 8 heads, D 128, on 128 SMs: 209
+//     us with an empty join, 0.66 PFLOP/s.
 //   own_tokens_kernel  each sequence's own tokens, beside the prefix kernel where it
 //     leaves SMs: G heads are too few rows for those tiles, so mma.sync with the
-//     tokens on the M side, codes copied as they are.  Bound: the cache's bytes (256
-//     sequences of 523 tokens on average, 154 MB: 48 us alone, 3.2 TB/s).  Where one CTA has all of a
+//     tokens on the M side, codes copied as they are.  Bound: latency (256 sequences of
+//     523 tokens on average, 154 MB: 47 us alone, 3.3 TB/s, half of the copy rate; issue is at
+//     36 %): a warp has 8 steps there, behind a page look-up and a filled ring and before a join.
+//     8 sequences of 30000 tokens, 277 MB: 73 us, 3.8 TB/s.  Where one CTA has all of a
 //     sequence's own tokens it may also join them with the prefix's parts.
 //   prefix_combine_kernel  else joins the parts (maximum, sum, o) in a fixed order.
 #include <cuda_fp16.h>
@@ -164,6 +166,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = 0;   // all 512 columns are this CTA's: they start at column 0
+  // In this order: own_tokens_kernel starts at the trigger and relies on the work before this kernel being done.
   pdl_wait();
   pdl_trigger();
 
@@ -941,7 +944,7 @@ int prefix_splits(const PrefixArgs& a) {
   int64_t n = device_sm_count() / (row_blocks(a) * a.Hkv);   // one CTA per SM
   n = n < 1 ? 1 : (n > kMaxSplits ? kMaxSplits : n);
   // no more than the longest part's length asks for: fewer parts to write and join, and
-  // SMs for the own tokens (8191 x 64, 64 tiles: 34.4 us in 19 parts, 33.4 us in 16)
+  // SMs for the own tokens (8191 x 64, 64 tiles: 34.4 us in 19 parts where 16 took 33.4)
   const int64_t longest = (tiles + n - 1) / n;
   return (int)((tiles + longest - 1) / longest);
 }
@@ -990,10 +993,10 @@ cudaError_t launch_t(const PrefixArgs& a, cudaStream_t stream) {
     int per_sm = 0;
     // A few rows may be carried by few weights, whose rounding then nearly doubles the
     // error of the whole output; many rows average it (0.00028 against 0.00021 of the
-    // output's own rounding).  So one tile of rows takes second parts (a row carried by few
-    // weights: 0.00031 with one part, 0.00021 with two; 1000 x 4: 9.8 and 10.3 us, 24000 x
-    // 32: 38.9 and 44.8); the softmax of two tiles bounds its kernel and has no
-    // registers for them (52 bytes of spills).
+    // output's own rounding).  So one tile of rows takes second parts (1000 x 4: 9.6 us
+    // and 0.00022 with one part, 10.1 us and 0.00021 with two; 24000 x 32: 32.9 us and 0.00027, 38.8 us and
+    // 0.00021); two tiles do not, whose softmax bounds their kernel (8191 x 64: 34.2 us with one
+    // part, 37.2 with two; 32768 x 256: 227 and 276 us, 0.00028 and 0.00022).
     auto kernel = a.B <= p.tps ? prefix_tc_kernel<D, true> : prefix_tc_kernel<D, false>;
     e = prepare_launch_tmem(kernel, kPrefixThreads, PrefixCfg<D>::BYTES, 512, &per_sm);
     if (e != cudaSuccess) return e;

@@ -23,9 +23,13 @@
 // 4096 395 us against 386; with a block per item 4 x 4096 took 431).  Blocks
 // past a sequence's end are passed over; a grid that counts only the items there are took
 // 103 us on the ragged batch, whose long items it starts later.  4 x 4096, 32 / 8
-// heads, D 128: 386 us, 1.42 PFLOP/s, 74 % of the measured rate of a large matrix
-// product.  The softmax bounds it: a step of 128 keys for both tiles is 2052 cycles of
-// MMAs and about 3400 in all.  Warp roles:
+// heads, D 128: 386 us run again and again on one state, 420 us with cold inputs (1.31
+// PFLOP/s, 68 % of the measured rate of a large matrix product).  The softmax bounds
+// it: a step of 128 keys for both tiles is 2052 cycles of MMAs and about 3400 in all.
+// P in one fp16 part is a choice: the output's error against 64 bits is 0.00022 to 0.00029 where
+// its own rounding alone is 0.00021 (0.00031 in calls of a few rows).  Two parts, the second in
+// the rows that tiles of 64 leave idle, made those calls exact to the output's rounding
+// and 15 to 25 % slower (1 query behind 2168 tokens 26 and 31 us, 64 behind 32768 355 and 430).  Warp roles:
 //  * warps 0-3 and 4-7: softmax of tile 0 and 1, one row per thread: running
 //    maximum (base 2, moved only by more than 2^8, when the row's O is
 //    rescaled) and sum in fp32 registers;

@@ -307,7 +307,7 @@ struct Fp8GemmArgs {
 // cannot be encoded.
 cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, cudaStream_t stream);
 
-// Launches of the Paley rotate+quant, W4A4 prefill, FP8 GEMM and prompt attention kernels still
+// Launches of the Paley rotate+quant, W4A4 prefill, FP8 GEMM, prompt and prefix attention kernels still
 // to issue no input copies (spinq_debug_stall_launches); take_debug_stall()
 // consumes one.
 bool take_debug_stall();
