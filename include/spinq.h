@@ -532,6 +532,119 @@ spinq_status spinq_prefix_attention_kv4(const void* q, const spinq_kv4_pages* ca
                                         void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
+ * spinq_kv4_plan -- the bookkeeping of one step of the paged cache, from the
+ * requests' lengths: sequence b drops its last drop[b] tokens (all of them, where
+ * it has no more), then add[b] tokens are to come behind the rest.  Pages that no
+ * token is left on go back to the free pages, new tokens get theirs from there:
+ *   start = max(lens[b] - drop[b], 0);  lens[b] <- start + add[b];
+ *   token i of the sequence: row t = cu_tokens[b] + i, position
+ *   start + i + position_offset, slot of token start + i of its row of page_table.
+ * The free pages are a stack, free_pages[0 .. *free_count - 1], freed pages on
+ * top in such order that a sequence which drops and adds gets its own back.
+ * Sequences are served in their order; where the pages run out, the first that is
+ * not to be had in full and every later one that needs a page are refused, as is one
+ * longer than its row of page_table or whose rows end past `total`: lens[b] <- start,
+ * its slots are -1 (spinq_kv4_append passes over them), granted[b] = 0.
+ *   lens       [batch] int32, in and out (clamped to the row's capacity);
+ *   drop, add  [batch] int32, or NULL (none); below 0 counts as 0;
+ *   page_table [batch][table_width] int32, in and out: entries past a sequence's
+ *              pages are left as they are;
+ *   free_pages [free_capacity] int32, free_count [1] int32, in and out; pages that
+ *              the list has no room for are lost (no list as long as the cache is full);
+ *   depths     [total] int32 or NULL: position start + depths[t] + position_offset
+ *              in place of i (a drafted tree's nodes);
+ *   cu_tokens  [batch + 1] int32 (at most total);  positions [total] int32, slots
+ *              [total] int64: 0 and -1 in rows behind the last token;
+ *   granted    [batch] int32 or NULL.
+ *   All of it stays on the GPU, so a captured step replays with new lengths.
+ *   Arrays must not overlap.  page_size 16, 32, 64, 128 or 256; batch at most 4096.
+ */
+spinq_status spinq_kv4_plan(int32_t* lens, const int32_t* drop, const int32_t* add, int64_t batch,
+                            int32_t* page_table, int64_t table_width, int32_t page_size, int32_t* free_pages,
+                            int32_t* free_count, int64_t free_capacity, const int32_t* depths,
+                            int64_t position_offset, int64_t total, int32_t* cu_tokens, int32_t* positions,
+                            int64_t* slots, int32_t* granted, void* stream);
+
+/*
+ * spinq_kv4_keep -- the accepted path of each drafted tree moves together: token
+ * starts[b] + path[b][i] of sequence b is moved to starts[b] + i, i < counts[b],
+ * codes and scales of K and V as they are (a node's rotation is that of its depth,
+ * which is its place on the path).
+ *   page_table [batch][table_width], starts, counts [batch], path
+ *          [batch][path_width] int32 (device); counts are clamped to [0, path_width].
+ *   A path ascends (path[b][i] >= i, each larger than the one before: a parent comes
+ *   before its node); where one does not, which of its tokens arrive is not
+ *   specified.  A token outside the page table or the cache is not moved.
+ *   Supported: batch * kv_heads < 2^31.
+ */
+spinq_status spinq_kv4_keep(const spinq_kv4_pages* cache, const int32_t* page_table, int64_t batch,
+                            int64_t table_width, const int32_t* starts, const int32_t* path, int64_t path_width,
+                            const int32_t* counts, void* stream);
+
+/*
+ * spinq_window_prompt_attention -- spinq_prompt_attention (causal) where a query
+ * sees the last positions and a few first tokens only: key j of a query at position
+ * p = i + lk - lq is seen if j <= p and (p - j < window or j < sinks).
+ *   window >= 1, sinks >= 0.  Other arguments, layouts and limits as
+ *   spinq_prompt_attention; tiles of keys that no query of a tile sees are not read.
+ */
+spinq_status spinq_window_prompt_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                                           int64_t ldv, const int32_t* cu_q, const int32_t* cu_k, int64_t batch,
+                                           int64_t total_q, int64_t total_k, int64_t max_q, int64_t max_k, int64_t Hq,
+                                           int64_t Hkv, int64_t D, int64_t window, int64_t sinks, float softmax_scale,
+                                           void* out, void* stream);
+
+/*
+ * spinq_tree_attention_kv4 -- attention of the last tokens of each sequence, a
+ * drafted tree that is to be verified, over the paged 4-bit cache.  Sequence b has
+ * lens[b] tokens in the cache, the last nq = cu_q[b+1] - cu_q[b] of them its
+ * queries' own (appended before the call).  Query i sees the context (the tokens
+ * before those nq), its ancestors, and itself:
+ *   o_i = sum_j softmax_j(softmax_scale q_i . k_j) v_j,
+ * K and V as in spinq_decode_attention_kv4.  With window >= 1 it sees only those of
+ * them that are less than `window` positions before its own or below position
+ * `sinks`; a context token's position is its place, a query's the context's length plus
+ * its depth.  A query that sees no key (lens[b] below nq) gives zeros.
+ *   q, out  [total_q][Hq][D] fp16, q rotated by R3 (spinq_kv4_append's q_out);
+ *           rows of out behind the last sequence are not written;
+ *   page_table [B][table_width] int32, lens [B] int32 (device), each in
+ *           [0, table_width * page_size] (others are clamped); entries of pages that
+ *           no query sees may be anything (pages given back);
+ *   cu_q    [B + 1] int32 (device) ascending from 0;
+ *   max_q   no less than any sequence's number of queries, at most 128;
+ *   parents [total_q] int32: the number, within the sequence, of the query's parent,
+ *           which comes before it; -1 (or any other number) for one that follows the
+ *           context.  NULL: each query's parent is the one before it (a chain).
+ *   window  0: none.
+ *   workspace  spinq_tree_attention_workspace_bytes(...) bytes, 16-byte aligned (no
+ *           zeroing needed); 0 where the call refuses the sizes.
+ *   Supported: Hq / kv_heads whole and at most 128, Hq and B at most 65535.
+ *   Scores and sums in fp32, the weights p alpha in two fp16 parts (2^-22).  How the
+ *   keys are split over the GPU depends on the lengths of the whole batch, so a sequence's
+ *   output may change in its last bits when the batch does.
+ */
+int64_t spinq_tree_attention_workspace_bytes(int64_t B, int64_t max_q, int64_t table_width, int32_t page_size,
+                                             int64_t Hq, int64_t Hkv, int64_t D);
+spinq_status spinq_tree_attention_kv4(const void* q, const spinq_kv4_pages* cache, const int32_t* page_table,
+                                      int64_t table_width, const int32_t* lens, const int32_t* cu_q,
+                                      const int32_t* parents, int64_t B, int64_t total_q, int64_t max_q, int64_t Hq,
+                                      int64_t window, int64_t sinks, float softmax_scale, void* out, void* workspace,
+                                      int64_t workspace_bytes, void* stream);
+
+/*
+ * spinq_window_attention_kv4 -- decode attention of one query per (sequence, query
+ * head), the sequence's last token, over the last `window` of its lens[b] tokens and
+ * the first `sinks` of the paged 4-bit cache (window 0: all of them).
+ *   q, out  [B][Hq][D] fp16, q rotated by R3.  A sequence without tokens gives zeros.
+ *   workspace  spinq_tree_attention_workspace_bytes(B, 1, ...) bytes.
+ *   Other arguments, limits and arithmetic as spinq_tree_attention_kv4.
+ */
+spinq_status spinq_window_attention_kv4(const void* q, const spinq_kv4_pages* cache, const int32_t* page_table,
+                                        int64_t table_width, const int32_t* lens, int64_t B, int64_t Hq,
+                                        int64_t window, int64_t sinks, float softmax_scale, void* out,
+                                        void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
  * 8-bit variants (main results table, W4A8 rows "4-8-x"; appendix "Latency
  * measurement on GPU": W-fp8-A-fp8 with the dequantization fused into the
  * GEMM epilogue).  They share the rotation convention above and run on the

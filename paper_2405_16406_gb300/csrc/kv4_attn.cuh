@@ -1,0 +1,68 @@
+// kv4_attn.cuh -- what the attention kernels on the paged 4-bit cache share:
+// value scales in the weights, codes as fp16 operands, and a warp's ring of
+// 16-token steps.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "spinq_device.cuh"
+
+namespace spinq {
+
+// A row of values with a smaller scale (equal values have 0) counts as one of this scale, 2^-40:
+// 15 steps of it, 2^-36, are nothing beside fp16's smallest step, 2^-24, and w stays
+// above 2^-126 beside any alpha' up to 2^80.  (A scale that is not a number stays one.)
+constexpr float kMinValueScale = 9.094947017729282e-13f;
+__device__ __forceinline__ float value_scale(float x) { return x < kMinValueScale ? kMinValueScale : x; }
+__device__ __forceinline__ float log2_of_scale(float x) {   // within 2^-22; no subnormal numbers come here
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float one_over_scale(float x) {   // within 2^-23
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Eight codes of a word as fp16 pairs u - 8: (0, 4), (1, 5), (2, 6), (3, 7).
+__device__ __forceinline__ uint32_t code_pair(uint32_t x) {   // nibbles at bits 0 and 16
+  const uint32_t m = (x & 0x000F000Fu) | 0x64006400u;         // 1024 + u
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x6408)));   // 1032
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint4 code_pairs(uint32_t x) {
+  return make_uint4(code_pair(x), code_pair(x >> 4), code_pair(x >> 8), code_pair(x >> 12));
+}
+
+__device__ __forceinline__ uint32_t own_transpose(uint32_t x) {   // 8x8 fp16 transpose over the warp
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+  return y;
+}
+
+constexpr int kOwnStages = 4;
+
+__device__ __forceinline__ void own_copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+
+// A warp's ring of stages: 16 tokens' key rows, value rows (D/2 bytes each) and
+// scales.  Key rows lie as in the page (a fragment load covers eight whole rows);
+// a fragment load of the values takes 8 or 4 bytes of rows 0, 2, 4, 6 (or 1, 3,
+// ..), so their 16-byte pieces are moved about to fall in different banks.
+template <int D>
+struct OwnRing {
+  static constexpr int KB = 16 * (D / 2), STAGE = 2 * KB + 256, WARP = kOwnStages * STAGE;
+  static constexpr int CPR = D / 32;   // 16-byte pieces of a row
+  static __device__ __forceinline__ int value_at(int row, int piece) {   // byte offset of a value row's piece
+    if (D == 128) {
+      const int pair = row >> 1;
+      return pair * 128 + (((row ^ pair) & 1) << 6) + ((piece ^ (pair & 2)) << 4);
+    }
+    return row * 32 + ((piece ^ ((row >> 2) & 1)) << 4);
+  }
+};
+
+}  // namespace spinq

@@ -1,0 +1,264 @@
+// kv4_plan.cu -- bookkeeping of the paged 4-bit cache on the GPU:
+// spinq_kv4_plan (pages, positions and slots of a step's tokens from the
+// requests' lengths) and spinq_kv4_keep (the accepted path of each drafted tree
+// moves together).
+//
+// Plan.  With P tokens a page and, for sequence b,
+//   start = max(lens - drop, 0),  kept = ceil(start / P),
+//   freed = ceil(lens / P) - kept,  need = ceil((start + add) / P) - kept,
+// the free pages are a stack: freed page i of all (sequences in order, pages in
+// order) lies i below its top, and page a of all that are needed is the a-th from
+// the top, so a sequence that gives and takes gets its own pages back.  Three
+// prefix sums over the batch (tokens, freed, needed pages) say where everything is:
+// every CTA of a cluster takes them by itself, in shared memory, then the
+// cluster's threads share the pages and tokens.  The stack is written before the
+// cluster's barrier and read behind it.  Bound: latency (a chain of the lengths'
+// loads, three block-wide sums, a barrier, and two dependent loads).
+//
+// Keep.  A path ascends, so a token never moves up and never onto one that is
+// still to be read by a later part of its path: a CTA takes the 16-byte pieces of
+// a sequence and a kv head in rounds, reads all of a round, then writes it.
+#include "launch_util.h"
+#include "spinq_device.cuh"
+#include "spinq_internal.h"
+
+namespace spinq {
+namespace {
+
+constexpr int kPlanThreads = 512;
+constexpr int kPlanCluster = 8;
+constexpr int kPlanPer = kPlanMaxBatch / kPlanThreads;   // sequences per thread at most
+
+// Sums of whole numbers in [0, 2^31) that stay there.
+constexpr uint32_t kPlanMost = 0x7fffffffu;
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, kPlanMost); }
+
+// Exclusive prefix sum of x over the block and the total; `part`: a word per warp.
+__device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t* part, uint32_t* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t s = x;
+#pragma unroll
+  for (int w = 1; w < 32; w <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, s, w);
+    if (lane >= w) s = sat_add(s, y);
+  }
+  __syncthreads();   // the last sum's parts have been read
+  if (lane == 31) part[warp] = s;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 32; ++w) {
+    if (w == warp) before = all;
+    all = sat_add(all, part[w]);
+  }
+  *total = all;
+  uint32_t ex = __shfl_up_sync(0xffffffffu, s, 1);
+  if (lane == 0) ex = 0;
+  return sat_add(before, ex);
+}
+
+// The last i of [0, n) with start[i] <= x, where start ascends from 0.
+__device__ __forceinline__ int last_at_most(const uint32_t* start, int n, uint32_t x) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (start[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ void plan_barrier(bool cluster) {
+  __threadfence();
+  if (cluster)
+    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;\n" ::: "memory");
+  else
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(kPlanThreads) kv4_plan_kernel(const PlanArgs a) {
+  extern __shared__ uint32_t plan_smem[];
+  __shared__ uint32_t part[kPlanThreads / 32];
+  const int B = (int)a.batch;
+  uint32_t* start = plan_smem;        // tokens that stay
+  uint32_t* cu = start + B;           // tokens asked for before this sequence
+  uint32_t* freed = cu + B;           // pages freed before it
+  uint32_t* taken = freed + B;        // pages needed before it
+  uint32_t* gets = taken + B;         // pages it gets, or kPlanMost: refused
+  const int tid = threadIdx.x, shift = a.page_shift;
+  const bool cluster = gridDim.x > 1;
+  const uint32_t stride = gridDim.x * kPlanThreads, first = blockIdx.x * kPlanThreads + tid;
+  const uint32_t page1 = (1u << shift) - 1, cap = (uint32_t)(a.table_width << shift), total = (uint32_t)a.total;
+  auto pages = [&](uint32_t tokens) { return (tokens + page1) >> shift; };   // tokens <= 2^31 - 256
+  pdl_wait();
+  pdl_trigger();
+
+  for (int b = tid; b < B; b += kPlanThreads) {
+    const uint32_t len = min((uint32_t)max(a.lens[b], 0), cap), drop = a.drop ? (uint32_t)max(a.drop[b], 0) : 0u;
+    const uint32_t s = len > drop ? len - drop : 0u;
+    start[b] = s;
+    freed[b] = pages(len) - pages(s);
+    cu[b] = a.add ? (uint32_t)max(a.add[b], 0) : 0u;
+  }
+  const int32_t count0 = *a.free_count;
+  __syncthreads();
+  // a thread's sequences lie next to one another
+  const int per = (B + kPlanThreads - 1) / kPlanThreads, b0 = min(tid * per, B), b1 = min(b0 + per, B);
+  uint32_t sum_add = 0, sum_freed = 0;
+  for (int b = b0; b < b1; ++b) sum_add = sat_add(sum_add, cu[b]), sum_freed = sat_add(sum_freed, freed[b]);
+  uint32_t all_add, all_freed, all_need;
+  uint32_t at_add = block_prefix(sum_add, part, &all_add), at_freed = block_prefix(sum_freed, part, &all_freed);
+  uint32_t need[kPlanPer], sum_need = 0;
+#pragma unroll
+  for (int k = 0; k < kPlanPer; ++k) {
+    need[k] = 0;
+    if (b0 + k < b1) {
+      const int b = b0 + k;
+      const uint32_t add = cu[b], f = freed[b];
+      cu[b] = at_add;
+      freed[b] = at_freed;
+      at_add = sat_add(at_add, add);
+      at_freed = sat_add(at_freed, f);
+      // it fits the answer's arrays and its row of the table (start <= cap)
+      const bool fits = add == 0 || (at_add <= total && add <= cap - start[b]);
+      need[k] = fits ? pages(start[b] + (fits ? add : 0)) - pages(start[b]) : 0u;
+      gets[b] = fits ? need[k] : kPlanMost;
+      sum_need = sat_add(sum_need, need[k]);
+    }
+  }
+  uint32_t at_need = block_prefix(sum_need, part, &all_need);
+  const uint32_t count = (uint32_t)min(max((int64_t)count0, (int64_t)0), a.free_capacity);
+  const uint32_t there = (uint32_t)min((int64_t)sat_add(count, all_freed), a.free_capacity);   // free pages
+  uint32_t given = 0;   // a lower bound of the pages handed out: what precedes the last that got some, and its own
+#pragma unroll
+  for (int k = 0; k < kPlanPer; ++k)
+    if (b0 + k < b1) {
+      const int b = b0 + k;
+      taken[b] = at_need;
+      at_need = sat_add(at_need, need[k]);
+      if (need[k] > 0) {
+        if (at_need > there) gets[b] = kPlanMost;
+        else given = at_need;
+      }
+    }
+  // (pages needed so far ascend: the largest sum that was granted is what was handed out)
+  given = __reduce_max_sync(0xffffffffu, given);
+  __syncthreads();
+  if ((tid & 31) == 0) part[tid >> 5] = given;
+  __syncthreads();
+  given = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 32; ++w) given = max(given, part[w]);
+
+  // freed pages onto the stack
+  for (uint32_t i = first; i < all_freed && i < there; i += stride) {
+    const int b = last_at_most(freed, B, i);
+    const uint32_t p = pages(start[b]) + i - freed[b], to = there - 1 - i;
+    if (to >= count && p < (uint32_t)a.table_width) a.free_pages[to] = a.table[(int64_t)b * a.table_width + p];
+  }
+  plan_barrier(cluster);
+
+  // pages from its top into the tables
+  for (uint32_t i = first; i < given; i += stride) {
+    const int b = last_at_most(taken, B, i);
+    a.table[(int64_t)b * a.table_width + pages(start[b]) + i - taken[b]] = __ldcg(a.free_pages + (there - 1 - i));
+  }
+  // positions and slots
+  for (uint32_t t = first; t < total; t += stride) {
+    int64_t slot = -1, pos = 0;
+    if (t < all_add) {
+      const int b = last_at_most(cu, B, t);
+      const uint32_t s = start[b], i = t - cu[b], at = s + i, kept = pages(s);
+      const uint32_t got = gets[b];
+      pos = min(max((int64_t)s + (a.depths ? (int64_t)a.depths[t] : (int64_t)i) + a.position_offset, (int64_t)0),
+                (int64_t)INT32_MAX);
+      if (got != kPlanMost) {
+        const uint32_t p = at >> shift;
+        const int32_t page = p < kept ? __ldcg(a.table + (int64_t)b * a.table_width + p)
+                                      : __ldcg(a.free_pages + (there - 1 - (taken[b] + p - kept)));
+        slot = ((int64_t)page << shift) + (at & page1);
+      }
+    }
+    a.positions[t] = (int32_t)pos;
+    a.slots[t] = slot;
+  }
+  // the batch's numbers, the last of all: every CTA has read the lengths
+  for (uint32_t b = first; b <= (uint32_t)B; b += stride) {
+    if (b == (uint32_t)B) {
+      a.cu_tokens[B] = (int32_t)min(all_add, total);
+      *a.free_count = (int32_t)(there - given);
+      break;
+    }
+    const bool ok = gets[b] != kPlanMost;
+    const uint32_t next = b + 1 < (uint32_t)B ? cu[b + 1] : all_add;
+    a.cu_tokens[b] = (int32_t)min(cu[b], total);
+    if (a.granted) a.granted[b] = ok;
+    a.lens[b] = (int32_t)(start[b] + (ok ? next - cu[b] : 0u));
+  }
+}
+
+constexpr int kKeepThreads = 128;
+
+template <int D>
+__global__ void __launch_bounds__(kKeepThreads) kv4_keep_kernel(const KeepArgs a) {
+  constexpr int CP = D / 32, PIECES = 2 * CP + 1;   // 16-byte pieces of a token's codes, and its scales
+  const int64_t b = blockIdx.x / (uint32_t)a.Hkv, h = blockIdx.x - b * a.Hkv;
+  pdl_wait();
+  pdl_trigger();
+  const int n = min(max(__ldg(a.counts + b), 0), (int)a.path_width);
+  const int64_t start = __ldg(a.starts + b);
+  const int32_t* path = a.path + b * a.path_width;
+  const int32_t* table = a.table + b * a.table_width;
+  // the token's place in the page arrays, or -1
+  auto place = [&](int64_t t) {
+    if (t < 0 || (t >> a.page_shift) >= a.table_width) return (int64_t)-1;
+    const int64_t page = __ldg(table + (t >> a.page_shift));
+    return page < 0 || page >= a.num_pages ? (int64_t)-1 : (page * a.Hkv + h) * a.page_size + (t & (a.page_size - 1));
+  };
+  auto piece = [&](int64_t at, int k) {
+    return k < CP ? reinterpret_cast<uint4*>(a.k_codes + at * (D / 2)) + k
+                  : (k < 2 * CP ? reinterpret_cast<uint4*>(a.v_codes + at * (D / 2)) + (k - CP)
+                                : reinterpret_cast<uint4*>(a.scales) + at);
+  };
+  const int64_t items = (int64_t)n * PIECES;
+  for (int64_t i0 = 0; i0 < items; i0 += kKeepThreads) {
+    const int64_t i = i0 + threadIdx.x;
+    uint4* to = nullptr;
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (i < items) {
+      const int64_t token = i / PIECES;
+      const int k = (int)(i - token * PIECES);
+      const int64_t node = __ldg(path + token);
+      if (node != token && node >= 0) {
+        const int64_t from = place(start + node), at = place(start + token);
+        if (from >= 0 && at >= 0) {
+          x = *piece(from, k);
+          to = piece(at, k);
+        }
+      }
+    }
+    __syncthreads();
+    if (to) *to = x;
+    __syncthreads();
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_kv4_plan(const PlanArgs& a, cudaStream_t stream) {
+  const int smem = (int)a.batch * 5 * 4;
+  int per_sm = 1;
+  cudaError_t e = prepare_launch(kv4_plan_kernel, kPlanThreads, kPlanMaxBatch * 5 * 4, &per_sm);
+  if (e != cudaSuccess) return e;
+  // one CTA where each of its threads has little to do: no cluster's barrier
+  const int ctas = a.total + a.batch * 4 <= 4 * kPlanThreads ? 1 : kPlanCluster;
+  e = launch_pdl(kv4_plan_kernel, dim3((unsigned)ctas), dim3(kPlanThreads), (size_t)smem, stream, ctas, a);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+cudaError_t launch_kv4_keep(const KeepArgs& a, cudaStream_t stream) {
+  auto kernel = a.D == 128 ? kv4_keep_kernel<128> : kv4_keep_kernel<64>;
+  const cudaError_t e = launch_pdl(kernel, dim3((unsigned)(a.batch * a.Hkv)), dim3(kKeepThreads), 0, stream, 1, a);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace spinq

@@ -72,6 +72,7 @@ struct PromptParams {
   int Hq, Hkv, batch, G, tpt;   // tpt: queries per tile
   int tiles;                    // items along a sequence's queries
   bool causal;
+  int window, sinks;            // the windowed form's (causal; window >= 1)
   float scale_log2;             // |scale| log2 e
   uint32_t idesc_qk;
   int* status;
@@ -104,7 +105,8 @@ constexpr int kPromptThreads = 384;
 // the item's readers: copy thread, two MMA threads, eight softmax warps
 constexpr int kItemReaders = 11;
 
-template <int D>
+// WIN: a query at position p sees keys j <= p with p - j < window or j < sinks.
+template <int D, bool WIN>
 __global__ void __launch_bounds__(kPromptThreads, 1)
     prompt_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                      const __grid_constant__ CUtensorMap mv, const PromptParams a) {
@@ -167,15 +169,27 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
   struct Work {
     int hk, t0, lq, lk, nt[2], ntile;
     int64_t q0, k0;
+    // WIN: the tiles are the first `front` of the sequence (the sinks), then, `skip` further on, those from the
+    // first that the window of the item's first query reaches
+    int front, skip;
+    __device__ __forceinline__ int at(int j) const { return WIN && j >= front ? j + skip : j; }   // tile j of the list
   };
   auto read_item = [&](int slot, Work& w) {
     const volatile PromptItem& x = items[slot];
     w.hk = x.hk, w.t0 = x.t0, w.lq = x.lq, w.lk = x.lk, w.q0 = x.q0, w.k0 = x.k0;
+    w.front = w.skip = 0;
+    if constexpr (WIN) {
+      const int first = w.t0 + w.lk - w.lq;   // position of the item's first query
+      const int reach = first >= a.window ? (first - a.window + 1) >> 7 : 0;
+      w.front = min((int)(((int64_t)a.sinks + 127) >> 7), reach);
+      w.skip = reach - w.front;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int first = w.t0 + i * a.tpt, last = min(first + a.tpt, w.lq) - 1;
       const int nk = first < w.lq ? (a.causal ? max(0, min(w.lk, last + 1 + w.lk - w.lq)) : w.lk) : 0;
       w.nt[i] = (nk + 127) / 128;
+      if (WIN && nk > 0) w.nt[i] -= w.skip;   // (a tile with a key reaches past the item's first query)
     }
     w.ntile = max(w.nt[0], w.nt[1]);
     return x.more != 0;
@@ -212,7 +226,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
 #pragma unroll
             for (int at = 0; at < D / 64; ++at)
               tma_load_3d(smem + C::OFF_KV + sk * C::TILE + at * kAttnAtom, n & 1 ? &mv : &mk, &full[sk], at * 64, w.hk,
-                          (int32_t)(w.k0 + (n >> 1) * 128));
+                          (int32_t)(w.k0 + w.at(n >> 1) * 128));
             ++issued[0];
             if (++sk == NSTG) sk = 0, pk ^= 1;
           }
@@ -361,6 +375,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
     for (int it = 0; ok; ++it) {
       if (!(ok = attn_wait_warp(&item[it & 1], (uint32_t)(it >> 1) & 1u, abort_flag, g_prompt_wait_ns))) break;
       int nti, lk, kv_after, n;   // n: keys of this row
+      int low = 0, front = 0, skip = 0;   // WIN: its window's first key; the list of tiles
       {
         Work w;
         if (!read_item(it & 1, w)) break;
@@ -369,6 +384,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         kv_after = kv + 2 * w.ntile;
         const int tok = w.t0 + i * a.tpt + row_t;
         n = r < a.G * a.tpt && tok < w.lq ? (a.causal ? min(lk, tok + 1 + lk - w.lq) : lk) : 128 * nti;
+        if constexpr (WIN) {
+          front = w.front, skip = w.skip;
+          if (r < a.G * a.tpt && tok < w.lq)
+            low = tok + lk - w.lq >= a.window ? tok + lk - w.lq - a.window + 1 : 0;
+          else
+            n = 128 * (nti + skip);   // a row without a query: every key of the list
+        }
       }
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < nti; ++j, ++ns) {
@@ -378,11 +400,21 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
 #pragma unroll
         for (int c = 0; c < 128; c += 32) tmem_ld_32x32b_x32(st + c, s + c);
         tmem_ld_wait_all<128>(s);
-        const int seen = n - j * 128;
+        const int base = 128 * (WIN && j >= front ? j + skip : j);   // first key of the tile
+        const int seen = n - base;
         if (__any_sync(0xffffffffu, seen < 128)) {
 #pragma unroll
           for (int c = 0; c < 128; ++c)
             if (c >= seen) s[c] = 0xFF800000u;   // -inf
+        }
+        if constexpr (WIN) {
+          // keys between the sinks and the row's window
+          const int from = a.sinks - base, to = low - base;
+          if (__any_sync(0xffffffffu, to > 0 && from < 128 && from < to)) {
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (c >= from && c < to) s[c] = 0xFF800000u;
+          }
         }
         const float mx = attn_row_max(s) * a.scale_log2;
         const float mn = mx > m + kAttnSlack ? mx : m;
@@ -411,12 +443,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         l = x + y;
         tmem_st_32x32b_x32(st, s);
         tmem_st_32x32b_x32(st + 32, s + 32);
-        if (j * 128 + 128 > lk) {
+        if (base + 128 > lk) {
           // this V tile ends past the sequence: thread r zeroes row r if it lies there
           // (the threads of the other tile may write the same zeros)
           const int nv = kv + 2 * j + 1;
           if (!(ok = attn_wait_warp(&full[nv % NSTG], (uint32_t)(nv / NSTG) & 1u, abort_flag, g_prompt_wait_ns))) break;
-          if (j * 128 + r >= lk) {
+          if (base + r >= lk) {
             const uint32_t vb = sb + C::OFF_KV + (nv % NSTG) * C::TILE + r * 128;
 #pragma unroll
             for (int at = 0; at < D / 64; ++at)
@@ -495,7 +527,7 @@ bool encode_heads(EncodeTiledFn enc, CUtensorMap* map, const void* p, int64_t to
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
+template <int D, bool WIN>
 cudaError_t launch_t(const PromptArgs& a, cudaStream_t stream) {
   using C = PromptCfg<D>;
   EncodeTiledFn enc = get_encode_fn();
@@ -519,6 +551,8 @@ cudaError_t launch_t(const PromptArgs& a, cudaStream_t stream) {
   p.Hkv = (int)a.Hkv;
   p.batch = (int)a.batch;
   p.causal = a.causal;
+  p.window = (int)(a.window < INT32_MAX ? a.window : INT32_MAX);
+  p.sinks = (int)(a.sinks < INT32_MAX ? a.sinks : INT32_MAX);
   // a negative scale is |scale| times negated queries; zero makes every
   // weight equal, as any product too small to move 2^x does
   p.scale_log2 = fmaxf(fabsf(a.scale) * kAttnLog2e, 1e-30f);
@@ -529,9 +563,9 @@ cudaError_t launch_t(const PromptArgs& a, cudaStream_t stream) {
   const int64_t items = (int64_t)p.tiles * a.Hkv * a.batch;
   if (items > INT32_MAX) return cudaErrorNotSupported;
   int per_sm = 0;
-  cudaError_t e = prepare_launch_tmem(prompt_tc_kernel<D>, kPromptThreads, C::BYTES, 512, &per_sm);
+  cudaError_t e = prepare_launch_tmem(prompt_tc_kernel<D, WIN>, kPromptThreads, C::BYTES, 512, &per_sm);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(prompt_tc_kernel<D>, dim3((unsigned)items), dim3(kPromptThreads),
+  e = launch_pdl(prompt_tc_kernel<D, WIN>, dim3((unsigned)items), dim3(kPromptThreads),
                  C::BYTES, stream, 1, mq, mk, mv, p);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -541,8 +575,8 @@ cudaError_t launch_t(const PromptArgs& a, cudaStream_t stream) {
 cudaError_t set_wait_limit_prompt(uint64_t ns) { return cudaMemcpyToSymbol(g_prompt_wait_ns, &ns, sizeof(ns)); }
 
 cudaError_t launch_prompt_attention(const PromptArgs& a, cudaStream_t stream) {
-  if (a.D == 128) return launch_t<128>(a, stream);
-  if (a.D == 64) return launch_t<64>(a, stream);
+  if (a.D == 128) return a.window > 0 ? launch_t<128, true>(a, stream) : launch_t<128, false>(a, stream);
+  if (a.D == 64) return a.window > 0 ? launch_t<64, true>(a, stream) : launch_t<64, false>(a, stream);
   return cudaErrorNotSupported;
 }
 

@@ -516,13 +516,14 @@ spinq_status spinq_kv4_read(const spinq_kv4_pages* cache, const int32_t* page_ta
 // The kernel keeps everything on the chip.
 int64_t spinq_prompt_attention_workspace_bytes(int64_t, int64_t, int64_t, int64_t, int64_t, int64_t) { return 0; }
 
-spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
-                                    const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t total_q,
-                                    int64_t total_k, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv, int64_t D,
-                                    int32_t causal, float softmax_scale, void* out, void*, int64_t, void* stream) {
+static spinq_status prompt_call(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t total_q,
+                                int64_t total_k, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv, int64_t D,
+                                bool causal, int64_t window, int64_t sinks, float softmax_scale, void* out,
+                                void* stream) {
   if (batch < 0 || total_q < 0 || total_k < 0 || max_q < 0 || max_k < 0 || Hq <= 0 || Hkv <= 0 || D <= 0)
     return SPINQ_EINVAL;
-  if (Hq % Hkv != 0 || (causal != 0 && causal != 1) || !std::isfinite(softmax_scale)) return SPINQ_EINVAL;
+  if (Hq % Hkv != 0 || !std::isfinite(softmax_scale)) return SPINQ_EINVAL;
   if (total_q > 0) {
     if (batch == 0 || max_q == 0 || !cu_q || !cu_k || !out || !aligned16(out)) return SPINQ_EINVAL;
     if (!rows_ok(q, ldq, Hq * D)) return SPINQ_EINVAL;
@@ -549,10 +550,31 @@ spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, i
   a.cu_k = cu_k;
   a.total_q = total_q;
   a.total_k = total_k;
-  a.causal = causal != 0;
+  a.causal = causal;
+  a.window = window;
+  a.sinks = sinks;
   a.scale = softmax_scale;
   a.out = out;
   return from_cuda(launch_prompt_attention(a, static_cast<cudaStream_t>(stream)));
+}
+
+spinq_status spinq_prompt_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                    const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t total_q,
+                                    int64_t total_k, int64_t max_q, int64_t max_k, int64_t Hq, int64_t Hkv, int64_t D,
+                                    int32_t causal, float softmax_scale, void* out, void*, int64_t, void* stream) {
+  if (causal != 0 && causal != 1) return SPINQ_EINVAL;
+  return prompt_call(q, ldq, k, ldk, v, ldv, cu_q, cu_k, batch, total_q, total_k, max_q, max_k, Hq, Hkv, D, causal != 0,
+                     0, 0, softmax_scale, out, stream);
+}
+
+spinq_status spinq_window_prompt_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                                           int64_t ldv, const int32_t* cu_q, const int32_t* cu_k, int64_t batch,
+                                           int64_t total_q, int64_t total_k, int64_t max_q, int64_t max_k, int64_t Hq,
+                                           int64_t Hkv, int64_t D, int64_t window, int64_t sinks, float softmax_scale,
+                                           void* out, void* stream) {
+  if (window < 1 || sinks < 0) return SPINQ_EINVAL;
+  return prompt_call(q, ldq, k, ldk, v, ldv, cu_q, cu_k, batch, total_q, total_k, max_q, max_k, Hq, Hkv, D, true, window,
+                     sinks, softmax_scale, out, stream);
 }
 
 static PrefixArgs prefix_shape(int64_t B, int64_t prefix_len, int64_t table_width, int32_t page_size, int64_t Hq,
@@ -613,6 +635,129 @@ spinq_status spinq_prefix_attention_kv4(const void* q, const spinq_kv4_pages* ca
   a.out = out;
   a.workspace = workspace;
   return from_cuda(launch_prefix_attention(a, static_cast<cudaStream_t>(stream)));
+}
+
+spinq_status spinq_kv4_plan(int32_t* lens, const int32_t* drop, const int32_t* add, int64_t batch,
+                            int32_t* page_table, int64_t table_width, int32_t page_size, int32_t* free_pages,
+                            int32_t* free_count, int64_t free_capacity, const int32_t* depths,
+                            int64_t position_offset, int64_t total, int32_t* cu_tokens, int32_t* positions,
+                            int64_t* slots, int32_t* granted, void* stream) {
+  if (batch < 0 || table_width < 0 || free_capacity < 0 || total < 0 || page_size <= 0) return SPINQ_EINVAL;
+  if (!free_count || !cu_tokens || (free_capacity > 0 && !free_pages)) return SPINQ_EINVAL;
+  if (total > 0 && (!positions || !slots)) return SPINQ_EINVAL;
+  if (batch > 0 && (!lens || (table_width > 0 && !page_table))) return SPINQ_EINVAL;
+  for (const void* p : {(const void*)lens, (const void*)drop, (const void*)add, (const void*)page_table,
+                        (const void*)free_pages, (const void*)free_count, (const void*)depths, (const void*)cu_tokens,
+                        (const void*)positions, (const void*)granted})
+    if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return SPINQ_EINVAL;
+  if (reinterpret_cast<uintptr_t>(slots) % 8 != 0) return SPINQ_EINVAL;
+  if (!page_size_ok(page_size) || batch > kPlanMaxBatch || table_width > (INT32_MAX - 256) / page_size ||
+      total >= INT32_MAX || free_capacity >= INT32_MAX || position_offset < INT32_MIN || position_offset > INT32_MAX)
+    return SPINQ_EUNSUPPORTED;
+  PlanArgs a{lens, drop, add, batch, page_table, table_width, log2_of(page_size), free_pages, free_count, free_capacity,
+             depths, position_offset, total, cu_tokens, positions, slots, granted};
+  return from_cuda(launch_kv4_plan(a, static_cast<cudaStream_t>(stream)));
+}
+
+spinq_status spinq_kv4_keep(const spinq_kv4_pages* cache, const int32_t* page_table, int64_t batch,
+                            int64_t table_width, const int32_t* starts, const int32_t* path, int64_t path_width,
+                            const int32_t* counts, void* stream) {
+  if (batch < 0 || table_width < 0 || path_width < 0) return SPINQ_EINVAL;
+  spinq_status st = check_pages(cache);
+  if (st != SPINQ_OK) return st;
+  if (batch > 0 && (!starts || !counts || (path_width > 0 && !path) || (table_width > 0 && !page_table)))
+    return SPINQ_EINVAL;
+  if (batch > INT32_MAX || batch * cache->kv_heads > INT32_MAX || table_width > INT32_MAX || path_width > INT32_MAX)
+    return SPINQ_EUNSUPPORTED;
+  if (batch == 0 || table_width == 0 || path_width == 0 || cache->num_pages == 0) return SPINQ_OK;
+  KeepArgs a{cache->k_codes, cache->v_codes, cache->scales, cache->num_pages, cache->kv_heads, cache->page_size,
+             log2_of(cache->page_size), cache->head_dim, page_table, batch, table_width, starts, path, path_width, counts};
+  return from_cuda(launch_kv4_keep(a, static_cast<cudaStream_t>(stream)));
+}
+
+static TreeArgs tree_shape(int64_t B, int64_t max_q, int64_t table_width, int32_t page_size, int64_t Hq, int64_t Hkv,
+                           int64_t D) {
+  TreeArgs a{};
+  a.B = B;
+  a.max_q = max_q;
+  a.table_width = table_width;
+  a.page_size = page_size;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.D = (int)D;
+  return a;
+}
+
+// What the launch and its plan hold for; the workspace query plans too.  (The units of
+// all jobs, at most a job per row and a unit per 16 tokens here, stay below 2^52.)
+static bool tree_limits_ok(int64_t B, int64_t max_q, int64_t table_width, int64_t page_size, int64_t Hq, int64_t Hkv) {
+  return Hq / Hkv <= 128 && Hq <= 65535 && B <= 65535 && max_q <= 128 && table_width <= (INT32_MAX - 256) / page_size &&
+         (double)B * (double)(max_q * Hq) * ((double)table_width * (double)page_size / 16. + 1.) < 4503599627370496.;
+}
+
+int64_t spinq_tree_attention_workspace_bytes(int64_t B, int64_t max_q, int64_t table_width, int32_t page_size,
+                                             int64_t Hq, int64_t Hkv, int64_t D) {
+  if (B <= 0 || max_q <= 0 || table_width < 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || (D != 64 && D != 128) ||
+      !page_size_ok(page_size) || !tree_limits_ok(B, max_q, table_width, page_size, Hq, Hkv))
+    return 0;
+  return tree_attention_workspace(tree_shape(B, max_q, table_width, page_size, Hq, Hkv, D));
+}
+
+// cu_q null: one query a sequence.
+static spinq_status tree_call(const void* q, const spinq_kv4_pages* cache, const int32_t* page_table,
+                              int64_t table_width, const int32_t* lens, const int32_t* cu_q, const int32_t* parents,
+                              int64_t B, int64_t total_q, int64_t max_q, int64_t Hq, int64_t window, int64_t sinks,
+                              float softmax_scale, void* out, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (B < 0 || total_q < 0 || max_q < 0 || table_width < 0 || Hq <= 0 || window < 0 || sinks < 0 ||
+      !std::isfinite(softmax_scale))
+    return SPINQ_EINVAL;
+  spinq_status st = check_pages(cache);
+  if (st != SPINQ_OK) return st;
+  const int64_t Hkv = cache->kv_heads, D = cache->head_dim;
+  if (Hq % Hkv != 0) return SPINQ_EINVAL;
+  if (total_q > 0) {
+    if (B == 0 || max_q == 0 || !q || !out || !lens || !aligned16(q) || !aligned16(out)) return SPINQ_EINVAL;
+    if (table_width > 0 && (!page_table || cache->num_pages == 0)) return SPINQ_EINVAL;
+  }
+  if (!tree_limits_ok(B, max_q, table_width, cache->page_size, Hq, Hkv) || total_q > INT32_MAX) return SPINQ_EUNSUPPORTED;
+  if (total_q == 0) return SPINQ_OK;
+  TreeArgs a = tree_shape(B, max_q, table_width, cache->page_size, Hq, Hkv, D);
+  if (!workspace || !aligned16(workspace) || workspace_bytes < tree_attention_workspace(a)) return SPINQ_EINVAL;
+  a.q = q;
+  a.k_codes = cache->k_codes;
+  a.v_codes = cache->v_codes;
+  a.scales = cache->scales;
+  a.num_pages = cache->num_pages;
+  a.table = page_table;
+  a.lens = lens;
+  a.cu_q = cu_q;
+  a.parents = parents;
+  a.total_q = total_q;
+  // (positions are below 2^31: a longer window is as good as that)
+  a.window = window < INT32_MAX ? window : INT32_MAX;
+  a.sinks = sinks < INT32_MAX ? sinks : INT32_MAX;
+  a.scale = softmax_scale;
+  a.out = out;
+  a.workspace = workspace;
+  return from_cuda(launch_tree_attention(a, static_cast<cudaStream_t>(stream)));
+}
+
+spinq_status spinq_tree_attention_kv4(const void* q, const spinq_kv4_pages* cache, const int32_t* page_table,
+                                      int64_t table_width, const int32_t* lens, const int32_t* cu_q,
+                                      const int32_t* parents, int64_t B, int64_t total_q, int64_t max_q, int64_t Hq,
+                                      int64_t window, int64_t sinks, float softmax_scale, void* out, void* workspace,
+                                      int64_t workspace_bytes, void* stream) {
+  if (total_q > 0 && !cu_q) return SPINQ_EINVAL;
+  return tree_call(q, cache, page_table, table_width, lens, cu_q, parents, B, total_q, max_q, Hq, window, sinks,
+                   softmax_scale, out, workspace, workspace_bytes, stream);
+}
+
+spinq_status spinq_window_attention_kv4(const void* q, const spinq_kv4_pages* cache, const int32_t* page_table,
+                                        int64_t table_width, const int32_t* lens, int64_t B, int64_t Hq,
+                                        int64_t window, int64_t sinks, float softmax_scale, void* out,
+                                        void* workspace, int64_t workspace_bytes, void* stream) {
+  return tree_call(q, cache, page_table, table_width, lens, nullptr, nullptr, B, B, 1, Hq, window, sinks, softmax_scale,
+                   out, workspace, workspace_bytes, stream);
 }
 
 spinq_status spinq_debug_set_wait_limit_ns(int64_t ns) {

@@ -144,6 +144,44 @@ struct ReadArgs {
 };
 cudaError_t launch_kv4_read(const ReadArgs& a, cudaStream_t stream);
 
+// Pages, positions and slots of a step's tokens (kv4_plan.cu).
+constexpr int kPlanMaxBatch = 4096;
+struct PlanArgs {
+  int32_t* lens;             // [batch] in and out
+  const int32_t* drop;       // [batch] or nullptr (none)
+  const int32_t* add;        // [batch] or nullptr (none)
+  int64_t batch;
+  int32_t* table;            // [batch][table_width]
+  int64_t table_width;
+  int page_shift;
+  int32_t* free_pages;       // [free_capacity], a stack of *free_count
+  int32_t* free_count;
+  int64_t free_capacity;
+  const int32_t* depths;     // [total] or nullptr
+  int64_t position_offset;
+  int64_t total;
+  int32_t* cu_tokens;        // [batch + 1]
+  int32_t* positions;        // [total]
+  int64_t* slots;            // [total]
+  int32_t* granted;          // [batch] or nullptr
+};
+cudaError_t launch_kv4_plan(const PlanArgs& a, cudaStream_t stream);
+
+struct KeepArgs {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* scales;
+  int64_t num_pages, Hkv;
+  int page_size, page_shift, D;
+  const int32_t* table;      // [batch][table_width]
+  int64_t batch, table_width;
+  const int32_t* starts;     // [batch]
+  const int32_t* path;       // [batch][path_width]
+  int64_t path_width;
+  const int32_t* counts;     // [batch]
+};
+cudaError_t launch_kv4_keep(const KeepArgs& a, cudaStream_t stream);
+
 struct PromptArgs {
   const void* q;          // fp16 [total_q] rows of Hq D values, ldq apart
   const void* k;          // fp16 [total_k] rows of Hkv D values
@@ -154,6 +192,7 @@ struct PromptArgs {
   int64_t batch, total_q, total_k, max_q, Hq, Hkv;
   int D;
   bool causal;
+  int64_t window, sinks;  // window 0: none; else causal, the last `window` positions and the first `sinks` tokens
   float scale;
   void* out;              // fp16 [total_q][Hq][D]
 };
@@ -178,6 +217,27 @@ struct PrefixArgs {
 };
 int64_t prefix_attention_workspace(const PrefixArgs& a);
 cudaError_t launch_prefix_attention(const PrefixArgs& a, cudaStream_t stream);
+
+struct TreeArgs {
+  const void* q;          // fp16 [total_q][Hq][D]
+  const uint8_t* k_codes;
+  const uint8_t* v_codes;
+  const float* scales;
+  int64_t num_pages, Hkv;
+  int page_size, D;
+  const int32_t* table;   // [B][table_width]
+  int64_t table_width;
+  const int32_t* lens;    // [B]
+  const int32_t* cu_q;    // [B + 1] or nullptr: one query each
+  const int32_t* parents; // [total_q] or nullptr: each query's parent is the one before it
+  int64_t B, total_q, max_q, Hq;
+  int64_t window, sinks;  // window 0: none
+  float scale;
+  void* out;              // fp16 [total_q][Hq][D]
+  void* workspace;
+};
+int64_t tree_attention_workspace(const TreeArgs& a);
+cudaError_t launch_tree_attention(const TreeArgs& a, cudaStream_t stream);
 
 // Chunks of the cache length that the decode attention splits over (the
 // workspace holds B * Hq * chunks * (D + 2) floats).

@@ -1,0 +1,612 @@
+// tree_attention.cu -- spinq_tree_attention_kv4 and spinq_window_attention_kv4:
+// the last tokens of each sequence (a tree of drafted ones, or one) over the
+// paged 4-bit cache.
+//
+// Sequence b has n tokens in the cache, the last nq of them its queries' own.  Query
+// i sees the context, tokens 0 .. n - nq - 1, its ancestors by `parents`, and
+// itself; with a window only those of them whose position (a context token's
+// place, a node's n - nq + depth) is less than `window` before its own or below
+// `sinks`.  Scores, weights and sums as in prefix_attention.cu:
+//   t = scale log2(e) q . k + log2 alpha',  w = 2^(t - M),
+//   o = [ sum w (u' - 8) + sum w (8 + beta' / alpha') ] / sum w / alpha'
+// with the codes as exact fp16 operands and w in two fp16 parts.
+//
+// Work.  A job is ROWS rows (query x head of a kv head's group, in that order) of a
+// sequence and a kv head; its keys are cut into units of UNIT tokens: the sinks, and
+// from the first that a window reaches to the end.  The units of all jobs in a row
+// are dealt to the CTAs in equal runs, so lengths may differ as they like: a CTA
+// finds its run by a sum over the batch, and has at most one job that it continues
+// and one that it begins but does not end.  Those two go to the workspace and
+// tree_combine_kernel joins them, in the order of the keys; every other job is
+// complete in its CTA.
+#include <cuda_fp16.h>
+
+#include "../../include/spinq.h"
+#include "attn_tc.cuh"
+#include "kv4_attn.cuh"
+#include "launch_util.h"
+#include "spinq_internal.h"
+
+namespace spinq {
+namespace {
+
+constexpr int kTreeNodes = 128;   // queries of a sequence at most
+constexpr int kRowsWarps = 4;
+constexpr int kCombineThreads = 256;
+
+struct TreeParams {
+  TreeArgs a;
+  int G, shift;
+  int ctas;           // of the attention kernel's grid
+  int rows, unit;     // of a job; tokens
+  int least;          // units a CTA gets at least
+  float scale_log2;
+  float* o;           // [2 * ctas][rows][D]: of CTA c the job it continues (2 c) and the one it leaves (2 c + 1)
+  float2* ml;         // [2 * ctas][rows]: M, and sum of w / alpha'
+};
+
+// What the lengths say of a sequence.
+struct TreeSeq {
+  int n, nq, ctx;     // tokens, queries, tokens before the queries' own (below 0: the first queries have none)
+  int64_t q0;
+  int front, skip;    // units of sinks; units left out behind them
+  int units, rts, jobs;
+};
+
+__device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
+  const TreeArgs& a = p.a;
+  TreeSeq s;
+  s.n = (int)min((int64_t)max(__ldg(a.lens + b), 0), a.table_width << p.shift);
+  s.q0 = b;
+  s.nq = 1;
+  if (a.cu_q) {
+    s.q0 = max(__ldg(a.cu_q + b), 0);
+    s.nq = (int)max((int64_t)0, min(min((int64_t)__ldg(a.cu_q + b + 1), a.total_q) - s.q0, a.max_q));
+  }
+  s.ctx = s.n - s.nq;
+  const int reach = a.window > 0 && s.ctx >= a.window ? (int)((s.ctx - a.window + 1) / p.unit) : 0;
+  s.front = (int)min((a.sinks + p.unit - 1) / p.unit, (int64_t)reach);
+  s.skip = reach - s.front;
+  s.units = max(1, (s.n + p.unit - 1) / p.unit - s.skip);   // one at least: a sequence without tokens has rows too
+  s.rts = (s.nq * p.G + p.rows - 1) / p.rows;
+  s.jobs = s.rts * (int)a.Hkv;
+  return s;
+}
+
+// Where run c of the units lies: [x0, x1) of all, x0 in sequence b, whose units begin at `base`.
+struct TreeRun {
+  int64_t all, x0, x1, base;
+  int ctas;   // runs that there are
+  int b;
+};
+__device__ __forceinline__ int64_t tree_bound(int64_t all, int c, int ctas) { return all * c / ctas; }
+
+template <int THREADS>
+__device__ __forceinline__ TreeRun tree_run(const TreeParams& p, int c) {
+  __shared__ int64_t sums[THREADS / 32], found[2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = (int)p.a.B;
+  const int per = (B + THREADS - 1) / THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const TreeSeq s = tree_seq(p, b);
+    mine += (int64_t)s.units * s.jobs;
+  }
+  int64_t sum = mine;
+#pragma unroll
+  for (int w = 1; w < 32; w <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, sum, w);
+    if (lane >= w) sum += y;
+  }
+  if (lane == 31) sums[warp] = sum;
+  __syncthreads();
+  TreeRun r;
+  int64_t at = sum - mine;
+  r.all = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    if (w == warp) at += r.all;
+    r.all += sums[w];
+  }
+  r.ctas = (int)min((int64_t)p.ctas, (r.all + p.least - 1) / p.least);
+  r.x0 = r.x1 = r.base = 0;
+  r.b = B;
+  if (c < r.ctas) {
+    r.x0 = tree_bound(r.all, c, r.ctas);
+    r.x1 = tree_bound(r.all, c + 1, r.ctas);
+    if (at <= r.x0 && r.x0 < at + mine) {
+      int b = b0;
+      for (; b < b1 - 1; ++b) {
+        const TreeSeq s = tree_seq(p, b);
+        const int64_t t = (int64_t)s.units * s.jobs;
+        if (r.x0 < at + t) break;
+        at += t;
+      }
+      found[0] = b;
+      found[1] = at;
+    }
+    __syncthreads();
+    r.b = (int)found[0];
+    r.base = found[1];
+  }
+  return r;
+}
+
+// A row's view of the keys.
+struct TreeRow {
+  uint32_t line[4];   // its ancestors that it sees, and itself
+  int low;            // first context token that its window reaches
+};
+
+// The queries' parents in shared memory (all threads), then a thread's row of them.
+__device__ __forceinline__ void tree_parents(const TreeParams& p, const TreeSeq& s, int* parent, int threads) {
+  for (int i = threadIdx.x; i < s.nq; i += threads) parent[i] = p.a.parents ? __ldg(p.a.parents + s.q0 + i) : i - 1;
+}
+__device__ __forceinline__ TreeRow tree_row(const TreeParams& p, const TreeSeq& s, const int* parent, int node) {
+  auto up = [&](int i) {   // (a parent comes before its node; any other number: none)
+    const int x = parent[i];
+    return x >= 0 && x < i ? x : -1;
+  };
+  TreeRow r;
+  int depth = 0;
+  for (int i = up(node); i >= 0; i = up(i)) ++depth;
+  r.line[0] = r.line[1] = r.line[2] = r.line[3] = 0;
+  const int64_t window = p.a.window > 0 ? p.a.window : INT64_MAX;
+  for (int i = node, k = 0; i >= 0; i = up(i), ++k)
+    if (k < window || (int64_t)s.ctx + depth - k < p.a.sinks) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        if (w == i >> 5) r.line[w] |= 1u << (i & 31);
+    }
+  r.low = p.a.window > 0 ? (int)max((int64_t)0, (int64_t)s.ctx + depth - p.a.window + 1) : 0;
+  return r;
+}
+
+__device__ __forceinline__ bool tree_sees(const TreeParams& p, const TreeSeq& s, const TreeRow& r, int t) {
+  if (t >= s.n) return false;
+  if (t < s.ctx) return t >= r.low || t < p.a.sinks;
+  const int i = t - s.ctx;
+  return (r.line[i >> 5] >> (i & 31)) & 1u;
+}
+
+__device__ __forceinline__ int64_t tree_page(const TreeArgs& a, const int32_t* table, int t, int shift) {
+  const int64_t page = __ldg(table + (t >> shift));
+  return page < 0 ? 0 : (page >= a.num_pages ? a.num_pages - 1 : page);
+}
+
+// ------------------------------------------------ few rows: warps and mma.sync
+// A job is 8 NB rows, a unit 64 tokens.  A warp takes 16 tokens of each unit,
+// which lie in one page, so its rows of codes are one run of memory, copied three
+// steps ahead into the warp's ring.  Fragments of lane 4 g + c: key rows g and
+// g + 8, bytes [c D/8, (c+1) D/8); value rows 2c, 2c+1, 2c+8, 2c+9, bytes [g D/16,
+// (g+1) D/16).  Scores: tokens on M, rows on N; values: head_dim on M, tokens on K,
+// rows on N.
+template <int D, int NB>
+__global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_kernel(const TreeParams p) {
+  constexpr int KW = D / 32, VW = D / 64, NM = D / 16, ROWS = 8 * NB, UNIT = 16 * kRowsWarps;
+  const TreeArgs& a = p.a;
+  using Ring = OwnRing<D>;
+  __shared__ __align__(16) uint8_t ring_s[kRowsWarps][Ring::WARP];   // after a job's loop: float o [ROWS][D]
+  static_assert(ROWS * D * 4 <= Ring::WARP, "the output fits in the ring");
+  __shared__ float m_s[kRowsWarps][ROWS], l_s[kRowsWarps][ROWS];
+  __shared__ int parent_s[kTreeNodes];
+  __shared__ TreeRow row_s[ROWS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  pdl_wait();
+  pdl_trigger();
+  const TreeRun run = tree_run<kRowsWarps * 32>(p, blockIdx.x);
+  int b = run.b;
+  int64_t base = run.base;
+  for (int64_t x = run.x0; x < run.x1 && b < (int)a.B;) {
+    const TreeSeq s = tree_seq(p, b);
+    const int64_t in_seq = x - base;
+    if (in_seq >= (int64_t)s.units * s.jobs) {
+      base += (int64_t)s.units * s.jobs;
+      ++b;
+      continue;
+    }
+    const int job = (int)(in_seq / s.units), v0 = (int)(in_seq - (int64_t)job * s.units);
+    const int v1 = (int)min((int64_t)s.units, v0 + (run.x1 - x));
+    x += v1 - v0;
+    const int hk = job / s.rts, r0 = (job - hk * s.rts) * ROWS;   // first row of the group's
+    const int rows = min(ROWS, s.nq * p.G - r0);
+    auto row_at = [&](int r) {   // its place among [query][head] rows
+      const int node = (r0 + r) / p.G, head = r0 + r - node * p.G;
+      return (s.q0 + node) * a.Hq + (int64_t)hk * p.G + head;
+    };
+
+    // what the rows see
+    tree_parents(p, s, parent_s, kRowsWarps * 32);
+    __syncthreads();
+    if (tid < ROWS) {
+      TreeRow r = {};
+      if (tid < rows) r = tree_row(p, s, parent_s, (r0 + tid) / p.G);
+      row_s[tid] = r;
+    }
+    // query fragments (k order as the codes come), their sums.  A key
+    // code is masked out of its word in place: as fp16 bits the nibbles at bits 0 and 16
+    // are u 2^-24, those at bits 4 and 20 are 16 u 2^-24, both exact operands; each
+    // kind has a product of its own, the latter's is divided by 16 in fp32.
+    uint32_t qb[NB][KW][4];
+    float qsk[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int r = 8 * nb + g;
+      const __half* qh = reinterpret_cast<const __half*>(a.q) + (r < rows ? row_at(r) : row_at(0)) * D + c * (D / 4);
+      float qs = 0.f;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        uint4 y = __ldg(reinterpret_cast<const uint4*>(qh + 8 * w));
+        if (r >= rows) y = make_uint4(0, 0, 0, 0);
+        const uint32_t ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&ys[q]));
+          qs += f.x + f.y;
+        }
+        qb[nb][w][0] = __byte_perm(y.x, y.z, 0x5410);
+        qb[nb][w][1] = __byte_perm(y.y, y.w, 0x5410);
+        qb[nb][w][2] = __byte_perm(y.x, y.z, 0x7632);
+        qb[nb][w][3] = __byte_perm(y.y, y.w, 0x7632);
+      }
+      qs += __shfl_xor_sync(0xffffffffu, qs, 1);
+      qs += __shfl_xor_sync(0xffffffffu, qs, 2);
+      qsk[nb][0] = p.scale_log2 * __shfl_sync(0xffffffffu, qs, 8 * c);
+      qsk[nb][1] = p.scale_log2 * __shfl_sync(0xffffffffu, qs, 8 * c + 4);
+    }
+    const float ks24 = p.scale_log2 * 16777216.f;
+    __syncthreads();   // rows' views written
+    // tokens that every row sees: those below `ctx`, from the last row's window on or in the sinks
+    int low = 0;
+    for (int r = 0; r < rows; ++r) low = max(low, row_s[r].low);
+
+    const int nstep = v1 - v0;
+    auto token_of = [&](int i) {   // first token of this warp's step i
+      const int v = v0 + i;
+      return (v < s.front ? v : v + s.skip) * UNIT + 16 * warp;
+    };
+    const int32_t* table = a.table + (int64_t)b * a.table_width;
+    // Lane k holds the place in the page arrays of the warp's step 32 j + k (of
+    // head hk, in tokens; -1: no token): one look-up for 32 steps.
+    int64_t place = -1;
+    const uint32_t ring = smem_u32(ring_s[warp]);
+    auto issue = [&](int i) {   // copies of step i (an empty group past the end keeps the count)
+      if (i < nstep) {
+        if ((i & 31) == 0) {
+          place = -1;
+          if (i + lane < nstep) {
+            const int t = token_of(i + lane);
+            if (t < s.n) place = (tree_page(a, table, t, p.shift) * a.Hkv + hk) * a.page_size + (t & (a.page_size - 1));
+          }
+        }
+        const int64_t at = __shfl_sync(0xffffffffu, place, i & 31);
+        const uint32_t st = ring + (uint32_t)(i % kOwnStages) * Ring::STAGE;
+        if (at >= 0) {
+          const uint8_t* kr = a.k_codes + at * (D / 2);
+          const uint8_t* vr = a.v_codes + at * (D / 2);
+#pragma unroll
+          for (int k = 0; k < D / 64; ++k) {
+            const int piece = lane + 32 * k;
+            own_copy16(st + piece * 16, kr + piece * 16);
+            own_copy16(st + Ring::KB + Ring::value_at(piece / Ring::CPR, piece % Ring::CPR), vr + piece * 16);
+          }
+          if (lane < 16) own_copy16(st + 2 * Ring::KB + lane * 16, a.scales + (at + lane) * 4);
+        }
+      }
+      asm volatile("cp.async.commit_group;\n" ::: "memory");
+    };
+
+    float o[NB][NM][4], m[NB][2], off[NB][2], l[NB][2], z[NB][2];   // m: M
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int mu = 0; mu < NM; ++mu) o[nb][mu][0] = o[nb][mu][1] = o[nb][mu][2] = o[nb][mu][3] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) m[nb][e] = -INFINITY, off[nb][e] = l[nb][e] = z[nb][e] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kOwnStages - 1; ++i) issue(i);
+    for (int i = 0; i < nstep; ++i) {
+      asm volatile("cp.async.wait_group %0;\n" ::"n"(kOwnStages - 2) : "memory");
+      __syncwarp();   // step i has landed for every lane, and step i - 1's stage has been read
+      issue(i + kOwnStages - 1);
+      const int t0 = token_of(i);
+      if (t0 >= s.n) continue;   // (nothing was copied)
+      const uint8_t* st = ring_s[warp] + (i % kOwnStages) * Ring::STAGE;
+      uint32_t kx[2][KW], vx[4][VW];
+      float4 sc[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t* kr = st + (g + 8 * h) * (D / 2) + c * (D / 8);
+        if constexpr (KW == 4) {
+          const uint4 w = *reinterpret_cast<const uint4*>(kr);
+          kx[h][0] = w.x, kx[h][1] = w.y, kx[h][2] = w.z, kx[h][3] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(kr);
+          kx[h][0] = w.x, kx[h][1] = w.y;
+        }
+        sc[h] = *reinterpret_cast<const float4*>(st + 2 * Ring::KB + (g + 8 * h) * 16);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = 8 * (q >> 1) + 2 * c + (q & 1);
+        const uint8_t* vr = st + Ring::KB + Ring::value_at(row, g * (D / 16) / 16) + g * (D / 16) % 16;
+        if constexpr (VW == 2) {
+          const uint2 w = *reinterpret_cast<const uint2*>(vr);
+          vx[q][0] = w.x, vx[q][1] = w.y;
+        } else {
+          vx[q][0] = *reinterpret_cast<const uint32_t*>(vr);
+        }
+      }
+      float sa[NB][4] = {}, s16[NB][4] = {};
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const uint32_t x0 = kx[0][w], x1 = kx[1][w], y0 = x0 >> 8, y1 = x1 >> 8;
+        const uint32_t a0[4] = {x0 & 0x000F000Fu, x1 & 0x000F000Fu, y0 & 0x000F000Fu, y1 & 0x000F000Fu};
+        const uint32_t a1[4] = {x0 & 0x00F000F0u, x1 & 0x00F000F0u, y0 & 0x00F000F0u, y1 & 0x00F000F0u};
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          mma_16816_f16_f32_acc(sa[nb], a0, qb[nb][w][0], qb[nb][w][1]);
+          mma_16816_f16_f32_acc(s16[nb], a1, qb[nb][w][2], qb[nb][w][3]);
+        }
+      }
+      // t = s + log2 alpha' (base 2) of tokens g, g + 8 for rows 8 nb + 2c, + 1
+      float t[NB][2][2], rv[2], vz[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float ka = ks24 * sc[h].x;
+        const float va = value_scale(sc[h].z), la = log2_of_scale(va);
+        rv[h] = one_over_scale(va);
+        vz[h] = fmaf(rv[h], sc[h].w, 8.f);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            t[nb][h][e] = fmaf(ka, fmaf(0.0625f, s16[nb][2 * h + e], sa[nb][2 * h + e]), fmaf(sc[h].y, qsk[nb][e], la));
+      }
+      // Not every row sees every token: -inf, and no share of the sums, whose factors may
+      // be anything (a slot that was never written, a page given back).
+      uint32_t hidden = 0;   // bit 4 nb + 2 h + e
+      if (t0 + 16 > s.ctx || (t0 < low && t0 + 16 > a.sinks)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const TreeRow& r = row_s[8 * nb + 2 * c + e];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (!tree_sees(p, s, r, t0 + g + 8 * h)) {
+                hidden |= 1u << (4 * nb + 2 * h + e);
+                t[nb][h][e] = -INFINITY;
+              }
+          }
+      }
+      bool grow = false;
+      float mx[NB][2];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          mx[nb][e] = fmaxf(t[nb][0][e], t[nb][1][e]);
+          grow |= mx[nb][e] > m[nb][e] + kAttnSlack;
+        }
+      if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          float f[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) mx[nb][e] = fmaxf(mx[nb][e], __shfl_xor_sync(0xffffffffu, mx[nb][e], w));
+            const float mn = mx[nb][e] > m[nb][e] + kAttnSlack ? mx[nb][e] : m[nb][e];
+            const float to = mn == -INFINITY ? 0.f : mn;
+            f[e] = m[nb][e] == -INFINITY ? 0.f : attn_exp2(off[nb][e] - to);
+            // (a sum so far that is not a number stays one)
+            if (m[nb][e] == -INFINITY && l[nb][e] != l[nb][e]) f[e] = 1.f;
+            m[nb][e] = mn;
+            off[nb][e] = to;
+            l[nb][e] *= f[e];
+            z[nb][e] *= f[e];
+          }
+#pragma unroll
+          for (int mu = 0; mu < NM; ++mu) {
+            o[nb][mu][0] *= f[0], o[nb][mu][2] *= f[0];
+            o[nb][mu][1] *= f[1], o[nb][mu][3] *= f[1];
+          }
+        }
+      }
+      // the weights as two fp16 parts, the second what the first leaves: with one part the
+      // few weights that carry a row would all but double its error
+      uint32_t p0[NB][2], p1[NB][2];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float w[2][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            w[h][e] = attn_exp2(t[nb][h][e] - off[nb][e]);
+            const bool seen = !((hidden >> (4 * nb + 2 * h + e)) & 1u);
+            l[nb][e] = fmaf(w[h][e], seen ? rv[h] : 0.f, l[nb][e]);
+            z[nb][e] = fmaf(w[h][e], seen ? vz[h] : 0.f, z[nb][e]);
+          }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t hi = pack_half2_bits(w[h][0], w[h][1]);
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+          p0[nb][h] = own_transpose(hi);
+          p1[nb][h] = own_transpose(pack_half2_bits(w[h][0] - f.x, w[h][1] - f.y));
+        }
+      }
+#pragma unroll
+      for (int vw = 0; vw < VW; ++vw)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          // two bytes of two tokens' rows: one dimension of both in a pair
+          const uint32_t xa = __byte_perm(vx[0][vw], vx[1][vw], q ? 0x7632 : 0x5410);
+          const uint32_t xb = __byte_perm(vx[2][vw], vx[3][vw], q ? 0x7632 : 0x5410);
+          const uint4 ya = code_pairs(xa), yb = code_pairs(xb);
+          const uint32_t a0[4] = {ya.x, ya.y, yb.x, yb.y}, a1[4] = {ya.z, ya.w, yb.z, yb.w};
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q], a0, p0[nb][0], p0[nb][1]);
+            mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q + 1], a1, p0[nb][0], p0[nb][1]);
+            mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q], a0, p1[nb][0], p1[nb][1]);
+            mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q + 1], a1, p1[nb][0], p1[nb][1]);
+          }
+        }
+    }
+    // join the lanes' shares, then the warps
+    asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+    __syncwarp();   // the ring is free
+    float* o_w = reinterpret_cast<float*>(ring_s[warp]);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float ls = l[nb][e], zs = z[nb][e];
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) {
+          ls += __shfl_xor_sync(0xffffffffu, ls, w);
+          zs += __shfl_xor_sync(0xffffffffu, zs, w);
+        }
+        const int r = 8 * nb + 2 * c + e;
+#pragma unroll
+        for (int mu = 0; mu < NM; ++mu) {
+          o_w[r * D + g * (D / 8) + 2 * mu] = o[nb][mu][e] + zs;
+          o_w[r * D + g * (D / 8) + 2 * mu + 1] = o[nb][mu][2 + e] + zs;
+        }
+        if (g == 0) {
+          m_s[warp][r] = m[nb][e];
+          l_s[warp][r] = ls;
+        }
+      }
+    __syncthreads();
+    const bool whole = v0 == 0 && v1 == s.units;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (v0 == 0 ? 1 : 0);
+    for (int i = tid; i < rows * (D / 4); i += kRowsWarps * 32) {   // four values of a row
+      const int r = i / (D / 4), d = i % (D / 4) * 4;
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kRowsWarps; ++w) M = fmaxf(M, m_s[w][r]);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      float ls = 0.f;
+#pragma unroll
+      for (int w = 0; w < kRowsWarps; ++w) {
+        const float lw = l_s[w][r];
+        if (lw == 0.f) continue;
+        const float f = attn_exp2(m_s[w][r] - M);
+        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring_s[w]) + r * D + d);
+        v.x = fmaf(f, y.x, v.x), v.y = fmaf(f, y.y, v.y), v.z = fmaf(f, y.z, v.z), v.w = fmaf(f, y.w, v.w);
+        ls = fmaf(f, lw, ls);
+      }
+      if (whole) {
+        const float inv = ls != 0.f ? 1.f / ls : 0.f;
+        *reinterpret_cast<uint2*>(reinterpret_cast<__half*>(a.out) + row_at(r) * D + d) =
+            make_uint2(pack_half2_bits(v.x * inv, v.y * inv), pack_half2_bits(v.z * inv, v.w * inv));
+      } else {
+        *reinterpret_cast<float4*>(p.o + (slot * ROWS + r) * D + d) = v;
+        if (d == 0) p.ml[slot * ROWS + r] = make_float2(M, ls);
+      }
+    }
+    __syncthreads();   // the ring and the rows' views serve the next job
+  }
+}
+
+// Joins the parts of a job that several CTAs share.  Block (c, y): the job that
+// the runs' border c cuts first, rows 8 y .. 8 y + 7; a thread has four values of a row.
+template <int D>
+__global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const TreeParams p) {
+  static_assert(kCombineThreads * 4 >= 8 * D, "a thread per four values");
+  const TreeArgs& a = p.a;
+  const int c = blockIdx.x + 1;
+  // (the attention kernel started behind what wrote the lengths, and this one behind its start)
+  const TreeRun run = tree_run<kCombineThreads>(p, c);
+  pdl_wait();
+  pdl_trigger();
+  if (c >= run.ctas) return;
+  const TreeSeq s = tree_seq(p, run.b);
+  const int64_t job = (run.x0 - run.base) / s.units;
+  const int64_t begin = run.base + job * s.units, end = begin + s.units;
+  if (run.x0 == begin || tree_bound(run.all, c - 1, run.ctas) > begin) return;   // no job cut, or cut before
+  const int hk = (int)(job / s.rts), r = blockIdx.y * 8 + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
+  const int row = (int)(job - (int64_t)hk * s.rts) * p.rows + r;
+  if (threadIdx.x >= 8 * (D / 4) || row >= s.nq * p.G) return;
+  // parts: the one that CTA c - 1 left, then those that c, c + 1, .. continued
+  auto slot = [&](int i) { return (int64_t)(i < c ? 2 * i + 1 : 2 * i) * p.rows + r; };
+  int last = c;
+  while (last + 1 < run.ctas && tree_bound(run.all, last + 1, run.ctas) < end) ++last;
+  float M = -INFINITY;
+#pragma unroll 4
+  for (int i = c - 1; i <= last; ++i) {
+    const float2 x = p.ml[slot(i)];
+    if (x.y != 0.f) M = fmaxf(M, x.x);
+  }
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  float l = 0.f;
+#pragma unroll 4
+  for (int i = c - 1; i <= last; ++i) {
+    const float2 x = p.ml[slot(i)];
+    const float4 y = *reinterpret_cast<const float4*>(p.o + slot(i) * D + d);
+    if (x.y != 0.f) {
+      const float f = attn_exp2(x.x - M);
+      v.x = fmaf(f, y.x, v.x), v.y = fmaf(f, y.y, v.y), v.z = fmaf(f, y.z, v.z), v.w = fmaf(f, y.w, v.w);
+      l = fmaf(f, x.y, l);
+    }
+  }
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+  const int node = row / p.G, head = row - node * p.G;
+  *reinterpret_cast<uint2*>(reinterpret_cast<__half*>(a.out) + ((s.q0 + node) * a.Hq + (int64_t)hk * p.G + head) * D + d) =
+      make_uint2(pack_half2_bits(v.x * inv, v.y * inv), pack_half2_bits(v.z * inv, v.w * inv));
+}
+
+int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
+
+// The variant for these sizes and its grid.
+struct TreePlan {
+  int rows, unit, ctas, least;
+};
+TreePlan tree_plan(const TreeArgs& a) {
+  TreePlan t;
+  const int64_t rows = a.max_q * (a.Hq / a.Hkv);
+  t.rows = rows <= 8 ? 8 : 16;
+  t.unit = 16 * kRowsWarps;
+  t.ctas = device_sm_count() * (t.rows == 8 ? 4 : 3);
+  t.least = 2;
+  return t;
+}
+
+template <int D>
+cudaError_t launch_t(const TreeArgs& a, cudaStream_t stream) {
+  const TreePlan t = tree_plan(a);
+  TreeParams p{};
+  p.a = a;
+  p.G = (int)(a.Hq / a.Hkv);
+  while ((1 << p.shift) < a.page_size) ++p.shift;
+  p.ctas = t.ctas;
+  p.rows = t.rows;
+  p.unit = t.unit;
+  p.least = t.least;
+  p.scale_log2 = a.scale * kAttnLog2e;
+  p.ml = static_cast<float2*>(a.workspace);
+  p.o = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256((int64_t)2 * t.ctas * t.rows * 8));
+  auto kernel = t.rows == 8 ? tree_rows_kernel<D, 1> : tree_rows_kernel<D, 2>;
+  cudaError_t e = launch_pdl(kernel, dim3((unsigned)t.ctas), dim3(kRowsWarps * 32), 0, stream, 1, p);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(tree_combine_kernel<D>, dim3((unsigned)(t.ctas - 1), (unsigned)(t.rows / 8)), dim3(kCombineThreads), 0, stream, 1, p);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+int64_t tree_attention_workspace(const TreeArgs& a) {
+  const TreePlan t = tree_plan(a);
+  return align256((int64_t)2 * t.ctas * t.rows * 8) + (int64_t)2 * t.ctas * t.rows * a.D * 4;
+}
+
+cudaError_t launch_tree_attention(const TreeArgs& a, cudaStream_t stream) {
+  if (a.D == 128) return launch_t<128>(a, stream);
+  if (a.D == 64) return launch_t<64>(a, stream);
+  return cudaErrorNotSupported;
+}
+
+}  // namespace spinq

@@ -44,6 +44,8 @@ EXPORTED = (
     "spinq_rotated_linear", "spinq_debug_set_wait_limit_ns", "spinq_debug_fail_launches",
     "spinq_debug_stall_launches", "spinq_kv4_append", "spinq_kv4_read", "spinq_prompt_attention_workspace_bytes",
     "spinq_prompt_attention", "spinq_prefix_attention_workspace_bytes", "spinq_prefix_attention_kv4",
+    "spinq_kv4_plan", "spinq_kv4_keep", "spinq_window_prompt_attention", "spinq_tree_attention_workspace_bytes",
+    "spinq_tree_attention_kv4", "spinq_window_attention_kv4",
 )
 SPINQ_FMT_INT8_PLANES, SPINQ_FMT_E4M3, SPINQ_FMT_INT4_BYTES = 1, 2, 3
 
@@ -162,6 +164,22 @@ _lib.spinq_prefix_attention_workspace_bytes.restype = ctypes.c_int64
 _lib.spinq_prefix_attention_workspace_bytes.argtypes = [_I64, _I64, _I64, ctypes.c_int32, _I64, _I64, _I64]
 _lib.spinq_prefix_attention_kv4.restype = ctypes.c_int
 _lib.spinq_prefix_attention_kv4.argtypes = [_P, ctypes.POINTER(Kv4PagesCfg), _P, _I64, _P, _I64, _P, _I64, _I64,
+                                            ctypes.c_float, _P, _P, _I64, _P]
+_lib.spinq_kv4_plan.restype = ctypes.c_int
+_lib.spinq_kv4_plan.argtypes = [_P, _P, _P, _I64, _P, _I64, ctypes.c_int32, _P, _P, _I64, _P, _I64, _I64, _P, _P, _P, _P,
+                                _P]
+_lib.spinq_kv4_keep.restype = ctypes.c_int
+_lib.spinq_kv4_keep.argtypes = [ctypes.POINTER(Kv4PagesCfg), _P, _I64, _I64, _P, _P, _I64, _P, _P]
+_lib.spinq_window_prompt_attention.restype = ctypes.c_int
+_lib.spinq_window_prompt_attention.argtypes = [_P, _I64, _P, _I64, _P, _I64, _P, _P] + [_I64] * 10 + [
+    ctypes.c_float, _P, _P]
+_lib.spinq_tree_attention_workspace_bytes.restype = ctypes.c_int64
+_lib.spinq_tree_attention_workspace_bytes.argtypes = [_I64, _I64, _I64, ctypes.c_int32, _I64, _I64, _I64]
+_lib.spinq_tree_attention_kv4.restype = ctypes.c_int
+_lib.spinq_tree_attention_kv4.argtypes = [_P, ctypes.POINTER(Kv4PagesCfg), _P, _I64, _P, _P, _P] + [_I64] * 6 + [
+    ctypes.c_float, _P, _P, _I64, _P]
+_lib.spinq_window_attention_kv4.restype = ctypes.c_int
+_lib.spinq_window_attention_kv4.argtypes = [_P, ctypes.POINTER(Kv4PagesCfg), _P, _I64, _P, _I64, _I64, _I64, _I64,
                                             ctypes.c_float, _P, _P, _I64, _P]
 
 
@@ -283,6 +301,38 @@ def spinq_prefix_attention_kv4(q, cache, prefix_table, prefix_len, page_table, t
                                ws, ws_bytes, stream) -> int:
     return _lib.spinq_prefix_attention_kv4(q, cache, prefix_table, prefix_len, page_table, table_width, lens, B, Hq,
                                            scale, out, ws, ws_bytes, stream)
+
+
+def spinq_kv4_plan(lens, drop, add, batch, page_table, table_width, page_size, free_pages, free_count, free_capacity,
+                   depths, position_offset, total, cu_tokens, positions, slots, granted, stream) -> int:
+    return _lib.spinq_kv4_plan(lens, drop, add, batch, page_table, table_width, page_size, free_pages, free_count,
+                               free_capacity, depths, position_offset, total, cu_tokens, positions, slots, granted, stream)
+
+
+def spinq_kv4_keep(cache, page_table, batch, table_width, starts, path, path_width, counts, stream) -> int:
+    return _lib.spinq_kv4_keep(cache, page_table, batch, table_width, starts, path, path_width, counts, stream)
+
+
+def spinq_window_prompt_attention(q, ldq, k, ldk, v, ldv, cu_q, cu_k, batch, total_q, total_k, max_q, max_k, Hq, Hkv, D,
+                                  window, sinks, scale, out, stream) -> int:
+    return _lib.spinq_window_prompt_attention(q, ldq, k, ldk, v, ldv, cu_q, cu_k, batch, total_q, total_k, max_q, max_k,
+                                              Hq, Hkv, D, window, sinks, scale, out, stream)
+
+
+def spinq_tree_attention_workspace_bytes(B, max_q, table_width, page_size, Hq, Hkv, D) -> int:
+    return int(_lib.spinq_tree_attention_workspace_bytes(B, max_q, table_width, page_size, Hq, Hkv, D))
+
+
+def spinq_tree_attention_kv4(q, cache, page_table, table_width, lens, cu_q, parents, B, total_q, max_q, Hq, window,
+                             sinks, scale, out, ws, ws_bytes, stream) -> int:
+    return _lib.spinq_tree_attention_kv4(q, cache, page_table, table_width, lens, cu_q, parents, B, total_q, max_q, Hq,
+                                         window, sinks, scale, out, ws, ws_bytes, stream)
+
+
+def spinq_window_attention_kv4(q, cache, page_table, table_width, lens, B, Hq, window, sinks, scale, out, ws, ws_bytes,
+                               stream) -> int:
+    return _lib.spinq_window_attention_kv4(q, cache, page_table, table_width, lens, B, Hq, window, sinks, scale, out, ws,
+                                           ws_bytes, stream)
 
 
 def spinq_debug_set_wait_limit_ns(ns: int) -> int:
@@ -849,4 +899,140 @@ def prefix_attention_kv4(q: torch.Tensor, cache: KV4Pages, prefix_table: torch.T
                                            _full(page_table, _I32, (B, width), dev), width,
                                            _full(lens, _I32, (B,), dev), B, Hq, D ** -0.5 if scale is None else scale,
                                            out_ptr, ws, need, queue), "spinq_prefix_attention_kv4")
+    return out
+
+
+@dataclass
+class KV4Plan:
+    """A step's tokens, as ``kv4_plan`` lays them out (spinq_kv4_plan in include/spinq.h)."""
+    cu_tokens: torch.Tensor   # int32 [B + 1]: rows of each sequence's new tokens
+    positions: torch.Tensor   # int32 [total]
+    slots: torch.Tensor       # int64 [total]; -1: not to be written
+    granted: torch.Tensor     # int32 [B]; 0: the sequence's tokens have no pages
+
+
+def kv4_plan(lens: torch.Tensor, add: Optional[torch.Tensor], page_table: torch.Tensor, free_pages: torch.Tensor,
+             free_count: torch.Tensor, page_size: int, total: int, drop: Optional[torch.Tensor] = None,
+             depths: Optional[torch.Tensor] = None, position_offset: int = 0, plan: Optional[KV4Plan] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> KV4Plan:
+    """Drops the last ``drop`` [B] tokens of each sequence and makes room for ``add``
+    [B] more: ``lens`` [B], ``page_table`` [B, W], the stack ``free_pages`` [N] and
+    ``free_count`` [1] (all int32) are updated in place; returns positions and slots of the
+    new tokens, ``total`` rows of them (``depths`` [total]: places of a tree's nodes)."""
+    dev, queue = _queue(lens, stream)
+    B, W = page_table.shape
+    optional = lambda x, shape: None if x is None else _full(x, _I32, shape, dev)   # noqa: E731
+    if plan is None:
+        plan = KV4Plan(*(_empty(n, t, lens.device, stream) for n, t in ((B + 1, _I32), (total, _I32), (total, _I64T), (B, _I32))))
+    _check(_lib.spinq_kv4_plan(_full(lens, _I32, (B,), dev), optional(drop, (B,)), optional(add, (B,)), B,
+                               _full(page_table, _I32, (B, W), dev), W, page_size,
+                               _full(free_pages, _I32, (free_pages.numel(),), dev), _full(free_count, _I32, (1,), dev),
+                               free_pages.numel(), optional(depths, (total,)), position_offset, total,
+                               _full(plan.cu_tokens, _I32, (B + 1,), dev), _full(plan.positions, _I32, (total,), dev),
+                               _full(plan.slots, _I64T, (total,), dev), _full(plan.granted, _I32, (B,), dev), queue),
+           "spinq_kv4_plan")
+    return plan
+
+
+def kv4_keep(cache: KV4Pages, page_table: torch.Tensor, starts: torch.Tensor, path: torch.Tensor, counts: torch.Tensor,
+             stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Moves token ``starts[b] + path[b, i]`` of every sequence to ``starts[b] + i``,
+    i < ``counts[b]``: the accepted path of a drafted tree (``path`` [B, n] ascends; int32)."""
+    dev, queue = _queue(cache.k_codes, stream)
+    pages = _pages(cache, dev)
+    batch, width = page_table.shape
+    n = path.shape[1]
+    _check(_lib.spinq_kv4_keep(pages, _full(page_table, _I32, (batch, width), dev), batch, width,
+                               _full(starts, _I32, (batch,), dev), _full(path, _I32, (batch, n), dev), n,
+                               _full(counts, _I32, (batch,), dev), queue), "spinq_kv4_keep")
+
+
+def window_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor,
+                            max_q: int, max_k: int, window: int, sinks: int = 0, scale: Optional[float] = None,
+                            out: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """``prompt_attention`` (causal) where a query sees the last ``window`` positions,
+    its own among them, and the first ``sinks`` tokens."""
+    Tq, Hq, D = q.shape
+    Tk, Hkv, _ = k.shape
+    dev, queue = _queue(q, stream)
+    if k.shape != v.shape or k.shape[2] != D:
+        _refuse("queries, keys and values differ in shape")
+    batch = cu_q.shape[0] - 1
+    if out is None:
+        out = _empty((Tq, Hq, D), _F16, q.device, stream)
+        out_ptr = out.data_ptr()
+    else:
+        out_ptr = _full(out, _F16, (Tq, Hq, D), dev)
+    _check(_lib.spinq_window_prompt_attention(q.data_ptr(), _token_rows(q, dev), k.data_ptr(), _token_rows(k, dev),
+                                              v.data_ptr(), _token_rows(v, dev), _full(cu_q, _I32, (batch + 1,), dev),
+                                              _full(cu_k, _I32, (batch + 1,), dev), batch, Tq, Tk, max_q, max_k, Hq, Hkv,
+                                              D, window, sinks, D ** -0.5 if scale is None else scale, out_ptr, queue),
+           "spinq_window_prompt_attention")
+    return out
+
+
+def _tree_space(workspace: Optional[torch.Tensor], B: int, max_q: int, width: int, pages: Kv4PagesCfg, Hq: int, dev: int,
+                device, stream: Optional[torch.cuda.Stream]):
+    """The workspace of the two calls below (kept alive by the caller), its address and bytes."""
+    if workspace is None:
+        need = _lib.spinq_tree_attention_workspace_bytes(B, max_q, width, pages.page_size, Hq, pages.kv_heads, pages.head_dim)
+        if need == 0:
+            return None, None, 0
+        workspace = _empty(need, _U8, device, stream)
+        return workspace, workspace.data_ptr(), need
+    return (workspace,) + _space(workspace, dev)
+
+
+def tree_attention_kv4(q: torch.Tensor, cache: KV4Pages, page_table: torch.Tensor, lens: torch.Tensor, cu_q: torch.Tensor,
+                       max_q: int, parents: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0,
+                       scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention of drafted tokens q [T, Hq, D] (rotated) over the paged cache: the
+    last cu_q[b + 1] - cu_q[b] of a sequence's ``lens`` [B] tokens, each over the context,
+    its ancestors by ``parents`` [T] (within the sequence, -1: none; None: a chain)
+    and itself.  ``window`` and ``sinks`` as window_prompt_attention, by depth."""
+    T, Hq, D = q.shape
+    dev, queue = _queue(q, stream)
+    pages = _pages(cache, dev)
+    B, width = page_table.shape
+    if D != pages.head_dim:
+        _refuse("queries and pages differ in head_dim")
+    if out is None:
+        out = _empty((T, Hq, D), _F16, q.device, stream)
+        out_ptr = out.data_ptr()
+    else:
+        out_ptr = _full(out, _F16, (T, Hq, D), dev)
+    workspace, ws, size = _tree_space(workspace, B, max_q, width, pages, Hq, dev, q.device, stream)
+    _check(_lib.spinq_tree_attention_kv4(_full(q, _F16, (T, Hq, D), dev), pages, _full(page_table, _I32, (B, width), dev),
+                                         width, _full(lens, _I32, (B,), dev), _full(cu_q, _I32, (B + 1,), dev),
+                                         None if parents is None else _full(parents, _I32, (T,), dev), B, T, max_q, Hq,
+                                         window, sinks, D ** -0.5 if scale is None else scale, out_ptr, ws, size, queue),
+           "spinq_tree_attention_kv4")
+    return out
+
+
+def window_attention_kv4(q: torch.Tensor, cache: KV4Pages, page_table: torch.Tensor, lens: torch.Tensor, window: int = 0,
+                         sinks: int = 0, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Decode attention of q [B, Hq, D] (rotated), the last of each sequence's ``lens``
+    [B] tokens, over the last ``window`` (0: all) and the first ``sinks`` of them."""
+    B, Hq, D = q.shape
+    dev, queue = _queue(q, stream)
+    pages = _pages(cache, dev)
+    width = page_table.shape[1]
+    if D != pages.head_dim:
+        _refuse("queries and pages differ in head_dim")
+    if out is None:
+        out = _empty((B, Hq, D), _F16, q.device, stream)
+        out_ptr = out.data_ptr()
+    else:
+        out_ptr = _full(out, _F16, (B, Hq, D), dev)
+    workspace, ws, size = _tree_space(workspace, B, 1, width, pages, Hq, dev, q.device, stream)
+    _check(_lib.spinq_window_attention_kv4(_full(q, _F16, (B, Hq, D), dev), pages, _full(page_table, _I32, (B, width), dev),
+                                           width, _full(lens, _I32, (B,), dev), B, Hq, window, sinks,
+                                           D ** -0.5 if scale is None else scale, out_ptr, ws, size, queue),
+           "spinq_window_attention_kv4")
     return out
