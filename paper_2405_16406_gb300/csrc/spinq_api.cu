@@ -765,7 +765,7 @@ spinq_status spinq_debug_set_wait_limit_ns(int64_t ns) {
   const uint64_t v = (uint64_t)ns;
   if (set_wait_limit_paley(v) != cudaSuccess || set_wait_limit_gemm(v) != cudaSuccess ||
       set_wait_limit_fp8(v) != cudaSuccess || set_wait_limit_prompt(v) != cudaSuccess ||
-      set_wait_limit_prefix(v) != cudaSuccess)
+      set_wait_limit_prefix(v) != cudaSuccess || set_wait_limit_tree(v) != cudaSuccess)
     return SPINQ_ECUDA;
   return SPINQ_OK;
 }

@@ -26,152 +26,13 @@
 #include "kv4_attn.cuh"
 #include "launch_util.h"
 #include "spinq_internal.h"
+#include "tree_attention.cuh"
 
 namespace spinq {
 namespace {
 
-constexpr int kTreeNodes = 128;   // queries of a sequence at most
 constexpr int kRowsWarps = 4;
 constexpr int kCombineThreads = 256;
-
-struct TreeParams {
-  TreeArgs a;
-  int G, shift;
-  int ctas;           // of the attention kernel's grid
-  int rows, unit;     // of a job; tokens
-  int least;          // units a CTA gets at least
-  float scale_log2;
-  float* o;           // [2 * ctas][rows][D]: of CTA c the job it continues (2 c) and the one it leaves (2 c + 1)
-  float2* ml;         // [2 * ctas][rows]: M, and sum of w / alpha'
-};
-
-// What the lengths say of a sequence.
-struct TreeSeq {
-  int n, nq, ctx;     // tokens, queries, tokens before the queries' own (below 0: the first queries have none)
-  int64_t q0;
-  int front, skip;    // units of sinks; units left out behind them
-  int units, rts, jobs;
-};
-
-__device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
-  const TreeArgs& a = p.a;
-  TreeSeq s;
-  s.n = (int)min((int64_t)max(__ldg(a.lens + b), 0), a.table_width << p.shift);
-  s.q0 = b;
-  s.nq = 1;
-  if (a.cu_q) {
-    s.q0 = max(__ldg(a.cu_q + b), 0);
-    s.nq = (int)max((int64_t)0, min(min((int64_t)__ldg(a.cu_q + b + 1), a.total_q) - s.q0, a.max_q));
-  }
-  s.ctx = s.n - s.nq;
-  const int reach = a.window > 0 && s.ctx >= a.window ? (int)((s.ctx - a.window + 1) / p.unit) : 0;
-  s.front = (int)min((a.sinks + p.unit - 1) / p.unit, (int64_t)reach);
-  s.skip = reach - s.front;
-  s.units = max(1, (s.n + p.unit - 1) / p.unit - s.skip);   // one at least: a sequence without tokens has rows too
-  s.rts = (s.nq * p.G + p.rows - 1) / p.rows;
-  s.jobs = s.rts * (int)a.Hkv;
-  return s;
-}
-
-// Where run c of the units lies: [x0, x1) of all, x0 in sequence b, whose units begin at `base`.
-struct TreeRun {
-  int64_t all, x0, x1, base;
-  int ctas;   // runs that there are
-  int b;
-};
-__device__ __forceinline__ int64_t tree_bound(int64_t all, int c, int ctas) { return all * c / ctas; }
-
-template <int THREADS>
-__device__ __forceinline__ TreeRun tree_run(const TreeParams& p, int c) {
-  __shared__ int64_t sums[THREADS / 32], found[2];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = (int)p.a.B;
-  const int per = (B + THREADS - 1) / THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
-  int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    const TreeSeq s = tree_seq(p, b);
-    mine += (int64_t)s.units * s.jobs;
-  }
-  int64_t sum = mine;
-#pragma unroll
-  for (int w = 1; w < 32; w <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, sum, w);
-    if (lane >= w) sum += y;
-  }
-  if (lane == 31) sums[warp] = sum;
-  __syncthreads();
-  TreeRun r;
-  int64_t at = sum - mine;
-  r.all = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) {
-    if (w == warp) at += r.all;
-    r.all += sums[w];
-  }
-  r.ctas = (int)min((int64_t)p.ctas, (r.all + p.least - 1) / p.least);
-  r.x0 = r.x1 = r.base = 0;
-  r.b = B;
-  if (c < r.ctas) {
-    r.x0 = tree_bound(r.all, c, r.ctas);
-    r.x1 = tree_bound(r.all, c + 1, r.ctas);
-    if (at <= r.x0 && r.x0 < at + mine) {
-      int b = b0;
-      for (; b < b1 - 1; ++b) {
-        const TreeSeq s = tree_seq(p, b);
-        const int64_t t = (int64_t)s.units * s.jobs;
-        if (r.x0 < at + t) break;
-        at += t;
-      }
-      found[0] = b;
-      found[1] = at;
-    }
-    __syncthreads();
-    r.b = (int)found[0];
-    r.base = found[1];
-  }
-  return r;
-}
-
-// A row's view of the keys.
-struct TreeRow {
-  uint32_t line[4];   // its ancestors that it sees, and itself
-  int low;            // first context token that its window reaches
-};
-
-// The queries' parents in shared memory (all threads), then a thread's row of them.
-__device__ __forceinline__ void tree_parents(const TreeParams& p, const TreeSeq& s, int* parent, int threads) {
-  for (int i = threadIdx.x; i < s.nq; i += threads) parent[i] = p.a.parents ? __ldg(p.a.parents + s.q0 + i) : i - 1;
-}
-__device__ __forceinline__ TreeRow tree_row(const TreeParams& p, const TreeSeq& s, const int* parent, int node) {
-  auto up = [&](int i) {   // (a parent comes before its node; any other number: none)
-    const int x = parent[i];
-    return x >= 0 && x < i ? x : -1;
-  };
-  TreeRow r;
-  int depth = 0;
-  for (int i = up(node); i >= 0; i = up(i)) ++depth;
-  r.line[0] = r.line[1] = r.line[2] = r.line[3] = 0;
-  const int64_t window = p.a.window > 0 ? p.a.window : INT64_MAX;
-  for (int i = node, k = 0; i >= 0; i = up(i), ++k)
-    if (k < window || (int64_t)s.ctx + depth - k < p.a.sinks) {
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-        if (w == i >> 5) r.line[w] |= 1u << (i & 31);
-    }
-  r.low = p.a.window > 0 ? (int)max((int64_t)0, (int64_t)s.ctx + depth - p.a.window + 1) : 0;
-  return r;
-}
-
-__device__ __forceinline__ bool tree_sees(const TreeParams& p, const TreeSeq& s, const TreeRow& r, int t) {
-  if (t >= s.n) return false;
-  if (t < s.ctx) return t >= r.low || t < p.a.sinks;
-  const int i = t - s.ctx;
-  return (r.line[i >> 5] >> (i & 31)) & 1u;
-}
-
-__device__ __forceinline__ int64_t tree_page(const TreeArgs& a, const int32_t* table, int t, int shift) {
-  const int64_t page = __ldg(table + (t >> shift));
-  return page < 0 ? 0 : (page >= a.num_pages ? a.num_pages - 1 : page);
-}
 
 // ------------------------------------------------ few rows: warps and mma.sync
 // A job is 8 NB rows, a unit 64 tokens.  A warp takes 16 tokens of each unit,
@@ -193,33 +54,16 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   pdl_wait();
   pdl_trigger();
-  const TreeRun run = tree_run<kRowsWarps * 32>(p, blockIdx.x);
-  int b = run.b;
-  int64_t base = run.base;
-  for (int64_t x = run.x0; x < run.x1 && b < (int)a.B;) {
-    const TreeSeq s = tree_seq(p, b);
-    const int64_t in_seq = x - base;
-    if (in_seq >= (int64_t)s.units * s.jobs) {
-      base += (int64_t)s.units * s.jobs;
-      ++b;
-      continue;
-    }
-    const int job = (int)(in_seq / s.units), v0 = (int)(in_seq - (int64_t)job * s.units);
-    const int v1 = (int)min((int64_t)s.units, v0 + (run.x1 - x));
-    x += v1 - v0;
-    const int hk = job / s.rts, r0 = (job - hk * s.rts) * ROWS;   // first row of the group's
-    const int rows = min(ROWS, s.nq * p.G - r0);
-    auto row_at = [&](int r) {   // its place among [query][head] rows
-      const int node = (r0 + r) / p.G, head = r0 + r - node * p.G;
-      return (s.q0 + node) * a.Hq + (int64_t)hk * p.G + head;
-    };
-
+  TreeWalk walk(tree_run<kRowsWarps * 32>(p, blockIdx.x), blockIdx.x);
+  for (TreeJob j; walk.next(p, j);) {
+    const TreeSeq& s = j.s;
+    const int rows = j.rows;
     // what the rows see
     tree_parents(p, s, parent_s, kRowsWarps * 32);
     __syncthreads();
     if (tid < ROWS) {
       TreeRow r = {};
-      if (tid < rows) r = tree_row(p, s, parent_s, (r0 + tid) / p.G);
+      if (tid < rows) r = tree_row(p, s, parent_s, (j.r0 + tid) / p.G);
       row_s[tid] = r;
     }
     // query fragments (k order as the codes come), their sums.  A key
@@ -231,7 +75,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const int r = 8 * nb + g;
-      const __half* qh = reinterpret_cast<const __half*>(a.q) + (r < rows ? row_at(r) : row_at(0)) * D + c * (D / 4);
+      const __half* qh = reinterpret_cast<const __half*>(a.q) + j.row_at(p, r < rows ? r : 0) * D + c * (D / 4);
       float qs = 0.f;
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
@@ -259,12 +103,11 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
     int low = 0;
     for (int r = 0; r < rows; ++r) low = max(low, row_s[r].low);
 
-    const int nstep = v1 - v0;
+    const int nstep = j.v1 - j.v0;
     auto token_of = [&](int i) {   // first token of this warp's step i
-      const int v = v0 + i;
-      return (v < s.front ? v : v + s.skip) * UNIT + 16 * warp;
+      return j.token(j.v0 + i, UNIT) + 16 * warp;
     };
-    const int32_t* table = a.table + (int64_t)b * a.table_width;
+    const int32_t* table = a.table + (int64_t)j.b * a.table_width;
     // Lane k holds the place in the page arrays of the warp's step 32 j + k (of
     // head hk, in tokens; -1: no token): one look-up for 32 steps.
     int64_t place = -1;
@@ -275,7 +118,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
           place = -1;
           if (i + lane < nstep) {
             const int t = token_of(i + lane);
-            if (t < s.n) place = (tree_page(a, table, t, p.shift) * a.Hkv + hk) * a.page_size + (t & (a.page_size - 1));
+            if (t < s.n) place = (tree_page(a, table, t, p.shift) * a.Hkv + j.hk) * a.page_size + (t & (a.page_size - 1));
           }
         }
         const int64_t at = __shfl_sync(0xffffffffu, place, i & 31);
@@ -366,15 +209,15 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
       // Not every row sees every token: -inf, and no share of the sums, whose factors may
       // be anything (a slot that was never written, a page given back).
       uint32_t hidden = 0;   // bit 4 nb + 2 h + e
-      if (t0 + 16 > s.ctx || (t0 < low && t0 + 16 > a.sinks)) {
+      if (t0 + 16 > s.ctx || (t0 < low && t0 + 16 > p.sinks)) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const TreeRow& r = row_s[8 * nb + 2 * c + e];
+            const uint32_t bits = tree_sees(p, s, row_s[8 * nb + 2 * c + e], t0) >> g;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              if (!tree_sees(p, s, r, t0 + g + 8 * h)) {
+              if (!((bits >> (8 * h)) & 1u)) {
                 hidden |= 1u << (4 * nb + 2 * h + e);
                 t[nb][h][e] = -INFINITY;
               }
@@ -481,8 +324,8 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
         }
       }
     __syncthreads();
-    const bool whole = v0 == 0 && v1 == s.units;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (v0 == 0 ? 1 : 0);
+    const bool whole = j.whole();
+    const int64_t slot = j.slot(blockIdx.x);
     for (int i = tid; i < rows * (D / 4); i += kRowsWarps * 32) {   // four values of a row
       const int r = i / (D / 4), d = i % (D / 4) * 4;
       float M = -INFINITY;
@@ -501,7 +344,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
       }
       if (whole) {
         const float inv = ls != 0.f ? 1.f / ls : 0.f;
-        *reinterpret_cast<uint2*>(reinterpret_cast<__half*>(a.out) + row_at(r) * D + d) =
+        *reinterpret_cast<uint2*>(reinterpret_cast<__half*>(a.out) + j.row_at(p, r) * D + d) =
             make_uint2(pack_half2_bits(v.x * inv, v.y * inv), pack_half2_bits(v.z * inv, v.w * inv));
       } else {
         *reinterpret_cast<float4*>(p.o + (slot * ROWS + r) * D + d) = v;
@@ -525,16 +368,17 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
   pdl_trigger();
   if (c >= run.ctas) return;
   const TreeSeq s = tree_seq(p, run.b);
-  const int64_t job = (run.x0 - run.base) / s.units;
+  const int64_t x = run.bound(c), job = (x - run.base) / s.units;
   const int64_t begin = run.base + job * s.units, end = begin + s.units;
-  if (run.x0 == begin || tree_bound(run.all, c - 1, run.ctas) > begin) return;   // no job cut, or cut before
+  if (x == begin || run.bound(c - 1) > begin) return;   // no job cut, or cut before
+  const int rows = 1 << p.rows_log2;
   const int hk = (int)(job / s.rts), r = blockIdx.y * 8 + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
-  const int row = (int)(job - (int64_t)hk * s.rts) * p.rows + r;
+  const int row = ((int)(job - (int64_t)hk * s.rts) << p.rows_log2) + r;
   if (threadIdx.x >= 8 * (D / 4) || row >= s.nq * p.G) return;
   // parts: the one that CTA c - 1 left, then those that c, c + 1, .. continued
-  auto slot = [&](int i) { return (int64_t)(i < c ? 2 * i + 1 : 2 * i) * p.rows + r; };
+  auto slot = [&](int i) { return (int64_t)(i < c ? 2 * i + 1 : 2 * i) * rows + r; };
   int last = c;
-  while (last + 1 < run.ctas && tree_bound(run.all, last + 1, run.ctas) < end) ++last;
+  while (last + 1 < run.ctas && run.bound(last + 1) < end) ++last;
   float M = -INFINITY;
 #pragma unroll 4
   for (int i = c - 1; i <= last; ++i) {
@@ -555,7 +399,7 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
   }
   const float inv = l != 0.f ? 1.f / l : 0.f;
   const int node = row / p.G, head = row - node * p.G;
-  *reinterpret_cast<uint2*>(reinterpret_cast<__half*>(a.out) + ((s.q0 + node) * a.Hq + (int64_t)hk * p.G + head) * D + d) =
+  *reinterpret_cast<uint2*>(reinterpret_cast<__half*>(a.out) + ((int64_t)(s.q0 + node) * a.Hq + hk * p.G + head) * D + d) =
       make_uint2(pack_half2_bits(v.x * inv, v.y * inv), pack_half2_bits(v.z * inv, v.w * inv));
 }
 
@@ -563,17 +407,17 @@ int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
 // The variant for these sizes and its grid.
 struct TreePlan {
-  int rows, unit, ctas, least;
+  int rows_log2, unit_log2, ctas, least;
 };
 TreePlan tree_plan(const TreeArgs& a) {
-  TreePlan t;
   const int64_t rows = a.max_q * (a.Hq / a.Hkv);
-  t.rows = rows <= 8 ? 8 : 16;
-  t.unit = 16 * kRowsWarps;
-  t.ctas = device_sm_count() * (t.rows == 8 ? 4 : 3);
-  t.least = 2;
-  return t;
+  if (rows > 16) return {rows <= 32 ? 5 : (rows <= 64 ? 6 : 7), kTreeTcUnitLog2, device_sm_count(), 2};
+  return {rows <= 8 ? 3 : 4, 6, device_sm_count() * (rows <= 8 ? 4 : 3), 2};
 }
+static_assert(16 * kRowsWarps == 1 << 6, "unit of the kernel for few rows");
+
+// M and sums, then the weighted sums of values.
+int64_t tree_sums_bytes(const TreePlan& t) { return align256(((int64_t)2 * t.ctas << t.rows_log2) * 8); }
 
 template <int D>
 cudaError_t launch_t(const TreeArgs& a, cudaStream_t stream) {
@@ -582,17 +426,26 @@ cudaError_t launch_t(const TreeArgs& a, cudaStream_t stream) {
   p.a = a;
   p.G = (int)(a.Hq / a.Hkv);
   while ((1 << p.shift) < a.page_size) ++p.shift;
+  p.window = (int)a.window;
+  p.sinks = (int)a.sinks;
+  p.cap = (int)(a.table_width << p.shift);
   p.ctas = t.ctas;
-  p.rows = t.rows;
-  p.unit = t.unit;
+  p.rows_log2 = t.rows_log2;
+  p.unit_log2 = t.unit_log2;
   p.least = t.least;
   p.scale_log2 = a.scale * kAttnLog2e;
   p.ml = static_cast<float2*>(a.workspace);
-  p.o = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256((int64_t)2 * t.ctas * t.rows * 8));
-  auto kernel = t.rows == 8 ? tree_rows_kernel<D, 1> : tree_rows_kernel<D, 2>;
-  cudaError_t e = launch_pdl(kernel, dim3((unsigned)t.ctas), dim3(kRowsWarps * 32), 0, stream, 1, p);
+  p.o = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + tree_sums_bytes(t));
+  cudaError_t e;
+  if (t.rows_log2 >= 5) {
+    e = launch_tree_tc(p, stream);
+  } else {
+    auto kernel = t.rows_log2 == 3 ? tree_rows_kernel<D, 1> : tree_rows_kernel<D, 2>;
+    e = launch_pdl(kernel, dim3((unsigned)t.ctas), dim3(kRowsWarps * 32), 0, stream, 1, p);
+  }
   if (e != cudaSuccess) return e;
-  e = launch_pdl(tree_combine_kernel<D>, dim3((unsigned)(t.ctas - 1), (unsigned)(t.rows / 8)), dim3(kCombineThreads), 0, stream, 1, p);
+  e = launch_pdl(tree_combine_kernel<D>, dim3((unsigned)(t.ctas - 1), 1u << (t.rows_log2 - 3)), dim3(kCombineThreads), 0,
+                 stream, 1, p);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -600,7 +453,7 @@ cudaError_t launch_t(const TreeArgs& a, cudaStream_t stream) {
 
 int64_t tree_attention_workspace(const TreeArgs& a) {
   const TreePlan t = tree_plan(a);
-  return align256((int64_t)2 * t.ctas * t.rows * 8) + (int64_t)2 * t.ctas * t.rows * a.D * 4;
+  return tree_sums_bytes(t) + ((int64_t)2 * t.ctas << t.rows_log2) * a.D * 4;
 }
 
 cudaError_t launch_tree_attention(const TreeArgs& a, cudaStream_t stream) {
