@@ -4,16 +4,15 @@
 //
 // A job is up to 32 NE rows of a sequence and a kv head, in groups of 8 dealt to the four
 // lane quarters of the MMAs' 128 lanes, so that few rows are little work for every
-// warp instead of all of it for one.  Two warpgroups share a tile of 128 tokens: the first
-// has lanes 0 .. 15 of each quarter, the second 16 .. 31.
-//   NE 4: two groups each; the weights' second fp16 parts are columns behind the first's,
-//         with products of their own.
-//   NE 2: one group each, on 8 of the 16 lanes; the second parts lie on the other 8
-//         and cost no product.
-//   NE 1: the same group for both, who take the tiles in turn (the other one's weights
-//         are zeros) and join their sums at the end.
-// So nothing passes between the warpgroups within a job, and scores of three tiles in
-// tensor memory (with O its 512 columns) let the products run ahead of the softmax.
+// warp instead of all of it for one.  Two warpgroups take 64 tokens each of a tile of 128, with
+// an accumulator, maximum and sums of their own until the job's end: nothing passes
+// between them before.  A lane holds 4 rows (NE 4) of a quarter of its warp's tokens, so that
+// the tokens' numbers, which come from shared memory at a quarter of its rate, are loaded for
+// all of them at once.
+// The second fp16 parts of the weights lie on lanes without rows (NE 1: 8 .. 15 of each quarter,
+// NE 2: 16 .. 31) and cost no product; with NE 4 they are columns behind the first's.
+// Scores of two tiles in tensor memory (with the accumulators its 512 columns) let the
+// products run ahead of the softmax.
 // Warp roles: 0-7 softmax; 8 one thread that issues the MMAs; 9 and 10 copy the codes of values
 // and keys, a bulk copy per 16 tokens, two tiles ahead; 11 one thread that walks the CTA's
 // jobs and writes them down for the others; 12-15 expand the codes into operand tiles, a
@@ -55,10 +54,10 @@ template <int D>
 struct TreeCfg {
   static constexpr int TILE = 128 * D * 2;   // bytes of a Q, K or V operand tile
   static constexpr int NSTG = 2;             // tiles of keys, and of values
-  static constexpr int NS = 3;               // tiles of scores
+  static constexpr int NS = 2;               // tiles of scores
   // Tiles of per-token numbers.  Tile n + 2's are written when tile n's scores are done; those
-  // came behind tile n - 3's weights.
-  static constexpr int NCOL = 5;
+  // came behind tile n - 2's weights.
+  static constexpr int NCOL = 4;
   static constexpr int NRAW = D == 128 ? 2 : 4;
   // codes and scales as copied: keys' codes of NRAW tiles, the values', the scales
   static constexpr int CODES = 128 * (D / 2), SCALES = 128 * 16;
@@ -70,18 +69,18 @@ struct TreeCfg {
   static constexpr int OFF_COL = OFF_RAW + NRAW * (2 * CODES + SCALES);
   static constexpr int OFF_ROW = OFF_COL + NCOL * COL;               // TreeRow [128]
   static constexpr int OFF_PARENT = OFF_ROW + 128 * (int)sizeof(TreeRow);
-  static constexpr int OFF_X = OFF_PARENT + kTreeNodes * 4;          // float [3][128]: M, l, z of every lane; query sums
-  static constexpr int OFF_JOB = OFF_X + 3 * 128 * 4;
+  static constexpr int OFF_X = OFF_PARENT + kTreeNodes * 4;          // float [2][3][128]: the warpgroups' M, l, z; query sums
+  static constexpr int OFF_JOB = OFF_X + 6 * 128 * 4;
   static constexpr int OFF_BAR = (OFF_JOB + kJobSlots * (int)sizeof(TreeJobSlot) + 7) / 8 * 8;
-  // q, full, free [2][NSTG], col [NCOL], raw, rawfree [2][NRAW], s, p, o [NS], drain, job, taken [kJobSlots]
-  static constexpr int NBAR = 1 + 4 * NSTG + NCOL + 4 * NRAW + 3 * NS + 1 + 2 * kJobSlots;
+  // q, full, free [2][NSTG], raw, rawfree [2][NRAW], s [NS], p, o [2][NS], drain, job, taken [kJobSlots]
+  static constexpr int NBAR = 1 + 4 * NSTG + 4 * NRAW + 5 * NS + 1 + 2 * kJobSlots;
   static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
   static constexpr int BYTES = OFF_MISC + 16 + 1024;
   static_assert(OFF_BAR % 8 == 0 && BYTES <= 232448, "shared memory");
 };
 
-// O[tmem] (+)= P V: the weights of 64 tokens on 32 columns, their second parts (`part` = 1) on the
-// 32 behind them, 8 K steps of 16 tokens.
+// O[tmem] (+)= P V of 64 tokens: their weights on 32 columns, the second parts (`part` = 1) on the 32
+// behind them, 4 K steps of 16 tokens.
 template <int D>
 __device__ __forceinline__ void tree_mma_pv(uint32_t o_tmem, uint32_t p_tmem, uint32_t v_lo, int part, bool accumulate) {
   constexpr uint32_t idesc = umma_idesc_f16_f32_bmn(128, D);
@@ -91,8 +90,7 @@ __device__ __forceinline__ void tree_mma_pv(uint32_t o_tmem, uint32_t p_tmem, ui
   else
     attn_mma_ts<false>(o_tmem, w, v_lo, idesc);
 #pragma unroll
-  for (int ks = 1; ks < 8; ++ks)
-    attn_mma_ts<true>(o_tmem, w + (ks >> 2) * 64 + (ks & 3) * 8, v_lo + ks * (2048 >> 4), idesc);
+  for (int ks = 1; ks < 4; ++ks) attn_mma_ts<true>(o_tmem, w + ks * 8, v_lo + ks * (2048 >> 4), idesc);
 }
 
 // code_pairs with one shift in place of three: the codes at bits 4 and 20 are 1024 + 16 u, exact,
@@ -114,22 +112,21 @@ template <int D, int NE>
 __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreeParams p) {
   using C = TreeCfg<D>;
   constexpr int NSTG = C::NSTG, NCOL = C::NCOL, NRAW = C::NRAW, NS = C::NS;
-  constexpr int NG = NE == 4 ? 2 : 1;   // groups of rows of a warp
+  constexpr int NH = NE == 4 ? 2 : 1;   // 16-lane halves of a quarter that hold rows
   const TreeArgs& a = p.a;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t* qbar = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);   // a job's queries are in (8 warps)
-  uint64_t* kfull = qbar + 1;       // key tile written (4 warps)
+  uint64_t* kfull = qbar + 1;       // key tile and per-token numbers written (4 warps)
   uint64_t* vfull = kfull + NSTG;   // value tile
   uint64_t* kfree = vfull + NSTG;   // its products are done
   uint64_t* vfree = kfree + NSTG;
-  uint64_t* cbar = vfree + NSTG;    // per-token numbers of a tile written (4 warps)
-  uint64_t* raw = cbar + NCOL;      // a tile's key codes and scales copied; NRAW further on: its value codes
+  uint64_t* raw = vfree + NSTG;     // a tile's key codes and scales copied; NRAW further on: its value codes
   uint64_t* rawfree = raw + 2 * NRAW;   // and read (4 warps)
-  uint64_t* sbar = rawfree + 2 * NRAW;  // a tile's scores written
-  uint64_t* pbar = sbar + NS;       // its weights written (8 warps)
-  uint64_t* obar = pbar + NS;       // their products done
-  uint64_t* drain = obar + NS;      // every MMA done
+  uint64_t* sbar = rawfree + 2 * NRAW;  // a tile's scores written, and its per-token numbers before
+  uint64_t* pbar = sbar + NS;       // weights of warpgroup i written (4 warps), at i NS ..
+  uint64_t* obar = pbar + 2 * NS;   // their products done
+  uint64_t* drain = obar + 2 * NS;  // every MMA done
   uint64_t* jbar = drain + 1;       // job written
   uint64_t* taken = jbar + kJobSlots;   // and no longer read
   TreeJobSlot* job_s = reinterpret_cast<TreeJobSlot*>(smem + C::OFF_JOB);
@@ -146,14 +143,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
       mbar_init(&kfull[s], 4);
       mbar_init(&kfree[s], 1);
     }
-    for (int s = 0; s < NCOL; ++s) mbar_init(&cbar[s], 4);
     for (int s = 0; s < 2 * NRAW; ++s) {
       mbar_init(&raw[s], 1);
       mbar_init(&rawfree[s], 4);
     }
-    for (int s = 0; s < NS; ++s) {
-      mbar_init(&sbar[s], 1);
-      mbar_init(&pbar[s], 8);
+    for (int s = 0; s < NS; ++s) mbar_init(&sbar[s], 1);
+    for (int s = 0; s < 2 * NS; ++s) {
+      mbar_init(&pbar[s], 4);
       mbar_init(&obar[s], 1);
     }
     mbar_init(drain, 1);
@@ -269,8 +265,6 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
         // (in the order of the lanes: pairs c of groups 2 k and 2 k + 1 of eight tokens in one load)
         const int to = (t & 64) + (t >> 4 & 3) * 16 + (t >> 1 & 3) * 4 + (t >> 3 & 1) * 2 + (t & 1);
         reinterpret_cast<float*>(cols + C::COL_LOG)[to] = bad ? __int_as_float(0x7fc00000) : log2_of_scale(va);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&cbar[n % NCOL]);
         expand(w, smem + C::OFF_K + (n % NSTG) * C::TILE, &kfull[n % NSTG]);
         if (n >= 2 && !(ok = values(n - 2))) break;
       }
@@ -306,12 +300,17 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
           for (int m = n; m < min(end, n + NS); ++m) scores(m);
 #pragma unroll 1
           for (; ok && n < end; ++n) {
-            if (!wait(vfull, n, NSTG) || !wait(pbar, n, NS)) break;
-            tc_fence_after();
-            const uint32_t vd = v_lo + (n % NSTG) * (C::TILE >> 4);
-            tree_mma_pv<D>(OCOL, (n % NS) * 128, vd, 0, n > first);
-            if (NE == 4) tree_mma_pv<D>(OCOL, (n % NS) * 128, vd, 1, true);
-            tc_commit(&obar[n % NS]);
+            if (!wait(vfull, n, NSTG)) break;
+            const uint32_t vd = v_lo + (n % NSTG) * (C::TILE >> 4), pt = (n % NS) * 128;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              if (!wait(pbar + i * NS, n, NS)) break;
+              tc_fence_after();
+              tree_mma_pv<D>(OCOL + i * D, pt + 64 * i, vd + 4 * i * (2048 >> 4), 0, n > first);
+              if (NE == 4) tree_mma_pv<D>(OCOL + i * D, pt + 64 * i, vd + 4 * i * (2048 >> 4), 1, true);
+              tc_commit(&obar[i * NS + n % NS]);
+            }
+            if (!ok) break;
             tc_commit(&vfree[n % NSTG]);
             if (n + NS < end) scores(n + NS);
           }
@@ -374,17 +373,14 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
       }
     }
   } else {
-    // ---------------- softmax.  Warpgroup i has lanes 16 i .. of each quarter; lane 4 g + c holds
-    // rows g (and g + 8, NE 4) of them and tokens 8 k + 2 c, + 1.
+    // ---------------- softmax.  Warpgroup i has tokens 64 i .. of a tile; lane 4 g + c holds rows
+    // g + 8 e of its quarter and tokens 8 k + 2 c, + 1.
     asm volatile("setmaxnreg.inc.sync.aligned.u32 184;\n");
     const int i = warp >> 2, quad = warp & 3, g = lane >> 2, c = lane & 3;
-    const uint32_t half = (uint32_t)(quad * 32 + 16 * i) << 16, quarter = (uint32_t)(quad * 32) << 16;
+    const uint32_t quarter = (uint32_t)(quad * 32) << 16, ot = tmem + OCOL + i * D + quarter;
     float* xs = reinterpret_cast<float*>(smem + C::OFF_X);
     // the job's row on lane l of quarter q, or -1
-    auto row_of = [&](int q, int l) {
-      if (NE == 4) return (l >> 3) * 32 + q * 8 + (l & 7);
-      return l & 8 ? -1 : (NE == 2 ? (l >> 4) * 32 : 0) + q * 8 + (l & 7);
-    };
+    auto row_of = [&](int q, int l) { return l < 8 * NE ? (l >> 3) * 32 + q * 8 + (l & 7) : -1; };
     // OR of a predicate over the softmax threads, a barrier for them.
     auto named_or = [&](bool x) {
       uint32_t r;
@@ -447,9 +443,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
         if (r >= 0 && r < j.rows) v = tree_row(p, s, parent_s, (j.r0 + r) / p.G);
         row_s[tid] = v;
       }
-      float qs[NG];
+      float qs[NE];
 #pragma unroll
-      for (int e = 0; e < NG; ++e) qs[e] = xs[quad * 32 + 16 * i + 8 * e + g];
+      for (int e = 0; e < NE; ++e) qs[e] = xs[quad * 32 + 8 * e + g];
       named_bar_sync(kSoftmaxBarrier, 256);   // the rows' views written, the sums read
       // tokens that every row sees: those below `ctx`, from the last row's window on or in the sinks
       const int ctx = s.ctx;
@@ -458,166 +454,155 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
       for (int k = 0; k < 4; ++k) low = max(low, row_s[k * 32 + lane].low);
       low = (int)__reduce_max_sync(0xffffffffu, (unsigned)low);
 
-      float m[NG], l[NG], z[NG];   // M; l, z: of this lane's tokens
+      float m[NE], l[NE], z[NE];   // M; l, z: of this lane's tokens
 #pragma unroll
-      for (int e = 0; e < NG; ++e) m[e] = -INFINITY, l[e] = z[e] = 0.f;
+      for (int e = 0; e < NE; ++e) m[e] = -INFINITY, l[e] = z[e] = 0.f;
       const int end = n + j.v1 - j.v0, start = n, v0 = j.v0, front = s.front, skip = s.skip;
 #pragma unroll 1
       for (; n < end; ++n) {
-        const int v = v0 + n - start, base = (v < front ? v : v + skip) * kTreeTcUnit;
-        const uint32_t st = tmem + (n % NS) * 128 + half;
-        if (!(ok = wait_full(cbar, n, NCOL) && wait_full(sbar, n, NS))) break;
+        const int v = v0 + n - start, at = (v < front ? v : v + skip) * kTreeTcUnit + 64 * i;
+        const uint32_t st = tmem + (n % NS) * 128 + quarter + 64 * i;
+        if (!(ok = wait_full(sbar, n, NS))) break;
         tc_fence_after();
-        if (NE == 1 && ((n - start) & 1) != i) {
-          // the other warpgroup's tile: weights 0
-          uint32_t w[16];
+        // the numbers of tokens 8 k + 2 c, 8 k + 2 c + 1
+        const uint8_t* cols = smem + C::OFF_COL + (n % NCOL) * C::COL;
+        const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(cols + i * 512) + c;
+        const ulonglong2* fv = reinterpret_cast<const ulonglong2*>(cols + C::COL_V + i * 512) + c;
+        const ulonglong2* la = reinterpret_cast<const ulonglong2*>(cols + C::COL_LOG + i * 256) + c;
+        uint32_t x[NH][32];   // x[h][4 k + 2 e + y]: row 16 h + 8 e + g, token 8 k + 2 c + y
 #pragma unroll
-          for (int k = 0; k < 16; ++k) w[k] = 0;
-          tmem_st_16x128b_x8(st, w);
-          tmem_st_16x128b_x8(st + 64, w);
-        } else {
-          // the numbers of tokens 8 k + 2 c, 8 k + 2 c + 1
-          const uint8_t* cols = smem + C::OFF_COL + (n % NCOL) * C::COL;
-          const ulonglong2* ab = reinterpret_cast<const ulonglong2*>(cols) + c;
-          const ulonglong2* fv = reinterpret_cast<const ulonglong2*>(cols + C::COL_V) + c;
-          const ulonglong2* la = reinterpret_cast<const ulonglong2*>(cols + C::COL_LOG) + c;
-          // 64 tokens at a time: this loop's code stays in the instruction cache
-#pragma unroll 1
-          for (int q = 0; q < 2; ++q, ab += 32, fv += 32, la += 16) {
-            uint32_t x[32];   // x[4 k + 2 e + y]: row 8 e + g, token 64 q + 8 k + 2 c + y
-            tmem_ld_16x256b_x8(st + 64 * q, x);
-            tmem_ld_wait_all<32>(x);
+        for (int h = 0; h < NH; ++h) tmem_ld_16x256b_x8(st + ((16u * h) << 16), x[h]);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const ulonglong2 w = ab[4 * k], l2 = la[4 * (k >> 1)];
-              const F2 lg = F2{k & 1 ? l2.y : l2.x};
+        for (int h = 0; h < NH; ++h) tmem_ld_wait_all<32>(x[h]);
 #pragma unroll
-              for (int e = 0; e < NG; ++e) {
-                uint32_t* y = &x[4 * k + 2 * e];
-                float t0, t1;
-                f2_split(f2_fma(f2_from_bits(y[0], y[1]), F2{w.x}, f2_fma(F2{w.y}, f2_make(qs[e], qs[e]), lg)), t0, t1);
-                y[0] = __float_as_uint(t0);
-                y[1] = __float_as_uint(t1);
-              }
-            }
-            const int at = base + 64 * q;
-            if (at + 64 > ctx || (at < low && at + 64 > p.sinks)) {
-              // not every row sees every token: lane r has a bit per token for its row
+        for (int k = 0; k < 8; ++k) {
+          const ulonglong2 w = ab[4 * k], l2 = la[4 * (k >> 1)];
+          const F2 lg = F2{k & 1 ? l2.y : l2.x};
 #pragma unroll
-              for (int w = 0; w < 2; ++w) {
-                const uint32_t seen = tree_sees(p, s, row_s[quad * 32 + lane], at + 32 * w);
-#pragma unroll
-                for (int e = 0; e < NG; ++e) {
-                  const uint32_t bits = __shfl_sync(0xffffffffu, seen, 16 * i + 8 * e + g) >> (2 * c);
-#pragma unroll
-                  for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-                      if (!((bits >> (8 * k + y)) & 1u)) x[4 * (4 * w + k) + 2 * e + y] = 0xFF800000u;   // -inf
-                }
-              }
-            }
-            float mx[NG];
-            bool grow = false;
-#pragma unroll
-            for (int e = 0; e < NG; ++e) {
-              const uint32_t* y = &x[2 * e];
-              float p0 = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])), p1 = fmaxf(__uint_as_float(y[4]), __uint_as_float(y[5]));
-#pragma unroll
-              for (int k = 2; k < 8; k += 2) {
-                p0 = attn_max3(p0, __uint_as_float(y[4 * k]), __uint_as_float(y[4 * k + 1]));
-                p1 = attn_max3(p1, __uint_as_float(y[4 * k + 4]), __uint_as_float(y[4 * k + 5]));
-              }
-              mx[e] = fmaxf(p0, p1);
-              grow |= mx[e] > m[e] + kAttnSlack;
-            }
-            if (__any_sync(0xffffffffu, grow)) {   // seldom: M moves
-              float f[NG];
-#pragma unroll
-              for (int e = 0; e < NG; ++e) {
-                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
-                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
-                // (whole numbers: the factor is a power of two, which leaves the weights' parts exact)
-                const float mn = mx[e] > m[e] + kAttnSlack ? ceilf(mx[e]) : m[e];
-                // (a row without a maximum has no weights, or sums that are not numbers and stay so)
-                f[e] = m[e] == -INFINITY || mn == m[e] ? 1.f : __int_as_float(((int)fmaxf(m[e] - mn, -127.f) + 127) << 23);
-                m[e] = mn;
-                l[e] *= f[e];
-                z[e] *= f[e];
-              }
-              // the factors of rows g and g + 8 of the 16 lanes (the upper 8 of a single group: its second parts)
-              const float fr[2] = {f[0], NG == 2 ? f[NG - 1] : f[0]};
-              if (n > start) {
-                // the products so far are done (this tile's wait for its weights)
-                if (!(ok = wait_full(obar, n - 1, NS))) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int d = 0; d < D; d += 16) {
-                  uint32_t y[8];
-                  tmem_ld_16x256b_x2(tmem + OCOL + half + d, y);
-#pragma unroll
-                  for (int k = 0; k < 8; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * fr[(k >> 1) & 1]);
-                  tmem_st_16x256b_x2(tmem + OCOL + half + d, y);
-                }
-              }
-              if (q > 0) {   // and the tile's first weights and second parts
-                tmem_st_wait();
-#pragma unroll 1
-                for (int d = 0; d < 64; d += 16) {
-                  uint32_t y[8];
-                  tmem_ld_16x256b_x2(st + d, y);
-#pragma unroll
-                  for (int k = 0; k < 8; ++k) {
-                    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&y[k]));
-                    y[k] = pack_half2_bits(h.x * fr[(k >> 1) & 1], h.y * fr[(k >> 1) & 1]);
-                  }
-                  tmem_st_16x256b_x2(st + d, y);
-                }
-              }
-              tmem_st_wait();
-            }
-            uint32_t w0[16], w1[16];   // first and second parts: 32-bit columns 4 k + c
-#pragma unroll
-            for (int e = 0; e < NG; ++e) {
-              const float off = m[e] == -INFINITY ? 0.f : -m[e];
-              const F2 of2 = f2_make(off, off);
-              F2 sum = f2_make(l[e], 0.f), zs = f2_make(z[e], 0.f);
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const ulonglong2 f = fv[4 * k];
-                float t0, t1;
-                f2_split(f2_add(f2_from_bits(x[4 * k + 2 * e], x[4 * k + 2 * e + 1]), of2), t0, t1);
-                const F2 ex = f2_make(attn_exp2(t0), attn_exp2(t1));
-                sum = f2_fma(ex, F2{f.x}, sum);
-                zs = f2_fma(ex, F2{f.y}, zs);
-                f2_split(ex, t0, t1);
-                const uint32_t hi = pack_half2_bits(t0, t1);
-                const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                f2_split(f2_sub(ex, f2_make(r.x, r.y)), t0, t1);
-                const uint32_t lo = pack_half2_bits(t0, t1);
-                w0[2 * k + e] = hi;
-                (NG == 1 ? w0[2 * k + 1] : w1[2 * k + e]) = lo;
-              }
-              float t0, t1;
-              f2_split(sum, t0, t1);
-              l[e] = t0 + t1;
-              f2_split(zs, t0, t1);
-              z[e] = t0 + t1;
-            }
-            tmem_st_16x128b_x8(st + 64 * q, w0);
-            if (NE == 4) tmem_st_16x128b_x8(st + 64 * q + 32, w1);
+          for (int e = 0; e < NE; ++e) {
+            uint32_t* y = &x[e >> 1][4 * k + 2 * (e & 1)];
+            float t0, t1;
+            f2_split(f2_fma(f2_from_bits(y[0], y[1]), F2{w.x}, f2_fma(F2{w.y}, f2_make(qs[e], qs[e]), lg)), t0, t1);
+            y[0] = __float_as_uint(t0);
+            y[1] = __float_as_uint(t1);
           }
-          if (!ok) break;
+        }
+        if (at + 64 > ctx || (at < low && at + 64 > p.sinks)) {
+          // not every row sees every token: lane r has a bit per token for its row
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const uint32_t seen = tree_sees(p, s, row_s[quad * 32 + lane], at + 32 * w);
+#pragma unroll
+            for (int e = 0; e < NE; ++e) {
+              const uint32_t bits = __shfl_sync(0xffffffffu, seen, 8 * e + g) >> (2 * c);
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                  if (!((bits >> (8 * k + y)) & 1u)) x[e >> 1][4 * (4 * w + k) + 2 * (e & 1) + y] = 0xFF800000u;   // -inf
+            }
+          }
+        }
+        float mx[NE];
+        bool grow = false;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          const uint32_t* y = &x[e >> 1][2 * (e & 1)];
+          float p0 = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])), p1 = fmaxf(__uint_as_float(y[4]), __uint_as_float(y[5]));
+#pragma unroll
+          for (int k = 2; k < 8; k += 2) {
+            p0 = attn_max3(p0, __uint_as_float(y[4 * k]), __uint_as_float(y[4 * k + 1]));
+            p1 = attn_max3(p1, __uint_as_float(y[4 * k + 4]), __uint_as_float(y[4 * k + 5]));
+          }
+          mx[e] = fmaxf(p0, p1);
+          grow |= mx[e] > m[e] + kAttnSlack;
+        }
+        if (__any_sync(0xffffffffu, grow)) {   // seldom: M moves
+          float f[4];
+#pragma unroll
+          for (int e = 0; e < NE; ++e) {
+            mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
+            mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
+            const float mn = mx[e] > m[e] + kAttnSlack ? mx[e] : m[e];
+            // (a row without a maximum has no weights, or sums that are not numbers and stay so)
+            f[e] = m[e] == -INFINITY || mn == m[e] ? 1.f : attn_exp2(m[e] - mn);
+            m[e] = mn;
+            l[e] *= f[e];
+            z[e] *= f[e];
+          }
+          if constexpr (NE == 1) f[1] = f[0];   // the second parts' rows
+          if constexpr (NE == 2) f[2] = f[0], f[3] = f[1];
+          if (n > start) {
+            if (!(ok = wait_full(obar + i * NS, n - 1, NS))) break;   // the products so far are done
+            tc_fence_after();
+#pragma unroll 1
+            for (int d = 0; d < D; d += 16) {
+#pragma unroll
+              for (int h = 0; h < (NE == 1 ? 1 : 2); ++h) {
+                uint32_t y[8];
+                tmem_ld_16x256b_x2(ot + ((16u * h) << 16) + d, y);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * f[2 * h + ((k >> 1) & 1)]);
+                tmem_st_16x256b_x2(ot + ((16u * h) << 16) + d, y);
+              }
+            }
+          }
+        }
+        uint32_t w0[NH][16], w1[NH][16];   // first and second parts: 32-bit columns 4 k + c
+        F2 of2[NE], sum[NE], zs[NE];
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          const float off = m[e] == -INFINITY ? 0.f : -m[e];
+          of2[e] = f2_make(off, off);
+          sum[e] = f2_make(l[e], 0.f);
+          zs[e] = f2_make(z[e], 0.f);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const ulonglong2 f = fv[4 * k];
+#pragma unroll
+          for (int e = 0; e < NE; ++e) {
+            const uint32_t* y = &x[e >> 1][4 * k + 2 * (e & 1)];
+            float t0, t1;
+            f2_split(f2_add(f2_from_bits(y[0], y[1]), of2[e]), t0, t1);
+            const F2 ex = f2_make(attn_exp2(t0), attn_exp2(t1));
+            sum[e] = f2_fma(ex, F2{f.x}, sum[e]);
+            zs[e] = f2_fma(ex, F2{f.y}, zs[e]);
+            f2_split(ex, t0, t1);
+            const uint32_t hi = pack_half2_bits(t0, t1);
+            const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+            f2_split(f2_sub(ex, f2_make(r.x, r.y)), t0, t1);
+            const uint32_t lo = pack_half2_bits(t0, t1);
+            w0[e >> 1][2 * k + (e & 1)] = hi;
+            if (NE == 1)
+              w0[0][2 * k + 1] = lo;
+            else
+              w1[e >> 1][2 * k + (e & 1)] = lo;
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+          tmem_st_16x128b_x8(st + ((16u * h) << 16), w0[h]);
+          if (NE == 2) tmem_st_16x128b_x8(st + (16u << 16), w1[h]);
+          if (NE == 4) tmem_st_16x128b_x8(st + ((16u * h) << 16) + 32, w1[h]);
+        }
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+          float t0, t1;
+          f2_split(sum[e], t0, t1);
+          l[e] = t0 + t1;
+          f2_split(zs[e], t0, t1);
+          z[e] = t0 + t1;
         }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&pbar[n % NS]);
+        if (lane == 0) mbar_arrive(&pbar[i * NS + n % NS]);
       }
-      if (ok) ok = wait_full(obar, end - 1, NS);
+      if (ok) ok = wait_full(obar + i * NS, end - 1, NS);
       // the rows' numbers, and whether a wait was given up
 #pragma unroll
-      for (int e = 0; e < NG; ++e)
+      for (int e = 0; e < NE; ++e)
 #pragma unroll
         for (int w = 1; w < 4; w <<= 1) {
           l[e] += __shfl_xor_sync(0xffffffffu, l[e], w);
@@ -625,24 +610,23 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
         }
       if (c == 0) {
 #pragma unroll
-        for (int e = 0; e < NG; ++e) {
-          float* y = xs + quad * 32 + 16 * i + 8 * e + g;
+        for (int e = 0; e < NE; ++e) {
+          float* y = xs + 384 * i + quad * 32 + 8 * e + g;
           y[0] = m[e], y[128] = l[e], y[256] = z[e];
         }
       }
       ok = !named_or(!ok);
       if (!ok) break;
       tc_fence_after();
-      // A row per lane, half of D per warpgroup.  NE 1: the row's other sums are 16 lanes further on.
+      // a row per lane, half of D per warpgroup
       {
         const int r = row_of(quad, lane);
-        const bool mine = r >= 0 && r < j.rows && (NE > 1 || lane < 8);
+        const bool mine = r >= 0 && r < j.rows;
         const float* y = xs + quad * 32 + lane;
-        const float l0 = mine ? y[128] : 0.f, l1 = NE == 1 && mine ? y[128 + 16] : 0.f;
-        const float m0 = l0 != 0.f ? y[0] : -INFINITY, m1 = l1 != 0.f ? y[16] : -INFINITY, M = fmaxf(m0, m1);
+        const float l0 = mine ? y[128] : 0.f, l1 = mine ? y[384 + 128] : 0.f;
+        const float m0 = l0 != 0.f ? y[0] : -INFINITY, m1 = l1 != 0.f ? y[384] : -INFINITY, M = fmaxf(m0, m1);
         const float f0 = l0 != 0.f ? attn_exp2(m0 - M) : 0.f, f1 = l1 != 0.f ? attn_exp2(m1 - M) : 0.f;
-        float ls = l0 != 0.f ? f0 * l0 : 0.f, zz = l0 != 0.f ? f0 * y[256] : 0.f;
-        if (l1 != 0.f) ls = fmaf(f1, l1, ls), zz = fmaf(f1, y[256 + 16], zz);
+        const float ls = fmaf(f1, l1, f0 * l0), zz = fmaf(f1, mine ? y[384 + 256] : 0.f, f0 * (mine ? y[256] : 0.f));
         const bool whole = j.whole();
         const float inv = whole ? (ls != 0.f ? 1.f / ls : 0.f) : 1.f;
         const int64_t slot = j.slot(blockIdx.x) * (32 * NE) + r;
@@ -651,19 +635,20 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
 #pragma unroll 1
         for (int q = 0; q < D / 2; q += 16) {
           const int d0 = i * (D / 2) + q;
-          uint32_t o0[16];
+          uint32_t o0[16], o1[16];
           tmem_ld_32x32b_x16(tmem + OCOL + quarter + d0, o0);
+          tmem_ld_32x32b_x16(tmem + OCOL + D + quarter + d0, o1);
           tmem_ld_wait(o0);
+          tmem_ld_wait(o1);
           float o[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            float u = __uint_as_float(o0[k]), w = 0.f;
-            if (NE < 4) u += __shfl_down_sync(0xffffffffu, u, 8);   // and what the second parts gave
-            if (NE == 1) w = __shfl_down_sync(0xffffffffu, u, 16);
-            // (a row that saw no token: zeros, whatever the accumulator holds)
-            float val = l0 != 0.f ? fmaf(f0, u, zz) : zz;
-            if (NE == 1 && l1 != 0.f) val = fmaf(f1, w, val);
-            o[k] = val * inv;
+            float u = __uint_as_float(o0[k]), w = __uint_as_float(o1[k]);
+            if (NE < 4) {   // and what the second parts gave
+              u += __shfl_down_sync(0xffffffffu, u, NE == 1 ? 8 : 16);
+              w += __shfl_down_sync(0xffffffffu, w, NE == 1 ? 8 : 16);
+            }
+            o[k] = fmaf(f1, w, fmaf(f0, u, zz)) * inv;
           }
           if (mine) {   // column 0, 1, .. of eight holds value 0, 4, 1, 5, 2, 6, 3, 7
 #pragma unroll
