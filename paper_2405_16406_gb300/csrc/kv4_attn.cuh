@@ -26,9 +26,15 @@ __device__ __forceinline__ float one_over_scale(float x) {   // within 2^-23
   return y;
 }
 
+// (x & m) | c in one instruction, both constants in registers.
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t m, uint32_t c) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;\n" : "=r"(y) : "r"(x), "r"(m), "r"(c));
+  return y;
+}
 // Eight codes of a word as fp16 pairs u - 8: (0, 4), (1, 5), (2, 6), (3, 7).
 __device__ __forceinline__ uint32_t code_pair(uint32_t x) {   // nibbles at bits 0 and 16
-  const uint32_t m = (x & 0x000F000Fu) | 0x64006400u;         // 1024 + u
+  const uint32_t m = and_or(x, 0x000F000Fu, 0x64006400u);     // 1024 + u
   const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x6408)));   // 1032
   return *reinterpret_cast<const uint32_t*>(&h);
 }

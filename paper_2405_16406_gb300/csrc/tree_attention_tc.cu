@@ -96,7 +96,7 @@ __device__ __forceinline__ void tree_mma_pv(uint32_t o_tmem, uint32_t p_tmem, ui
 // code_pairs with one shift in place of three: the codes at bits 4 and 20 are 1024 + 16 u, exact,
 // and so is their sixteenth less 72.
 __device__ __forceinline__ uint32_t tree_pair16(uint32_t x) {
-  const uint32_t m = (x & 0x00F000F0u) | 0x64006400u;
+  const uint32_t m = and_or(x, 0x00F000F0u, 0x64006400u);
   const __half2 h = __hfma2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x2c00)),    // 1 / 16
                             __half2half2(__ushort_as_half(0xd480)));                                        // -72
   return *reinterpret_cast<const uint32_t*>(&h);
