@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
     __syncthreads();
     if (tid < ROWS) {
       TreeRow r = {};
-      if (tid < rows) r = tree_row(p, s, parent_s, (j.r0 + tid) / p.G);
+      if (tid < rows) r = tree_row(p, s, parent_s, tree_node(p, j.r0 + tid));
       row_s[tid] = r;
     }
     // query fragments (k order as the codes come), their sums.  A key
@@ -364,16 +364,17 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
   const int c = blockIdx.x + 1;
   // (the attention kernel started behind what wrote the lengths, and this one behind its start)
   const TreeRun run = tree_run<kCombineThreads>(p, c);
+  const TreeSeq& s = run.s;
+  const int64_t x = c < run.ctas ? run.bound(c) : run.base, in = x - run.base;
+  const int64_t job = in <= INT32_MAX ? (uint32_t)in / (uint32_t)max(1, s.units) : in / s.units;
+  const int64_t begin = run.base + job * s.units, end = begin + s.units;
   pdl_wait();
   pdl_trigger();
   if (c >= run.ctas) return;
-  const TreeSeq s = tree_seq(p, run.b);
-  const int64_t x = run.bound(c), job = (x - run.base) / s.units;
-  const int64_t begin = run.base + job * s.units, end = begin + s.units;
   if (x == begin || run.bound(c - 1) > begin) return;   // no job cut, or cut before
   const int rows = 1 << p.rows_log2;
-  const int hk = (int)(job / s.rts), r = blockIdx.y * 8 + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
-  const int row = ((int)(job - (int64_t)hk * s.rts) << p.rows_log2) + r;
+  const int hk = (int)job / s.rts, r = blockIdx.y * 8 + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
+  const int row = (((int)job - hk * s.rts) << p.rows_log2) + r;
   if (threadIdx.x >= 8 * (D / 4) || row >= s.nq * p.G) return;
   // parts: the one that CTA c - 1 left, then those that c, c + 1, .. continued
   auto slot = [&](int i) { return (int64_t)(i < c ? 2 * i + 1 : 2 * i) * rows + r; };
@@ -398,7 +399,7 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
     }
   }
   const float inv = l != 0.f ? 1.f / l : 0.f;
-  const int node = row / p.G, head = row - node * p.G;
+  const int node = tree_node(p, row), head = row - node * p.G;
   *reinterpret_cast<uint2*>(reinterpret_cast<__half*>(a.out) + ((int64_t)(s.q0 + node) * a.Hq + hk * p.G + head) * D + d) =
       make_uint2(pack_half2_bits(v.x * inv, v.y * inv), pack_half2_bits(v.z * inv, v.w * inv));
 }
@@ -425,6 +426,7 @@ cudaError_t launch_t(const TreeArgs& a, cudaStream_t stream) {
   TreeParams p{};
   p.a = a;
   p.G = (int)(a.Hq / a.Hkv);
+  p.g_inv = p.G > 1 ? (uint32_t)(((1ull << 32) + p.G - 1) / p.G) : 0;
   while ((1 << p.shift) < a.page_size) ++p.shift;
   p.window = (int)a.window;
   p.sinks = (int)a.sinks;

@@ -14,6 +14,7 @@ constexpr int kTreeNodes = 128;   // queries of a sequence at most
 struct TreeParams {
   TreeArgs a;
   int G, shift;            // query heads per kv head; page_size = 1 << shift
+  uint32_t g_inv;          // ceil(2^32 / G); 0 for G = 1
   int window, sinks, cap;  // window 0: none; tokens that a row of the table has room for
   int ctas;                // of the attention kernel's grid
   int rows_log2, unit_log2;   // rows of a job, tokens of a unit
@@ -24,6 +25,9 @@ struct TreeParams {
   int* status;
   int debug_stall;
 };
+
+// x / G of a row number x < 2^16: x ceil(2^32 / G) is less than x + 2^32 / G off 2^32 x / G.
+__device__ __forceinline__ int tree_node(const TreeParams& p, int x) { return p.g_inv ? (int)__umulhi((uint32_t)x, p.g_inv) : x; }
 
 // What the lengths say of a sequence.
 struct TreeSeq {
@@ -59,19 +63,22 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
 struct TreeRun {
   int64_t per, base;
   int rest, ctas, b;
+  TreeSeq s;   // of sequence b
   __device__ __forceinline__ int64_t bound(int c) const { return per * c + min(c, rest); }
 };
 
 template <int THREADS>
 __device__ __forceinline__ TreeRun tree_run(const TreeParams& p, int c) {
-  __shared__ int64_t sums[THREADS / 32];
-  __shared__ TreeRun found;
+  __shared__ int64_t sums[THREADS / 32], base_s;
+  __shared__ int b_s;
+  __shared__ TreeSeq seq_s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = (int)p.a.B;
-  const int per = (B + THREADS - 1) / THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
+  const int per = B <= THREADS ? 1 : (B + THREADS - 1) / THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
   int64_t mine = 0;
+  TreeSeq s = {};
 #pragma unroll 1
   for (int b = b0; b < b1; ++b) {
-    const TreeSeq s = tree_seq(p, b);
+    s = tree_seq(p, b);
     mine += (int64_t)s.units * s.jobs;
   }
   int64_t sum = mine;
@@ -81,6 +88,7 @@ __device__ __forceinline__ TreeRun tree_run(const TreeParams& p, int c) {
     if (lane >= w) sum += y;
   }
   if (lane == 31) sums[warp] = sum;
+  if (tid == 0) b_s = B;
   __syncthreads();
   int64_t at = sum - mine, all = 0;
 #pragma unroll
@@ -88,35 +96,39 @@ __device__ __forceinline__ TreeRun tree_run(const TreeParams& p, int c) {
     if (w == warp) at += all;
     all += sums[w];
   }
-  if (tid == 0) {
-    TreeRun r;
-    const int64_t runs = all >= (int64_t)p.least * p.ctas ? p.ctas : (all + p.least - 1) / p.least;
-    r.ctas = (int)runs;
-    r.per = runs ? all / runs : 0;
-    r.rest = (int)(all - r.per * runs);
-    r.base = 0;
-    r.b = B;
-    found = r;
+  TreeRun r;
+  if (all <= INT32_MAX) {   // (32-bit divisions: a wave of CTAs waits for these)
+    const uint32_t n = (uint32_t)all;
+    r.ctas = (int)min((uint32_t)p.ctas, (n + p.least - 1) / p.least);
+    r.per = r.ctas ? n / (uint32_t)r.ctas : 0;
+  } else {
+    r.ctas = p.ctas;
+    r.per = all / p.ctas;
   }
-  __syncthreads();
-  const TreeRun r = found;
+  r.rest = (int)(all - r.per * r.ctas);
   if (c < r.ctas) {
     const int64_t x = r.bound(c);
     if (at <= x && x < at + mine) {
       int b = b0;
+      if (per > 1) {
 #pragma unroll 1
-      for (; b < b1 - 1; ++b) {
-        const TreeSeq s = tree_seq(p, b);
-        const int64_t t = (int64_t)s.units * s.jobs;
-        if (x < at + t) break;
-        at += t;
+        for (; b < b1; ++b) {
+          s = tree_seq(p, b);
+          const int64_t t = (int64_t)s.units * s.jobs;
+          if (x < at + t) break;
+          at += t;
+        }
       }
-      found.b = b;
-      found.base = at;
+      b_s = b;
+      base_s = at;
+      seq_s = s;
     }
   }
   __syncthreads();
-  return found;
+  r.b = b_s;
+  r.base = base_s;
+  r.s = seq_s;
+  return r;
 }
 
 // A row's view of the keys.
@@ -178,7 +190,7 @@ struct TreeJob {
   __device__ __forceinline__ int token(int v, int unit) const { return (v < s.front ? v : v + s.skip) * unit; }
   // a row's place among [query][head] rows
   __device__ __forceinline__ int64_t row_at(const TreeParams& p, int r) const {
-    const int node = (r0 + r) / p.G, head = r0 + r - node * p.G;
+    const int node = tree_node(p, r0 + r), head = r0 + r - node * p.G;
     return (int64_t)(s.q0 + node) * p.a.Hq + hk * p.G + head;
   }
 };
@@ -186,18 +198,19 @@ struct TreeJob {
 struct TreeWalk {
   int64_t x, x1, base;
   int b;
+  TreeSeq s;   // of sequence b
   __device__ __forceinline__ TreeWalk(const TreeRun& r, int c)
-      : x(c < r.ctas ? r.bound(c) : 0), x1(c < r.ctas ? r.bound(c + 1) : 0), base(r.base), b(r.b) {}
+      : x(c < r.ctas ? r.bound(c) : 0), x1(c < r.ctas ? r.bound(c + 1) : 0), base(r.base), b(r.b), s(r.s) {}
   __device__ __forceinline__ bool next(const TreeParams& p, TreeJob& j) {
     while (x < x1 && b < (int)p.a.B) {
-      j.s = tree_seq(p, b);
+      j.s = s;
       const int64_t all = (int64_t)j.s.units * j.s.jobs, at = x - base;
       if (at >= all) {
         base += all;
-        ++b;
+        if (++b < (int)p.a.B) s = tree_seq(p, b);
         continue;
       }
-      const int job = all <= INT32_MAX ? (int)at / j.s.units : (int)(at / j.s.units);
+      const int job = all <= INT32_MAX ? (int)((uint32_t)at / (uint32_t)j.s.units) : (int)(at / j.s.units);
       j.b = b;
       j.v0 = (int)(at - (int64_t)job * j.s.units);
       j.v1 = (int)min((int64_t)j.s.units, j.v0 + (x1 - x));

@@ -47,6 +47,7 @@ constexpr int kTreeTcUnit = 1 << kTreeTcUnitLog2;
 // A job as the roles read it.
 struct TreeJobSlot {
   int more;   // 0: no further job
+  int low;    // from here on (or in the sinks) the windows of all its rows reach
   TreeJob j;
 };
 
@@ -67,13 +68,14 @@ struct TreeCfg {
   static constexpr int OFF_K = TILE, OFF_V = OFF_K + NSTG * TILE;
   static constexpr int OFF_RAW = OFF_V + NSTG * TILE;
   static constexpr int OFF_COL = OFF_RAW + NRAW * (2 * CODES + SCALES);
-  static constexpr int OFF_ROW = OFF_COL + NCOL * COL;               // TreeRow [128]
-  static constexpr int OFF_PARENT = OFF_ROW + 128 * (int)sizeof(TreeRow);
+  static constexpr int NVIEW = 2;                                    // jobs whose queries' views are kept
+  static constexpr int OFF_VIEW = OFF_COL + NCOL * COL;              // TreeRow [NVIEW][128], of a job's queries
+  static constexpr int OFF_PARENT = OFF_VIEW + NVIEW * 128 * (int)sizeof(TreeRow);
   static constexpr int OFF_X = OFF_PARENT + kTreeNodes * 4;          // float [2][3][128]: the warpgroups' M, l, z; query sums
   static constexpr int OFF_JOB = OFF_X + 6 * 128 * 4;
   static constexpr int OFF_BAR = (OFF_JOB + kJobSlots * (int)sizeof(TreeJobSlot) + 7) / 8 * 8;
-  // q, full, free [2][NSTG], raw, rawfree [2][NRAW], s [NS], p, o [2][NS], drain, job, taken [kJobSlots]
-  static constexpr int NBAR = 1 + 4 * NSTG + 4 * NRAW + 5 * NS + 1 + 2 * kJobSlots;
+  // q, full, free [2][NSTG], raw, rawfree [2][NRAW], s [NS], p, o [2][NS], drain, job, taken [kJobSlots], view, viewed [NVIEW]
+  static constexpr int NBAR = 1 + 4 * NSTG + 4 * NRAW + 5 * NS + 1 + 2 * kJobSlots + 2 * NVIEW;
   static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
   static constexpr int BYTES = OFF_MISC + 16 + 1024;
   static_assert(OFF_BAR % 8 == 0 && BYTES <= 232448, "shared memory");
@@ -130,7 +132,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
   uint64_t* jbar = drain + 1;       // job written
   uint64_t* taken = jbar + kJobSlots;   // and no longer read
   TreeJobSlot* job_s = reinterpret_cast<TreeJobSlot*>(smem + C::OFF_JOB);
-  TreeRow* row_s = reinterpret_cast<TreeRow*>(smem + C::OFF_ROW);
+  uint64_t* vbar = taken + kJobSlots;   // views of a job's queries written
+  uint64_t* viewed = vbar + C::NVIEW;   // and no longer read (8 warps)
   int* parent_s = reinterpret_cast<int*>(smem + C::OFF_PARENT);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_MISC + 4);
@@ -156,6 +159,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
     for (int s = 0; s < kJobSlots; ++s) {
       mbar_init(&jbar[s], 1);
       mbar_init(&taken[s], kJobReaders);
+    }
+    for (int s = 0; s < C::NVIEW; ++s) {
+      mbar_init(&vbar[s], 1);
+      mbar_init(&viewed[s], 8);
     }
     *abort_flag = 0;
     copied[0] = copied[1] = 0;
@@ -357,19 +364,31 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
           }
         }
       }
-    } else if (attn_elect()) {
-      // ---------------- jobs
+    } else {
+      // ---------------- jobs: written down by lane 0; then what their queries see, a query per lane
       bool more = true;
       for (int it = 0; more; ++it) {
         TreeJob j = {};
-        more = walk.next(p, j);
-        if (it >= kJobSlots &&
-            !attn_wait(&taken[it % kJobSlots], (uint32_t)(it / kJobSlots - 1) & 1u, abort_flag, g_tree_wait_ns))
-          break;
+        more = walk.next(p, j);   // (every lane walks)
+        if (!wait_free(taken, it, kJobSlots)) break;
         TreeJobSlot* x = &job_s[it % kJobSlots];
-        x->more = more;
-        x->j = j;
-        mbar_arrive(&jbar[it % kJobSlots]);
+        // the window of the deepest query that there can be
+        const int deepest = j.s.ctx + min(j.s.nq - 1, tree_node(p, max(0, j.r0 + j.rows - 1)));
+        if (lane == 0) {
+          x->more = more;
+          x->low = p.window > 0 && deepest >= p.window ? deepest - p.window + 1 : 0;
+          x->j = j;
+          mbar_arrive(&jbar[it % kJobSlots]);
+        }
+        if (!more) break;
+        for (int i = lane; i < j.s.nq; i += 32) parent_s[i] = a.parents ? __ldg(a.parents + j.s.q0 + i) : i - 1;
+        if (!wait_free(viewed, it, C::NVIEW)) break;
+        __syncwarp();
+        const int first = tree_node(p, j.r0), last = tree_node(p, j.r0 + j.rows - 1);
+        TreeRow* view = reinterpret_cast<TreeRow*>(smem + C::OFF_VIEW) + (it % C::NVIEW) * 128;
+        for (int i = first + lane; i <= last; i += 32) view[i - first] = tree_row(p, j.s, parent_s, i);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&vbar[it % C::NVIEW]);
       }
     }
   } else {
@@ -400,8 +419,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
       if (!job) break;
       const TreeJob& j = *job;
       const TreeSeq& s = j.s;
-      // (every thread is here past the last job's end: its views, sums and queries are free)
-      if (tid < s.nq) parent_s[tid] = a.parents ? __ldg(a.parents + s.q0 + tid) : tid - 1;
+      // (every thread is here past the last job's end: its sums and queries are free)
       // The queries, their pairs in the order of code_pairs, and their sums: D / 8 lanes share a
       // row, warp w has MMA lanes 16 w .. 16 w + 15.
       {
@@ -436,23 +454,17 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
         __syncwarp();
         if (lane == 0) mbar_arrive(qbar);
       }
-      named_bar_sync(kSoftmaxBarrier, 256);   // parents and sums written
-      if (tid < 128) {
-        const int r = row_of(quad, lane);
-        TreeRow v = {};
-        if (r >= 0 && r < j.rows) v = tree_row(p, s, parent_s, (j.r0 + r) / p.G);
-        row_s[tid] = v;
-      }
+      named_bar_sync(kSoftmaxBarrier, 256);   // the sums are written
       float qs[NE];
 #pragma unroll
       for (int e = 0; e < NE; ++e) qs[e] = xs[quad * 32 + 8 * e + g];
-      named_bar_sync(kSoftmaxBarrier, 256);   // the rows' views written, the sums read
-      // tokens that every row sees: those below `ctx`, from the last row's window on or in the sinks
-      const int ctx = s.ctx;
-      int low = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) low = max(low, row_s[k * 32 + lane].low);
-      low = (int)__reduce_max_sync(0xffffffffu, (unsigned)low);
+      named_bar_sync(kSoftmaxBarrier, 256);   // and read
+      const int ctx = s.ctx, low = job_s[it % kJobSlots].low;
+      // the view of this lane's row, where there is one
+      const int my_row = row_of(quad, lane);
+      const TreeRow* view = reinterpret_cast<const TreeRow*>(smem + C::OFF_VIEW) + (it % C::NVIEW) * 128 +
+                            (my_row >= 0 && my_row < j.rows ? tree_node(p, j.r0 + my_row) - tree_node(p, j.r0) : 0);
+      bool viewing = false;
 
       float m[NE], l[NE], z[NE];   // M; l, z: of this lane's tokens
 #pragma unroll
@@ -489,9 +501,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
         }
         if (at + 64 > ctx || (at < low && at + 64 > p.sinks)) {
           // not every row sees every token: lane r has a bit per token for its row
+          if (!viewing && !(ok = wait_full(vbar, it, C::NVIEW))) break;
+          viewing = true;
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
-            const uint32_t seen = tree_sees(p, s, row_s[quad * 32 + lane], at + 32 * w);
+            const uint32_t seen = tree_sees(p, s, *view, at + 32 * w);
 #pragma unroll
             for (int e = 0; e < NE; ++e) {
               const uint32_t bits = __shfl_sync(0xffffffffu, seen, 8 * e + g) >> (2 * c);
@@ -668,7 +682,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
         tc_fence_before();
       }
       __syncwarp();
-      if (lane == 0) job_done(it);
+      if (lane == 0) {
+        job_done(it);
+        mbar_arrive(&viewed[it % C::NVIEW]);
+      }
       named_bar_sync(kSoftmaxBarrier, 256);   // the rows' numbers have been read
     }
   }
