@@ -355,11 +355,13 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
   }
 }
 
-// Joins the parts of a job that several CTAs share.  Block (c, y): the job that
-// the runs' border c cuts first, rows 8 y .. 8 y + 7; a thread has four values of a row.
+// Joins the parts of a job that several CTAs share, in their order.  Block (c, y): the job that
+// the runs' border c cuts first, rows 8 y .. 8 y + 7; D / 4 lanes share a row, each has four
+// of its values and looks every (D / 4)th part's numbers up for all of them.
 template <int D>
 __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const TreeParams p) {
-  static_assert(kCombineThreads * 4 >= 8 * D, "a thread per four values");
+  constexpr int LPR = D / 4;
+  static_assert(kCombineThreads >= 8 * LPR && LPR <= 32, "eight rows");
   const TreeArgs& a = p.a;
   const int c = blockIdx.x + 1;
   // (the attention kernel started behind what wrote the lengths, and this one behind its start)
@@ -371,33 +373,39 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
   pdl_wait();
   pdl_trigger();
   if (c >= run.ctas) return;
-  if (x == begin || run.bound(c - 1) > begin) return;   // no job cut, or cut before
+  if (x == begin || run.bound(c - 1) > begin || threadIdx.x >= 8 * LPR) return;   // no job cut, or cut before
   const int rows = 1 << p.rows_log2;
-  const int hk = (int)job / s.rts, r = blockIdx.y * 8 + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
+  const int hk = (int)job / s.rts, r = blockIdx.y * 8 + threadIdx.x / LPR, k0 = threadIdx.x % LPR, d = 4 * k0;
   const int row = (((int)job - hk * s.rts) << p.rows_log2) + r;
-  if (threadIdx.x >= 8 * (D / 4) || row >= s.nq * p.G) return;
+  const bool valid = row < s.nq * p.G;
   // parts: the one that CTA c - 1 left, then those that c, c + 1, .. continued
-  auto slot = [&](int i) { return (int64_t)(i < c ? 2 * i + 1 : 2 * i) * rows + r; };
-  int last = c;
-  while (last + 1 < run.ctas && run.bound(last + 1) < end) ++last;
+  auto slot = [&](int i) { return (int64_t)(i ? 2 * (c - 1 + i) : 2 * (c - 1) + 1) * rows + r; };
+  int parts = 2;
+  while (c + parts - 1 < run.ctas && run.bound(c + parts - 1) < end) ++parts;
   float M = -INFINITY;
-#pragma unroll 4
-  for (int i = c - 1; i <= last; ++i) {
-    const float2 x = p.ml[slot(i)];
-    if (x.y != 0.f) M = fmaxf(M, x.x);
+  for (int i = k0; i < parts; i += LPR) {
+    const float2 y = valid ? p.ml[slot(i)] : make_float2(0.f, 0.f);
+    if (y.y != 0.f) M = fmaxf(M, y.x);
   }
+#pragma unroll
+  for (int w = 1; w < LPR; w <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, w));
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   float l = 0.f;
-#pragma unroll 4
-  for (int i = c - 1; i <= last; ++i) {
-    const float2 x = p.ml[slot(i)];
-    const float4 y = *reinterpret_cast<const float4*>(p.o + slot(i) * D + d);
-    if (x.y != 0.f) {
-      const float f = attn_exp2(x.x - M);
-      v.x = fmaf(f, y.x, v.x), v.y = fmaf(f, y.y, v.y), v.z = fmaf(f, y.z, v.z), v.w = fmaf(f, y.w, v.w);
-      l = fmaf(f, x.y, l);
+  for (int i0 = 0; i0 < parts; i0 += LPR) {
+    const float2 y = valid && i0 + k0 < parts ? p.ml[slot(i0 + k0)] : make_float2(0.f, 0.f);
+    const float mine = y.y != 0.f ? attn_exp2(y.x - M) : 0.f;
+    const int n = min(LPR, parts - i0);
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+      const float f = __shfl_sync(0xffffffffu, mine, i, LPR), t = __shfl_sync(0xffffffffu, y.y, i, LPR);
+      if (f != 0.f) {
+        const float4 o = *reinterpret_cast<const float4*>(p.o + slot(i0 + i) * D + d);
+        v.x = fmaf(f, o.x, v.x), v.y = fmaf(f, o.y, v.y), v.z = fmaf(f, o.z, v.z), v.w = fmaf(f, o.w, v.w);
+        l = fmaf(f, t, l);
+      }
     }
   }
+  if (!valid) return;
   const float inv = l != 0.f ? 1.f / l : 0.f;
   const int node = tree_node(p, row), head = row - node * p.G;
   *reinterpret_cast<uint2*>(reinterpret_cast<__half*>(a.out) + ((int64_t)(s.q0 + node) * a.Hq + hk * p.G + head) * D + d) =

@@ -55,7 +55,7 @@ template <int D>
 struct TreeCfg {
   static constexpr int TILE = 128 * D * 2;   // bytes of a Q, K or V operand tile
   static constexpr int NSTG = 2;             // tiles of keys, and of values
-  static constexpr int NS = 2;               // tiles of scores
+  static constexpr int NS = 2;               // tiles of scores; keys are expanded as far ahead of values
   // Tiles of per-token numbers.  Tile n + 2's are written when tile n's scores are done; those
   // came behind tile n - 2's weights.
   static constexpr int NCOL = 4;
@@ -106,6 +106,24 @@ __device__ __forceinline__ uint32_t tree_pair16(uint32_t x) {
 __device__ __forceinline__ uint4 tree_pairs(uint32_t x) {
   const uint32_t y = x >> 8;
   return make_uint4(code_pair(x), tree_pair16(x), code_pair(y), tree_pair16(y));
+}
+
+// attn_wait for whatever `ready` asks for.
+template <typename F>
+__device__ __forceinline__ bool attn_wait_until(F ready, volatile int* abort_flag, uint64_t limit_ns) {
+  uint64_t t0 = 0;
+  while (true) {
+#pragma unroll 1
+    for (int k = 0; k < 512; ++k)
+      if (ready()) return true;
+    if (*abort_flag) return false;
+    const uint64_t t = globaltimer_ns();
+    if (t0 == 0) t0 = t;
+    if (t - t0 > limit_ns) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
 }
 
 constexpr int kSoftmaxBarrier = 1;   // named barrier of the 256 softmax threads
@@ -229,17 +247,19 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
       if (lane == 0) mbar_arrive(bar);
     };
     // Keys are expanded two tiles ahead of values: those wait for products behind a
-    // softmax, and the next scores would wait with them.
-    auto values = [&](int n) {
-      if (!wait_full(raw + NRAW, n, NRAW)) return false;
+    // softmax, and the next scores would wait with them.  A step is the keys of tile n and the
+    // values of tile n - 2, all it waits for asked for at once: an answer takes some 200
+    // cycles, and four in a row were 800 of a step's 2100 for a few rows.
+    auto value_tile = [&](int m) {
       uint4 w[NW];
-      load(smem + C::OFF_RAW + (NRAW + n % NRAW) * C::CODES, w);
+      load(smem + C::OFF_RAW + (NRAW + m % NRAW) * C::CODES, w);
       __syncwarp();
-      if (lane == 0) mbar_arrive(&rawfree[NRAW + n % NRAW]);
-      if (!wait_free(vfree, n, NSTG)) return false;
-      expand(w, smem + C::OFF_V + (n % NSTG) * C::TILE, &vfull[n % NSTG]);
-      return true;
+      if (lane == 0) mbar_arrive(&rawfree[NRAW + m % NRAW]);
+      expand(w, smem + C::OFF_V + (m % NSTG) * C::TILE, &vfull[m % NSTG]);
     };
+    // phases complete: a tile's codes there, its stage free (from the third tile on)
+    auto there = [&](uint64_t* bars, int m, int N) { return attn_test(&bars[m % N], (uint32_t)(m / N) & 1u); };
+    auto left = [&](uint64_t* bars, int m, int N) { return m < N || attn_test(&bars[m % N], (uint32_t)(m / N - 1) & 1u); };
     int n = 0;   // tiles so far
     bool ok = true;
     for (int it = 0; ok; ++it) {
@@ -250,14 +270,21 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
       __syncwarp();
       if (lane == 0) job_done(it);
       for (; v < v1; ++v, ++n) {
-        if (!(ok = wait_full(raw, n, NRAW))) break;
+        const int m = n - 2;
+        ok = attn_wait_until(
+            [&]() {
+              const bool a0 = there(raw, n, NRAW), a1 = left(kfree, n, NSTG);
+              const bool a2 = m < 0 || there(raw + NRAW, m, NRAW), a3 = m < 0 || left(vfree, m, NSTG);
+              return a0 & a1 & a2 & a3;
+            },
+            abort_flag, g_tree_wait_ns);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
         uint4 w[NW];
         load(smem + C::OFF_RAW + (n % NRAW) * C::CODES, w);
         const float4 sc =
             *reinterpret_cast<const float4*>(smem + C::OFF_RAW + 2 * NRAW * C::CODES + (n % NRAW) * C::SCALES + t * 16);
         __syncwarp();
         if (lane == 0) mbar_arrive(&rawfree[n % NRAW]);
-        if (!(ok = wait_free(kfree, n, NSTG))) break;
         const bool in = (v < front ? v : v + skip) * kTreeTcUnit + t < tokens;
         uint8_t* cols = smem + C::OFF_COL + (n % NCOL) * C::COL;
         float* col = reinterpret_cast<float*>(cols) + (t >> 1) * 4 + (t & 1);
@@ -273,12 +300,14 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
         const int to = (t & 64) + (t >> 4 & 3) * 16 + (t >> 1 & 3) * 4 + (t >> 3 & 1) * 2 + (t & 1);
         reinterpret_cast<float*>(cols + C::COL_LOG)[to] = bad ? __int_as_float(0x7fc00000) : log2_of_scale(va);
         expand(w, smem + C::OFF_K + (n % NSTG) * C::TILE, &kfull[n % NSTG]);
-        if (n >= 2 && !(ok = values(n - 2))) break;
+        if (m >= 0) value_tile(m);
       }
     }
     if (ok)
-      for (int m = max(0, n - 2); m < n; ++m)
-        if (!values(m)) break;
+      for (int m = max(0, n - 2); m < n; ++m) {
+        if (!wait_full(raw + NRAW, m, NRAW) || !wait_free(vfree, m, NSTG)) break;
+        value_tile(m);
+      }
   } else if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
     if (warp == 8) {
@@ -292,7 +321,6 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
           return ok = ok && attn_wait(&bars[m % N], (uint32_t)(m / N) & 1u, abort_flag, g_tree_wait_ns);
         };
         auto scores = [&](int m) {   // (its columns' weights were taken by products issued before)
-          if (!wait(kfull, m, NSTG)) return;
           tc_fence_after();
           attn_mma_qk<D>((m % NS) * 128, q_lo, k_lo + (m % NSTG) * (C::TILE >> 4), idesc);
           tc_commit(&sbar[m % NS]);
@@ -304,14 +332,22 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
           const int end = n + job->v1 - job->v0, first = n;
           job_done(it);
           if (!wait(qbar, it, 1)) break;
-          for (int m = n; m < min(end, n + NS); ++m) scores(m);
+          for (int m = n; m < min(end, n + NS) && wait(kfull, m, NSTG); ++m) scores(m);
 #pragma unroll 1
           for (; ok && n < end; ++n) {
-            if (!wait(vfull, n, NSTG)) break;
+            // (values and the first weights asked for at once; the keys two tiles on were written before the values)
+            if (!(ok = attn_wait_until(
+                      [&]() {
+                        const bool a0 = attn_test(&vfull[n % NSTG], (uint32_t)(n / NSTG) & 1u);
+                        const bool a1 = attn_test(&pbar[n % NS], (uint32_t)(n / NS) & 1u);
+                        return a0 & a1;
+                      },
+                      abort_flag, g_tree_wait_ns)))
+              break;
             const uint32_t vd = v_lo + (n % NSTG) * (C::TILE >> 4), pt = (n % NS) * 128;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              if (!wait(pbar + i * NS, n, NS)) break;
+              if (i && !wait(pbar + NS, n, NS)) break;
               tc_fence_after();
               tree_mma_pv<D>(OCOL + i * D, pt + 64 * i, vd + 4 * i * (2048 >> 4), 0, n > first);
               if (NE == 4) tree_mma_pv<D>(OCOL + i * D, pt + 64 * i, vd + 4 * i * (2048 >> 4), 1, true);
