@@ -42,6 +42,19 @@ __device__ __forceinline__ uint4 code_pairs(uint32_t x) {
   return make_uint4(code_pair(x), code_pair(x >> 4), code_pair(x >> 8), code_pair(x >> 12));
 }
 
+// code_pairs with one shift in place of three: the codes at bits 4 and 20 are 1024 + 16 u, exact,
+// and so is their sixteenth less 72.
+__device__ __forceinline__ uint32_t code_pair16(uint32_t x) {
+  const uint32_t m = and_or(x, 0x00F000F0u, 0x64006400u);
+  const __half2 h = __hfma2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x2c00)),    // 1 / 16
+                            __half2half2(__ushort_as_half(0xd480)));                                        // -72
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint4 code_pairs1(uint32_t x) {
+  const uint32_t y = x >> 8;
+  return make_uint4(code_pair(x), code_pair16(x), code_pair(y), code_pair16(y));
+}
+
 __device__ __forceinline__ uint32_t own_transpose(uint32_t x) {   // 8x8 fp16 transpose over the warp
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));

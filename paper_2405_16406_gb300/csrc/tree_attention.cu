@@ -20,6 +20,7 @@
 // tree_combine_kernel joins them, in the order of the keys; every other job is
 // complete in its CTA.
 #include <cuda_fp16.h>
+#include <float.h>
 
 #include "../../include/spinq.h"
 #include "attn_tc.cuh"
@@ -206,22 +207,22 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
           for (int e = 0; e < 2; ++e)
             t[nb][h][e] = fmaf(ka, fmaf(0.0625f, s16[nb][2 * h + e], sa[nb][2 * h + e]), fmaf(sc[h].y, qsk[nb][e], la));
       }
-      // Not every row sees every token: -inf, and no share of the sums, whose factors may
-      // be anything (a slot that was never written, a page given back).
-      uint32_t hidden = 0;   // bit 4 nb + 2 h + e
+      // Not every row sees every token: -inf.  Factors that are not finite (a slot that was never
+      // written, a page given back, a row of NaN) would give 0 times them: they are 0 here, and the
+      // score of a row that does see the token is not a number.
       if (t0 + 16 > s.ctx || (t0 < low && t0 + 16 > p.sinks)) {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int h = 0; h < 2; ++h) {
+          const bool bad = !(fabsf(rv[h]) <= FLT_MAX && fabsf(vz[h]) <= FLT_MAX);
+          if (bad) rv[h] = vz[h] = 0.f;
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t bits = tree_sees(p, s, row_s[8 * nb + 2 * c + e], t0) >> g;
+          for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (!((bits >> (8 * h)) & 1u)) {
-                hidden |= 1u << (4 * nb + 2 * h + e);
-                t[nb][h][e] = -INFINITY;
-              }
-          }
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t bits = tree_sees(p, s, row_s[8 * nb + 2 * c + e], t0) >> (g + 8 * h);
+              t[nb][h][e] = bits & 1u ? (bad ? __int_as_float(0x7fc00000) : t[nb][h][e]) : -INFINITY;
+            }
+        }
       }
       bool grow = false;
       float mx[NB][2];
@@ -268,9 +269,8 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             w[h][e] = attn_exp2(t[nb][h][e] - off[nb][e]);
-            const bool seen = !((hidden >> (4 * nb + 2 * h + e)) & 1u);
-            l[nb][e] = fmaf(w[h][e], seen ? rv[h] : 0.f, l[nb][e]);
-            z[nb][e] = fmaf(w[h][e], seen ? vz[h] : 0.f, z[nb][e]);
+            l[nb][e] = fmaf(w[h][e], rv[h], l[nb][e]);
+            z[nb][e] = fmaf(w[h][e], vz[h], z[nb][e]);
           }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
           // two bytes of two tokens' rows: one dimension of both in a pair
           const uint32_t xa = __byte_perm(vx[0][vw], vx[1][vw], q ? 0x7632 : 0x5410);
           const uint32_t xb = __byte_perm(vx[2][vw], vx[3][vw], q ? 0x7632 : 0x5410);
-          const uint4 ya = code_pairs(xa), yb = code_pairs(xb);
+          // (as u - 8: the values' sums would lose bits on the numbers that fp16 has below its normal ones)
+          const uint4 ya = code_pairs1(xa), yb = code_pairs1(xb);
           const uint32_t a0[4] = {ya.x, ya.y, yb.x, yb.y}, a1[4] = {ya.z, ya.w, yb.z, yb.w};
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
@@ -398,8 +399,8 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
 #pragma unroll 8
     for (int i = 0; i < n; ++i) {
       const float f = __shfl_sync(0xffffffffu, mine, i, LPR), t = __shfl_sync(0xffffffffu, y.y, i, LPR);
-      if (f != 0.f) {
-        const float4 o = *reinterpret_cast<const float4*>(p.o + slot(i0 + i) * D + d);
+      const float4 o = *reinterpret_cast<const float4*>(p.o + slot(i0 + i) * D + d);
+      if (f != 0.f) {   // (a row past the queries' end was not written)
         v.x = fmaf(f, o.x, v.x), v.y = fmaf(f, o.y, v.y), v.z = fmaf(f, o.z, v.z), v.w = fmaf(f, o.w, v.w);
         l = fmaf(f, t, l);
       }

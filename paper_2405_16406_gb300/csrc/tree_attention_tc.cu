@@ -95,19 +95,6 @@ __device__ __forceinline__ void tree_mma_pv(uint32_t o_tmem, uint32_t p_tmem, ui
   for (int ks = 1; ks < 4; ++ks) attn_mma_ts<true>(o_tmem, w + ks * 8, v_lo + ks * (2048 >> 4), idesc);
 }
 
-// code_pairs with one shift in place of three: the codes at bits 4 and 20 are 1024 + 16 u, exact,
-// and so is their sixteenth less 72.
-__device__ __forceinline__ uint32_t tree_pair16(uint32_t x) {
-  const uint32_t m = and_or(x, 0x00F000F0u, 0x64006400u);
-  const __half2 h = __hfma2(*reinterpret_cast<const __half2*>(&m), __half2half2(__ushort_as_half(0x2c00)),    // 1 / 16
-                            __half2half2(__ushort_as_half(0xd480)));                                        // -72
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint4 tree_pairs(uint32_t x) {
-  const uint32_t y = x >> 8;
-  return make_uint4(code_pair(x), tree_pair16(x), code_pair(y), tree_pair16(y));
-}
-
 // attn_wait for whatever `ready` asks for.
 template <typename F>
 __device__ __forceinline__ bool attn_wait_until(F ready, volatile int* abort_flag, uint64_t limit_ns) {
@@ -239,7 +226,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int ch = 4 * piece + q;   // 16-byte chunk (8 values) of the row
-          *reinterpret_cast<uint4*>(dst + (ch >> 3) * kAttnAtom + (((ch & 7) ^ (t & 7)) << 4)) = tree_pairs(x[q]);
+          *reinterpret_cast<uint4*>(dst + (ch >> 3) * kAttnAtom + (((ch & 7) ^ (t & 7)) << 4)) = code_pairs1(x[q]);
         }
       }
       fence_proxy_async_smem();
