@@ -381,8 +381,7 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
   const bool valid = row < s.nq * p.G;
   // parts: the one that CTA c - 1 left, then those that c, c + 1, .. continued
   auto slot = [&](int i) { return (int64_t)(i ? 2 * (c - 1 + i) : 2 * (c - 1) + 1) * rows + r; };
-  int parts = 2;
-  while (c + parts - 1 < run.ctas && run.bound(c + parts - 1) < end) ++parts;
+  const int parts = run.owner(end - 1) - (c - 1) + 1;
   float M = -INFINITY;
   for (int i = k0; i < parts; i += LPR) {
     const float2 y = valid ? p.ml[slot(i)] : make_float2(0.f, 0.f);
@@ -396,13 +395,21 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
     const float2 y = valid && i0 + k0 < parts ? p.ml[slot(i0 + k0)] : make_float2(0.f, 0.f);
     const float mine = y.y != 0.f ? attn_exp2(y.x - M) : 0.f;
     const int n = min(LPR, parts - i0);
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-      const float f = __shfl_sync(0xffffffffu, mine, i, LPR), t = __shfl_sync(0xffffffffu, y.y, i, LPR);
-      const float4 o = *reinterpret_cast<const float4*>(p.o + slot(i0 + i) * D + d);
-      if (f != 0.f) {   // (a row past the queries' end was not written)
-        v.x = fmaf(f, o.x, v.x), v.y = fmaf(f, o.y, v.y), v.z = fmaf(f, o.z, v.z), v.w = fmaf(f, o.w, v.w);
-        l = fmaf(f, t, l);
+    for (int i1 = 0; i1 < n; i1 += 8) {   // eight parts' values under way at once
+      float4 o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];\n"
+                     : "=f"(o[i].x), "=f"(o[i].y), "=f"(o[i].z), "=f"(o[i].w)
+                     : "l"(p.o + slot(i0 + min(i1 + i, n - 1)) * D + d));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int k = min(i1 + i, n - 1);
+        const float f = __shfl_sync(0xffffffffu, mine, k, LPR), t = __shfl_sync(0xffffffffu, y.y, k, LPR);
+        if (i1 + i < n && f != 0.f) {   // (a row past the queries' end was not written)
+          v.x = fmaf(f, o[i].x, v.x), v.y = fmaf(f, o[i].y, v.y), v.z = fmaf(f, o[i].z, v.z), v.w = fmaf(f, o[i].w, v.w);
+          l = fmaf(f, t, l);
+        }
       }
     }
   }

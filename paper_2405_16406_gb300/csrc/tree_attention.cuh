@@ -65,6 +65,13 @@ struct TreeRun {
   int rest, ctas, b;
   TreeSeq s;   // of sequence b
   __device__ __forceinline__ int64_t bound(int c) const { return per * c + min(c, rest); }
+  // the run that unit x is in
+  __device__ __forceinline__ int owner(int64_t x) const {
+    const int64_t longer = (per + 1) * rest;   // units of the runs that have one more
+    const int64_t y = x < longer ? x : x - longer, by = x < longer ? per + 1 : per;
+    const int c = y <= INT32_MAX && by <= INT32_MAX ? (int)((uint32_t)y / (uint32_t)by) : (int)(y / by);
+    return x < longer ? c : rest + c;
+  }
 };
 
 template <int THREADS>
