@@ -10,10 +10,14 @@
 // order) lies i below its top, and page a of all that are needed is the a-th from
 // the top, so a sequence that gives and takes gets its own pages back.  Three
 // prefix sums over the batch (tokens, freed, needed pages) say where everything is:
-// every CTA of a cluster takes them by itself, in shared memory, then the
-// cluster's threads share the pages and tokens.  The stack is written before the
-// cluster's barrier and read behind it.  Bound: latency (a chain of the lengths'
-// loads, three block-wide sums, a barrier, and two dependent loads).
+// every CTA takes them by itself, in shared memory.
+//  * Up to kPlanTokens rows: one kernel, of one CTA or a cluster, whose threads share the pages
+//    and tokens.  The stack is written before a barrier and read behind it.
+//  * More: the tokens by a kernel that fills the GPU and reads the lists as they were, then
+//    the lists and lengths by the one cluster (1000 sequences, 251 K tokens: 60 us in one
+//    kernel, whose 4096 threads had 64 dependent look-ups each).
+// Bound: latency (a chain of the lengths' loads, three block-wide sums, a barrier, and
+// two dependent loads).
 //
 // Keep.  A path ascends, so a token never moves up and never onto one that is
 // still to be read by a later part of its path: a CTA takes the 16-byte pieces of
@@ -25,15 +29,16 @@
 namespace spinq {
 namespace {
 
-constexpr int kPlanThreads = 512;
 constexpr int kPlanCluster = 8;
-constexpr int kPlanPer = kPlanMaxBatch / kPlanThreads;   // sequences per thread at most
+constexpr int64_t kPlanTokens = 8192;
+enum PlanPart { kPlanAll = 0, kPlanRows = 1, kPlanLists = 2 };
 
 // Sums of whole numbers in [0, 2^31) that stay there.
 constexpr uint32_t kPlanMost = 0x7fffffffu;
 __device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, kPlanMost); }
 
 // Exclusive prefix sum of x over the block and the total; `part`: a word per warp.
+template <int THREADS>
 __device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t* part, uint32_t* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t s = x;
@@ -47,7 +52,7 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t* part, uin
   __syncthreads();
   uint32_t before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kPlanThreads / 32; ++w) {
+  for (int w = 0; w < THREADS / 32; ++w) {
     if (w == warp) before = all;
     all = sat_add(all, part[w]);
   }
@@ -67,17 +72,11 @@ __device__ __forceinline__ int last_at_most(const uint32_t* start, int n, uint32
   return lo;
 }
 
-__device__ __forceinline__ void plan_barrier(bool cluster) {
-  __threadfence();
-  if (cluster)
-    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;\n" ::: "memory");
-  else
-    __syncthreads();
-}
-
-__global__ void __launch_bounds__(kPlanThreads) kv4_plan_kernel(const PlanArgs a) {
+// PER: sequences per thread at most.
+template <int THREADS, int PER, int PART>
+__global__ void __launch_bounds__(THREADS) kv4_plan_kernel(const PlanArgs a) {
   extern __shared__ uint32_t plan_smem[];
-  __shared__ uint32_t part[kPlanThreads / 32];
+  __shared__ uint32_t part[THREADS / 32];
   const int B = (int)a.batch;
   uint32_t* start = plan_smem;        // tokens that stay
   uint32_t* cu = start + B;           // tokens asked for before this sequence
@@ -85,31 +84,31 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_plan_kernel(const PlanArgs a
   uint32_t* taken = freed + B;        // pages needed before it
   uint32_t* gets = taken + B;         // pages it gets, or kPlanMost: refused
   const int tid = threadIdx.x, shift = a.page_shift;
-  const bool cluster = gridDim.x > 1;
-  const uint32_t stride = gridDim.x * kPlanThreads, first = blockIdx.x * kPlanThreads + tid;
+  const uint32_t stride = gridDim.x * THREADS, first = blockIdx.x * THREADS + tid;
   const uint32_t page1 = (1u << shift) - 1, cap = (uint32_t)(a.table_width << shift), total = (uint32_t)a.total;
   auto pages = [&](uint32_t tokens) { return (tokens + page1) >> shift; };   // tokens <= 2^31 - 256
   pdl_wait();
   pdl_trigger();
 
-  for (int b = tid; b < B; b += kPlanThreads) {
+  const int32_t count0 = *a.free_count;
+  for (int b = tid; b < B; b += THREADS) {
     const uint32_t len = min((uint32_t)max(a.lens[b], 0), cap), drop = a.drop ? (uint32_t)max(a.drop[b], 0) : 0u;
     const uint32_t s = len > drop ? len - drop : 0u;
     start[b] = s;
     freed[b] = pages(len) - pages(s);
     cu[b] = a.add ? (uint32_t)max(a.add[b], 0) : 0u;
   }
-  const int32_t count0 = *a.free_count;
   __syncthreads();
   // a thread's sequences lie next to one another
-  const int per = (B + kPlanThreads - 1) / kPlanThreads, b0 = min(tid * per, B), b1 = min(b0 + per, B);
+  const int per = (B + THREADS - 1) / THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
   uint32_t sum_add = 0, sum_freed = 0;
   for (int b = b0; b < b1; ++b) sum_add = sat_add(sum_add, cu[b]), sum_freed = sat_add(sum_freed, freed[b]);
   uint32_t all_add, all_freed, all_need;
-  uint32_t at_add = block_prefix(sum_add, part, &all_add), at_freed = block_prefix(sum_freed, part, &all_freed);
-  uint32_t need[kPlanPer], sum_need = 0;
+  uint32_t at_add = block_prefix<THREADS>(sum_add, part, &all_add);
+  uint32_t at_freed = block_prefix<THREADS>(sum_freed, part, &all_freed);
+  uint32_t need[PER], sum_need = 0;
 #pragma unroll
-  for (int k = 0; k < kPlanPer; ++k) {
+  for (int k = 0; k < PER; ++k) {
     need[k] = 0;
     if (b0 + k < b1) {
       const int b = b0 + k;
@@ -120,17 +119,17 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_plan_kernel(const PlanArgs a
       at_freed = sat_add(at_freed, f);
       // it fits the answer's arrays and its row of the table (start <= cap)
       const bool fits = add == 0 || (at_add <= total && add <= cap - start[b]);
-      need[k] = fits ? pages(start[b] + (fits ? add : 0)) - pages(start[b]) : 0u;
+      need[k] = fits ? pages(start[b] + add) - pages(start[b]) : 0u;
       gets[b] = fits ? need[k] : kPlanMost;
       sum_need = sat_add(sum_need, need[k]);
     }
   }
-  uint32_t at_need = block_prefix(sum_need, part, &all_need);
+  uint32_t at_need = block_prefix<THREADS>(sum_need, part, &all_need);
   const uint32_t count = (uint32_t)min(max((int64_t)count0, (int64_t)0), a.free_capacity);
   const uint32_t there = (uint32_t)min((int64_t)sat_add(count, all_freed), a.free_capacity);   // free pages
-  uint32_t given = 0;   // a lower bound of the pages handed out: what precedes the last that got some, and its own
+  uint32_t given = 0;
 #pragma unroll
-  for (int k = 0; k < kPlanPer; ++k)
+  for (int k = 0; k < PER; ++k)
     if (b0 + k < b1) {
       const int b = b0 + k;
       taken[b] = at_need;
@@ -147,52 +146,63 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_plan_kernel(const PlanArgs a
   __syncthreads();
   given = 0;
 #pragma unroll
-  for (int w = 0; w < kPlanThreads / 32; ++w) given = max(given, part[w]);
+  for (int w = 0; w < THREADS / 32; ++w) given = max(given, part[w]);
 
-  // freed pages onto the stack
-  for (uint32_t i = first; i < all_freed && i < there; i += stride) {
+  // where freed page i of all lies, as long as the table has not been written
+  auto freed_page = [&](uint32_t i) -> const int32_t* {
     const int b = last_at_most(freed, B, i);
-    const uint32_t p = pages(start[b]) + i - freed[b], to = there - 1 - i;
-    if (to >= count && p < (uint32_t)a.table_width) a.free_pages[to] = a.table[(int64_t)b * a.table_width + p];
-  }
-  plan_barrier(cluster);
-
-  // pages from its top into the tables
-  for (uint32_t i = first; i < given; i += stride) {
-    const int b = last_at_most(taken, B, i);
-    a.table[(int64_t)b * a.table_width + pages(start[b]) + i - taken[b]] = __ldcg(a.free_pages + (there - 1 - i));
+    return a.table + (int64_t)b * a.table_width + pages(start[b]) + i - freed[b];
+  };
+  if (PART != kPlanRows) {
+    // freed pages onto the stack (where a list that is too short left room for them)
+    for (uint32_t i = first; i < all_freed && i < there; i += stride)
+      if (there - 1 - i >= count) a.free_pages[there - 1 - i] = *freed_page(i);
+    if (gridDim.x > 1) {
+      __threadfence();
+      asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;\n" ::: "memory");
+    } else {
+      __syncthreads();
+    }
+    // pages from its top into the tables
+    for (uint32_t i = first; i < given; i += stride) {
+      const int b = last_at_most(taken, B, i);
+      a.table[(int64_t)b * a.table_width + pages(start[b]) + i - taken[b]] = __ldcg(a.free_pages + (there - 1 - i));
+    }
   }
   // positions and slots
-  for (uint32_t t = first; t < total; t += stride) {
-    int64_t slot = -1, pos = 0;
-    if (t < all_add) {
-      const int b = last_at_most(cu, B, t);
-      const uint32_t s = start[b], i = t - cu[b], at = s + i, kept = pages(s);
-      const uint32_t got = gets[b];
-      pos = min(max((int64_t)s + (a.depths ? (int64_t)a.depths[t] : (int64_t)i) + a.position_offset, (int64_t)0),
-                (int64_t)INT32_MAX);
-      if (got != kPlanMost) {
-        const uint32_t p = at >> shift;
-        const int32_t page = p < kept ? __ldcg(a.table + (int64_t)b * a.table_width + p)
-                                      : __ldcg(a.free_pages + (there - 1 - (taken[b] + p - kept)));
-        slot = ((int64_t)page << shift) + (at & page1);
+  if (PART != kPlanLists) {
+    for (uint32_t t = first; t < total; t += stride) {
+      int64_t slot = -1, pos = 0;
+      if (t < all_add) {
+        const int b = last_at_most(cu, B, t);
+        const uint32_t s = start[b], i = t - cu[b], at = s + i, kept = pages(s);
+        pos = min(max((int64_t)s + (a.depths ? (int64_t)a.depths[t] : (int64_t)i) + a.position_offset, (int64_t)0),
+                  (int64_t)INT32_MAX);
+        if (gets[b] != kPlanMost) {
+          const uint32_t p = at >> shift, k = taken[b] + p - kept;   // a new page: number k from the stack's top
+          const int32_t* where = p < kept ? a.table + (int64_t)b * a.table_width + p : a.free_pages + (there - 1 - k);
+          if (PART == kPlanRows && p >= kept && there - 1 - k >= count) where = freed_page(k);   // not on the stack yet
+          slot = ((int64_t)__ldcg(where) << shift) + (at & page1);
+        }
       }
+      a.positions[t] = (int32_t)pos;
+      a.slots[t] = slot;
     }
-    a.positions[t] = (int32_t)pos;
-    a.slots[t] = slot;
   }
   // the batch's numbers, the last of all: every CTA has read the lengths
-  for (uint32_t b = first; b <= (uint32_t)B; b += stride) {
-    if (b == (uint32_t)B) {
-      a.cu_tokens[B] = (int32_t)min(all_add, total);
-      *a.free_count = (int32_t)(there - given);
-      break;
+  if (PART != kPlanRows) {
+    for (uint32_t b = first; b <= (uint32_t)B; b += stride) {
+      if (b == (uint32_t)B) {
+        a.cu_tokens[B] = (int32_t)min(all_add, total);
+        *a.free_count = (int32_t)(there - given);
+        break;
+      }
+      const bool ok = gets[b] != kPlanMost;
+      const uint32_t next = b + 1 < (uint32_t)B ? cu[b + 1] : all_add;
+      a.cu_tokens[b] = (int32_t)min(cu[b], total);
+      if (a.granted) a.granted[b] = ok;
+      a.lens[b] = (int32_t)(start[b] + (ok ? next - cu[b] : 0u));
     }
-    const bool ok = gets[b] != kPlanMost;
-    const uint32_t next = b + 1 < (uint32_t)B ? cu[b + 1] : all_add;
-    a.cu_tokens[b] = (int32_t)min(cu[b], total);
-    if (a.granted) a.granted[b] = ok;
-    a.lens[b] = (int32_t)(start[b] + (ok ? next - cu[b] : 0u));
   }
 }
 
@@ -244,14 +254,26 @@ __global__ void __launch_bounds__(kKeepThreads) kv4_keep_kernel(const KeepArgs a
 
 }  // namespace
 
-cudaError_t launch_kv4_plan(const PlanArgs& a, cudaStream_t stream) {
-  const int smem = (int)a.batch * 5 * 4;
+template <int THREADS, int PER, int PART>
+static cudaError_t launch_plan_t(const PlanArgs& a, int ctas, int cluster, cudaStream_t stream) {
   int per_sm = 1;
-  cudaError_t e = prepare_launch(kv4_plan_kernel, kPlanThreads, kPlanMaxBatch * 5 * 4, &per_sm);
+  cudaError_t e = prepare_launch(kv4_plan_kernel<THREADS, PER, PART>, THREADS, THREADS * PER * 5 * 4, &per_sm);
   if (e != cudaSuccess) return e;
-  // one CTA where each of its threads has little to do: no cluster's barrier
-  const int ctas = a.total + a.batch * 4 <= 4 * kPlanThreads ? 1 : kPlanCluster;
-  e = launch_pdl(kv4_plan_kernel, dim3((unsigned)ctas), dim3(kPlanThreads), (size_t)smem, stream, ctas, a);
+  return launch_pdl(kv4_plan_kernel<THREADS, PER, PART>, dim3((unsigned)ctas), dim3(THREADS), (size_t)a.batch * 5 * 4,
+                    stream, cluster, a);
+}
+
+cudaError_t launch_kv4_plan(const PlanArgs& a, cudaStream_t stream) {
+  cudaError_t e;
+  if (a.total + a.batch * 4 <= 1024) {   // one small CTA: short sums, no cluster's barrier
+    e = launch_plan_t<128, 2, kPlanAll>(a, 1, 1, stream);
+  } else if (a.total <= kPlanTokens) {
+    e = launch_plan_t<512, 8, kPlanAll>(a, kPlanCluster, kPlanCluster, stream);
+  } else {
+    const int64_t want = (a.total + 511) / 512, most = device_sm_count();
+    e = launch_plan_t<512, 8, kPlanRows>(a, (int)(want < most ? want : most), 1, stream);
+    if (e == cudaSuccess) e = launch_plan_t<512, 8, kPlanLists>(a, kPlanCluster, kPlanCluster, stream);
+  }
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
