@@ -102,14 +102,21 @@ struct PromptCfg {
 // three warpgroups: two of softmax with 216 registers a thread, one with the
 // copies and the MMAs with 72; 2 * 216 + 72 = 3 * 168, what the launch holds
 constexpr int kPromptThreads = 384;
+constexpr int kSinkRows = 32;
 // the item's readers: copy thread, two MMA threads, eight softmax warps
 constexpr int kItemReaders = 11;
 
-// WIN: a query at position p sees keys j <= p with p - j < window or j < sinks.
+// WIN: a query at position p sees keys j <= p with p - j < window or j < sinks.  An item's keys are
+// then a list: the sinks in whole groups of kSinkRows, and behind them those from the first that the
+// window of the item's first query reaches, so that a few sinks cost a part of a tile and
+// no tile starts before the window (2 x 32 queries with a window of 512 and 4 sinks: 5 tiles of
+// 128; with a tile of sinks and tiles at whole multiples of 128 tokens 6.5: 16 ragged sequences of
+// 32767 tokens 471 us so).
 template <int D, bool WIN>
 __global__ void __launch_bounds__(kPromptThreads, 1)
     prompt_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-                     const __grid_constant__ CUtensorMap mv, const PromptParams a) {
+                     const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mks,
+                     const __grid_constant__ CUtensorMap mvs, const PromptParams a) {
   using C = PromptCfg<D>;
   constexpr int NSTG = C::NSTG;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -169,27 +176,28 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
   struct Work {
     int hk, t0, lq, lk, nt[2], ntile;
     int64_t q0, k0;
-    // WIN: the tiles are the first `front` of the sequence (the sinks), then, `skip` further on, those from the
-    // first that the window of the item's first query reaches
-    int front, skip;
-    __device__ __forceinline__ int at(int j) const { return WIN && j >= front ? j + skip : j; }   // tile j of the list
+    int front, from;   // WIN: rows of sinks at the list's start; the token behind them
   };
   auto read_item = [&](int slot, Work& w) {
     const volatile PromptItem& x = items[slot];
     w.hk = x.hk, w.t0 = x.t0, w.lq = x.lq, w.lk = x.lk, w.q0 = x.q0, w.k0 = x.k0;
-    w.front = w.skip = 0;
+    w.front = w.from = 0;
     if constexpr (WIN) {
       const int first = w.t0 + w.lk - w.lq;   // position of the item's first query
-      const int reach = first >= a.window ? (first - a.window + 1) >> 7 : 0;
-      w.front = min((int)(((int64_t)a.sinks + 127) >> 7), reach);
-      w.skip = reach - w.front;
+      const int low = first >= a.window ? first - a.window + 1 : 0;
+      // (rows of the front are tokens before the window, and so of the sequence)
+      const int64_t front = ((int64_t)a.sinks + kSinkRows - 1) / kSinkRows * kSinkRows;
+      if (front <= low) {
+        w.front = (int)front;
+        w.from = low;
+      }
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int first = w.t0 + i * a.tpt, last = min(first + a.tpt, w.lq) - 1;
       const int nk = first < w.lq ? (a.causal ? max(0, min(w.lk, last + 1 + w.lk - w.lq)) : w.lk) : 0;
-      w.nt[i] = (nk + 127) / 128;
-      if (WIN && nk > 0) w.nt[i] -= w.skip;   // (a tile with a key reaches past the item's first query)
+      // (WIN: a tile that sees a key sees it behind the window's start)
+      w.nt[i] = ((WIN && nk > 0 ? nk - w.from + w.front : nk) + 127) / 128;
     }
     w.ntile = max(w.nt[0], w.nt[1]);
     return x.more != 0;
@@ -223,10 +231,22 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
             // (a fresh barrier answers the parity before its first phase at once)
             if (!(ok = attn_wait(&free_[sk], pk, abort_flag, g_prompt_wait_ns))) break;
             mbar_arrive_expect_tx(&full[sk], (uint32_t)C::TILE);
+            const int row = (n >> 1) * 128;
+            if (WIN && row < w.front && row + 128 > w.front) {
+              // the last sinks and the window's first keys
+#pragma unroll 1
+              for (int r = 0; r < 128; r += kSinkRows)
 #pragma unroll
-            for (int at = 0; at < D / 64; ++at)
-              tma_load_3d(smem + C::OFF_KV + sk * C::TILE + at * kAttnAtom, n & 1 ? &mv : &mk, &full[sk], at * 64, w.hk,
-                          (int32_t)(w.k0 + w.at(n >> 1) * 128));
+                for (int at = 0; at < D / 64; ++at)
+                  tma_load_3d(smem + C::OFF_KV + sk * C::TILE + at * kAttnAtom + r * 128, n & 1 ? &mvs : &mks, &full[sk], at * 64,
+                              w.hk, (int32_t)(w.k0 + (row + r < w.front ? row + r : row + r - w.front + w.from)));
+            } else {
+              const int token = WIN && row >= w.front ? row - w.front + w.from : row;
+#pragma unroll
+              for (int at = 0; at < D / 64; ++at)
+                tma_load_3d(smem + C::OFF_KV + sk * C::TILE + at * kAttnAtom, n & 1 ? &mv : &mk, &full[sk], at * 64, w.hk,
+                            (int32_t)(w.k0 + token));
+            }
             ++issued[0];
             if (++sk == NSTG) sk = 0, pk ^= 1;
           }
@@ -375,7 +395,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
     for (int it = 0; ok; ++it) {
       if (!(ok = attn_wait_warp(&item[it & 1], (uint32_t)(it >> 1) & 1u, abort_flag, g_prompt_wait_ns))) break;
       int nti, lk, kv_after, n;   // n: keys of this row
-      int low = 0, front = 0, skip = 0;   // WIN: its window's first key; the list of tiles
+      int low = 0;   // WIN: the list's first key of its window.  n and lk are places in the list too.
       {
         Work w;
         if (!read_item(it & 1, w)) break;
@@ -385,11 +405,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         const int tok = w.t0 + i * a.tpt + row_t;
         n = r < a.G * a.tpt && tok < w.lq ? (a.causal ? min(lk, tok + 1 + lk - w.lq) : lk) : 128 * nti;
         if constexpr (WIN) {
-          front = w.front, skip = w.skip;
-          if (r < a.G * a.tpt && tok < w.lq)
-            low = tok + lk - w.lq >= a.window ? tok + lk - w.lq - a.window + 1 : 0;
-          else
-            n = 128 * (nti + skip);   // a row without a query: every key of the list
+          const int shift = w.front - w.from;   // of a window's key, from its token to its place
+          lk += shift;
+          if (r < a.G * a.tpt && tok < w.lq) {
+            const int pos = tok + w.lk - w.lq;
+            low = (pos >= a.window ? pos - a.window + 1 : 0) + shift;
+            n += shift;
+          }
         }
       }
       float m = -INFINITY, l = 0.f;
@@ -400,8 +422,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
 #pragma unroll
         for (int c = 0; c < 128; c += 32) tmem_ld_32x32b_x32(st + c, s + c);
         tmem_ld_wait_all<128>(s);
-        const int base = 128 * (WIN && j >= front ? j + skip : j);   // first key of the tile
-        const int seen = n - base;
+        const int seen = n - j * 128;
         if (__any_sync(0xffffffffu, seen < 128)) {
 #pragma unroll
           for (int c = 0; c < 128; ++c)
@@ -409,7 +430,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         }
         if constexpr (WIN) {
           // keys between the sinks and the row's window
-          const int from = a.sinks - base, to = low - base;
+          const int from = a.sinks - j * 128, to = low - j * 128;
           if (__any_sync(0xffffffffu, to > 0 && from < 128 && from < to)) {
 #pragma unroll
             for (int c = 0; c < 128; ++c)
@@ -443,12 +464,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
         l = x + y;
         tmem_st_32x32b_x32(st, s);
         tmem_st_32x32b_x32(st + 32, s + 32);
-        if (base + 128 > lk) {
+        if (j * 128 + 128 > lk) {
           // this V tile ends past the sequence: thread r zeroes row r if it lies there
           // (the threads of the other tile may write the same zeros)
           const int nv = kv + 2 * j + 1;
           if (!(ok = attn_wait_warp(&full[nv % NSTG], (uint32_t)(nv / NSTG) & 1u, abort_flag, g_prompt_wait_ns))) break;
-          if (base + r >= lk) {
+          if (j * 128 + r >= lk) {
             const uint32_t vb = sb + C::OFF_KV + (nv % NSTG) * C::TILE + r * 128;
 #pragma unroll
             for (int at = 0; at < D / 64; ++at)
@@ -535,12 +556,16 @@ cudaError_t launch_t(const PromptArgs& a, cudaStream_t stream) {
   PromptParams p{};
   p.G = (int)(a.Hq / a.Hkv);
   p.tpt = 128 / p.G;
-  CUtensorMap mq, mk, mv;
+  CUtensorMap mq, mk, mv, mks, mvs;
   // without any key no K or V tile is copied: their maps only have to be valid
   const bool keys = a.total_k > 0;
   if (!encode_heads(enc, &mq, a.q, a.total_q, a.Hq, D, a.ldq, p.G, p.tpt) ||
       !encode_heads(enc, &mk, keys ? a.k : a.q, keys ? a.total_k : 1, keys ? a.Hkv : 1, D, keys ? a.ldk : D, 1, 128) ||
       !encode_heads(enc, &mv, keys ? a.v : a.q, keys ? a.total_k : 1, keys ? a.Hkv : 1, D, keys ? a.ldv : D, 1, 128))
+    return cudaErrorNotSupported;
+  mks = mk, mvs = mv;
+  if (WIN && keys && (!encode_heads(enc, &mks, a.k, a.total_k, a.Hkv, D, a.ldk, 1, kSinkRows) ||
+                      !encode_heads(enc, &mvs, a.v, a.total_k, a.Hkv, D, a.ldv, 1, kSinkRows)))
     return cudaErrorNotSupported;
   p.cu_q = a.cu_q;
   p.cu_k = a.cu_k;
@@ -566,7 +591,7 @@ cudaError_t launch_t(const PromptArgs& a, cudaStream_t stream) {
   cudaError_t e = prepare_launch_tmem(prompt_tc_kernel<D, WIN>, kPromptThreads, C::BYTES, 512, &per_sm);
   if (e != cudaSuccess) return e;
   e = launch_pdl(prompt_tc_kernel<D, WIN>, dim3((unsigned)items), dim3(kPromptThreads),
-                 C::BYTES, stream, 1, mq, mk, mv, p);
+                 C::BYTES, stream, 1, mq, mk, mv, mks, mvs, p);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
