@@ -42,7 +42,9 @@ constexpr int kCombineThreads = 256;
 // g + 8, bytes [c D/8, (c+1) D/8); value rows 2c, 2c+1, 2c+8, 2c+9, bytes [g D/16,
 // (g+1) D/16).  Scores: tokens on M, rows on N; values: head_dim on M, tokens on K,
 // rows on N.
-template <int D, int NB>
+// HALF: four rows at most; the second parts of the weights are the product's columns 4 .. 7 and
+// cost no product of their own.
+template <int D, int NB, bool HALF>
 __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_kernel(const TreeParams p) {
   constexpr int KW = D / 32, VW = D / 64, NM = D / 16, ROWS = 8 * NB, UNIT = 16 * kRowsWarps;
   const TreeArgs& a = p.a;
@@ -250,6 +252,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
             off[nb][e] = to;
             l[nb][e] *= f[e];
             z[nb][e] *= f[e];
+            if constexpr (HALF) f[e] = __shfl_sync(0xffffffffu, f[e], lane & 29);   // second parts: their rows' factor
           }
 #pragma unroll
           for (int mu = 0; mu < NM; ++mu) {
@@ -276,8 +279,14 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
         for (int h = 0; h < 2; ++h) {
           const uint32_t hi = pack_half2_bits(w[h][0], w[h][1]);
           const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-          p0[nb][h] = own_transpose(hi);
-          p1[nb][h] = own_transpose(pack_half2_bits(w[h][0] - f.x, w[h][1] - f.y));
+          const uint32_t lo = pack_half2_bits(w[h][0] - f.x, w[h][1] - f.y);
+          if constexpr (HALF) {
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, lo, 2);
+            p0[nb][h] = own_transpose(c & 2 ? other : hi);
+          } else {
+            p0[nb][h] = own_transpose(hi);
+            p1[nb][h] = own_transpose(lo);
+          }
         }
       }
 #pragma unroll
@@ -294,8 +303,10 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
           for (int nb = 0; nb < NB; ++nb) {
             mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q], a0, p0[nb][0], p0[nb][1]);
             mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q + 1], a1, p0[nb][0], p0[nb][1]);
-            mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q], a0, p1[nb][0], p1[nb][1]);
-            mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q + 1], a1, p1[nb][0], p1[nb][1]);
+            if constexpr (!HALF) {
+              mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q], a0, p1[nb][0], p1[nb][1]);
+              mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q + 1], a1, p1[nb][0], p1[nb][1]);
+            }
           }
         }
     }
@@ -314,6 +325,13 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
           zs += __shfl_xor_sync(0xffffffffu, zs, w);
         }
         const int r = 8 * nb + 2 * c + e;
+        if constexpr (HALF) {
+#pragma unroll
+          for (int mu = 0; mu < NM; ++mu) {
+            o[nb][mu][e] += __shfl_xor_sync(0xffffffffu, o[nb][mu][e], 2);
+            o[nb][mu][2 + e] += __shfl_xor_sync(0xffffffffu, o[nb][mu][2 + e], 2);
+          }
+        }
 #pragma unroll
         for (int mu = 0; mu < NM; ++mu) {
           o_w[r * D + g * (D / 8) + 2 * mu] = o[nb][mu][e] + zs;
@@ -428,7 +446,9 @@ struct TreePlan {
 };
 TreePlan tree_plan(const TreeArgs& a) {
   const int64_t rows = a.max_q * (a.Hq / a.Hkv);
-  if (rows > 16) return {rows <= 32 ? 5 : (rows <= 64 ? 6 : 7), kTreeTcUnitLog2, device_sm_count(), 2};
+  // (D 64, 24 sequences of 25 rows: 1000 tokens 24.9 us on warps in two jobs, 28.3 on the tensor core, 8000 tokens
+  // 93 and 101; D 128, 8 x 2000 tokens and 32 rows 29.8 and 25.1, 32 x 8000 198 and 145; 16 rows 107 and 144)
+  if (rows > (a.D == 64 ? 32 : 16)) return {rows <= 32 ? 5 : (rows <= 64 ? 6 : 7), kTreeTcUnitLog2, device_sm_count(), 2};
   return {rows <= 8 ? 3 : 4, 6, device_sm_count() * (rows <= 8 ? 4 : 3), 2};
 }
 static_assert(16 * kRowsWarps == 1 << 6, "unit of the kernel for few rows");
@@ -458,7 +478,8 @@ cudaError_t launch_t(const TreeArgs& a, cudaStream_t stream) {
   if (t.rows_log2 >= 5) {
     e = launch_tree_tc(p, stream);
   } else {
-    auto kernel = t.rows_log2 == 3 ? tree_rows_kernel<D, 1> : tree_rows_kernel<D, 2>;
+    const int64_t rows = a.max_q * p.G;
+    auto kernel = rows <= 4 ? tree_rows_kernel<D, 1, true> : (rows <= 8 ? tree_rows_kernel<D, 1, false> : tree_rows_kernel<D, 2, false>);
     e = launch_pdl(kernel, dim3((unsigned)t.ctas), dim3(kRowsWarps * 32), 0, stream, 1, p);
   }
   if (e != cudaSuccess) return e;
