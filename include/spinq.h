@@ -544,7 +544,9 @@ spinq_status spinq_prefix_attention_kv4(const void* q, const spinq_kv4_pages* ca
  * Sequences are served in their order; where the pages run out, the first that is
  * not to be had in full and every later one that needs a page are refused, as is one
  * longer than its row of page_table or whose rows end past `total`: lens[b] <- start,
- * its slots are -1 (spinq_kv4_append passes over them), granted[b] = 0.
+ * its slots are -1 (spinq_kv4_append passes over them), granted[b] = 0.  What later calls
+ * of the step give for its rows means nothing, and none of its tokens is to be kept
+ * (a count of 0 for spinq_kv4_keep).
  *   lens       [batch] int32, in and out (clamped to the row's capacity);
  *   drop, add  [batch] int32, or NULL (none); below 0 counts as 0;
  *   page_table [batch][table_width] int32, in and out: entries past a sequence's
@@ -620,8 +622,9 @@ spinq_status spinq_window_prompt_attention(const void* q, int64_t ldq, const voi
  *           zeroing needed); 0 where the call refuses the sizes.
  *   Supported: Hq / kv_heads whole and at most 128, Hq and B at most 65535.
  *   Scores and sums in fp32, the weights p alpha in two fp16 parts (2^-22).  How the
- *   keys are split over the GPU depends on the lengths of the whole batch, so a sequence's
- *   output may change in its last bits when the batch does.
+ *   keys are split over the GPU depends on max_q and the lengths of the whole batch, so a
+ *   sequence's output may change in its last bits when those do; the same call gives the same
+ *   bits every time.
  */
 int64_t spinq_tree_attention_workspace_bytes(int64_t B, int64_t max_q, int64_t table_width, int32_t page_size,
                                              int64_t Hq, int64_t Hkv, int64_t D);

@@ -12,6 +12,7 @@ take raw pointers; the tensor-level helpers below them (``rotate_quant_act``
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Tuple
@@ -921,16 +922,21 @@ def kv4_plan(lens: torch.Tensor, add: Optional[torch.Tensor], page_table: torch.
     new tokens, ``total`` rows of them (``depths`` [total]: places of a tree's nodes)."""
     dev, queue = _queue(lens, stream)
     B, W = page_table.shape
-    optional = lambda x, shape: None if x is None else _full(x, _I32, shape, dev)   # noqa: E731
     if plan is None:
-        plan = KV4Plan(*(_empty(n, t, lens.device, stream) for n, t in ((B + 1, _I32), (total, _I32), (total, _I64T), (B, _I32))))
-    _check(_lib.spinq_kv4_plan(_full(lens, _I32, (B,), dev), optional(drop, (B,)), optional(add, (B,)), B,
-                               _full(page_table, _I32, (B, W), dev), W, page_size,
-                               _full(free_pages, _I32, (free_pages.numel(),), dev), _full(free_count, _I32, (1,), dev),
-                               free_pages.numel(), optional(depths, (total,)), position_offset, total,
-                               _full(plan.cu_tokens, _I32, (B + 1,), dev), _full(plan.positions, _I32, (total,), dev),
-                               _full(plan.slots, _I64T, (total,), dev), _full(plan.granted, _I32, (B,), dev), queue),
-           "spinq_kv4_plan")
+        plan = KV4Plan(_empty(B + 1, _I32, lens.device, stream), _empty(total, _I32, lens.device, stream),
+                       _empty(total, _I64T, lens.device, stream), _empty(B, _I32, lens.device, stream))
+        cu, positions, slots, granted = (plan.cu_tokens.data_ptr(), plan.positions.data_ptr(), plan.slots.data_ptr(),
+                                         plan.granted.data_ptr())
+    else:
+        cu, positions = _full(plan.cu_tokens, _I32, (B + 1,), dev), _full(plan.positions, _I32, (total,), dev)
+        slots, granted = _full(plan.slots, _I64T, (total,), dev), _full(plan.granted, _I32, (B,), dev)
+    N = free_pages.numel()
+    _check(_lib.spinq_kv4_plan(_full(lens, _I32, (B,), dev), None if drop is None else _full(drop, _I32, (B,), dev),
+                               None if add is None else _full(add, _I32, (B,), dev), B,
+                               _full(page_table, _I32, (B, W), dev), W, page_size, _full(free_pages, _I32, (N,), dev),
+                               _full(free_count, _I32, (1,), dev), N,
+                               None if depths is None else _full(depths, _I32, (total,), dev), position_offset, total, cu,
+                               positions, slots, granted, queue), "spinq_kv4_plan")
     return plan
 
 
@@ -972,16 +978,21 @@ def window_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c
     return out
 
 
+@functools.lru_cache(maxsize=1024)
+def _tree_bytes(dev: int, *shape) -> int:
+    return spinq_tree_attention_workspace_bytes(*shape)
+
+
 def _tree_space(workspace: Optional[torch.Tensor], B: int, max_q: int, width: int, pages: Kv4PagesCfg, Hq: int, dev: int,
                 device, stream: Optional[torch.cuda.Stream]):
     """The workspace of the two calls below (kept alive by the caller), its address and bytes."""
-    if workspace is None:
-        need = _lib.spinq_tree_attention_workspace_bytes(B, max_q, width, pages.page_size, Hq, pages.kv_heads, pages.head_dim)
-        if need == 0:
-            return None, None, 0
-        workspace = _empty(need, _U8, device, stream)
-        return workspace, workspace.data_ptr(), need
-    return (workspace,) + _space(workspace, dev)
+    if workspace is not None:
+        return (workspace,) + _space(workspace, dev)
+    need = _tree_bytes(dev, B, max_q, width, pages.page_size, Hq, pages.kv_heads, pages.head_dim)
+    if need == 0:
+        return None, None, 0
+    workspace = _empty(need, _U8, device, stream)
+    return workspace, workspace.data_ptr(), need
 
 
 def tree_attention_kv4(q: torch.Tensor, cache: KV4Pages, page_table: torch.Tensor, lens: torch.Tensor, cu_q: torch.Tensor,
