@@ -33,34 +33,105 @@ namespace spinq {
 namespace {
 
 constexpr int kRowsWarps = 4;
+// Parts of a job at most.  (4 rows of D 128 and one sequence of 16000 tokens: 29.6 us without a limit, 18.6 with 16,
+// 17.6 with 20, 19.1 with 24; four such sequences 28.1, 29.4, 28.3 and 28.4)
+constexpr int kRowsParts = 20;
 constexpr int kCombineThreads = 256;
 
+// Shared memory: each warp's ring (after a job's loop: float o [ROWS][D]), a stage the
+// value rows, key rows (D/2 bytes each) and scales of 16 T tokens.  Four CTAs with three
+// stages of 32 tokens fill an SM.
+template <int D, int T>
+struct RowsRing {
+  static constexpr int STAGES = T == 1 ? 4 : 3, KB = 16 * T * (D / 2), SB = 256 * T, KEYS = STAGES * KB, SCALES = 2 * KEYS,
+                       WARP = SCALES + STAGES * SB, BYTES = kRowsWarps * WARP;
+};
+
 // ------------------------------------------------ few rows: warps and mma.sync
-// A job is 8 NB rows, a unit 64 tokens.  A warp takes 16 tokens of each unit,
-// which lie in one page, so its rows of codes are one run of memory, copied three
-// steps ahead into the warp's ring.  Fragments of lane 4 g + c: key rows g and
-// g + 8, bytes [c D/8, (c+1) D/8); value rows 2c, 2c+1, 2c+8, 2c+9, bytes [g D/16,
-// (g+1) D/16).  Scores: tokens on M, rows on N; values: head_dim on M, tokens on K,
-// rows on N.
+// A job is 8 NB rows, a unit 64 T tokens.  A warp takes 16 T tokens of each unit, whose
+// rows of codes are one run of memory (two where pages have 16 tokens), copied ahead into the
+// warp's ring.  Fragments of lane 4 g + c: key rows g and g + 8, bytes [c D/8, (c+1) D/8);
+// of the values a transposing load of 8 rows x 16 bytes, which gives it dimensions 4 g ..
+// 4 g + 3 of the 32 for tokens 2c and 2c + 1.  Those rows' pieces are moved about, so that
+// eight of them lie in different banks.  Scores: tokens on M, rows on N; values: head_dim on M,
+// tokens on K, rows on N.
 // HALF: four rows at most; the second parts of the weights are the product's columns 4 .. 7 and
 // cost no product of their own.
-template <int D, int NB, bool HALF>
+// T = 2, two tiles of tokens a step: their chains of products and exponentials overlap, and
+// the step's own cost is shared (4 rows of D 128, 128 windows of 4096 tokens: 140 us with one, 122 with
+// two; 16 rows of D 64, 32 x 8000: 71 and 63).  16 rows of D 128 have no registers for it.
+// The ring's copies by one lane (bulk copies, the values' with a tensor map's swizzle) read as fast as
+// 104 us alone, but cost more instructions than these: 131 us.
+// Bound: HBM gives the bytes of the same case in 88 us and these copies alone take 117; of the rest each step's
+// instructions (about 300 for 16 tokens and a warp) take 60 % of the issue slots.
+template <int D, int NB, int T, bool HALF>
 __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_kernel(const TreeParams p) {
-  constexpr int KW = D / 32, VW = D / 64, NM = D / 16, ROWS = 8 * NB, UNIT = 16 * kRowsWarps;
+  constexpr int KW = D / 32, NM = D / 16, ROWS = 8 * NB, UNIT = 16 * T * kRowsWarps;
   const TreeArgs& a = p.a;
-  using Ring = OwnRing<D>;
-  __shared__ __align__(16) uint8_t ring_s[kRowsWarps][Ring::WARP];   // after a job's loop: float o [ROWS][D]
+  using Ring = RowsRing<D, T>;
+  extern __shared__ __align__(512) uint8_t ring_s[];
+  static_assert(Ring::WARP % 512 == 0 && Ring::KB % 512 == 0, "whole tiles of moved pieces");
   static_assert(ROWS * D * 4 <= Ring::WARP, "the output fits in the ring");
   __shared__ float m_s[kRowsWarps][ROWS], l_s[kRowsWarps][ROWS];
   __shared__ int parent_s[kTreeNodes];
   __shared__ TreeRow row_s[ROWS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  uint8_t* const ring = ring_s + warp * Ring::WARP;
+  // a value row's 16-byte piece (of the first 16 rows; the rest repeat them)
+  auto value_at = [](int row, int piece) { return row * (D / 2) + ((piece ^ (row / (256 / D) & (D / 32 - 1))) << 4); };
+  // what the lane copies, and the row it names in a transposing load: matrix m has rows 8 (m % 2) .. and piece m / 2
+  const uint32_t copy_k = smem_u32(ring) + Ring::KEYS + lane * 16, copy_s = smem_u32(ring) + Ring::SCALES + lane * 16;
+  const uint32_t copy_v = smem_u32(ring) + value_at(lane / (D / 32), lane % (D / 32));
+  const uint32_t load_v = smem_u32(ring) + value_at(lane & 15, lane >> 4);
+  const bool halves = a.page_size < 16 * T;   // a step's tokens lie in two pages
   pdl_wait();
   pdl_trigger();
-  TreeWalk walk(tree_run<kRowsWarps * 32>(p, blockIdx.x), blockIdx.x);
+  TreeWalk walk(tree_run<kRowsWarps * 32, kRowsParts>(p, blockIdx.x), blockIdx.x);
   for (TreeJob j; walk.next(p, j);) {
     const TreeSeq& s = j.s;
     const int rows = j.rows;
+    const int nstep = j.v1 - j.v0;
+    auto token_of = [&](int i) {   // first token of this warp's step i
+      return j.token(j.v0 + i, UNIT) + 16 * T * warp;
+    };
+    const int32_t* table = a.table + (int64_t)j.b * a.table_width;
+    // Lane k holds the pages of the warp's step 32 j + k: one look-up for 32 steps.
+    int page = 0, page16 = 0;   // (of the second 16 tokens, where that is another)
+    int ks = 0, kr = 0;   // stages of the next step to copy, of the next to use
+    auto issue = [&](int i) {   // copies of step i
+      const int t = token_of(i);
+      if (i >= nstep || t >= s.n) {   // an empty group keeps the count
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
+        return;
+      }
+      if ((i & 31) == 0) {
+        const int ti = token_of(min(i + lane, nstep - 1));
+        page = ti < s.n ? (int)tree_page(a, table, ti, p.shift) : 0;
+        if (halves) page16 = ti + 16 < s.n ? (int)tree_page(a, table, ti + 16, p.shift) : 0;
+      }
+      const int pg = __shfl_sync(0xffffffffu, page, i & 31);
+      const bool two = halves && t + 16 < s.n;
+      const int pg16 = two ? __shfl_sync(0xffffffffu, page16, i & 31) : 0;
+      const int64_t at = ((int64_t)pg * a.Hkv + j.hk) * a.page_size + (t & (a.page_size - 1));
+      const int64_t at16 = two ? ((int64_t)pg16 * a.Hkv + j.hk) * a.page_size : at + 16;
+#pragma unroll
+      for (int u = 0; u < T; ++u) {
+        if (u > 0 && t + 16 * u >= s.n) continue;
+        const int64_t x = (u ? at16 : at) * (D / 2) + lane * 16;
+#pragma unroll
+        for (int k = 0; k < D / 64; ++k) {
+          own_copy16(copy_k + ks * Ring::KB + u * (Ring::KB / T) + 512 * k, a.k_codes + x + 512 * k);
+          own_copy16(copy_v + ks * Ring::KB + u * (Ring::KB / T) + 512 * k, a.v_codes + x + 512 * k);
+        }
+      }
+      if (lane < 16 || (T == 2 && t + 16 < s.n))
+        own_copy16(copy_s + ks * Ring::SB, a.scales + ((lane < 16 ? at : at16 - 16) + lane) * 4);
+      asm volatile("cp.async.commit_group;\n" ::: "memory");
+      ks = ks + 1 == Ring::STAGES ? 0 : ks + 1;
+    };
+    // (before the set-up, which takes as long as a copy)
+#pragma unroll
+    for (int i = 0; i < Ring::STAGES - 1; ++i) issue(i);
     // what the rows see
     tree_parents(p, s, parent_s, kRowsWarps * 32);
     __syncthreads();
@@ -106,41 +177,6 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
     int low = 0;
     for (int r = 0; r < rows; ++r) low = max(low, row_s[r].low);
 
-    const int nstep = j.v1 - j.v0;
-    auto token_of = [&](int i) {   // first token of this warp's step i
-      return j.token(j.v0 + i, UNIT) + 16 * warp;
-    };
-    const int32_t* table = a.table + (int64_t)j.b * a.table_width;
-    // Lane k holds the place in the page arrays of the warp's step 32 j + k (of
-    // head hk, in tokens; -1: no token): one look-up for 32 steps.
-    int64_t place = -1;
-    const uint32_t ring = smem_u32(ring_s[warp]);
-    auto issue = [&](int i) {   // copies of step i (an empty group past the end keeps the count)
-      if (i < nstep) {
-        if ((i & 31) == 0) {
-          place = -1;
-          if (i + lane < nstep) {
-            const int t = token_of(i + lane);
-            if (t < s.n) place = (tree_page(a, table, t, p.shift) * a.Hkv + j.hk) * a.page_size + (t & (a.page_size - 1));
-          }
-        }
-        const int64_t at = __shfl_sync(0xffffffffu, place, i & 31);
-        const uint32_t st = ring + (uint32_t)(i % kOwnStages) * Ring::STAGE;
-        if (at >= 0) {
-          const uint8_t* kr = a.k_codes + at * (D / 2);
-          const uint8_t* vr = a.v_codes + at * (D / 2);
-#pragma unroll
-          for (int k = 0; k < D / 64; ++k) {
-            const int piece = lane + 32 * k;
-            own_copy16(st + piece * 16, kr + piece * 16);
-            own_copy16(st + Ring::KB + Ring::value_at(piece / Ring::CPR, piece % Ring::CPR), vr + piece * 16);
-          }
-          if (lane < 16) own_copy16(st + 2 * Ring::KB + lane * 16, a.scales + (at + lane) * 4);
-        }
-      }
-      asm volatile("cp.async.commit_group;\n" ::: "memory");
-    };
-
     float o[NB][NM][4], m[NB][2], off[NB][2], l[NB][2], z[NB][2];   // m: M
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -149,72 +185,65 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
 #pragma unroll
       for (int e = 0; e < 2; ++e) m[nb][e] = -INFINITY, off[nb][e] = l[nb][e] = z[nb][e] = 0.f;
     }
-#pragma unroll
-    for (int i = 0; i < kOwnStages - 1; ++i) issue(i);
     for (int i = 0; i < nstep; ++i) {
-      asm volatile("cp.async.wait_group %0;\n" ::"n"(kOwnStages - 2) : "memory");
-      __syncwarp();   // step i has landed for every lane, and step i - 1's stage has been read
-      issue(i + kOwnStages - 1);
       const int t0 = token_of(i);
-      if (t0 >= s.n) continue;   // (nothing was copied)
-      const uint8_t* st = ring_s[warp] + (i % kOwnStages) * Ring::STAGE;
-      uint32_t kx[2][KW], vx[4][VW];
-      float4 sc[2];
+      if (t0 >= s.n) break;   // (nothing was copied)
+      asm volatile("cp.async.wait_group %0;\n" ::"n"(Ring::STAGES - 2) : "memory");
+      __syncwarp();   // step i has landed for every lane, and step i - 1's stage has been read
+      issue(i + Ring::STAGES - 1);
+      const uint8_t* st = ring + Ring::KEYS + kr * Ring::KB + g * (D / 2) + c * (D / 8);
+      const uint8_t* sp = ring + Ring::SCALES + kr * Ring::SB + g * 16;
+      const uint32_t va = load_v + kr * Ring::KB;
+      float sa[T][NB][4] = {}, s16[T][NB][4] = {};
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint8_t* kr = st + (g + 8 * h) * (D / 2) + c * (D / 8);
-        if constexpr (KW == 4) {
-          const uint4 w = *reinterpret_cast<const uint4*>(kr);
-          kx[h][0] = w.x, kx[h][1] = w.y, kx[h][2] = w.z, kx[h][3] = w.w;
-        } else {
-          const uint2 w = *reinterpret_cast<const uint2*>(kr);
-          kx[h][0] = w.x, kx[h][1] = w.y;
+      for (int u = 0; u < T; ++u) {
+        uint32_t kx[2][KW];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint8_t* k = st + (16 * u + 8 * h) * (D / 2);
+          if constexpr (KW == 4) {
+            const uint4 w = *reinterpret_cast<const uint4*>(k);
+            kx[h][0] = w.x, kx[h][1] = w.y, kx[h][2] = w.z, kx[h][3] = w.w;
+          } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(k);
+            kx[h][0] = w.x, kx[h][1] = w.y;
+          }
         }
-        sc[h] = *reinterpret_cast<const float4*>(st + 2 * Ring::KB + (g + 8 * h) * 16);
-      }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int row = 8 * (q >> 1) + 2 * c + (q & 1);
-        const uint8_t* vr = st + Ring::KB + Ring::value_at(row, g * (D / 16) / 16) + g * (D / 16) % 16;
-        if constexpr (VW == 2) {
-          const uint2 w = *reinterpret_cast<const uint2*>(vr);
-          vx[q][0] = w.x, vx[q][1] = w.y;
-        } else {
-          vx[q][0] = *reinterpret_cast<const uint32_t*>(vr);
-        }
-      }
-      float sa[NB][4] = {}, s16[NB][4] = {};
+        for (int w = 0; w < KW; ++w) {
+          const uint32_t x0 = kx[0][w], x1 = kx[1][w], y0 = x0 >> 8, y1 = x1 >> 8;
+          const uint32_t a0[4] = {x0 & 0x000F000Fu, x1 & 0x000F000Fu, y0 & 0x000F000Fu, y1 & 0x000F000Fu};
+          const uint32_t a1[4] = {x0 & 0x00F000F0u, x1 & 0x00F000F0u, y0 & 0x00F000F0u, y1 & 0x00F000F0u};
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        const uint32_t x0 = kx[0][w], x1 = kx[1][w], y0 = x0 >> 8, y1 = x1 >> 8;
-        const uint32_t a0[4] = {x0 & 0x000F000Fu, x1 & 0x000F000Fu, y0 & 0x000F000Fu, y1 & 0x000F000Fu};
-        const uint32_t a1[4] = {x0 & 0x00F000F0u, x1 & 0x00F000F0u, y0 & 0x00F000F0u, y1 & 0x00F000F0u};
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          mma_16816_f16_f32_acc(sa[nb], a0, qb[nb][w][0], qb[nb][w][1]);
-          mma_16816_f16_f32_acc(s16[nb], a1, qb[nb][w][2], qb[nb][w][3]);
+          for (int nb = 0; nb < NB; ++nb) {
+            mma_16816_f16_f32_acc(sa[u][nb], a0, qb[nb][w][0], qb[nb][w][1]);
+            mma_16816_f16_f32_acc(s16[u][nb], a1, qb[nb][w][2], qb[nb][w][3]);
+          }
         }
       }
-      // t = s + log2 alpha' (base 2) of tokens g, g + 8 for rows 8 nb + 2c, + 1
-      float t[NB][2][2], rv[2], vz[2];
+      if (++kr == Ring::STAGES) kr = 0;
+      // t = s + log2 alpha' (base 2) of tokens g, g + 8, .. for rows 8 nb + 2c, + 1
+      float t[NB][2 * T][2], rv[2 * T], vz[2 * T];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float ka = ks24 * sc[h].x;
-        const float va = value_scale(sc[h].z), la = log2_of_scale(va);
-        rv[h] = one_over_scale(va);
-        vz[h] = fmaf(rv[h], sc[h].w, 8.f);
+      for (int h = 0; h < 2 * T; ++h) {
+        const float4 sc = *reinterpret_cast<const float4*>(sp + h * 128);
+        const float ka = ks24 * sc.x;
+        const float av = value_scale(sc.z), la = log2_of_scale(av);
+        rv[h] = one_over_scale(av);
+        vz[h] = fmaf(rv[h], sc.w, 8.f);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            t[nb][h][e] = fmaf(ka, fmaf(0.0625f, s16[nb][2 * h + e], sa[nb][2 * h + e]), fmaf(sc[h].y, qsk[nb][e], la));
+            t[nb][h][e] = fmaf(ka, fmaf(0.0625f, s16[h >> 1][nb][2 * (h & 1) + e], sa[h >> 1][nb][2 * (h & 1) + e]),
+                               fmaf(sc.y, qsk[nb][e], la));
       }
       // Not every row sees every token: -inf.  Factors that are not finite (a slot that was never
       // written, a page given back, a row of NaN) would give 0 times them: they are 0 here, and the
       // score of a row that does see the token is not a number.
-      if (t0 + 16 > s.ctx || (t0 < low && t0 + 16 > p.sinks)) {
+      if (t0 + 16 * T > s.ctx || (t0 < low && t0 + 16 * T > p.sinks)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 2 * T; ++h) {
           const bool bad = !(fabsf(rv[h]) <= FLT_MAX && fabsf(vz[h]) <= FLT_MAX);
           if (bad) rv[h] = vz[h] = 0.f;
 #pragma unroll
@@ -233,6 +262,8 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           mx[nb][e] = fmaxf(t[nb][0][e], t[nb][1][e]);
+#pragma unroll
+          for (int h = 2; h < 2 * T; ++h) mx[nb][e] = fmaxf(mx[nb][e], t[nb][h][e]);
           grow |= mx[nb][e] > m[nb][e] + kAttnSlack;
         }
       if (__any_sync(0xffffffffu, grow)) {
@@ -263,20 +294,20 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
       }
       // the weights as two fp16 parts, the second what the first leaves: with one part the
       // few weights that carry a row would all but double its error
-      uint32_t p0[NB][2], p1[NB][2];
+      uint32_t p0[NB][2 * T], p1[NB][2 * T];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        float w[2][2];
+        float w[2 * T][2];
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
+          for (int h = 0; h < 2 * T; ++h) {
             w[h][e] = attn_exp2(t[nb][h][e] - off[nb][e]);
             l[nb][e] = fmaf(w[h][e], rv[h], l[nb][e]);
             z[nb][e] = fmaf(w[h][e], vz[h], z[nb][e]);
           }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 2 * T; ++h) {
           const uint32_t hi = pack_half2_bits(w[h][0], w[h][1]);
           const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi));
           const uint32_t lo = pack_half2_bits(w[h][0] - f.x, w[h][1] - f.y);
@@ -290,22 +321,25 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
         }
       }
 #pragma unroll
-      for (int vw = 0; vw < VW; ++vw)
+      for (int u = 0; u < T; ++u)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          // two bytes of two tokens' rows: one dimension of both in a pair
-          const uint32_t xa = __byte_perm(vx[0][vw], vx[1][vw], q ? 0x7632 : 0x5410);
-          const uint32_t xb = __byte_perm(vx[2][vw], vx[3][vw], q ? 0x7632 : 0x5410);
-          // (as u - 8: the values' sums would lose bits on the numbers that fp16 has below its normal ones)
-          const uint4 ya = code_pairs1(xa), yb = code_pairs1(xb);
-          const uint32_t a0[4] = {ya.x, ya.y, yb.x, yb.y}, a1[4] = {ya.z, ya.w, yb.z, yb.w};
+        for (int v = 0; v < D / 64; ++v) {
+          uint32_t vx[4];   // two bytes of tokens 2c and 2c + 1, 2c + 8 and 2c + 9 in piece 2 v, then in piece 2 v + 1
+          ldmatrix_x4_trans(vx, (va + u * 16 * (D / 2)) ^ (32 * v));
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q], a0, p0[nb][0], p0[nb][1]);
-            mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q + 1], a1, p0[nb][0], p0[nb][1]);
-            if constexpr (!HALF) {
-              mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q], a0, p1[nb][0], p1[nb][1]);
-              mma_16816_f16_f32_acc(o[nb][4 * vw + 2 * q + 1], a1, p1[nb][0], p1[nb][1]);
+          for (int q = 0; q < 2; ++q) {
+            // one dimension of both tokens in a pair
+            // (as u - 8: the values' sums would lose bits on the numbers that fp16 has below its normal ones)
+            const uint4 ya = code_pairs1(vx[2 * q]), yb = code_pairs1(vx[2 * q + 1]);
+            const uint32_t a0[4] = {ya.x, ya.y, yb.x, yb.y}, a1[4] = {ya.z, ya.w, yb.z, yb.w};
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+              mma_16816_f16_f32_acc(o[nb][4 * v + 2 * q], a0, p0[nb][2 * u], p0[nb][2 * u + 1]);
+              mma_16816_f16_f32_acc(o[nb][4 * v + 2 * q + 1], a1, p0[nb][2 * u], p0[nb][2 * u + 1]);
+              if constexpr (!HALF) {
+                mma_16816_f16_f32_acc(o[nb][4 * v + 2 * q], a0, p1[nb][2 * u], p1[nb][2 * u + 1]);
+                mma_16816_f16_f32_acc(o[nb][4 * v + 2 * q + 1], a1, p1[nb][2 * u], p1[nb][2 * u + 1]);
+              }
             }
           }
         }
@@ -313,7 +347,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
     // join the lanes' shares, then the warps
     asm volatile("cp.async.wait_group 0;\n" ::: "memory");
     __syncwarp();   // the ring is free
-    float* o_w = reinterpret_cast<float*>(ring_s[warp]);
+    float* o_w = reinterpret_cast<float*>(ring);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -333,10 +367,9 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
           }
         }
 #pragma unroll
-        for (int mu = 0; mu < NM; ++mu) {
-          o_w[r * D + g * (D / 8) + 2 * mu] = o[nb][mu][e] + zs;
-          o_w[r * D + g * (D / 8) + 2 * mu + 1] = o[nb][mu][2 + e] + zs;
-        }
+        for (int q = 0; q < D / 32; ++q)
+          *reinterpret_cast<float4*>(o_w + r * D + 32 * q + 4 * g) =
+              make_float4(o[nb][2 * q][e] + zs, o[nb][2 * q][2 + e] + zs, o[nb][2 * q + 1][e] + zs, o[nb][2 * q + 1][2 + e] + zs);
         if (g == 0) {
           m_s[warp][r] = m[nb][e];
           l_s[warp][r] = ls;
@@ -357,7 +390,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
         const float lw = l_s[w][r];
         if (lw == 0.f) continue;
         const float f = attn_exp2(m_s[w][r] - M);
-        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring_s[w]) + r * D + d);
+        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(ring_s + w * Ring::WARP) + r * D + d);
         v.x = fmaf(f, y.x, v.x), v.y = fmaf(f, y.y, v.y), v.z = fmaf(f, y.z, v.z), v.w = fmaf(f, y.w, v.w);
         ls = fmaf(f, lw, ls);
       }
@@ -377,14 +410,14 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
 // Joins the parts of a job that several CTAs share, in their order.  Block (c, y): the job that
 // the runs' border c cuts first, rows 8 y .. 8 y + 7; D / 4 lanes share a row, each has four
 // of its values and looks every (D / 4)th part's numbers up for all of them.
-template <int D>
+template <int D, int PARTS>
 __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const TreeParams p) {
   constexpr int LPR = D / 4;
   static_assert(kCombineThreads >= 8 * LPR && LPR <= 32, "eight rows");
   const TreeArgs& a = p.a;
   const int c = blockIdx.x + 1;
   // (the attention kernel started behind what wrote the lengths, and this one behind its start)
-  const TreeRun run = tree_run<kCombineThreads>(p, c);
+  const TreeRun run = tree_run<kCombineThreads, PARTS>(p, c);
   const TreeSeq& s = run.s;
   const int64_t x = c < run.ctas ? run.bound(c) : run.base, in = x - run.base;
   const int64_t job = in <= INT32_MAX ? (uint32_t)in / (uint32_t)max(1, s.units) : in / s.units;
@@ -449,9 +482,10 @@ TreePlan tree_plan(const TreeArgs& a) {
   // (D 64, 24 sequences of 25 rows: 1000 tokens 24.9 us on warps in two jobs, 28.3 on the tensor core, 8000 tokens
   // 93 and 101; D 128, 8 x 2000 tokens and 32 rows 29.8 and 25.1, 32 x 8000 198 and 145; 16 rows 107 and 144)
   if (rows > (a.D == 64 ? 32 : 16)) return {rows <= 32 ? 5 : (rows <= 64 ? 6 : 7), kTreeTcUnitLog2, device_sm_count(), 2};
-  return {rows <= 8 ? 3 : 4, 6, device_sm_count() * (rows <= 8 ? 4 : 3), 2};
+  if (rows <= 8) return {3, 7, device_sm_count() * 4, 1};
+  if (a.D == 64) return {4, 7, device_sm_count() * 3, 1};
+  return {4, 6, device_sm_count() * 3, 2};
 }
-static_assert(16 * kRowsWarps == 1 << 6, "unit of the kernel for few rows");
 
 // M and sums, then the weighted sums of values.
 int64_t tree_sums_bytes(const TreePlan& t) { return align256(((int64_t)2 * t.ctas << t.rows_log2) * 8); }
@@ -479,11 +513,18 @@ cudaError_t launch_t(const TreeArgs& a, cudaStream_t stream) {
     e = launch_tree_tc(p, stream);
   } else {
     const int64_t rows = a.max_q * p.G;
-    auto kernel = rows <= 4 ? tree_rows_kernel<D, 1, true> : (rows <= 8 ? tree_rows_kernel<D, 1, false> : tree_rows_kernel<D, 2, false>);
-    e = launch_pdl(kernel, dim3((unsigned)t.ctas), dim3(kRowsWarps * 32), 0, stream, 1, p);
+    const int tiles = rows <= 8 || D == 64 ? 2 : 1;   // of 16 tokens a step
+    auto kernel = rows <= 4 ? tree_rows_kernel<D, 1, 2, true>
+                            : (rows <= 8 ? tree_rows_kernel<D, 1, 2, false> : tree_rows_kernel<D, 2, D == 64 ? 2 : 1, false>);
+    const int bytes = tiles == 2 ? RowsRing<D, 2>::BYTES : RowsRing<D, 1>::BYTES;
+    int per_sm = 0;
+    e = prepare_launch(kernel, kRowsWarps * 32, bytes, &per_sm);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(kernel, dim3((unsigned)t.ctas), dim3(kRowsWarps * 32), bytes, stream, 1, p);
   }
   if (e != cudaSuccess) return e;
-  e = launch_pdl(tree_combine_kernel<D>, dim3((unsigned)(t.ctas - 1), 1u << (t.rows_log2 - 3)), dim3(kCombineThreads), 0,
+  auto combine = t.rows_log2 >= 5 ? tree_combine_kernel<D, 0> : tree_combine_kernel<D, kRowsParts>;
+  e = launch_pdl(combine, dim3((unsigned)(t.ctas - 1), 1u << (t.rows_log2 - 3)), dim3(kCombineThreads), 0,
                  stream, 1, p);
   return e != cudaSuccess ? e : cudaGetLastError();
 }

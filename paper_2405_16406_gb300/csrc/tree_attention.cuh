@@ -74,19 +74,28 @@ struct TreeRun {
   }
 };
 
-template <int THREADS>
+// PARTS > 0: runs so long that a job is cut into about that many at most.  The parts of a job are
+// joined one after the other, which for few jobs takes longer than their keys.
+template <int THREADS, int PARTS>
 __device__ __forceinline__ TreeRun tree_run(const TreeParams& p, int c) {
   __shared__ int64_t sums[THREADS / 32], base_s;
+  __shared__ int jobs_s[PARTS > 0 ? THREADS / 32 : 1];
   __shared__ int b_s;
   __shared__ TreeSeq seq_s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = (int)p.a.B;
   const int per = B <= THREADS ? 1 : (B + THREADS - 1) / THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
   int64_t mine = 0;
+  int jobs = 0;   // (4096 stands for more: the limit is above any grid)
   TreeSeq s = {};
 #pragma unroll 1
   for (int b = b0; b < b1; ++b) {
     s = tree_seq(p, b);
     mine += (int64_t)s.units * s.jobs;
+    jobs = min(jobs + min(s.jobs, 4096), 4096);
+  }
+  if constexpr (PARTS > 0) {
+    jobs = __reduce_add_sync(0xffffffffu, jobs);
+    if (lane == 0) jobs_s[warp] = jobs;
   }
   int64_t sum = mine;
 #pragma unroll
@@ -98,19 +107,30 @@ __device__ __forceinline__ TreeRun tree_run(const TreeParams& p, int c) {
   if (tid == 0) b_s = B;
   __syncthreads();
   int64_t at = sum - mine, all = 0;
+  int ctas = p.ctas;
 #pragma unroll
   for (int w = 0; w < THREADS / 32; ++w) {
     if (w == warp) at += all;
     all += sums[w];
   }
+  if constexpr (PARTS > 0) {
+    jobs = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) jobs += jobs_s[w];
+    ctas = min(ctas, jobs * PARTS);
+  }
   TreeRun r;
   if (all <= INT32_MAX) {   // (32-bit divisions: a wave of CTAs waits for these)
     const uint32_t n = (uint32_t)all;
-    r.ctas = (int)min((uint32_t)p.ctas, (n + p.least - 1) / p.least);
+    r.ctas = (int)min((uint32_t)ctas, (n + p.least - 1) / p.least);
+    if (PARTS > 0 && n > (uint32_t)r.ctas && n < 4u * r.ctas) {   // (as few runs as the longest allows)
+      const uint32_t longest = (n + r.ctas - 1) / (uint32_t)r.ctas;
+      r.ctas = (int)((n + longest - 1) / longest);
+    }
     r.per = r.ctas ? n / (uint32_t)r.ctas : 0;
   } else {
-    r.ctas = p.ctas;
-    r.per = all / p.ctas;
+    r.ctas = ctas;
+    r.per = all / ctas;
   }
   r.rest = (int)(all - r.per * r.ctas);
   if (c < r.ctas) {

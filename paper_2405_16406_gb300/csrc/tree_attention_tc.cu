@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_tc_kernel(const TreePara
   constexpr uint32_t OCOL = NS * 128;
   pdl_wait();
   pdl_trigger();
-  TreeWalk walk(tree_run<kTreeThreads>(p, blockIdx.x), blockIdx.x);   // (of the thread that uses it)
+  TreeWalk walk(tree_run<kTreeThreads, 0>(p, blockIdx.x), blockIdx.x);   // (of the thread that uses it)
   const uint32_t sb = smem_u32(smem);
   // Job number `it` for a whole warp, or for the one thread that asks: its slot stays as it is until job_done.
   auto next_job = [&](int it, bool warp_wide) -> const TreeJob* {

@@ -108,3 +108,25 @@ def test_tokens_of_a_refused_sequence_are_not_written(S):
     assert plan.granted.tolist() == [1, 0] and lens.tolist() == [20, 0] and count.item() == 0
     assert table.tolist() == [[0, 2], [-1, -1]] and (plan.slots[20:] == -1).all()
     assert not cache.scales[1].any() and cache.scales[0].any() and cache.scales[2, :, :4].any() and not cache.scales[2, :, 4:].any()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens", [(2500,), (5130,), (20479,), (12000, 77)])
+def test_few_jobs_of_long_contexts(S, D, lens):
+    """One kv head: the runs end where a job has as many parts as are joined.  Each row against its own
+    attention over the keys that the pages hold."""
+    rng = np.random.default_rng(sum(lens) + D)
+    P = 64
+    table, pages = ku.page_tables(rng, list(lens), P)
+    cache = ku.random_cache(S, rng, pages, P, 1, D)
+    for G in (1, 3, 8, 16):
+        q = (rng.standard_normal((len(lens), G, D)) * 2).astype(np.float16)
+        got = S.window_attention_kv4(torch.from_numpy(q).cuda(), cache, torch.from_numpy(table.astype(np.int32)).cuda(),
+                                     i32(list(lens)), 0, 0).cpu().numpy().astype(np.float64)
+        for b, n in enumerate(lens):
+            (ku_, ka, kb), (vu, va, vb) = ku.slot_values(cache, ku.token_slots(table[b], P, 0, n))
+            k, v = ku_ * ka[..., None] + kb[..., None], vu * va[..., None] + vb[..., None]
+            o, size = ku.attention(q[b:b + 1].astype(np.float64), k, v, 1 / np.sqrt(D), np.ones((1, n), bool))
+            # (the output's rounding to fp16 is 2^-11 |o|; weights and sums are within 2^-13 of sum p |v|)
+            assert np.all(np.abs(got[b] - o[0]) <= 2.0 ** -13 * size[0] + 2.0 ** -11 * np.abs(o[0]) + 2.0 ** -24), (G, b)
+    assert S.spinq_device_status()[0] == S.SPINQ_OK
