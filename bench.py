@@ -1064,7 +1064,8 @@ def relaunch(args_n):
 
 PROFILE_CASES = ("attention", "rope_kv", "fp8_gemm", "w4a8_gemm", "rq8_paley", "cayley", "paley", "gemm",
                  "gemm_gate_up", "decode_gemm", "decode_gemm16", "rq_h8192", "kv2048", "act_quant",
-                 "kv4_append", "kv4_read", "prompt_attention", "prefix_attention")
+                 "kv4_append", "kv4_read", "prompt_attention", "prefix_attention",
+                 "window_prompt", "window_attention", "tree_attention", "kv4_plan", "kv4_keep")
 
 
 def profile_case(name, reps):
@@ -1086,7 +1087,11 @@ def profile_case(name, reps):
     rotation, asymmetric).  On the paged cache, 32 / 8 heads, D 128, pages of 64:
     kv4_append: 2 x 4096 new tokens with norms and RoPE; kv4_read: those tokens
     back; prompt_attention: one causal prompt of 4096; prefix_attention: 64
-    requests behind 8192 shared tokens, 256 own tokens each."""
+    requests behind 8192 shared tokens, 256 own tokens each; window_prompt: one
+    prompt of 8192 with a window of 4096 and 4 sinks; window_attention: one query
+    each of 64 sequences of 8192 tokens with that window; tree_attention: 64 nodes
+    each of 16 sequences of 8192; kv4_plan: the pages of 1000 prompts of 64 tokens;
+    kv4_keep: 11 tokens each of 256 sequences moved."""
     import numpy as np
     import torch
 
@@ -1184,6 +1189,38 @@ def profile_case(name, reps):
                     qd, lens = half(64, hq, d), ints([256] * 64)
                     shared, own = pages[:n // page], pages[n // page:].view(64, -1)
                     fn = lambda: spinq.prefix_attention_kv4(qd, cache, shared, n, own, lens)
+    elif name == "window_prompt":
+        half = lambda *shape: torch.randn(shape, device=dev).half()
+        q, k, v = half(8192, 32, 128), half(8192, 8, 128), half(8192, 8, 128)
+        cu = torch.tensor([0, 8192], dtype=torch.int32, device=dev)
+        fn = lambda: spinq.window_prompt_attention(q, k, v, cu, cu, 8192, 8192, 4096, 4)
+    elif name in ("window_attention", "tree_attention", "kv4_keep"):
+        B, nodes = {"window_attention": (64, 1), "tree_attention": (16, 64), "kv4_keep": (256, 12)}[name]
+        n = 1024 if name == "kv4_keep" else 8192
+        cache = spinq.kv4_pages(B * n // 64, 64, 8, 128)
+        for codes in (cache.k_codes, cache.v_codes):
+            codes.random_(0, 256)
+        cache.scales.uniform_(0.01, 0.02)
+        table = torch.randperm(B * n // 64, device=dev).int().view(B, -1)
+        lens = torch.full((B,), n, dtype=torch.int32, device=dev)
+        q = torch.randn(B * nodes, 32, 128, device=dev).half()
+        if name == "window_attention":
+            fn = lambda: spinq.window_attention_kv4(q, cache, table, lens, 4096, 4)
+        elif name == "tree_attention":
+            cu = torch.arange(0, B * nodes + 1, nodes, dtype=torch.int32, device=dev)
+            parents = ((torch.arange(nodes, device=dev) - 1) // 2).int().repeat(B)   # (the root's: -1)
+            fn = lambda: spinq.tree_attention_kv4(q, cache, table, lens, cu, nodes, parents)
+        else:
+            path = torch.arange(1, nodes, dtype=torch.int32, device=dev).repeat(B, 1)
+            counts = torch.full((B,), nodes - 1, dtype=torch.int32, device=dev)
+            fn = lambda: spinq.kv4_keep(cache, table, lens - nodes, path, counts)
+    elif name == "kv4_plan":
+        lens = torch.zeros(1000, dtype=torch.int32, device=dev)
+        add = torch.full((1000,), 64, dtype=torch.int32, device=dev)
+        table = torch.zeros(1000, 4, dtype=torch.int32, device=dev)
+        free = torch.arange(4000, dtype=torch.int32, device=dev)
+        count = torch.tensor([4000], dtype=torch.int32, device=dev)
+        fn = lambda: spinq.kv4_plan(lens.clone(), add, table, free, count.clone(), 64, 64000)
     elif name == "cayley":
         rng = np.random.default_rng(0)
         R = np.stack([np.linalg.qr(rng.standard_normal((128, 128)))[0] for _ in range(152)]).astype(np.float32)

@@ -33,8 +33,8 @@ namespace spinq {
 namespace {
 
 constexpr int kRowsWarps = 4;
-// Parts of a job at most.  (4 rows of D 128 and one sequence of 16000 tokens: 29.6 us without a limit, 18.6 with 16,
-// 17.6 with 20, 19.1 with 24; four such sequences 28.1, 29.4, 28.3 and 28.4)
+// Parts of a job at most.  (4 rows of D 128, one sequence of 4000 tokens: 9.9 us with 20, 11.2 with 60; of 8000 14.1
+// and 13.7; of 16000 15.3 and 15.8; two of 16000 19.2 and 21.3)
 constexpr int kRowsParts = 20;
 constexpr int kCombineThreads = 256;
 
@@ -408,12 +408,13 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
 }
 
 // Joins the parts of a job that several CTAs share, in their order.  Block (c, y): the job that
-// the runs' border c cuts first, rows 8 y .. 8 y + 7; D / 4 lanes share a row, each has four
-// of its values and looks every (D / 4)th part's numbers up for all of them.
+// the runs' border c cuts first, its y-th group of rows; D / 4 lanes share a row, each has four of its
+// values and looks every (D / 4)th part's numbers up for all of them.  Bound: latency; the first eight
+// parts' values are under way before their numbers are there.
 template <int D, int PARTS>
 __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const TreeParams p) {
-  constexpr int LPR = D / 4;
-  static_assert(kCombineThreads >= 8 * LPR && LPR <= 32, "eight rows");
+  constexpr int LPR = D / 4, RPB = kCombineThreads / LPR;
+  static_assert(LPR <= 32 && LPR % 8 == 0, "lanes of a row");
   const TreeArgs& a = p.a;
   const int c = blockIdx.x + 1;
   // (the attention kernel started behind what wrote the lengths, and this one behind its start)
@@ -425,44 +426,51 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
   pdl_wait();
   pdl_trigger();
   if (c >= run.ctas) return;
-  if (x == begin || run.bound(c - 1) > begin || threadIdx.x >= 8 * LPR) return;   // no job cut, or cut before
+  if (x == begin || run.bound(c - 1) > begin || (int)(threadIdx.x / LPR) >= 1 << p.rows_log2) return;   // no job cut, or cut before
   const int rows = 1 << p.rows_log2;
-  const int hk = (int)job / s.rts, r = blockIdx.y * 8 + threadIdx.x / LPR, k0 = threadIdx.x % LPR, d = 4 * k0;
+  const int hk = (int)job / s.rts, r = blockIdx.y * RPB + threadIdx.x / LPR, k0 = threadIdx.x % LPR, d = 4 * k0;
   const int row = (((int)job - hk * s.rts) << p.rows_log2) + r;
   const bool valid = row < s.nq * p.G;
   // parts: the one that CTA c - 1 left, then those that c, c + 1, .. continued
   auto slot = [&](int i) { return (int64_t)(i ? 2 * (c - 1 + i) : 2 * (c - 1) + 1) * rows + r; };
   const int parts = run.owner(end - 1) - (c - 1) + 1;
-  float M = -INFINITY;
-  for (int i = k0; i < parts; i += LPR) {
-    const float2 y = valid ? p.ml[slot(i)] : make_float2(0.f, 0.f);
-    if (y.y != 0.f) M = fmaxf(M, y.x);
+  float4 o[8];
+  auto load = [&](int i0) {   // eight parts' values under way at once (the last one's again past the end)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];\n"
+                   : "=f"(o[i].x), "=f"(o[i].y), "=f"(o[i].z), "=f"(o[i].w)
+                   : "l"(p.o + slot(min(i0 + i, parts - 1)) * D + d));
+  };
+  auto numbers = [&](int i) {   // M and sum of part i (the row of a part past the queries' end was not written)
+    float2 y = make_float2(0.f, 0.f);
+    if (valid && i < parts) asm volatile("ld.global.v2.f32 {%0, %1}, [%2];\n" : "=f"(y.x), "=f"(y.y) : "l"(p.ml + slot(i)));
+    return y;
+  };
+  float2 y = numbers(k0);
+  load(0);
+  float M = y.y != 0.f ? y.x : -INFINITY;
+  for (int i = k0 + LPR; i < parts; i += LPR) {
+    const float2 z = numbers(i);
+    if (z.y != 0.f) M = fmaxf(M, z.x);
   }
 #pragma unroll
   for (int w = 1; w < LPR; w <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, w));
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   float l = 0.f;
-  for (int i0 = 0; i0 < parts; i0 += LPR) {
-    const float2 y = valid && i0 + k0 < parts ? p.ml[slot(i0 + k0)] : make_float2(0.f, 0.f);
+  for (int i0 = 0; i0 < parts; i0 += 8) {
+    if (i0 % LPR == 0 && i0) y = numbers(i0 + k0);
     const float mine = y.y != 0.f ? attn_exp2(y.x - M) : 0.f;
-    const int n = min(LPR, parts - i0);
-    for (int i1 = 0; i1 < n; i1 += 8) {   // eight parts' values under way at once
-      float4 o[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];\n"
-                     : "=f"(o[i].x), "=f"(o[i].y), "=f"(o[i].z), "=f"(o[i].w)
-                     : "l"(p.o + slot(i0 + min(i1 + i, n - 1)) * D + d));
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int k = min(i1 + i, n - 1);
-        const float f = __shfl_sync(0xffffffffu, mine, k, LPR), t = __shfl_sync(0xffffffffu, y.y, k, LPR);
-        if (i1 + i < n && f != 0.f) {   // (a row past the queries' end was not written)
-          v.x = fmaf(f, o[i].x, v.x), v.y = fmaf(f, o[i].y, v.y), v.z = fmaf(f, o[i].z, v.z), v.w = fmaf(f, o[i].w, v.w);
-          l = fmaf(f, t, l);
-        }
+    for (int i = 0; i < 8; ++i) {
+      const int k = (i0 + i) % LPR;
+      const float f = __shfl_sync(0xffffffffu, mine, k, LPR), t = __shfl_sync(0xffffffffu, y.y, k, LPR);
+      if (f != 0.f) {   // (0 past the last part)
+        v.x = fmaf(f, o[i].x, v.x), v.y = fmaf(f, o[i].y, v.y), v.z = fmaf(f, o[i].z, v.z), v.w = fmaf(f, o[i].w, v.w);
+        l = fmaf(f, t, l);
       }
     }
+    if (i0 + 8 < parts) load(i0 + 8);
   }
   if (!valid) return;
   const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -523,8 +531,9 @@ cudaError_t launch_t(const TreeArgs& a, cudaStream_t stream) {
     e = launch_pdl(kernel, dim3((unsigned)t.ctas), dim3(kRowsWarps * 32), bytes, stream, 1, p);
   }
   if (e != cudaSuccess) return e;
+  constexpr int rpb = kCombineThreads / (D / 4);   // rows of a block
   auto combine = t.rows_log2 >= 5 ? tree_combine_kernel<D, 0> : tree_combine_kernel<D, kRowsParts>;
-  e = launch_pdl(combine, dim3((unsigned)(t.ctas - 1), 1u << (t.rows_log2 - 3)), dim3(kCombineThreads), 0,
+  e = launch_pdl(combine, dim3((unsigned)(t.ctas - 1), (unsigned)(((1 << t.rows_log2) + rpb - 1) / rpb)), dim3(kCombineThreads), 0,
                  stream, 1, p);
   return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -75,7 +75,7 @@ struct TreeRun {
 };
 
 // PARTS > 0: runs so long that a job is cut into about that many at most.  The parts of a job are
-// joined one after the other, which for few jobs takes longer than their keys.
+// joined eight at a time, which for few jobs takes as long as their keys.
 template <int THREADS, int PARTS>
 __device__ __forceinline__ TreeRun tree_run(const TreeParams& p, int c) {
   __shared__ int64_t sums[THREADS / 32], base_s;
