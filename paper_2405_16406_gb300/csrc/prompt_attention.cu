@@ -20,12 +20,13 @@
 // which see the most keys, first: the next item's copies and first products run
 // under this one's last weights, and O is read and stored after the next item's first
 // weights (before them: 16 ragged sequences of 9454 tokens 91.4 us against 87.7, 4 x
-// 4096 395 us against 386; with a block per item 4 x 4096 took 431).  Blocks
-// past a sequence's end are passed over; a grid that counts only the items there are took
-// 103 us on the ragged batch, whose long items it starts later.  4 x 4096, 32 / 8
-// heads, D 128: 386 us run again and again on one state, 420 us with cold inputs (1.31
-// PFLOP/s, 68 % of the measured rate of a large matrix product).  The softmax bounds
-// it: a step of 128 keys for both tiles is 2052 cycles of MMAs and about 3400 in all.
+// 4096 395 us against 386; with a block per item 4 x 4096 took 431), exchanged in quads so
+// that it leaves in runs of 64 bytes (with 16 bytes of a row per lane 87.5 us against 78.8, 384
+// against 365).  Blocks past a sequence's end are passed over; a grid that counts only the
+// items there are took 103 us for 91 on the ragged batch, whose long items it starts later.  4 x
+// 4096, 32 / 8 heads, D 128: 366 us run again and again on one state, 414 us with cold inputs (1.50 and
+// 1.33 PFLOP/s; the measured rate of a large matrix product is 1.91).  The softmax bounds
+// it: a step of 128 keys for both tiles is 2052 cycles of MMAs and about 3200 in all.
 // P in one fp16 part is a choice: the output's error against 64 bits is 0.00022 to 0.00029 where
 // its own rounding alone is 0.00021 (0.00031 in calls of a few rows).  Two parts, the second in
 // the rows that tiles of 64 leave idle, made those calls exact to the output's rounding
@@ -111,7 +112,8 @@ constexpr int kItemReaders = 11;
 // window of the item's first query reaches, so that a few sinks cost a part of a tile and
 // no tile starts before the window (2 x 32 queries with a window of 512 and 4 sinks: 5 tiles of
 // 128; with a tile of sinks and tiles at whole multiples of 128 tokens 6.5: 16 ragged sequences of
-// 32767 tokens 471 us so).
+// 32767 tokens 471 us so and 347 now, 0.92 PFLOP/s on visible pairs; 2 x 16384 with a window of 4096 1.31 ms, 1.48).
+// Bound: the softmax, as above, and the masks: the window's two edges cross 2 of those 5 tiles.
 template <int D, bool WIN>
 __global__ void __launch_bounds__(kPromptThreads, 1)
     prompt_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,

@@ -60,10 +60,11 @@ struct RowsRing {
 // T = 2, two tiles of tokens a step: their chains of products and exponentials overlap, and
 // the step's own cost is shared (4 rows of D 128, 128 windows of 4096 tokens: 140 us with one, 122 with
 // two; 16 rows of D 64, 32 x 8000: 71 and 63).  16 rows of D 128 have no registers for it.
-// The ring's copies by one lane (bulk copies, the values' with a tensor map's swizzle) read as fast as
-// 104 us alone, but cost more instructions than these: 131 us.
-// Bound: HBM gives the bytes of the same case in 88 us and these copies alone take 117; of the rest each step's
-// instructions (about 300 for 16 tokens and a warp) take 60 % of the issue slots.
+// Bound: instructions (310 for 16 tokens and a warp: 60 % of the issue slots at 4 warps a scheduler) beside
+// the bytes: that case's 582 MB in 120.5 us with the join are 4.83 TB/s, 73 % of the measured copy rate.
+// Bulk copies by one lane (the values' with a tensor map's swizzle) are faster alone (104 us for them, 118 to
+// 131 for these), but cost more instructions: 131 us in all.  5 CTAs an SM (spills) 149 against 145; two
+// chains of products for the scores 146 against 144; the scores multiplied a step ahead 170 against 151.
 template <int D, int NB, int T, bool HALF>
 __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_kernel(const TreeParams p) {
   constexpr int KW = D / 32, NM = D / 16, ROWS = 8 * NB, UNIT = 16 * T * kRowsWarps;
@@ -487,8 +488,8 @@ struct TreePlan {
 };
 TreePlan tree_plan(const TreeArgs& a) {
   const int64_t rows = a.max_q * (a.Hq / a.Hkv);
-  // (D 64, 24 sequences of 25 rows: 1000 tokens 24.9 us on warps in two jobs, 28.3 on the tensor core, 8000 tokens
-  // 93 and 101; D 128, 8 x 2000 tokens and 32 rows 29.8 and 25.1, 32 x 8000 198 and 145; 16 rows 107 and 144)
+  // (D 64, 24 sequences of 25 rows: 1000 tokens 24.0 us on warps in two jobs, 28.3 on the tensor core, 8000 tokens
+  // 93 and 101 (with one tile a step); D 128, 8 x 2000 tokens and 32 rows 29.8 and 25.1, 32 x 8000 198 and 145; 16 rows 107 and 144)
   if (rows > (a.D == 64 ? 32 : 16)) return {rows <= 32 ? 5 : (rows <= 64 ? 6 : 7), kTreeTcUnitLog2, device_sm_count(), 2};
   if (rows <= 8) return {3, 7, device_sm_count() * 4, 1};
   if (a.D == 64) return {4, 7, device_sm_count() * 3, 1};

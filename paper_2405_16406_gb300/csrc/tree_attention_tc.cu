@@ -18,6 +18,14 @@
 // jobs and writes them down for the others; 12-15 expand the codes into operand tiles, a
 // token per thread, keys two tiles ahead of values.
 //
+// 32 sequences of 9001 to 16384 tokens with 64 nodes each (32 / 8 heads, D 128, jobs of 128 rows): 545 us, 759
+// TFLOP/s, where the products alone would take 217 and the codes' bytes 74.  A tile is 1536 cycles of MMAs in about
+// 3000 (two fp16 parts of the weights: the values' product counts twice); the softmax and the expansion of
+// the codes take 59 % of the issue slots and wait for tensor memory and shared memory in between.
+// The same case with one part 505 us (error 0.00028 for 0.00021); rows split between the warpgroups 642; tokens split, one
+// maximum for both 663; a thread each for the two products 661; the numbers loaded a tile ahead 580; in the tree of these
+// steps each against 565.  32 rows (NE 1), 32 x 8000 tokens: 145 us.
+//
 // Every wait is bounded; one that gives up raises the CTA's abort flag, the MMAs and
 // copies in flight are drained and the status word is set.
 #include <cuda_fp16.h>
