@@ -39,11 +39,11 @@ constexpr int kRowsParts = 20;
 constexpr int kCombineThreads = 256;
 
 // Shared memory: each warp's ring (after a job's loop: float o [ROWS][D]), a stage the
-// value rows, key rows (D/2 bytes each) and scales of 16 T tokens.  Four CTAs with three
-// stages of 32 tokens fill an SM.
+// value rows, key rows (D/2 bytes each) and scales of 16 T tokens.  Three CTAs with two
+// stages of 64 tokens (D 128) fill an SM.
 template <int D, int T>
 struct RowsRing {
-  static constexpr int STAGES = T == 1 ? 4 : 3, KB = 16 * T * (D / 2), SB = 256 * T, KEYS = STAGES * KB, SCALES = 2 * KEYS,
+  static constexpr int STAGES = T == 1 ? 4 : (T == 2 || D == 64 ? 3 : 2), KB = 16 * T * (D / 2), SB = 256 * T, KEYS = STAGES * KB, SCALES = 2 * KEYS,
                        WARP = SCALES + STAGES * SB, BYTES = kRowsWarps * WARP;
 };
 
@@ -57,16 +57,16 @@ struct RowsRing {
 // tokens on K, rows on N.
 // HALF: four rows at most; the second parts of the weights are the product's columns 4 .. 7 and
 // cost no product of their own.
-// T = 2, two tiles of tokens a step: their chains of products and exponentials overlap, and
-// the step's own cost is shared (4 rows of D 128, 128 windows of 4096 tokens: 140 us with one, 122 with
-// two; 16 rows of D 64, 32 x 8000: 71 and 63).  16 rows of D 128 have no registers for it.
-// Bound: instructions (310 for 16 tokens and a warp: 60 % of the issue slots at 4 warps a scheduler) beside
-// the bytes: that case's 582 MB in 120.5 us with the join are 4.83 TB/s, 73 % of the measured copy rate.
+// T tiles of tokens a step: their chains of products and exponentials overlap, and the step's own
+// cost is shared (4 rows of D 128, 128 windows of 4096 tokens: 140 us with one, 120.5 with two, 113.4
+// with four; 16 rows of D 64, 32 x 8000: 71 and 63 with one and two).  16 rows of D 128 have no registers for two.
+// Bound: instructions (262 for 16 tokens and a warp, 56 % of the issue slots at 3 warps a scheduler) beside the
+// bytes: that case's 582 MB in 113.4 us with the join are 5.13 TB/s, 77 % of the measured copy rate.
 // Bulk copies by one lane (the values' with a tensor map's swizzle) are faster alone (104 us for them, 118 to
-// 131 for these), but cost more instructions: 131 us in all.  5 CTAs an SM (spills) 149 against 145; two
-// chains of products for the scores 146 against 144; the scores multiplied a step ahead 170 against 151.
+// 131 for these), but cost more instructions: 131 us in all where these took 124.  5 CTAs an SM (spills) 149
+// against 145; two chains of products for the scores 146 against 144; the scores multiplied a step ahead 170 against 151.
 template <int D, int NB, int T, bool HALF>
-__global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_kernel(const TreeParams p) {
+__global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 && T < 4 ? 4 : 3) tree_rows_kernel(const TreeParams p) {
   constexpr int KW = D / 32, NM = D / 16, ROWS = 8 * NB, UNIT = 16 * T * kRowsWarps;
   const TreeArgs& a = p.a;
   using Ring = RowsRing<D, T>;
@@ -84,7 +84,10 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
   const uint32_t copy_k = smem_u32(ring) + Ring::KEYS + lane * 16, copy_s = smem_u32(ring) + Ring::SCALES + lane * 16;
   const uint32_t copy_v = smem_u32(ring) + value_at(lane / (D / 32), lane % (D / 32));
   const uint32_t load_v = smem_u32(ring) + value_at(lane & 15, lane >> 4);
-  const bool halves = a.page_size < 16 * T;   // a step's tokens lie in two pages
+  // a step's tokens lie in 2^pieces pages
+  constexpr int STEP_LOG2 = T == 4 ? 6 : T + 3;
+  static_assert(16 * T == 1 << STEP_LOG2, "tokens of a step");
+  const int run_log2 = min(p.shift, STEP_LOG2), pieces = STEP_LOG2 - run_log2;
   pdl_wait();
   pdl_trigger();
   TreeWalk walk(tree_run<kRowsWarps * 32, kRowsParts>(p, blockIdx.x), blockIdx.x);
@@ -96,8 +99,12 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
       return j.token(j.v0 + i, UNIT) + 16 * T * warp;
     };
     const int32_t* table = a.table + (int64_t)j.b * a.table_width;
-    // Lane k holds the pages of the warp's step 32 j + k: one look-up for 32 steps.
-    int page = 0, page16 = 0;   // (of the second 16 tokens, where that is another)
+    // tokens before `none` that are not sinks are in no row's window: steps of them are passed over
+    const int none = p.window > 0 && s.ctx >= p.window ? s.ctx - p.window + 1 : 0;
+    auto unseen = [&](int t) { return T == 4 && t + 16 * T <= none && t >= p.sinks; };
+    // Lane k holds a page of the warp's step 32 j + k (of two or four pages a step: 16 j + k / 2,
+    // 8 j + k / 4): one look-up for many steps.
+    int page = 0;
     int ks = 0, kr = 0;   // stages of the next step to copy, of the next to use
     auto issue = [&](int i) {   // copies of step i
       const int t = token_of(i);
@@ -105,28 +112,51 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
         asm volatile("cp.async.commit_group;\n" ::: "memory");
         return;
       }
-      if ((i & 31) == 0) {
-        const int ti = token_of(min(i + lane, nstep - 1));
+      const int at_lane = (i << pieces) & 31;
+      if (at_lane == 0) {
+        const int ti = token_of(min(i + (lane >> pieces), nstep - 1)) + ((lane & ((1 << pieces) - 1)) << run_log2);
         page = ti < s.n ? (int)tree_page(a, table, ti, p.shift) : 0;
-        if (halves) page16 = ti + 16 < s.n ? (int)tree_page(a, table, ti + 16, p.shift) : 0;
       }
-      const int pg = __shfl_sync(0xffffffffu, page, i & 31);
-      const bool two = halves && t + 16 < s.n;
-      const int pg16 = two ? __shfl_sync(0xffffffffu, page16, i & 31) : 0;
-      const int64_t at = ((int64_t)pg * a.Hkv + j.hk) * a.page_size + (t & (a.page_size - 1));
-      const int64_t at16 = two ? ((int64_t)pg16 * a.Hkv + j.hk) * a.page_size : at + 16;
+      if (!unseen(t)) {
+        auto place = [&](int u) {   // of tile u, which begins a page or the step
+          const int pg = __shfl_sync(0xffffffffu, page, at_lane + (16 * u >> run_log2));
+          return ((int64_t)pg * a.Hkv + j.hk) * a.page_size + ((t + 16 * u) & (a.page_size - 1));
+        };
+        auto codes = [&](int u, int64_t at) {
+          const int64_t x = at * (D / 2) + lane * 16;
 #pragma unroll
-      for (int u = 0; u < T; ++u) {
-        if (u > 0 && t + 16 * u >= s.n) continue;
-        const int64_t x = (u ? at16 : at) * (D / 2) + lane * 16;
+          for (int k = 0; k < D / 64; ++k) {
+            own_copy16(copy_k + ks * Ring::KB + u * (Ring::KB / T) + 512 * k, a.k_codes + x + 512 * k);
+            own_copy16(copy_v + ks * Ring::KB + u * (Ring::KB / T) + 512 * k, a.v_codes + x + 512 * k);
+          }
+        };
+        auto scales = [&](int u, int64_t at, int64_t next) {   // of tile u in the first half of the lanes, and the next in the others
+          if (lane < 16 || (u + 1 < T && t + 16 * (u + 1) < s.n))
+            own_copy16(copy_s + ks * Ring::SB + u * 256, a.scales + ((lane < 16 ? at : next - 16) + lane) * 4);
+        };
+        int64_t at = place(0);
+        if (pieces == 0) {
 #pragma unroll
-        for (int k = 0; k < D / 64; ++k) {
-          own_copy16(copy_k + ks * Ring::KB + u * (Ring::KB / T) + 512 * k, a.k_codes + x + 512 * k);
-          own_copy16(copy_v + ks * Ring::KB + u * (Ring::KB / T) + 512 * k, a.v_codes + x + 512 * k);
+          for (int u = 0; u < T; ++u) {
+            if (u > 0 && t + 16 * u >= s.n) break;
+            codes(u, at + 16 * u);
+            if (u % 2 == 0) scales(u, at + 16 * u, at + 16 * (u + 1));
+          }
+        } else {
+#pragma unroll
+          for (int u = 0; u < T; u += 2) {
+            if (u > 0 && t + 16 * u >= s.n) break;
+            if (u > 0) at = place(u);   // (a step has two pages at least: one begins here)
+            codes(u, at);
+            int64_t next = at + 16;
+            if (u + 1 < T && t + 16 * (u + 1) < s.n) {
+              if (run_log2 == 4) next = place(u + 1);
+              codes(u + 1, next);
+            }
+            scales(u, at, next);
+          }
         }
       }
-      if (lane < 16 || (T == 2 && t + 16 < s.n))
-        own_copy16(copy_s + ks * Ring::SB, a.scales + ((lane < 16 ? at : at16 - 16) + lane) * 4);
       asm volatile("cp.async.commit_group;\n" ::: "memory");
       ks = ks + 1 == Ring::STAGES ? 0 : ks + 1;
     };
@@ -192,6 +222,10 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
       asm volatile("cp.async.wait_group %0;\n" ::"n"(Ring::STAGES - 2) : "memory");
       __syncwarp();   // step i has landed for every lane, and step i - 1's stage has been read
       issue(i + Ring::STAGES - 1);
+      if (unseen(t0)) {
+        if (++kr == Ring::STAGES) kr = 0;
+        continue;
+      }
       const uint8_t* st = ring + Ring::KEYS + kr * Ring::KB + g * (D / 2) + c * (D / 8);
       const uint8_t* sp = ring + Ring::SCALES + kr * Ring::SB + g * 16;
       const uint32_t va = load_v + kr * Ring::KB;
@@ -251,7 +285,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 3) tree_rows_ke
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const uint32_t bits = tree_sees(p, s, row_s[8 * nb + 2 * c + e], t0) >> (g + 8 * h);
+              const uint32_t bits = tree_sees(p, s, row_s[8 * nb + 2 * c + e], t0 + 32 * (h >> 2)) >> (g + 8 * (h & 3));
               t[nb][h][e] = bits & 1u ? (bad ? __int_as_float(0x7fc00000) : t[nb][h][e]) : -INFINITY;
             }
         }
@@ -484,14 +518,20 @@ int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
 // The variant for these sizes and its grid.
 struct TreePlan {
-  int rows_log2, unit_log2, ctas, least;
+  int rows_log2, unit_log2, ctas, least;   // ctas of the largest grid
 };
 TreePlan tree_plan(const TreeArgs& a) {
   const int64_t rows = a.max_q * (a.Hq / a.Hkv);
   // (D 64, 24 sequences of 25 rows: 1000 tokens 24.0 us on warps in two jobs, 28.3 on the tensor core, 8000 tokens
   // 93 and 101 (with one tile a step); D 128, 8 x 2000 tokens and 32 rows 29.8 and 25.1, 32 x 8000 198 and 145; 16 rows 107 and 144)
   if (rows > (a.D == 64 ? 32 : 16)) return {rows <= 32 ? 5 : (rows <= 64 ? 6 : 7), kTreeTcUnitLog2, device_sm_count(), 2};
-  if (rows <= 8) return {3, 7, device_sm_count() * 4, 1};
+  // A warp's step is four tiles of 16 tokens where there are jobs for the whole grid, of few jobs two
+  // (D 128, 4 rows: 32 x 8000 tokens 57.0 us with four, 61.8 with two; one sequence of 16000 16.9 and 15.1, of 500
+  // 8.4 and 7.6)
+  if (rows <= 8) {
+    if (a.B * a.Hkv * kRowsParts >= device_sm_count() * 3) return {3, 8, device_sm_count() * 3, 1};
+    return {3, 7, device_sm_count() * 4, 1};
+  }
   if (a.D == 64) return {4, 7, device_sm_count() * 3, 1};
   return {4, 6, device_sm_count() * 3, 2};
 }
@@ -521,11 +561,16 @@ cudaError_t launch_t(const TreeArgs& a, cudaStream_t stream) {
   if (t.rows_log2 >= 5) {
     e = launch_tree_tc(p, stream);
   } else {
-    const int64_t rows = a.max_q * p.G;
-    const int tiles = rows <= 8 || D == 64 ? 2 : 1;   // of 16 tokens a step
-    auto kernel = rows <= 4 ? tree_rows_kernel<D, 1, 2, true>
-                            : (rows <= 8 ? tree_rows_kernel<D, 1, 2, false> : tree_rows_kernel<D, 2, D == 64 ? 2 : 1, false>);
-    const int bytes = tiles == 2 ? RowsRing<D, 2>::BYTES : RowsRing<D, 1>::BYTES;
+    const bool half = a.max_q * p.G <= 4;
+    void (*kernel)(TreeParams) = tree_rows_kernel<D, 2, D == 64 ? 2 : 1, false>;
+    int bytes = RowsRing<D, D == 64 ? 2 : 1>::BYTES;
+    if (t.rows_log2 == 3 && t.unit_log2 == 8) {
+      kernel = half ? tree_rows_kernel<D, 1, 4, true> : tree_rows_kernel<D, 1, 4, false>;
+      bytes = RowsRing<D, 4>::BYTES;
+    } else if (t.rows_log2 == 3) {
+      kernel = half ? tree_rows_kernel<D, 1, 2, true> : tree_rows_kernel<D, 1, 2, false>;
+      bytes = RowsRing<D, 2>::BYTES;
+    }
     int per_sm = 0;
     e = prepare_launch(kernel, kRowsWarps * 32, bytes, &per_sm);
     if (e != cudaSuccess) return e;

@@ -130,3 +130,36 @@ def test_few_jobs_of_long_contexts(S, D, lens):
             # (the output's rounding to fp16 is 2^-11 |o|; weights and sums are within 2^-13 of sum p |v|)
             assert np.all(np.abs(got[b] - o[0]) <= 2.0 ** -13 * size[0] + 2.0 ** -11 * np.abs(o[0]) + 2.0 ** -24), (G, b)
     assert S.spinq_device_status()[0] == S.SPINQ_OK
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("P", [16, 32, 64, 256])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (70, 3), (300, 130), (1000, 4), (5000, 700)])
+def test_many_jobs_of_few_rows(S, D, P, window, sinks):
+    """Batches whose warps take 64 tokens a step: lengths around its, the units' and the pages' ends, windows that
+    leave steps and sinks in the middle of one; pages that no row sees hold numbers that are not."""
+    import test_gpu_tree_attention as trees
+    rng = np.random.default_rng(P + window + D)
+    ctx = [0, 1, 14, 15, 16, 30, 31, 47, 62, 63, 64, 127, 128, 191, 254, 255, 256, 257, 511, 700, 1023, 1500, 2047, 3001]
+    for nodes, Hq, Hkv in (([1] * 24, 4, 1), ([int(n) for n in rng.integers(0, 5, 24)], 2, 1),
+                           ([int(n) for n in rng.integers(1, 3, 24)], 6, 2)):
+        trees.run_tree(S, ctx, [trees.forest(rng, n) for n in nodes], Hq, Hkv, D, P, window, sinks, seed=P + sum(nodes))
+
+
+def test_few_jobs_and_many(S):
+    """A sequence alone and among copies of itself: other steps and parts, each within the bound of the
+    attention in 64 bits."""
+    import test_gpu_tree_attention as trees
+    rng = np.random.default_rng(5)
+    cache = ku.random_cache(S, rng, 80, 64, 1, 128)
+    row = rng.permutation(80).astype(np.int32)
+    q = rng.standard_normal((1, 4, 128)).astype(np.float16)
+    for window, sinks in ((0, 0), (900, 70)):
+        o, size = trees.reference(cache, row, q, 5001, trees.visible([-1], 5001, window, sinks), 64, 128 ** -0.5)
+        bound = 2.0 ** -13 * size + 2.0 ** -11 * np.abs(o) + 2.0 ** -24
+        for n in (1, 40):
+            got = S.window_attention_kv4(torch.from_numpy(np.repeat(q, n, 0)).cuda(), cache,
+                                         torch.from_numpy(np.repeat(row[None], n, 0)).cuda(), i32([5001] * n), window, sinks)
+            got = got.cpu().numpy().astype(np.float64)
+            assert np.all(np.abs(got - o) <= bound)
+    assert S.spinq_device_status()[0] == S.SPINQ_OK
