@@ -174,16 +174,21 @@ __device__ __forceinline__ TreeRow tree_row(const TreeParams& p, const TreeSeq& 
     return x >= 0 && x < i ? x : -1;
   };
   TreeRow r;
-  int depth = 0;
-  for (int i = up(node); i >= 0; i = up(i)) ++depth;
+  int depth = -1;
   r.line[0] = r.line[1] = r.line[2] = r.line[3] = 0;
-  const int window = p.window > 0 ? p.window : INT32_MAX;
-  for (int i = node, k = 0; i >= 0; i = up(i), ++k)
-    if (k < window || s.ctx + depth - k < p.sinks) {
+  auto see = [&](int i) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
-        if (w == i >> 5) r.line[w] |= 1u << (i & 31);
-    }
+    for (int w = 0; w < 4; ++w)
+      if (w == i >> 5) r.line[w] |= 1u << (i & 31);
+  };
+  const int window = p.window > 0 ? p.window : INT32_MAX;
+  if (window >= s.nq) {   // (no line is longer)
+    for (int i = node; i >= 0; i = up(i)) ++depth, see(i);
+  } else {
+    for (int i = node; i >= 0; i = up(i)) ++depth;
+    for (int i = node, k = 0; i >= 0; i = up(i), ++k)
+      if (k < window || s.ctx + depth - k < p.sinks) see(i);
+  }
   r.low = p.window > 0 && s.ctx + depth >= p.window ? s.ctx + depth - p.window + 1 : 0;
   return r;
 }
