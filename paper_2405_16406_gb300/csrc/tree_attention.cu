@@ -500,7 +500,9 @@ __global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const Tre
     for (int i = 0; i < 8; ++i) {
       const int k = (i0 + i) % LPR;
       const float f = __shfl_sync(0xffffffffu, mine, k, LPR), t = __shfl_sync(0xffffffffu, y.y, k, LPR);
-      if (f != 0.f) {   // (0 past the last part)
+      // (A part without a key that the row sees, or past the last one, has the sum 0.  One whose sum is not a number has
+      // no maximum or any: its factor may be 0, and the product with it keeps the sum what it is.)
+      if (t != 0.f) {
         v.x = fmaf(f, o[i].x, v.x), v.y = fmaf(f, o[i].y, v.y), v.z = fmaf(f, o[i].z, v.z), v.w = fmaf(f, o[i].w, v.w);
         l = fmaf(f, t, l);
       }
