@@ -550,7 +550,11 @@ spinq_status spinq_prefix_attention_kv4(const void* q, const spinq_kv4_pages* ca
  *   lens       [batch] int32, in and out (clamped to the row's capacity);
  *   drop, add  [batch] int32, or NULL (none); below 0 counts as 0;
  *   page_table [batch][table_width] int32, in and out: entries past a sequence's
- *              pages are left as they are;
+ *              pages are left as they are.  Of its first ceil(lens[b] / page_size)
+ *              entries one below 0 is no page: the program has given it back (put it on
+ *              the list itself) after a window passed it, and nothing comes of it when its
+ *              tokens are dropped.  Every other one is a page that neither the list nor
+ *              another entry holds: what was given back must not stay in the table;
  *   free_pages [free_capacity] int32, free_count [1] int32, in and out; pages that
  *              the list has no room for are lost (no list as long as the cache is full);
  *   depths     [total] int32 or NULL: position start + depths[t] + position_offset
@@ -611,7 +615,8 @@ spinq_status spinq_window_prompt_attention(const void* q, int64_t ldq, const voi
  *           rows of out behind the last sequence are not written;
  *   page_table [B][table_width] int32, lens [B] int32 (device), each in
  *           [0, table_width * page_size] (others are clamped); entries of pages that
- *           no query sees may be anything (pages given back);
+ *           no query sees may be anything here (pages given back; for spinq_kv4_plan they
+ *           are below 0);
  *   cu_q    [B + 1] int32 (device) ascending from 0;
  *   max_q   no less than any sequence's number of queries, at most 128;
  *   parents [total_q] int32: the number, within the sequence, of the query's parent,

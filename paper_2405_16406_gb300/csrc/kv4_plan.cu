@@ -5,15 +5,18 @@
 //
 // Plan.  With P tokens a page and, for sequence b,
 //   start = max(lens - drop, 0),  kept = ceil(start / P),
-//   freed = ceil(lens / P) - kept,  need = ceil((start + add) / P) - kept,
+//   freed = the entries kept .. ceil(lens / P) - 1 that are pages (not below 0: given back
+//   before, as a window passed them),  need = ceil((start + add) / P) - kept,
 // the free pages are a stack: freed page i of all (sequences in order, pages in
 // order) lies i below its top, and page a of all that are needed is the a-th from
 // the top, so a sequence that gives and takes gets its own pages back.  Three
 // prefix sums over the batch (tokens, freed, needed pages) say where everything is:
 // every CTA takes them by itself, in shared memory.
 //  * Up to kPlanTokens rows: one kernel, of one CTA or a cluster, whose threads share the pages
-//    and tokens.  The stack is written before a barrier and read behind it.
-//  * More: the tokens by a kernel that fills the GPU and reads the lists as they were, then
+//    and tokens.  The stack is written before a barrier and read behind it.  A few dropped entries of a
+//    sequence are looked through by the thread that loads its lengths, many by a warp of the grid.
+//  * More: the dropped entries are counted, a warp per sequence, by a kernel of its own; then the
+//    tokens by a kernel that fills the GPU and reads the lists as they were, then
 //    the lists and lengths by the one cluster (1000 sequences, 251 K tokens: 60 us in one
 //    kernel, whose 4096 threads had 64 dependent look-ups each).
 // Bound: latency (a chain of the lengths' loads, three block-wide sums, a barrier, and
@@ -34,6 +37,8 @@ namespace {
 constexpr int kPlanCluster = 8;
 constexpr int64_t kPlanTokens = 8192;
 enum PlanPart { kPlanAll = 0, kPlanRows = 1, kPlanLists = 2 };
+constexpr uint32_t kPlanOwn = 4;                 // dropped entries of a sequence that a thread looks through by itself
+constexpr uint32_t kPlanLong = 0x80000000u;      // more of them (a sequence has fewer than 2^27 pages)
 
 // Sums of whole numbers in [0, 2^31) that stay there.
 constexpr uint32_t kPlanMost = 0x7fffffffu;
@@ -74,11 +79,34 @@ __device__ __forceinline__ int last_at_most(const uint32_t* start, int n, uint32
   return lo;
 }
 
+// How many of a sequence's entries e[0 .. n - 1] are pages (a warp).
+__device__ __forceinline__ uint32_t count_pages(const int32_t* e, uint32_t n) {
+  uint32_t have = 0;
+#pragma unroll 16
+  for (uint32_t i = threadIdx.x & 31; i < n; i += 32) have += __ldcg(e + i) >= 0;
+  return __reduce_add_sync(0xffffffffu, have);
+}
+
+// Into cu_tokens, which the lists' kernel writes at its end: the pages that each sequence gives back, a warp each.
+constexpr int kPlanCountThreads = 256;
+__global__ void __launch_bounds__(kPlanCountThreads) kv4_plan_count_kernel(const PlanArgs a) {
+  const int b = blockIdx.x * (kPlanCountThreads / 32) + (threadIdx.x >> 5);
+  const uint32_t page1 = (1u << a.page_shift) - 1, cap = (uint32_t)(a.table_width << a.page_shift);
+  pdl_wait();
+  pdl_trigger();
+  if (b >= (int)a.batch) return;
+  const uint32_t len = min((uint32_t)max(a.lens[b], 0), cap), drop = (uint32_t)max(a.drop[b], 0);
+  const uint32_t s = len > drop ? len - drop : 0u, kept = (s + page1) >> a.page_shift;
+  const uint32_t have = count_pages(a.table + (int64_t)b * a.table_width + kept, ((len + page1) >> a.page_shift) - kept);
+  if ((threadIdx.x & 31) == 0) a.cu_tokens[b] = (int32_t)have;
+}
+
 // PER: sequences per thread at most.
 template <int THREADS, int PER, int PART>
-__global__ void __launch_bounds__(THREADS) kv4_plan_kernel(const PlanArgs a) {
+__global__ void __launch_bounds__(THREADS, 1) kv4_plan_kernel(const PlanArgs a) {
   extern __shared__ uint32_t plan_smem[];
   __shared__ uint32_t part[THREADS / 32];
+  __shared__ uint32_t holes[kPlanMaxBatch / 32], any_hole;   // sequences that drop entries which are no pages; whether one does
   const int B = (int)a.batch;
   uint32_t* start = plan_smem;        // tokens that stay
   uint32_t* cu = start + B;           // tokens asked for before this sequence
@@ -89,18 +117,63 @@ __global__ void __launch_bounds__(THREADS) kv4_plan_kernel(const PlanArgs a) {
   const uint32_t stride = gridDim.x * THREADS, first = blockIdx.x * THREADS + tid;
   const uint32_t page1 = (1u << shift) - 1, cap = (uint32_t)(a.table_width << shift), total = (uint32_t)a.total;
   auto pages = [&](uint32_t tokens) { return (tokens + page1) >> shift; };   // tokens <= 2^31 - 256
+  auto dropped = [&](int b) { return a.table + (int64_t)b * a.table_width + pages(start[b]); };   // the first dropped entry
+  auto hole = [&](int b) { return (holes[b >> 5] >> (b & 31) & 1u) != 0; };
+  auto count_is = [&](int b, uint32_t entries, uint32_t have) {   // of them are pages
+    freed[b] = have;
+    if (have != entries) {
+      atomicOr(&holes[b >> 5], 1u << (b & 31));
+      any_hole = 1;
+    }
+  };
+  auto grid_sync = [&]() {   // what the grid, one cluster, has written can be read
+    if (gridDim.x > 1) {
+      __threadfence();
+      asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;\n" ::: "memory");
+    } else {
+      __syncthreads();
+    }
+  };
+  for (int i = tid; i < (B + 31) / 32; i += THREADS) holes[i] = 0;
+  if (tid == 0) any_hole = 0;
+  __syncthreads();
   pdl_wait();
   pdl_trigger();
 
   const int32_t count0 = *a.free_count;
+  bool many = false;
   for (int b = tid; b < B; b += THREADS) {
     const uint32_t len = min((uint32_t)max(a.lens[b], 0), cap), drop = a.drop ? (uint32_t)max(a.drop[b], 0) : 0u;
-    const uint32_t s = len > drop ? len - drop : 0u;
+    const uint32_t s = len > drop ? len - drop : 0u, entries = pages(len) - pages(s);
     start[b] = s;
-    freed[b] = pages(len) - pages(s);
     cu[b] = a.add ? (uint32_t)max(a.add[b], 0) : 0u;
+    if (PART != kPlanAll) {
+      count_is(b, entries, a.drop ? (uint32_t)__ldcg(a.cu_tokens + b) : 0u);
+    } else if (entries <= kPlanOwn) {
+      const int32_t* e = dropped(b);
+      uint32_t have = 0;
+#pragma unroll
+      for (uint32_t k = 0; k < kPlanOwn; ++k)
+        if (k < entries) have += __ldcg(e + k) >= 0;
+      count_is(b, entries, have);
+    } else {
+      freed[b] = entries | kPlanLong;
+      many = true;
+    }
   }
-  __syncthreads();
+  // (every CTA finds the same)
+  if (__syncthreads_or(many)) {
+    // counted by the grid's warps in turn, and passed on through cu_tokens, which is written last of all
+    for (int b = (int)(first >> 5); b < B; b += (int)(stride >> 5))
+      if (freed[b] & kPlanLong) {
+        const uint32_t have = count_pages(dropped(b), freed[b] & ~kPlanLong);
+        if ((tid & 31) == 0) a.cu_tokens[b] = (int32_t)have;
+      }
+    grid_sync();
+    for (int b = tid; b < B; b += THREADS)
+      if (freed[b] & kPlanLong) count_is(b, freed[b] & ~kPlanLong, (uint32_t)__ldcg(a.cu_tokens + b));
+    __syncthreads();
+  }
   // a thread's sequences lie next to one another
   const int per = (B + THREADS - 1) / THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
   uint32_t sum_add = 0, sum_freed = 0;
@@ -153,18 +226,35 @@ __global__ void __launch_bounds__(THREADS) kv4_plan_kernel(const PlanArgs a) {
   // where freed page i of all lies, as long as the table has not been written
   auto freed_page = [&](uint32_t i) -> const int32_t* {
     const int b = last_at_most(freed, B, i);
-    return a.table + (int64_t)b * a.table_width + pages(start[b]) + i - freed[b];
+    const int32_t *e = dropped(b), *last = a.table + (int64_t)(b + 1) * a.table_width - 1;
+    uint32_t k = i - freed[b];
+    if (!hole(b)) return e + k;
+    while (e < last && (__ldcg(e) < 0 || k-- > 0)) ++e;   // (it has more than k pages)
+    return e;
   };
   if (PART != kPlanRows) {
     // freed pages onto the stack (where a list that is too short left room for them)
-    for (uint32_t i = first; i < all_freed && i < there; i += stride)
-      if (there - 1 - i >= count) a.free_pages[there - 1 - i] = *freed_page(i);
-    if (gridDim.x > 1) {
-      __threadfence();
-      asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;\n" ::: "memory");
-    } else {
-      __syncthreads();
+    const uint32_t room = there - count;
+    for (uint32_t i = first; i < all_freed && i < room; i += stride) {
+      const int b = last_at_most(freed, B, i);
+      if (!hole(b)) a.free_pages[there - 1 - i] = __ldcg(dropped(b) + i - freed[b]);
     }
+    if (any_hole) {   // a warp looks the others' entries through
+      for (int b = (int)(first >> 5); b < B; b += (int)(stride >> 5)) {
+        if (!hole(b)) continue;
+        const int32_t* e = dropped(b);
+        const uint32_t end = b + 1 < B ? freed[b + 1] : all_freed, width = (uint32_t)a.table_width - pages(start[b]);
+        uint32_t i = freed[b];
+        for (uint32_t k = tid & 31; i < end && (k & ~31u) < width; k += 32) {
+          const int32_t page = k < width ? __ldcg(e + k) : -1;   // (what lies behind the last dropped one comes too late)
+          const uint32_t has = __ballot_sync(0xffffffffu, page >= 0);
+          const uint32_t at = i + __popc(has & ((1u << (tid & 31)) - 1));
+          if (page >= 0 && at < end && at < room) a.free_pages[there - 1 - at] = page;
+          i += __popc(has);
+        }
+      }
+    }
+    grid_sync();
     // pages from its top into the tables
     for (uint32_t i = first; i < given; i += stride) {
       const int b = last_at_most(taken, B, i);
@@ -266,14 +356,17 @@ static cudaError_t launch_plan_t(const PlanArgs& a, int ctas, int cluster, cudaS
 }
 
 cudaError_t launch_kv4_plan(const PlanArgs& a, cudaStream_t stream) {
-  cudaError_t e;
+  cudaError_t e = cudaSuccess;
   if (a.total + a.batch * 4 <= 1024) {   // one small CTA: short sums, no cluster's barrier
     e = launch_plan_t<128, 2, kPlanAll>(a, 1, 1, stream);
   } else if (a.total <= kPlanTokens) {
     e = launch_plan_t<512, 8, kPlanAll>(a, kPlanCluster, kPlanCluster, stream);
   } else {
     const int64_t want = (a.total + 511) / 512, most = device_sm_count();
-    e = launch_plan_t<512, 8, kPlanRows>(a, (int)(want < most ? want : most), 1, stream);
+    constexpr int kWarps = kPlanCountThreads / 32;
+    if (a.drop && a.batch > 0)
+      e = launch_pdl(kv4_plan_count_kernel, dim3((unsigned)((a.batch + kWarps - 1) / kWarps)), dim3(kPlanCountThreads), 0, stream, 1, a);
+    if (e == cudaSuccess) e = launch_plan_t<512, 8, kPlanRows>(a, (int)(want < most ? want : most), 1, stream);
     if (e == cudaSuccess) e = launch_plan_t<512, 8, kPlanLists>(a, kPlanCluster, kPlanCluster, stream);
   }
   return e != cudaSuccess ? e : cudaGetLastError();

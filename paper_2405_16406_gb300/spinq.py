@@ -919,7 +919,8 @@ def kv4_plan(lens: torch.Tensor, add: Optional[torch.Tensor], page_table: torch.
     """Drops the last ``drop`` [B] tokens of each sequence and makes room for ``add``
     [B] more: ``lens`` [B], ``page_table`` [B, W], the stack ``free_pages`` [N] and
     ``free_count`` [1] (all int32) are updated in place; returns positions and slots of the
-    new tokens, ``total`` rows of them (``depths`` [total]: places of a tree's nodes)."""
+    new tokens, ``total`` rows of them (``depths`` [total]: places of a tree's nodes).  An
+    entry of the table below 0 is a page that was given back: nothing comes of dropping it."""
     dev, queue = _queue(lens, stream)
     B, W = page_table.shape
     if plan is None:
