@@ -543,8 +543,9 @@ spinq_status spinq_prefix_attention_kv4(const void* q, const spinq_kv4_pages* ca
  * top in such order that a sequence which drops and adds gets its own back.
  * Sequences are served in their order; where the pages run out, the first that is
  * not to be had in full and every later one that needs a page are refused, as is one
- * longer than its row of page_table or whose rows end past `total`: lens[b] <- start,
- * its slots are -1 (spinq_kv4_append passes over them), granted[b] = 0.  What later calls
+ * longer than its row of page_table, one whose rows end past `total`, or one whose
+ * new tokens would begin in a page that was given back (below): lens[b] <- start, its
+ * slots are -1 (spinq_kv4_append passes over them), granted[b] = 0.  What later calls
  * of the step give for its rows means nothing, and none of its tokens is to be kept
  * (a count of 0 for spinq_kv4_keep).
  *   lens       [batch] int32, in and out (clamped to the row's capacity);

@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_plan_kernel(const PlanArgs a) 
   extern __shared__ uint32_t plan_smem[];
   __shared__ uint32_t part[THREADS / 32];
   __shared__ uint32_t holes[kPlanMaxBatch / 32], any_hole;   // sequences that drop entries which are no pages; whether one does
+  __shared__ uint32_t lost[kPlanMaxBatch / 32];              // whose new tokens would begin in such an entry
   const int B = (int)a.batch;
   uint32_t* start = plan_smem;        // tokens that stay
   uint32_t* cu = start + B;           // tokens asked for before this sequence
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_plan_kernel(const PlanArgs a) 
       __syncthreads();
     }
   };
-  for (int i = tid; i < (B + 31) / 32; i += THREADS) holes[i] = 0;
+  for (int i = tid; i < (B + 31) / 32; i += THREADS) holes[i] = lost[i] = 0;
   if (tid == 0) any_hole = 0;
   __syncthreads();
   pdl_wait();
@@ -145,8 +146,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_plan_kernel(const PlanArgs a) 
   for (int b = tid; b < B; b += THREADS) {
     const uint32_t len = min((uint32_t)max(a.lens[b], 0), cap), drop = a.drop ? (uint32_t)max(a.drop[b], 0) : 0u;
     const uint32_t s = len > drop ? len - drop : 0u, entries = pages(len) - pages(s);
+    const uint32_t add = a.add ? (uint32_t)max(a.add[b], 0) : 0u;
     start[b] = s;
-    cu[b] = a.add ? (uint32_t)max(a.add[b], 0) : 0u;
+    cu[b] = add;
+    if (add > 0 && (s & page1) && __ldcg(a.table + (int64_t)b * a.table_width + (s >> shift)) < 0)
+      atomicOr(&lost[b >> 5], 1u << (b & 31));
     if (PART != kPlanAll) {
       count_is(b, entries, a.drop ? (uint32_t)__ldcg(a.cu_tokens + b) : 0u);
     } else if (entries <= kPlanOwn) {
@@ -192,8 +196,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv4_plan_kernel(const PlanArgs a) 
       freed[b] = at_freed;
       at_add = sat_add(at_add, add);
       at_freed = sat_add(at_freed, f);
-      // it fits the answer's arrays and its row of the table (start <= cap)
-      const bool fits = add == 0 || (at_add <= total && add <= cap - start[b]);
+      // it fits the answer's arrays and its row of the table (start <= cap), and its last page is there
+      const bool fits = add == 0 || (at_add <= total && add <= cap - start[b] && !(lost[b >> 5] >> (b & 31) & 1u));
       need[k] = fits ? pages(start[b] + add) - pages(start[b]) : 0u;
       gets[b] = fits ? need[k] : kPlanMost;
       sum_need = sat_add(sum_need, need[k]);

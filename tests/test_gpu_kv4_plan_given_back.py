@@ -119,3 +119,32 @@ def test_a_window_ends_and_its_pages_serve_another(S):
     step = (v.float().amax(-1) - v.float().amin(-1)) / 15
     # half a step of Eq. 1, and the output's rounding to fp16 (2^-11 of at most 8)
     assert ((v.float() - read.float()).abs().amax(-1) <= 0.51 * step + 2.0 ** -8).all()
+
+
+@pytest.mark.parametrize("total", [30, 3000, 9000])
+def test_no_tokens_into_a_page_that_was_given_back(S, total):
+    """A sequence whose last token lies in such a page (its program dropped tokens back to before its window) is
+    refused where it asks for more, as nothing could hold them; at a page's end, or without new tokens, it is not."""
+    P, W = 16, 6
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")   # noqa: E731
+    lens, drop, add = [40, 48, 33, 20, 50, 64], [3, 0, 0, 0, 17, 16], [4, 4, 0, 13, 1, 2]
+    start = [37, 48, 33, 20, 33, 48]
+    table = np.full((6, W), -1, np.int32)
+    for b, pages in enumerate([[0, 1, -1], [2, 3, -5], [4, 5, -1], [6, 7], [8, 9, -1, 10], [11, 12, 13, -(1 << 31)]]):
+        table[b, :len(pages)] = pages
+    t, free, count, n = torch.from_numpy(table.copy()).cuda(), i32([20, 21, 22, 23, -1, -1, -1, -1]), i32([4]), i32(lens)
+    plan = S.kv4_plan(n, i32(add), t, free, count, P, total, drop=i32(drop))
+    torch.cuda.synchronize()
+    granted = [0, 1, 1, 1, 0, 1]
+    assert plan.granted.tolist() == granted
+    assert n.tolist() == [s + a if g else s for s, a, g in zip(start, add, granted)]
+    # (sequence 4 gives page 10 back, sequence 5 nothing; sequences 1, 3 and 5 take a page each)
+    for b, at, page in ((1, 3, 10), (3, 2, 23), (5, 3, 22)):
+        table[b, at] = page
+    assert np.array_equal(t.cpu().numpy(), table)
+    assert count.item() == 2 and free[:2].tolist() == [20, 21]
+    want, cu = [], [0]
+    for b, (s, a, g) in enumerate(zip(start, add, granted)):
+        want += [int(table[b, (s + i) // P]) * P + (s + i) % P if g else -1 for i in range(a)]
+        cu.append(cu[-1] + a)
+    assert plan.slots.tolist() == want + [-1] * (total - len(want)) and plan.cu_tokens.tolist() == cu
