@@ -33,7 +33,9 @@ namespace spinq {
 namespace {
 
 constexpr int kRowsWarps = 4;
-// Parts of a job at most.  (4 rows of D 128, one sequence of 4000 tokens: 9.9 us with 20, 11.2 with 60; of 8000 14.1
+// Parts of a job on an average, at most: the runs are no more than this times the batch's jobs.  An even batch's jobs
+// have no more each; a long one among short ones has, as those leave it their share (30000 tokens of one kv head
+// beside 39 sequences of 10: 118 parts, 17.5 us; alone, in 20, 16.4).  (4 rows of D 128, one sequence of 4000 tokens: 9.9 us with 20, 11.2 with 60; of 8000 14.1
 // and 13.7; of 16000 15.3 and 15.8; two of 16000 19.2 and 21.3)
 constexpr int kRowsParts = 20;
 constexpr int kCombineThreads = 256;

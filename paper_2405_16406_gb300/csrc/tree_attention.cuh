@@ -74,7 +74,8 @@ struct TreeRun {
   }
 };
 
-// PARTS > 0: runs so long that a job is cut into about that many at most.  The parts of a job are
+// PARTS > 0: at most that many runs per job of the batch, so that even jobs are cut into about that many
+// at most (one that is far longer than the others into more).  The parts of a job are
 // joined eight at a time, which for few jobs takes as long as their keys.
 template <int THREADS, int PARTS>
 __device__ __forceinline__ TreeRun tree_run(const TreeParams& p, int c) {
