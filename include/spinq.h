@@ -593,7 +593,10 @@ spinq_status spinq_kv4_keep(const spinq_kv4_pages* cache, const int32_t* page_ta
  * sees the last positions and a few first tokens only: key j of a query at position
  * p = i + lk - lq is seen if j <= p and (p - j < window or j < sinks).
  *   window >= 1, sinks >= 0.  Other arguments, layouts and limits as
- *   spinq_prompt_attention; tiles of keys that no query of a tile sees are not read.
+ *   spinq_prompt_attention (keys and values of a sequence are finite, those that no query
+ *   sees among them).  A work item, two tiles of 128 rows (query x head of the group), reads
+ *   the sinks in whole groups of 32 and the keys from the first that a window of its queries
+ *   reaches.
  */
 spinq_status spinq_window_prompt_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
                                            int64_t ldv, const int32_t* cu_q, const int32_t* cu_k, int64_t batch,

@@ -1,6 +1,5 @@
 // kv4_attn.cuh -- what the attention kernels on the paged 4-bit cache share:
-// value scales in the weights, codes as fp16 operands, and a warp's ring of
-// 16-token steps.
+// value scales in the weights, codes as fp16 operands, and a warp's copies.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -61,27 +60,8 @@ __device__ __forceinline__ uint32_t own_transpose(uint32_t x) {   // 8x8 fp16 tr
   return y;
 }
 
-constexpr int kOwnStages = 4;
-
 __device__ __forceinline__ void own_copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
 }
-
-// A warp's ring of stages: 16 tokens' key rows, value rows (D/2 bytes each) and
-// scales.  Key rows lie as in the page (a fragment load covers eight whole rows);
-// a fragment load of the values takes 8 or 4 bytes of rows 0, 2, 4, 6 (or 1, 3,
-// ..), so their 16-byte pieces are moved about to fall in different banks.
-template <int D>
-struct OwnRing {
-  static constexpr int KB = 16 * (D / 2), STAGE = 2 * KB + 256, WARP = kOwnStages * STAGE;
-  static constexpr int CPR = D / 32;   // 16-byte pieces of a row
-  static __device__ __forceinline__ int value_at(int row, int piece) {   // byte offset of a value row's piece
-    if (D == 128) {
-      const int pair = row >> 1;
-      return pair * 128 + (((row ^ pair) & 1) << 6) + ((piece ^ (pair & 2)) << 4);
-    }
-    return row * 32 + ((piece ^ ((row >> 2) & 1)) << 4);
-  }
-};
 
 }  // namespace spinq

@@ -541,6 +541,24 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_tc_kernel(const Pref
 
 // ------------------------------------------------- the sequences' own tokens
 constexpr int kOwnWarps = 4;
+constexpr int kOwnStages = 4;
+
+// A warp's ring of stages: 16 tokens' key rows, value rows (D/2 bytes each) and
+// scales.  Key rows lie as in the page (a fragment load covers eight whole rows);
+// a fragment load of the values takes 8 or 4 bytes of rows 0, 2, 4, 6 (or 1, 3,
+// ..), so their 16-byte pieces are moved about to fall in different banks.
+template <int D>
+struct OwnRing {
+  static constexpr int KB = 16 * (D / 2), STAGE = 2 * KB + 256, WARP = kOwnStages * STAGE;
+  static constexpr int CPR = D / 32;   // 16-byte pieces of a row
+  static __device__ __forceinline__ int value_at(int row, int piece) {   // byte offset of a value row's piece
+    if (D == 128) {
+      const int pair = row >> 1;
+      return pair * 128 + (((row ^ pair) & 1) << 6) + ((piece ^ (pair & 2)) << 4);
+    }
+    return row * 32 + ((piece ^ ((row >> 2) & 1)) << 4);
+  }
+};
 
 // grid (chunk, kv head x group of 8 query heads, sequence).  A warp takes
 // steps of 16 tokens, which lie in one page, so its rows of codes are one run of

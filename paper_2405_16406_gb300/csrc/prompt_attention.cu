@@ -113,7 +113,9 @@ constexpr int kItemReaders = 11;
 // no tile starts before the window (2 x 32 queries with a window of 512 and 4 sinks: 5 tiles of
 // 128; with a tile of sinks and tiles at whole multiples of 128 tokens 6.5: 16 ragged sequences of
 // 32767 tokens 471 us so and 347 now, 0.92 PFLOP/s on visible pairs; 2 x 16384 with a window of 4096 1.31 ms, 1.48).
-// Bound: the softmax, as above, and the masks: the window's two edges cross 2 of those 5 tiles.
+// Bound: the softmax, as above, and the masks: the window's two edges cross 2 of those 5 tiles.  Both
+// tiles of an item work through its one list, so the second's first keys may lie before all of its windows (one
+// head a group, no sinks: one tile of 6 with a window of 512).
 template <int D, bool WIN>
 __global__ void __launch_bounds__(kPromptThreads, 1)
     prompt_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
