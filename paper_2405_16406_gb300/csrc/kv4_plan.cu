@@ -19,9 +19,10 @@
 //    tokens by a kernel that fills the GPU and reads the lists as they were, then
 //    the lists and lengths by the one cluster (1000 sequences, 251 K tokens: 60 us in one
 //    kernel, whose 4096 threads had 64 dependent look-ups each).
-// Bound: latency (a chain of the lengths' loads, three block-wide sums, a barrier, and
-// two dependent loads): 8 sequences of one token 6.1 us, those 1000 sequences 11.2 + 12.4 us one
-// after the other (24.7 us in a graph, with the copies that put the lengths back).
+// Bound: latency (a chain of the lengths' loads and the dropped entries, three block-wide sums, a
+// barrier, and two dependent loads).  Call after call in a graph: 8 sequences of one token 3.5 us, 512 of
+// one 6.9, those 1000 sequences 23.4 (3.7 of them for the count; 29.4 with the copies that put the lengths
+// back), 8 of 32768 tokens that end among 248 of one more 11.9, 256 that end among 256 95.8 (524 K pages of 16).
 //
 // Keep.  A path ascends, so a token never moves up and never onto one that is
 // still to be read by a later part of its path: a CTA takes the 16-byte pieces of
